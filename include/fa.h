@@ -264,6 +264,117 @@ int fa_decode_append(const void* q, const void* k_cache, const void* v_cache, vo
 size_t fa_decode_append_workspace_bytes(int B, int Sq, int Hq, int Hkv, int Skv_max, int d);
 
 /*
+ * Attention for a tree of drafted tokens over a cache (speculative decoding; the paper has no counterpart -- this is the
+ * decode of Appendix C for several rows whose mask is a tree's): sequence b's cache ends with the rows of its tree's
+ * nodes, and its T query rows are those nodes.  With n = tree_lens[b] (T where tree_lens is NULL) nodes and
+ * len = seqlens_k[b] keys, the tree's rows INCLUDED, node j's key and value are cache row len - n + j, and query row t sees
+ *     every key before the tree (rows below len - n), and
+ *     node j (0 <= j < n) iff bit j % 32 of mask[b * mask_stride + t * ceil(T / 32) + j / 32] is set
+ * (the mask holds ancestors, not parents, and each node's own bit; it need not be a tree's).  Rows t >= n, and rows that
+ * see nothing, give O = 0 and LSE = -inf.
+ *   q, o [B,T,Hq,d], lse [B,Hq,T] float or NULL, 1 <= T <= 256; d = 128 or 64; fp16 or bf16; q, o and the caches contiguous.
+ *   Caches and block table as for fa_decode_ex.  seqlens_k, tree_lens, mask: int32 on the DEVICE; lengths are clamped to
+ *   [0, Skv_max], tree_lens to [0, min(T, len)]; mask_stride: words from one sequence's mask to the next, 0 = all
+ *   sequences have one tree.
+ *   Cache rows past a sequence's end may hold anything.  Inside it, the KEY of a node that a row does not see may be
+ *   anything (NaN too); its VALUE must be finite, as it is multiplied by zero.
+ *   workspace: fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max or max_pages * page_size, d) bytes, 16-byte aligned.
+ * Errors: as fa_decode_ex; FA_ERR_UNSUPPORTED also for T > 256 or T > Skv_max, FA_ERR_NULL without a mask, FA_ERR_SHAPE for a
+ * negative mask_stride.
+ */
+typedef struct fa_tree_params {
+    const void* q;          /* [B,T,Hq,d] */
+    const void* k;          /* cache or page pool */
+    const void* v;
+    void* o;                /* [B,T,Hq,d] */
+    float* lse;             /* [B,Hq,T] or NULL */
+    const int* seqlens_k;   /* [B], device */
+    const int* tree_lens;   /* [B], device, or NULL: T */
+    const int* mask;        /* [B or 1, T, ceil(T/32)] words, device */
+    const int* block_table; /* NULL, or [B,table_stride] on the device */
+    int B, T, Hq, Hkv, Skv_max, d;
+    int dtype;              /* FA_DTYPE_FP16 or FA_DTYPE_BF16 */
+    int num_pages, page_size, max_pages, table_stride;
+    int64_t mask_stride;    /* words */
+    float scale;
+    void* workspace;
+    size_t workspace_bytes;
+} fa_tree_params;
+int fa_decode_tree(const fa_tree_params* p, void* stream);
+size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d);
+
+/*
+ * Verification of a tree of drafted tokens (speculative decoding) against the target's probabilities, from given random
+ * numbers: which of the tree's nodes stand, and the token after them.  The emitted tokens are distributed as the target's.
+ *   target_probs p [B,T,V]: row t is the target's distribution of the token after node t; draft_probs q [B,T,V]: the draft's, from
+ *   which the children of node t were drawn independently of one another -- or NULL: the draft proposed its tokens for
+ *   certain (a greedy or looked-up draft).  Both of type dtype (FA_DTYPE_FP16, FA_DTYPE_BF16 or FA_DTYPE_FP32), rows of a sum of 1.
+ *   tokens, parents int32 [B,T]: node 0 is the last token that stands, parents[b][0] is not read for it, parents[b][i] lies in [0, i);
+ *   tree_lens int32 [B] or NULL: how many of the T nodes there are (NULL: T; clamped to [1, T]); uniforms float [B,T] in [0, 1);
+ *   noise float [B,V], exponentially distributed with mean 1, positive.
+ * With cur = 0, s = 0, Z = 1, the nodes i whose parent is cur are tested in their order, x = tokens[i]:
+ *     with q:     r = max(p[cur][x] - s q[cur][x], 0); accepted iff uniforms[i] Z q[cur][x] < r; if not, s += Z and then
+ *                 Z = sum over v of max(p[cur][v] - s q[cur][v], 0)
+ *     without q:  r = p[cur][x], or 0 if an earlier child of cur had the token x; accepted iff uniforms[i] Z < r; if not,
+ *                 Z = max(Z - r, 0)
+ *     accepted:   cur = i, s = 0, Z = 1.
+ * The last token is the v of largest r(v) / noise[v], r(v) = max(p[cur][v] - s q[cur][v], 0), or p[cur][v] and 0 for rejected tokens
+ * without q; equal ones go to the lowest v.  If r has no positive entry p[cur] takes its place; if that has none, the token is -1.
+ * (Sums are fp32, comparisons with NaN fail.)
+ *   n_accept int32 [B]: drafted tokens that stand; path int32 [B,T]: the nodes that stand, from node 0 on, then -1;
+ *   out_tokens int32 [B,T]: their tokens without node 0's, the last token, then -1.
+ *   T <= 256, V <= 2^30; all contiguous and aligned to their elements.  A token outside [0, V) is never accepted.
+ * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (T, V, dtype, B > 65535), FA_ERR_NULL, FA_ERR_ALIGN.
+ */
+int fa_spec_verify(const void* target_probs, const void* draft_probs, const int* tokens, const int* parents,
+                   const int* tree_lens, const float* uniforms, const float* noise, int* n_accept, int* path, int* out_tokens,
+                   int B, int T, int V, int dtype, void* stream);
+
+/*
+ * After the verification: the cache rows of the accepted path move together, in place, in every layer.  Sequence b's cache
+ * ends with its tree's rows as in fa_decode_tree (len = seqlens_k[b], n = tree_lens[b] or T of them); with path and n_accept
+ * as fa_spec_verify gives them (path ascending),
+ *     row len - n + i  <-  row len - n + path[b][i],   i = 1 .. n_accept[b],      new_lens[b] = len - n + 1 + n_accept[b].
+ * (A sequence without tree rows keeps its length.)  Rows past the new length keep what they had or hold what was moved.
+ *   k, v: contiguous caches [layers,B,Skv_max,row] (block_table == NULL), or pools [layers,num_pages,page_size,row] behind
+ *   block_table [B,table_stride], page_size any positive number; row: row_bytes bytes, a multiple of 16 (Hkv * d elements of any
+ *   type); layer_stride: bytes from one layer to the next, a multiple of 16.  new_lens must not be seqlens_k.
+ *   Nodes outside (i, n) in path[b][i] and pages outside [0, num_pages) are skipped.
+ * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (B > 65535), FA_ERR_NULL, FA_ERR_ALIGN.
+ */
+int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlens_k, const int* tree_lens, const int* path,
+                     const int* n_accept, int* new_lens, int layers, int64_t layer_stride, int B, int T, int Skv_max, int num_pages,
+                     int page_size, int max_pages, int table_stride, int row_bytes, void* stream);
+
+/*
+ * Pages of a pool, reserved and given back.  The state is all on the DEVICE, int32: block_table [B,table_stride], held [B] (the
+ * pages of each sequence: the first held[b] entries of its row of the table) and refs [num_pages] (how many sequences hold
+ * a page; 0 = free).  Afterwards sequence b holds ceil(want[b] / page_size) pages (want: rows; negative counts as 0):
+ *   what it holds beyond them is given back first (refs - 1, table entry -1), in all sequences;
+ *   then pages are taken, in the order of the sequences and of their entries, the free ones of lowest index first (refs = 1).
+ * A sequence gets its pages iff the free pages suffice for all that it and the sequences before it ask for; if not, or if it asks
+ * for more than max_pages, it keeps what it holds and is counted in n_short [1].
+ *   B <= 4096 in a call.  The cache itself is not touched.
+ * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (B > 4096), FA_ERR_NULL, FA_ERR_ALIGN.
+ */
+int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int* n_short, int B, int num_pages, int page_size,
+                    int max_pages, int table_stride, void* stream);
+
+/*
+ * Sequences that go on from the same rows (parallel sampling, beams): for i = 0 .. n-1 sequence dst[i] becomes a copy of src[i], with
+ * the state of fa_pages_resize and seqlens_k [B] on the device.  Full pages are shared (refs + 1); of a last page that is
+ * partly filled, the filled rows are copied, K and V, all layers, to a fresh page -- the free ones of lowest index, in the order of
+ * the pairs -- so that a page with room is never shared and both sequences can append.  held and seqlens_k of dst follow, entries of its table row
+ * past its pages become -1.  A pair for which no free page is left is counted in n_short [1]; its dst then has no rows and no pages.
+ *   k, v, layers, layer_stride, row_bytes: as for fa_cache_compact (pools).  dst[i] holds no pages before the call (fa_pages_resize
+ *   to 0 rows), occurs once, and is no src of the same call.  n <= 4096.  Indices outside [0, B) are skipped.
+ * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (n > 4096, layers > 32767), FA_ERR_NULL, FA_ERR_ALIGN.
+ */
+int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k, int* refs, const int* src, const int* dst,
+                  int* n_short, int n, int layers, int64_t layer_stride, int B, int num_pages, int page_size, int max_pages,
+                  int table_stride, int row_bytes, void* stream);
+
+/*
  * Decode over an 8-bit cache (Appendix D.2 evaluates the operator with 8-bit operands; in the
  * decode stage the cache dominates the traffic, so here it is the cached K and V that are 8-bit):
  * the computation of fa_decode with K = k_scale * k_cache and V = v_scale * v_cache, where

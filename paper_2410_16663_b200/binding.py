@@ -62,6 +62,25 @@ class fa_decode_params(ctypes.Structure):
 
 lib.fa_decode_ex.restype = _i
 lib.fa_decode_ex.argtypes = [ctypes.POINTER(fa_decode_params), _p]
+class fa_tree_params(ctypes.Structure):
+    _fields_ = [("q", _p), ("k", _p), ("v", _p), ("o", _p), ("lse", _p), ("seqlens_k", _p), ("tree_lens", _p), ("mask", _p),
+                ("block_table", _p), ("B", _i), ("T", _i), ("Hq", _i), ("Hkv", _i), ("Skv_max", _i), ("d", _i), ("dtype", _i),
+                ("num_pages", _i), ("page_size", _i), ("max_pages", _i), ("table_stride", _i), ("mask_stride", ctypes.c_int64),
+                ("scale", _f), ("workspace", _p), ("workspace_bytes", _sz)]
+
+
+lib.fa_decode_tree.restype = _i
+lib.fa_decode_tree.argtypes = [ctypes.POINTER(fa_tree_params), _p]
+lib.fa_decode_tree_workspace_bytes.restype = _sz
+lib.fa_decode_tree_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i]
+lib.fa_spec_verify.restype = _i
+lib.fa_spec_verify.argtypes = [_p] * 10 + [_i, _i, _i, _i, _p]
+lib.fa_cache_compact.restype = _i
+lib.fa_cache_compact.argtypes = [_p] * 8 + [_i, ctypes.c_int64, _i, _i, _i, _i, _i, _i, _i, _i, _p]
+lib.fa_pages_resize.restype = _i
+lib.fa_pages_resize.argtypes = [_p] * 5 + [_i, _i, _i, _i, _i, _p]
+lib.fa_pages_fork.restype = _i
+lib.fa_pages_fork.argtypes = [_p] * 9 + [_i, _i, ctypes.c_int64, _i, _i, _i, _i, _i, _i, _p]
 lib.fa_decode_append.restype = _i
 lib.fa_decode_append.argtypes = [_p, _p, _p, _p, _p, _p, _i, _i, _i, _i, _i, _i, _f, _p, _sz, _p]
 lib.fa_decode_append_workspace_bytes.restype = _sz
@@ -100,6 +119,7 @@ FA_DECODE_NOALLOC_BYTES = 4 << 20
 
 EXPORTS = ["fa_forward", "fa_forward_bf16", "fa_forward_ex", "fa_forward_fp8", "fa_forward_proj", "fa_forward_proj_workspace_bytes", "fa_decode", "fa_decode_workspace_bytes",
            "fa_decode_noalloc", "fa_decode_paged", "fa_forward_varlen", "fa_decode_fp8", "fa_decode_fp8_paged", "fa_decode_fp8_bf16", "fa_decode_fp8_paged_bf16", "fa_decode_append", "fa_decode_append_workspace_bytes", "fa_decode_ex", "fa_forward_varlen_paged",
+           "fa_decode_tree", "fa_decode_tree_workspace_bytes", "fa_spec_verify", "fa_cache_compact", "fa_pages_resize", "fa_pages_fork",
            "fa_forward_host", "fa_forward_host_staging_bytes", "fa_device_status", "fa_selftest_wait", "fa_selftest_decode_cut", "fa_strerror",
            "fa_version", "fa_last_cuda_error"]
 
@@ -270,6 +290,127 @@ def fa_decode_ex(q, k, v, o, lse, seqlens_k, scale: float, workspace, block_tabl
     p.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     rc = lib.fa_decode_ex(ctypes.byref(p), _stream())
     return _check(rc, "fa_decode_ex", raise_on_error)
+
+
+def _contiguous(what: str, *tensors) -> None:
+    """The calls below take contiguous tensors; a view would be read as something else."""
+    for t in tensors:
+        if t is not None and not t.is_contiguous():
+            raise ValueError(f"{what}: a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not contiguous")
+
+
+def _int32(what: str, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.dtype != torch.int32:
+            raise ValueError(f"{what}: index tensors are int32, not {t.dtype}")
+
+
+def fa_decode_tree_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, Skv_max: int, d: int) -> int:
+    return int(lib.fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max, d))
+
+
+def fa_decode_tree(q, k, v, o, lse, seqlens_k, mask, scale: float, workspace, tree_lens=None, block_table=None,
+                   max_pages: int = None, raise_on_error: bool = True) -> int:
+    """``fa_decode_tree``: q, o [B,T,Hq,d], the nodes of each sequence's tree, whose rows end its cache; mask int32
+    [B,T,ceil(T/32)], or [T,ceil(T/32)] for one tree; k, v, block_table as for ``fa_decode_ex``; seqlens_k int32 [B] with the
+    tree's rows, tree_lens int32 [B] or None."""
+    _contiguous("fa_decode_tree", q, k, v, o, lse, seqlens_k, mask, tree_lens)
+    _int32("fa_decode_tree", seqlens_k, mask, tree_lens, block_table)
+    if k.dtype != q.dtype or v.dtype != q.dtype or o.dtype != q.dtype or q.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("fa_decode_tree: q, k, v and o share one 16-bit type")
+    p = fa_tree_params()
+    p.q, p.k, p.v, p.o, p.lse = _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse)
+    p.seqlens_k, p.tree_lens, p.mask, p.block_table = _ptr(seqlens_k), _ptr(tree_lens), _ptr(mask), _ptr(block_table)
+    p.B, p.T, p.Hq, p.d = q.shape
+    p.Hkv = k.shape[2]
+    if mask.shape[-2:] != (p.T, (p.T + 31) // 32) or (mask.dim() == 3 and mask.shape[0] != p.B):
+        raise ValueError(f"fa_decode_tree: a mask of shape {tuple(mask.shape)} for T = {p.T}")
+    p.mask_stride = 0 if mask.dim() == 2 else mask.stride(0)
+    p.dtype = FA_DTYPE_BF16 if q.dtype == torch.bfloat16 else FA_DTYPE_FP16
+    if block_table is None:
+        p.Skv_max = k.shape[1]
+    else:
+        p.num_pages, p.page_size = k.shape[0], k.shape[1]
+        p.max_pages = block_table.shape[1] if max_pages is None else int(max_pages)
+        p.table_stride = block_table.stride(0)
+    p.scale = float(scale)
+    p.workspace = _ptr(workspace)
+    p.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = lib.fa_decode_tree(ctypes.byref(p), _stream())
+    return _check(rc, "fa_decode_tree", raise_on_error)
+
+
+_PROB_DTYPES = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16, torch.float32: FA_DTYPE_FP32}
+
+
+def fa_spec_verify(target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens=None,
+                   raise_on_error: bool = True) -> int:
+    """``fa_spec_verify``: target_probs [B,T,V] (fp32, fp16 or bf16), draft_probs the same or None, tokens, parents int32 [B,T],
+    uniforms float32 [B,T], noise float32 [B,V]; writes n_accept int32 [B], path and out_tokens int32 [B,T]."""
+    _contiguous("fa_spec_verify", target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens)
+    _int32("fa_spec_verify", tokens, parents, n_accept, path, out_tokens, tree_lens)
+    if target_probs.dtype not in _PROB_DTYPES or (draft_probs is not None and draft_probs.dtype != target_probs.dtype):
+        raise ValueError("fa_spec_verify: probabilities are fp32, fp16 or bf16, both of one type")
+    if uniforms.dtype != torch.float32 or noise.dtype != torch.float32:
+        raise ValueError("fa_spec_verify: random numbers are float32")
+    B, T, V = target_probs.shape
+    rc = lib.fa_spec_verify(_ptr(target_probs), _ptr(draft_probs), _ptr(tokens), _ptr(parents), _ptr(tree_lens), _ptr(uniforms),
+                            _ptr(noise), _ptr(n_accept), _ptr(path), _ptr(out_tokens), B, T, V, _PROB_DTYPES[target_probs.dtype], _stream())
+    return _check(rc, "fa_spec_verify", raise_on_error)
+
+
+def _planes(what: str, k, v):
+    """(layers, bytes between layers, bytes of a row) of caches [layers, slabs, rows, ...]."""
+    _contiguous(what, k[0], v[0])
+    if k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+        raise ValueError(f"{what}: k and v are of one shape, type and layout")
+    size = k.element_size()
+    row = size
+    for n in k.shape[3:]:
+        row *= n
+    return k.shape[0], k.stride(0) * size, row
+
+
+def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, block_table=None, max_pages: int = None,
+                     raise_on_error: bool = True) -> int:
+    """``fa_cache_compact``: k, v the caches of all layers, [L,B,Smax,Hkv,d], or with a block table the pools
+    [L,num_pages,page_size,Hkv,d] (any element type); path int32 [B,T], n_accept int32 [B] as ``fa_spec_verify`` writes
+    them; writes new_lens int32 [B]."""
+    layers, stride, row = _planes("fa_cache_compact", k, v)
+    _contiguous("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
+    _int32("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens, block_table)
+    B, T = path.shape
+    if block_table is None:
+        args = (k.shape[2], 0, 0, 0, 0)
+    else:
+        args = (0, k.shape[1], k.shape[2], block_table.shape[1] if max_pages is None else int(max_pages), block_table.stride(0))
+    rc = lib.fa_cache_compact(_ptr(k), _ptr(v), _ptr(block_table), _ptr(seqlens_k), _ptr(tree_lens), _ptr(path), _ptr(n_accept),
+                              _ptr(new_lens), layers, stride, B, T, *args, row, _stream())
+    return _check(rc, "fa_cache_compact", raise_on_error)
+
+
+def fa_pages_resize(block_table, held, refs, want, n_short, page_size: int, raise_on_error: bool = True) -> int:
+    """``fa_pages_resize``: block_table int32 [B,max_pages], held int32 [B], refs int32 [num_pages], want int32 [B] (rows);
+    n_short int32 [1] counts the sequences that could not be served."""
+    _contiguous("fa_pages_resize", held, refs, want, n_short)
+    _int32("fa_pages_resize", block_table, held, refs, want, n_short)
+    rc = lib.fa_pages_resize(_ptr(block_table), _ptr(held), _ptr(refs), _ptr(want), _ptr(n_short), block_table.shape[0], refs.numel(),
+                             int(page_size), block_table.shape[1], block_table.stride(0), _stream())
+    return _check(rc, "fa_pages_resize", raise_on_error)
+
+
+def fa_pages_fork(k, v, block_table, held, seqlens_k, refs, src, dst, n_short, raise_on_error: bool = True) -> int:
+    """``fa_pages_fork``: pools k, v [L,num_pages,page_size,Hkv,d] with the state of ``fa_pages_resize`` and seqlens_k int32
+    [B]; sequence dst[i] becomes a copy of src[i] (int32 [n] each); n_short int32 [1] counts the pairs that got no page."""
+    layers, stride, row = _planes("fa_pages_fork", k, v)
+    _contiguous("fa_pages_fork", held, seqlens_k, refs, src, dst, n_short)
+    _int32("fa_pages_fork", block_table, held, seqlens_k, refs, src, dst, n_short)
+    if refs.numel() != k.shape[1]:
+        raise ValueError("fa_pages_fork: refs has an entry for each of the pool's pages")
+    rc = lib.fa_pages_fork(_ptr(k), _ptr(v), _ptr(block_table), _ptr(held), _ptr(seqlens_k), _ptr(refs), _ptr(src), _ptr(dst),
+                           _ptr(n_short), src.numel(), layers, stride, block_table.shape[0], k.shape[1], k.shape[2],
+                           block_table.shape[1], block_table.stride(0), row, _stream())
+    return _check(rc, "fa_pages_fork", raise_on_error)
 
 
 def fa_decode_append_workspace_bytes(B: int, Sq: int, Hq: int, Hkv: int, Skv_max: int, d: int) -> int:

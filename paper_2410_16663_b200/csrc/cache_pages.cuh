@@ -1,0 +1,339 @@
+// What happens to a cache between the steps of a decode: the rows of an accepted path move together (compact), pages are
+// reserved and given back (resize), and sequences share pages (fork).
+//
+// A pool's pages are counted by `refs`, one int per page: the sequences that hold it, 0 = free.  There is no other list
+// of free pages, and fresh pages are always the free ones of lowest index, so that the result depends on the state alone.
+#pragma once
+
+#include "prefill_simple.cuh"
+#include "sm100_ptx.cuh"
+
+namespace fa {
+
+// ---------------------------------------------------------------------------------------
+// Compaction: row prefix + i of sequence b <- row prefix + path[b][i], i = 1 .. n_accept[b], in every plane (a layer's K or V).
+// A thread owns 16 bytes of a row in some planes and moves them in the order of i, several rows' loads ahead of the
+// first store: as path[i] >= i and the path ascends, a row that is still to be read has not been written.
+struct CompactParams {
+    char* k;
+    char* v;
+    const int* seqlens;      // [B]
+    const int* tree_lens;    // [B] or nullptr
+    const int* path;         // [B,T]
+    const int* n_accept;     // [B]
+    int* new_lens;           // [B]
+    const int* block_table;  // nullptr: contiguous
+    int B, T, layers, page_size, table_stride, max_rows, num_pages;
+    int row_vecs;            // 16-byte pieces of a row
+    long long layer_stride;  // 16-byte pieces between layers
+};
+constexpr int kCompactThreads = 256;
+constexpr int kCompactBatch = 8;     // rows in flight per thread
+
+__global__ void __launch_bounds__(kCompactThreads) fa_cache_compact_kernel(const CompactParams p) {
+    grid_dep_wait();
+    const int b = blockIdx.y;
+    const int len = max(0, min(p.seqlens[b], p.max_rows));
+    const int live = max(0, min(p.tree_lens ? min(p.tree_lens[b], p.T) : p.T, len));
+    const int prefix = len - live;
+    const int n = max(0, min(p.n_accept[b], live - 1));
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.new_lens[b] = live > 0 ? prefix + 1 + n : len;
+    const int* path = p.path + (long long)b * p.T;
+    const int* table = p.block_table ? p.block_table + (long long)b * p.table_stride : nullptr;
+    // row `row` of the sequence in pieces from its plane's start; -1: not a row of the pool
+    auto place = [&](int row) -> long long {
+        if (!table) return ((long long)b * p.max_rows + row) * p.row_vecs;
+        const int page = table[row / p.page_size];
+        if (page < 0 || page >= p.num_pages) return -1;
+        return ((long long)page * p.page_size + row % p.page_size) * p.row_vecs;
+    };
+    const long long units = 2ll * p.layers * p.row_vecs;   // (plane, piece)
+    for (int i0 = 1; i0 <= n; i0 += kCompactBatch) {
+        long long from[kCompactBatch], to[kCompactBatch];
+#pragma unroll
+        for (int j = 0; j < kCompactBatch; ++j) {
+            from[j] = to[j] = -1;
+            const int i = i0 + j;
+            if (i > n) continue;
+            const int x = path[i];
+            if (x <= i || x >= live) continue;   // (it is there already; or no node)
+            from[j] = place(prefix + x);
+            to[j] = place(prefix + i);
+            if (to[j] < 0) from[j] = -1;
+        }
+        for (long long u = (long long)blockIdx.x * kCompactThreads + threadIdx.x; u < units; u += (long long)gridDim.x * kCompactThreads) {
+            const int plane = (int)(u / p.row_vecs), piece = (int)(u % p.row_vecs);
+            uint4* base = reinterpret_cast<uint4*>(plane & 1 ? p.v : p.k) + (long long)(plane >> 1) * p.layer_stride + piece;
+            uint4 x[kCompactBatch];
+#pragma unroll
+            for (int j = 0; j < kCompactBatch; ++j)
+                if (from[j] >= 0) x[j] = base[from[j]];
+#pragma unroll
+            for (int j = 0; j < kCompactBatch; ++j)
+                if (from[j] >= 0) base[to[j]] = x[j];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------
+// Pages of a pool.  One cluster looks the reference counts over, 16 pages per thread at a time; each CTA has the requests (pages
+// wanted, in order) as inclusive prefix sums in its shared memory, and a free page of rank r goes to the request whose
+// range r falls into.
+constexpr int kPagesThreads = 1024;
+constexpr int kPagesPerThread = 16;
+constexpr int kPagesMaxItems = 4096;   // sequences of a resize, pairs of a fork
+constexpr int kPagesMaxCluster = 8;
+
+struct PagesShared {
+    int upto[kPagesMaxItems];     // pages wanted by the items up to and including this one
+    int warp_sum[32];
+    int carry;
+    int count[2];                 // free pages of this CTA's part, of two looks in turn
+};
+
+// Inclusive prefix sums of count(i) over i < n into s.upto; every thread of the CTA calls this.
+template <typename Count>
+__device__ __forceinline__ void pages_prefix(PagesShared& s, int n, Count count) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) s.carry = 0;
+    for (int i0 = 0; i0 < n; i0 += kPagesThreads) {
+        const int i = i0 + tid;
+        int x = i < n ? count(i) : 0;
+#pragma unroll
+        for (int sh = 1; sh < 32; sh <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, sh);
+            if (lane >= sh) x += y;
+        }
+        if (lane == 31) s.warp_sum[warp] = x;
+        __syncthreads();
+        int before = s.carry;
+        for (int w = 0; w < warp; ++w) before += s.warp_sum[w];
+        if (i < n) s.upto[i] = before + x;
+        __syncthreads();
+        if (tid == kPagesThreads - 1) s.carry = before + x;
+    }
+    __syncthreads();
+}
+
+// This thread's pages of round `round` as bits (set: free), and how many free ones come before them in the round's part of this CTA.
+__device__ __forceinline__ uint32_t pages_look(PagesShared& s, const int* refs, int num_pages, long long first, int slot, int& before) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t free_bits = 0;
+    int r[kPagesPerThread];
+    if (first + kPagesPerThread <= num_pages && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
+#pragma unroll
+        for (int j = 0; j < kPagesPerThread / 4; ++j) {
+            const int4 x = __ldcg(reinterpret_cast<const int4*>(refs + first) + j);
+            r[4 * j] = x.x, r[4 * j + 1] = x.y, r[4 * j + 2] = x.z, r[4 * j + 3] = x.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPagesPerThread; ++j) r[j] = first + j < num_pages ? __ldcg(refs + first + j) : 1;
+    }
+#pragma unroll
+    for (int j = 0; j < kPagesPerThread; ++j) free_bits |= (r[j] == 0 ? 1u : 0u) << j;
+    const int mine = __popc(free_bits);
+    int x = mine;
+#pragma unroll
+    for (int sh = 1; sh < 32; sh <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, sh);
+        if (lane >= sh) x += y;
+    }
+    __syncthreads();   // (warp_sum of the round before has been read)
+    if (lane == 31) s.warp_sum[warp] = x;
+    __syncthreads();
+    before = x - mine;
+    for (int w = 0; w < warp; ++w) before += s.warp_sum[w];
+    if (tid == kPagesThreads - 1) s.count[slot] = before + mine;
+    return free_bits;
+}
+
+// Free pages in all and their distribution: for every free page whose rank is below `total` and whose request can be served in
+// full, give(item, how many of the item's pages come before it, page).  Returns the number of free pages, or some number >= total.
+// Every thread of every CTA of the cluster calls this.
+template <typename Give>
+__device__ __forceinline__ int pages_distribute(PagesShared& s, const int* refs, int num_pages, int n_items, int rank, int cluster, Give give) {
+    const int total = n_items > 0 ? s.upto[n_items - 1] : 0;
+    const long long per_round = (long long)cluster * kPagesThreads * kPagesPerThread;
+    const uint32_t count_at = smem_u32(s.count);
+    int found = 0, rounds = 0, before = 0, turn = 0;
+    uint32_t bits = 0;
+    auto look = [&](int round, int& base) {   // base: free pages in the round before this CTA's part; returns those of the round
+        const long long first = round * per_round + ((long long)rank * kPagesThreads + threadIdx.x) * kPagesPerThread;
+        bits = pages_look(s, refs, num_pages, first, turn, before);
+        cluster_sync_all();
+        int all = 0;
+        base = 0;
+        for (int c = 0; c < cluster; ++c) {
+            const int x = __float_as_int(cluster_ld(cluster_map(count_at + 4 * turn, c)));
+            if (c < rank) base += x;
+            all += x;
+        }
+        turn ^= 1;   // (a count is written again only after another meeting, by when all have read it)
+        return all;
+    };
+    int base = 0;
+    for (; rounds * per_round < num_pages && found < total; ++rounds) found += look(rounds, base);
+    // (one round, the usual case: its bits are still there; otherwise the counts are looked over again, in L2)
+    int seen = 0;
+    for (int r = 0; r < rounds && seen < total; ++r) {
+        const int all = rounds > 1 ? look(r, base) : found;
+        int at = seen + base + before;
+        const int first = (int)(r * per_round + ((long long)rank * kPagesThreads + threadIdx.x) * kPagesPerThread);
+        for (uint32_t left = bits; left != 0 && at < total; left &= left - 1, ++at) {
+            int lo = 0, hi = n_items - 1;      // the first item whose range ends past `at`
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (s.upto[mid] > at) hi = mid;
+                else lo = mid + 1;
+            }
+            if (s.upto[lo] <= found) give(lo, at - (lo > 0 ? s.upto[lo - 1] : 0), first + __ffs(left) - 1);
+        }
+        seen += all;
+    }
+    return found;
+}
+
+struct ResizeParams {
+    int* table;       // [B,table_stride]
+    int* held;        // [B]
+    int* refs;        // [num_pages]
+    const int* want;  // [B] rows
+    int* n_short;     // [1]
+    int B, max_pages, table_stride, page_size, num_pages;
+};
+
+// Sequence b is to hold ceil(want[b] / page_size) pages.  grid: one cluster.
+__global__ void __launch_bounds__(kPagesThreads) fa_pages_resize_kernel(const ResizeParams p, int cluster) {
+    __shared__ PagesShared s;
+    __shared__ int shorts;
+    const int tid = threadIdx.x, rank = blockIdx.x, lane = tid & 31;
+    grid_dep_wait();
+    auto had = [&](int b) { return max(0, min(p.held[b], p.max_pages)); };
+    auto need = [&](int b) { return (int)(((long long)max(p.want[b], 0) + p.page_size - 1) / p.page_size); };
+    // what is given back, a warp per sequence
+    for (int b = rank * 32 + (tid >> 5); b < p.B; b += cluster * 32) {
+        int* row = p.table + (long long)b * p.table_stride;
+        for (int e = need(b) + lane; e < had(b); e += 32) {
+            const int page = row[e];
+            if (page >= 0 && page < p.num_pages) atomicSub(p.refs + page, 1);
+            row[e] = -1;
+        }
+    }
+    pages_prefix(s, p.B, [&](int b) { return need(b) > p.max_pages ? 0 : max(need(b) - had(b), 0); });
+    if (tid == 0) shorts = 0;
+    __threadfence();
+    cluster_sync_all();
+    const int found = pages_distribute(s, p.refs, p.num_pages, p.B, rank, cluster, [&](int b, int i, int page) {
+        p.table[(long long)b * p.table_stride + had(b) + i] = page;
+        p.refs[page] = 1;
+    });
+    cluster_sync_all();   // held has been read, and so have the others' counts
+    if (rank != 0) return;
+    int mine = 0;
+    for (int b = tid; b < p.B; b += kPagesThreads) {
+        const int n = need(b), h = had(b);
+        const bool ok = n <= h || (n <= p.max_pages && s.upto[b] <= found);
+        if (ok) p.held[b] = n;
+        else ++mine;
+    }
+    if (mine) atomicAdd(&shorts, mine);
+    __syncthreads();
+    if (tid == 0) *p.n_short = shorts;
+}
+
+struct ForkParams {
+    uint4* k;
+    uint4* v;
+    int* table;
+    int* held;
+    int* seqlens;
+    int* refs;
+    const int* src;   // [n]
+    const int* dst;
+    int* n_short;
+    int n, B, layers, page_size, num_pages, max_pages, table_stride;
+    int row_vecs;
+    long long layer_stride;
+};
+
+// The tables of a fork: dst[i] gets src[i]'s full pages, and a fresh one for a last page that is partly filled.  grid: one cluster.
+__global__ void __launch_bounds__(kPagesThreads) fa_pages_fork_kernel(const ForkParams p, int cluster) {
+    __shared__ PagesShared s;
+    __shared__ int shorts;
+    const int tid = threadIdx.x, rank = blockIdx.x, lane = tid & 31;
+    grid_dep_wait();
+    auto ok_pair = [&](int i) { return p.src[i] >= 0 && p.src[i] < p.B && p.dst[i] >= 0 && p.dst[i] < p.B; };
+    auto rows = [&](int i) { return (int)max(0ll, min((long long)p.seqlens[p.src[i]], (long long)p.max_pages * p.page_size)); };
+    pages_prefix(s, p.n, [&](int i) { return ok_pair(i) && rows(i) % p.page_size != 0 ? 1 : 0; });
+    if (tid == 0) shorts = 0;
+    const int found = pages_distribute(s, p.refs, p.num_pages, p.n, rank, cluster, [&](int i, int, int page) {
+        p.table[(long long)p.dst[i] * p.table_stride + rows(i) / p.page_size] = page;
+        p.refs[page] = 1;
+    });
+    for (int i = rank * 32 + (tid >> 5); i < p.n; i += cluster * 32) {   // a warp per pair
+        if (!ok_pair(i)) continue;
+        const int len = rows(i), full = len / p.page_size;
+        const bool part = len % p.page_size != 0, served = !part || s.upto[i] <= found;
+        const int* from = p.table + (long long)p.src[i] * p.table_stride;
+        int* to = p.table + (long long)p.dst[i] * p.table_stride;
+        for (int e = lane; e < p.max_pages; e += 32) {
+            if (served && e < full) {
+                const int page = from[e];
+                to[e] = page;
+                if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
+            } else if (!(served && part && e == full)) {
+                to[e] = -1;
+            }
+        }
+    }
+    cluster_sync_all();   // the lengths have been read, and so have the others' counts
+    if (rank != 0) return;
+    int mine = 0;
+    for (int i = tid; i < p.n; i += kPagesThreads) {
+        if (!ok_pair(i)) continue;
+        const int len = rows(i);
+        const bool part = len % p.page_size != 0, served = !part || s.upto[i] <= found;
+        p.held[p.dst[i]] = served ? len / p.page_size + (part ? 1 : 0) : 0;
+        p.seqlens[p.dst[i]] = served ? len : 0;
+        if (!served) ++mine;
+    }
+    if (mine) atomicAdd(&shorts, mine);
+    __syncthreads();
+    if (tid == 0) *p.n_short = shorts;
+}
+
+// The rows of a fork: the filled rows of each last page, in every plane.  They lie one after the other.
+// grid: (parts, planes, pairs)
+constexpr int kForkThreads = 256;
+constexpr int kForkBatch = 8;
+__global__ void __launch_bounds__(kForkThreads) fa_pages_fork_copy_kernel(const ForkParams p) {
+    grid_dep_wait();
+    const int i = blockIdx.z, a = p.src[i], b = p.dst[i];
+    if (a < 0 || a >= p.B || b < 0 || b >= p.B) return;
+    const int len = p.seqlens[b];          // (0 where it was not served)
+    const int rows = len % p.page_size, e = len / p.page_size;
+    if (rows <= 0 || e >= p.max_pages) return;
+    const int from = p.table[(long long)a * p.table_stride + e], to = p.table[(long long)b * p.table_stride + e];
+    if (from < 0 || from >= p.num_pages || to < 0 || to >= p.num_pages) return;
+    uint4* base = (blockIdx.y & 1 ? p.v : p.k) + (long long)(blockIdx.y >> 1) * p.layer_stride;
+    const long long page_vecs = (long long)p.page_size * p.row_vecs;
+    const uint4* x = base + from * page_vecs;
+    uint4* y = base + to * page_vecs;
+    const int n = rows * p.row_vecs;
+    for (int u0 = blockIdx.x * kForkThreads * kForkBatch; u0 < n; u0 += gridDim.x * kForkThreads * kForkBatch) {
+        uint4 r[kForkBatch];
+#pragma unroll
+        for (int j = 0; j < kForkBatch; ++j) {
+            const int u = u0 + j * kForkThreads + threadIdx.x;
+            if (u < n) r[j] = x[u];
+        }
+#pragma unroll
+        for (int j = 0; j < kForkBatch; ++j) {
+            const int u = u0 + j * kForkThreads + threadIdx.x;
+            if (u < n) y[u] = r[j];
+        }
+    }
+}
+
+}  // namespace fa

@@ -73,7 +73,41 @@ struct DecodeParams {
     // sequences, and the tiles per chunk that are enough whatever the lengths are
     int slots = 0, most_tiles = 0;
     int bf16_io = 0;      // 8-bit cache kernel only: q and o are bf16 (fp16 otherwise)
+    // the query rows are the nodes of a tree (kDecTree): the last tree_lens[b] rows (all Sq where it is nullptr) of a sequence's
+    // cache, and node t sees node j iff bit j % 32 of word j / 32 of its row of the mask is set
+    const int* tree_lens = nullptr;   // [B] device
+    const int* tree_mask = nullptr;   // [B,Sq,mask_words] device, sequences mask_stride words apart
+    int mask_words = 0;
+    long long mask_stride = 0;
 };
+
+// What the query rows of a sequence are: one row, the last Sq positions of its cache in their order, or a tree's nodes.
+constexpr int kDecOne = 0, kDecAppend = 1, kDecTree = 2;
+
+// Which keys a node of a tree sees, 32 at a time.
+struct TreeRow {
+    const int* words = nullptr;   // its row of the mask; nullptr: a row that sees nothing
+    int n_words = 0;
+    // live: the sequence's nodes; node: this row's
+    __device__ __forceinline__ TreeRow(const int* mask, int n_words, int node, int live)
+        : words(node < live ? mask + (long long)node * n_words : nullptr), n_words(n_words) {}
+    __device__ __forceinline__ uint32_t word(int w) const {
+        return w < 0 ? 0xffffffffu : w < n_words ? (uint32_t)words[w] : 0u;   // (every key before the tree)
+    }
+    // Bit i: the key that is `first` + i nodes into the tree (first < 0: so many keys before it).
+    __device__ __forceinline__ uint32_t keys(int first) const {
+        if (words == nullptr) return 0u;
+        if (first <= -32) return 0xffffffffu;
+        const int w = first >> 5;
+        return __funnelshift_r(word(w), word(w + 1), (uint32_t)first & 31u);
+    }
+};
+// Nodes of a sequence of len keys.
+__device__ __forceinline__ int tree_nodes(const int* tree_lens, int b, int T, int len) {
+    return max(0, min(tree_lens != nullptr ? min(tree_lens[b], T) : T, len));
+}
+// The low n bits (all for n >= 32, none for n <= 0).
+__device__ __forceinline__ uint32_t low_bits(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
 
 // ---------------------------------------------------------------------------------------
@@ -287,16 +321,18 @@ __device__ __forceinline__ void dec_store4(void* o, long long at, const float4& 
 // keys of V by transposing ldmatrix, B = P^T, which is the accumulator layout of S^T transposed
 // 8 x 8 with movmatrix).  A tile then takes half the MMAs, a thread holds half the scores and
 // half the accumulators, and the row maxima and sums run over the lanes that share a column.
-// q_col: the query row that is this thread's column g of q^T (nullptr: padding).  kMulti: hide0,
+// q_col: the query row that is this thread's column g of q^T (nullptr: padding).  kForm == kDecAppend: hide0,
 // hide1 say how many of the sequence's last keys the rows in this thread's accumulator columns
 // 2 t4, 2 t4 + 1 must not see (they came after the row's token).
 // Leaves each warp's (max, sum, O) in mo / ml in the layout the merge expects; returns false
 // after a wait that gave up.
-template <bool kMulti, typename T, int D, bool kLower>
+// kForm == kDecTree: row0, row1 and `prefix`, the keys before the tree, say what those rows see instead.
+template <int kForm, typename T, int D, bool kLower>
 __device__ __forceinline__ bool dec_consume_key_rows(const DecodeParams& p, uint64_t* bars, volatile uint32_t* abort_flag,
                                                      uint32_t sK, uint32_t sV, float* mo, float* ml, int warp, int lane,
-                                                     const T* q_col, int hide0, int hide1, int len, int k_begin, int k_end,
-                                                     int n_tiles) {
+                                                     const T* q_col, int hide0, int hide1, const TreeRow& row0, const TreeRow& row1,
+                                                     int prefix, int len, int k_begin, int k_end, int n_tiles) {
+    constexpr bool kMulti = kForm != kDecOne;
     constexpr int kStages = DecShape<D>::kStages, kTileB = DecShape<D>::kTileBytes;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     const int g = lane >> 2, t4 = lane & 3;
@@ -351,16 +387,24 @@ __device__ __forceinline__ bool dec_consume_key_rows(const DecodeParams& p, uint
             // ---- mask, running max, probabilities
             // keys of this warp's 32 that a row may see: all valid ones, minus (several query
             // rows) those among the sequence's last that came after the row's token
-            const int seen0 = kMulti ? min(valid, len - hide0 - (k_begin + t * kDecTile) - key_w) : valid;
-            const int seen1 = kMulti ? min(valid, len - hide1 - (k_begin + t * kDecTile) - key_w) : valid;
+            const int seen0 = kForm == kDecAppend ? min(valid, len - hide0 - (k_begin + t * kDecTile) - key_w) : valid;
+            const int seen1 = kForm == kDecAppend ? min(valid, len - hide1 - (k_begin + t * kDecTile) - key_w) : valid;
+            uint32_t vis0 = 0, vis1 = 0;   // (a tree: a bit per key)
+            if (kForm == kDecTree) {
+                const int first = k_begin + t * kDecTile + key_w - prefix;
+                vis0 = row0.keys(first) & low_bits(valid);
+                vis1 = row1.keys(first) & low_bits(valid);
+            }
+            auto sees0 = [&](int key) { return kForm == kDecTree ? ((vis0 >> key) & 1u) != 0u : key < seen0; };
+            auto sees1 = [&](int key) { return kForm == kDecTree ? ((vis1 >> key) & 1u) != 0u : key < seen1; };
             float mx0 = -INFINITY, mx1 = -INFINITY;
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb) {
                 const int k_lo = mb * 16 + g;
-                if (k_lo >= seen0) sc[mb][0] = -INFINITY;
-                if (k_lo >= seen1) sc[mb][1] = -INFINITY;
-                if (k_lo + 8 >= seen0) sc[mb][2] = -INFINITY;
-                if (k_lo + 8 >= seen1) sc[mb][3] = -INFINITY;
+                if (!sees0(k_lo)) sc[mb][0] = -INFINITY;
+                if (!sees1(k_lo)) sc[mb][1] = -INFINITY;
+                if (!sees0(k_lo + 8)) sc[mb][2] = -INFINITY;
+                if (!sees1(k_lo + 8)) sc[mb][3] = -INFINITY;
                 mx0 = fmaxf(mx0, fmaxf(sc[mb][0], sc[mb][2]));
                 mx1 = fmaxf(mx1, fmaxf(sc[mb][1], sc[mb][3]));
             }
@@ -384,10 +428,10 @@ __device__ __forceinline__ bool dec_consume_key_rows(const DecodeParams& p, uint
             for (int mb = 0; mb < 2; ++mb) {
                 const int k_lo = mb * 16 + g;
                 float* e = sc[mb];
-                e[0] = (k_lo < seen0) ? fast_exp2(fmaf(e[0], p.scale_log2, nm0)) : 0.f;
-                e[1] = (k_lo < seen1) ? fast_exp2(fmaf(e[1], p.scale_log2, nm1)) : 0.f;
-                e[2] = (k_lo + 8 < seen0) ? fast_exp2(fmaf(e[2], p.scale_log2, nm0)) : 0.f;
-                e[3] = (k_lo + 8 < seen1) ? fast_exp2(fmaf(e[3], p.scale_log2, nm1)) : 0.f;
+                e[0] = sees0(k_lo) ? fast_exp2(fmaf(e[0], p.scale_log2, nm0)) : 0.f;
+                e[1] = sees1(k_lo) ? fast_exp2(fmaf(e[1], p.scale_log2, nm1)) : 0.f;
+                e[2] = sees0(k_lo + 8) ? fast_exp2(fmaf(e[2], p.scale_log2, nm0)) : 0.f;
+                e[3] = sees1(k_lo + 8) ? fast_exp2(fmaf(e[3], p.scale_log2, nm1)) : 0.f;
                 s0 += e[0] + e[2];
                 s1 += e[1] + e[3];
                 // (key g | heads 2 t4, 2 t4 + 1) -> transposed: (head g | keys 2 t4, 2 t4 + 1), the B fragment
@@ -462,10 +506,10 @@ __device__ __forceinline__ bool dec_consume_key_rows(const DecodeParams& p, uint
     return ok;
 }
 
-// kMulti: Sq > 1 query rows per sequence, the last Sq positions of its cache (decoding after
+// kForm == kDecAppend: Sq > 1 query rows per sequence, the last Sq positions of its cache (decoding after
 // several tokens were appended, Appendix C with more than one new token): the 16 MMA rows of a
 // CTA are then (token, head) pairs of one kv head, and query token t sees the keys up to
-// position len - Sq + t.  q is [B,Sq,Hq,d], the partials see DecodeParams.
+// position len - Sq + t.  kForm == kDecTree: the rows are a tree's nodes, which see what its mask says (see TreeRow).  q is [B,Sq,Hq,d], the partials see DecodeParams.
 // grid: (Hkv * ceil(Sq * g / 16), n_chunks, B), or (.., slots, 1) with kDecBalanced, with g = Hq / Hkv.  The kv head is the fastest
 // index: CTAs that run at the same time then read the same keys' rows of neighbouring heads,
 // which are contiguous in the cache (a key's Hkv * D elements), instead of key ranges whole
@@ -481,11 +525,12 @@ __device__ __forceinline__ bool dec_consume_key_rows(const DecodeParams& p, uint
 // next to it, and wait there.  16 sequences of up to 4096 keys, d = 64, 22.3 us with an early release, 20.5
 // without; one of 32768 keys, 24.9 / 23.2; 8 of up to 8000, 30.5 / 29.6; 5 heads x 8192, 7.03 / 6.85; calls
 // of 6 us level.)
-template <bool kMulti, typename T, int D, bool kKeyRows, int kMode>
+template <int kForm, typename T, int D, bool kKeyRows, int kMode>
 __global__ void __launch_bounds__(kDecMmaThreads, DecShape<D>::kCtasPerSm)
 fa_decode_split_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                            const DecodeParams p) {
     extern __shared__ uint8_t smem_raw[];
+    constexpr bool kMulti = kForm != kDecOne;
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     constexpr int kStages = DecShape<D>::kStages, kTileB = DecShape<D>::kTileBytes;
     const uint32_t sK = smem_base;
@@ -619,13 +664,15 @@ fa_decode_split_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
         float* mo = reinterpret_cast<float*>(smem_raw + (smem_base - smem_u32(smem_raw)));  // [4 warps][16 rows][D]
         float* ml = mo + 4 * 16 * D;                                                         // [4][16][2]: m, l
         bool ok = true;
+        const int live = kForm == kDecTree ? tree_nodes(p.tree_lens, b, Sq, len) : 0;
+        auto tree_row = [&](int r) { return TreeRow(kForm == kDecTree ? p.tree_mask + b * p.mask_stride : nullptr, p.mask_words, row_token(r), live); };
         if constexpr (kKeyRows) {
             // column g of q^T is row g of the CTA; accumulator columns 2 t4, 2 t4 + 1 are rows 2 t4, 2 t4 + 1
             const T* q_col = (g < G) ? static_cast<const T*>(p.q) + row_index(g) * D : nullptr;
             const int hide0 = kMulti ? Sq - 1 - row_token(min(2 * t4, G - 1)) : 0;
             const int hide1 = kMulti ? Sq - 1 - row_token(min(2 * t4 + 1, G - 1)) : 0;
-            ok = dec_consume_key_rows<kMulti, T, D, kMode != kDecPlain>(p, bars, &abort_flag, sK, sV, mo, ml, warp, lane, q_col, hide0, hide1,
-                                                    len, k_begin, k_end, n_tiles);
+            ok = dec_consume_key_rows<kForm, T, D, kMode != kDecPlain>(p, bars, &abort_flag, sK, sV, mo, ml, warp, lane, q_col, hide0, hide1,
+                                                    tree_row(min(2 * t4, G - 1)), tree_row(min(2 * t4 + 1, G - 1)), len - live, len, k_begin, k_end, n_tiles);
         } else {
         // Q as A fragments for the D / 16 k-steps (rows >= G are zero)
         uint32_t qa[D / 16][4];
@@ -644,6 +691,7 @@ fa_decode_split_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
         // keys an earlier query token must not see: the last Sq - 1 - t of the sequence
         const int hide_lo = kMulti ? Sq - 1 - row_token(g) : 0;
         const int hide_hi = kMulti ? Sq - 1 - row_token(min(g + 8, G - 1)) : 0;
+        const TreeRow tree_lo = tree_row(min(g, G - 1)), tree_hi = tree_row(min(g + 8, G - 1));
         float o[D / 8][4];
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -686,16 +734,24 @@ fa_decode_split_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 // ---- mask, running max, probabilities
                 // keys of this warp's 32 that the row may see: all valid ones, minus (several query
                 // rows) those among the sequence's last that came after the row's token
-                const int seen_lo = kMulti ? min(valid, len - hide_lo - (k_begin + t * kDecTile) - key_w) : valid;
-                const int seen_hi = kMulti ? min(valid, len - hide_hi - (k_begin + t * kDecTile) - key_w) : valid;
+                const int seen_lo = kForm == kDecAppend ? min(valid, len - hide_lo - (k_begin + t * kDecTile) - key_w) : valid;
+                const int seen_hi = kForm == kDecAppend ? min(valid, len - hide_hi - (k_begin + t * kDecTile) - key_w) : valid;
+                uint32_t vis_lo = 0, vis_hi = 0;   // (a tree: a bit per key)
+                if (kForm == kDecTree) {
+                    const int first = k_begin + t * kDecTile + key_w - (len - live);
+                    vis_lo = tree_lo.keys(first) & low_bits(valid);
+                    vis_hi = tree_hi.keys(first) & low_bits(valid);
+                }
+                auto sees_lo = [&](int key) { return kForm == kDecTree ? ((vis_lo >> key) & 1u) != 0u : key < seen_lo; };
+                auto sees_hi = [&](int key) { return kForm == kDecTree ? ((vis_hi >> key) & 1u) != 0u : key < seen_hi; };
                 float mx_lo = -INFINITY, mx_hi = -INFINITY;
 #pragma unroll
                 for (int nb = 0; nb < 4; ++nb) {
                     const int k0 = nb * 8 + 2 * t4;
-                    if (k0 >= seen_lo) sc[nb][0] = -INFINITY;
-                    if (k0 + 1 >= seen_lo) sc[nb][1] = -INFINITY;
-                    if (k0 >= seen_hi) sc[nb][2] = -INFINITY;
-                    if (k0 + 1 >= seen_hi) sc[nb][3] = -INFINITY;
+                    if (!sees_lo(k0)) sc[nb][0] = -INFINITY;
+                    if (!sees_lo(k0 + 1)) sc[nb][1] = -INFINITY;
+                    if (!sees_hi(k0)) sc[nb][2] = -INFINITY;
+                    if (!sees_hi(k0 + 1)) sc[nb][3] = -INFINITY;
                     mx_lo = fmaxf(mx_lo, fmaxf(sc[nb][0], sc[nb][1]));
                     mx_hi = fmaxf(mx_hi, fmaxf(sc[nb][2], sc[nb][3]));
                 }
@@ -717,10 +773,10 @@ fa_decode_split_mma_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
 #pragma unroll
                 for (int nb = 0; nb < 4; ++nb) {
                     const int k0 = nb * 8 + 2 * t4;
-                    sc[nb][0] = (k0 < seen_lo) ? fast_exp2(fmaf(sc[nb][0], p.scale_log2, nm_lo)) : 0.f;
-                    sc[nb][1] = (k0 + 1 < seen_lo) ? fast_exp2(fmaf(sc[nb][1], p.scale_log2, nm_lo)) : 0.f;
-                    sc[nb][2] = (k0 < seen_hi) ? fast_exp2(fmaf(sc[nb][2], p.scale_log2, nm_hi)) : 0.f;
-                    sc[nb][3] = (k0 + 1 < seen_hi) ? fast_exp2(fmaf(sc[nb][3], p.scale_log2, nm_hi)) : 0.f;
+                    sc[nb][0] = sees_lo(k0) ? fast_exp2(fmaf(sc[nb][0], p.scale_log2, nm_lo)) : 0.f;
+                    sc[nb][1] = sees_lo(k0 + 1) ? fast_exp2(fmaf(sc[nb][1], p.scale_log2, nm_lo)) : 0.f;
+                    sc[nb][2] = sees_hi(k0) ? fast_exp2(fmaf(sc[nb][2], p.scale_log2, nm_hi)) : 0.f;
+                    sc[nb][3] = sees_hi(k0 + 1) ? fast_exp2(fmaf(sc[nb][3], p.scale_log2, nm_hi)) : 0.f;
                     s_lo += sc[nb][0] + sc[nb][1];
                     s_hi += sc[nb][2] + sc[nb][3];
                 }

@@ -17,9 +17,11 @@
 #include "prefill_d64.cuh"
 #include "prefill_d64_stream.cuh"
 #include "prefill_d256.cuh"
+#include "cache_pages.cuh"
 #include "decode_fp8.cuh"
 #include "prefill_pipelined.cuh"
 #include "prefill_simple.cuh"
+#include "spec_verify.cuh"
 
 namespace {
 
@@ -125,6 +127,16 @@ int encode_map_matrix(CUtensorMap* tm, const void* base, int rows, int cols, boo
 
 // a page holds a multiple of the 128-key tile, or 16, 32 or 64 keys (several pages per tile)
 bool page_size_ok(int ps) { return ps > 0 && (ps % fa::kDecTile == 0 || ps == 16 || ps == 32 || ps == 64); }
+
+// A block table's sizes, of the decode forms that take a parameter block.
+int check_table(int num_pages, int page_size, int max_pages, int table_stride, const int* block_table) {
+    if (num_pages < 0 || max_pages < 0 || !page_size_ok(page_size)) return FA_ERR_SHAPE;
+    if (table_stride < max_pages) return FA_ERR_SHAPE;
+    if ((long long)max_pages * page_size > 0x7fffffffll) return FA_ERR_SHAPE;
+    if (max_pages > 0 && num_pages == 0) return FA_ERR_SHAPE;
+    if (reinterpret_cast<uintptr_t>(block_table) & 3u) return FA_ERR_ALIGN;
+    return FA_OK;
+}
 
 // sms: receives the device's SM count
 int check_device(int* sms = nullptr) {
@@ -441,8 +453,8 @@ int decode_chunk(int B, int Hkv, int Smax, bool long_ok = false) {
 // The clusters of a decode kernel that run at a time; kind: 0 = 16-bit, d = 128; 1 = 16-bit, d = 64; 2 = 8-bit.
 int decode_cluster_slots(int kind, fa::ClusterSlots* out) {
     const void* kern = kind == 2   ? reinterpret_cast<const void*>(fa::fa_decode_split_fp8_kernel<1, fa::kDecCluster>)
-                       : kind == 1 ? reinterpret_cast<const void*>(fa::fa_decode_split_mma_kernel<false, __half, 64, true, fa::kDecCluster>)
-                                   : reinterpret_cast<const void*>(fa::fa_decode_split_mma_kernel<false, __half, 128, true, fa::kDecCluster>);
+                       : kind == 1 ? reinterpret_cast<const void*>(fa::fa_decode_split_mma_kernel<fa::kDecOne, __half, 64, true, fa::kDecCluster>)
+                                   : reinterpret_cast<const void*>(fa::fa_decode_split_mma_kernel<fa::kDecOne, __half, 128, true, fa::kDecCluster>);
     const int smem = kind == 2 ? fa::kDec8Smem : kind == 1 ? fa::DecShape<64>::kSmem : fa::DecShape<128>::kSmem;
     const int ce = fa::cluster_slots(kern, smem, fa::kDecMmaThreads, out);
     return ce ? cuda_fail(static_cast<cudaError_t>(ce)) : FA_OK;
@@ -845,12 +857,14 @@ size_t fa_decode_append_workspace_bytes(int B, int Sq, int Hq, int Hkv, int Skv_
 }  // extern "C"
 
 namespace {
+constexpr int kTreeMaxNodes = 256;   // fa_decode_tree
+
 // The argument checks every 16-bit decode entry point shares, in the order the header documents
 // (shape, unsupported, NULL, alignment); no CUDA call.  B == 0 passes: the caller returns FA_OK.
 int decode_check_args(const void* q, const void* k_cache, const void* v_cache, const void* o, const int* seqlens_k,
-                      int B, int Hq, int Hkv, int Skv_max, int d, float scale, int Sq) {
+                      int B, int Hq, int Hkv, int Skv_max, int d, float scale, int Sq, int max_rows = 64) {
     if (B < 0 || Hq <= 0 || Hkv <= 0 || Skv_max < 0 || d <= 0 || Sq < 1) return FA_ERR_SHAPE;
-    if (Sq > 64 || Sq > Skv_max) return FA_ERR_UNSUPPORTED;   // several query rows are the LAST rows of the cache
+    if (Sq > max_rows || Sq > Skv_max) return FA_ERR_UNSUPPORTED;   // several query rows are the LAST rows of the cache
     if (Hq % Hkv) return FA_ERR_SHAPE;
     if (d != 128 && d != 64) return FA_ERR_UNSUPPORTED;
     if (!(scale >= 0.f) || isinf(scale)) return FA_ERR_UNSUPPORTED;
@@ -883,14 +897,15 @@ int decode_launch(const CUtensorMap& tk, const CUtensorMap& tv, const fa::Decode
         // at most 8 (token, head) rows per kv head: the keys-as-rows form of the consumers
         const bool key_rows = g * Sq <= 8;
         using Kernel = void (*)(CUtensorMap, CUtensorMap, fa::DecodeParams);
-        // by type, several query rows, consumer form, and how the sequences are cut
-        static const Kernel kernels[2][2][2][3] = {
+        // by type, what the query rows are, consumer form, and how the sequences are cut
+        static const Kernel kernels[2][3][2][3] = {
 #define FA_DEC(T, M, R) {fa::fa_decode_split_mma_kernel<M, T, D, R, fa::kDecPlain>, fa::fa_decode_split_mma_kernel<M, T, D, R, fa::kDecCluster>, fa::fa_decode_split_mma_kernel<M, T, D, R, fa::kDecBalanced>}
-            {{FA_DEC(__half, false, false), FA_DEC(__half, false, true)}, {FA_DEC(__half, true, false), FA_DEC(__half, true, true)}},
-            {{FA_DEC(__nv_bfloat16, false, false), FA_DEC(__nv_bfloat16, false, true)},
-             {FA_DEC(__nv_bfloat16, true, false), FA_DEC(__nv_bfloat16, true, true)}}};
+#define FA_DEC_FORMS(T) {{FA_DEC(T, fa::kDecOne, false), FA_DEC(T, fa::kDecOne, true)}, {FA_DEC(T, fa::kDecAppend, false), FA_DEC(T, fa::kDecAppend, true)}, {FA_DEC(T, fa::kDecTree, false), FA_DEC(T, fa::kDecTree, true)}}
+            FA_DEC_FORMS(__half), FA_DEC_FORMS(__nv_bfloat16)};
+#undef FA_DEC_FORMS
 #undef FA_DEC
-        const Kernel kern = kernels[bf16][Sq > 1][key_rows][dp.slots > 0 ? fa::kDecBalanced : dp.clustered ? fa::kDecCluster : fa::kDecPlain];
+        const int form = dp.tree_mask != nullptr ? fa::kDecTree : Sq > 1 ? fa::kDecAppend : fa::kDecOne;
+        const Kernel kern = kernels[bf16][form][key_rows][dp.slots > 0 ? fa::kDecBalanced : dp.clustered ? fa::kDecCluster : fa::kDecPlain];
         if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count))
             return cuda_fail(static_cast<cudaError_t>(ce));
         dim3 grid(Hkv * ((g * Sq + 15) / 16), dp.n_chunks, B);   // 16 (token, head) rows per CTA
@@ -910,8 +925,8 @@ int decode_launch(const CUtensorMap& tk, const CUtensorMap& tv, const fa::Decode
 int decode_impl(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse, const int* seqlens_k,
                 int B, int Hq, int Hkv, int Skv_max, int d, float scale, void* workspace, size_t workspace_bytes,
                 void* stream, const int* block_table, int num_pages, int page_size, int table_stride, int Sq = 1,
-                bool bf16 = false) {
-    int rc = decode_check_args(q, k_cache, v_cache, o, seqlens_k, B, Hq, Hkv, Skv_max, d, scale, Sq);
+                bool bf16 = false, const fa_tree_params* tree = nullptr) {
+    int rc = decode_check_args(q, k_cache, v_cache, o, seqlens_k, B, Hq, Hkv, Skv_max, d, scale, Sq, tree ? kTreeMaxNodes : 64);
     if (rc) return rc;
     if (B == 0) return FA_OK;
     if (!aligned16(workspace)) return FA_ERR_ALIGN;
@@ -940,6 +955,12 @@ int decode_impl(const void* q, const void* k_cache, const void* v_cache, void* o
     dp.page_size = block_table ? page_size : 1;
     dp.table_stride = table_stride;
     dp.v_scale = 1.f;
+    if (tree) {
+        dp.tree_lens = tree->tree_lens;
+        dp.tree_mask = tree->mask;
+        dp.mask_words = (Sq + 31) / 32;
+        dp.mask_stride = tree->mask_stride;
+    }
     // one chunk per sequence, or one cluster: the split kernel writes the result itself, no merge kernel
     const bool direct = Skv_max > 0 && (dp.n_chunks == 1 || dp.clustered);
     dp.o_final = direct ? o : nullptr;
@@ -1053,17 +1074,186 @@ int fa_decode_ex(const fa_decode_params* p, void* stream) {
     if (p->dtype != FA_DTYPE_FP16 && p->dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
     const int Sq = p->Sq > 0 ? p->Sq : 1;
     if (p->block_table) {
-        if (p->num_pages < 0 || p->max_pages < 0 || !page_size_ok(p->page_size)) return FA_ERR_SHAPE;
-        if (p->table_stride < p->max_pages) return FA_ERR_SHAPE;
-        if ((long long)p->max_pages * p->page_size > 0x7fffffffll) return FA_ERR_SHAPE;
-        if (p->max_pages > 0 && p->num_pages == 0) return FA_ERR_SHAPE;
-        if (reinterpret_cast<uintptr_t>(p->block_table) & 3u) return FA_ERR_ALIGN;
+        if (int rc = check_table(p->num_pages, p->page_size, p->max_pages, p->table_stride, p->block_table)) return rc;
         return decode_impl(p->q, p->k, p->v, p->o, p->lse, p->seqlens_k, p->B, p->Hq, p->Hkv, p->max_pages * p->page_size,
                            p->d, p->scale, p->workspace, p->workspace_bytes, stream, p->block_table, p->num_pages,
                            p->page_size, p->table_stride, Sq, p->dtype == FA_DTYPE_BF16);
     }
     return decode_impl(p->q, p->k, p->v, p->o, p->lse, p->seqlens_k, p->B, p->Hq, p->Hkv, p->Skv_max, p->d, p->scale,
                        p->workspace, p->workspace_bytes, stream, nullptr, 0, 0, 0, Sq, p->dtype == FA_DTYPE_BF16);
+}
+
+size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d) {
+    return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
+}
+
+int fa_decode_tree(const fa_tree_params* p, void* stream) {
+    if (!p) return FA_ERR_NULL;
+    if (p->dtype != FA_DTYPE_FP16 && p->dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    int Skv_max = p->Skv_max;
+    if (p->block_table) {
+        if (int rc = check_table(p->num_pages, p->page_size, p->max_pages, p->table_stride, p->block_table)) return rc;
+        Skv_max = p->max_pages * p->page_size;
+    }
+    if (p->mask_stride < 0) return FA_ERR_SHAPE;
+    if (p->B > 0 && !p->mask) return FA_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(p->mask) | reinterpret_cast<uintptr_t>(p->tree_lens) | reinterpret_cast<uintptr_t>(p->seqlens_k) |
+         reinterpret_cast<uintptr_t>(p->lse)) & 3u)
+        return FA_ERR_ALIGN;
+    return decode_impl(p->q, p->k, p->v, p->o, p->lse, p->seqlens_k, p->B, p->Hq, p->Hkv, Skv_max, p->d, p->scale, p->workspace,
+                       p->workspace_bytes, stream, p->block_table, p->num_pages, p->block_table ? p->page_size : 0, p->table_stride,
+                       p->T, p->dtype == FA_DTYPE_BF16, p);
+}
+
+int fa_spec_verify(const void* target_probs, const void* draft_probs, const int* tokens, const int* parents,
+                   const int* tree_lens, const float* uniforms, const float* noise, int* n_accept, int* path, int* out_tokens,
+                   int B, int T, int V, int dtype, void* stream) {
+    if (B < 0 || T <= 0 || V <= 0) return FA_ERR_SHAPE;
+    if (T > fa::kVerifyMaxNodes || V > (1 << 30) || B > 65535) return FA_ERR_UNSUPPORTED;
+    if (dtype != FA_DTYPE_FP16 && dtype != FA_DTYPE_BF16 && dtype != FA_DTYPE_FP32) return FA_ERR_UNSUPPORTED;
+    if (B == 0) return FA_OK;
+    if (!target_probs || !tokens || !parents || !uniforms || !noise || !n_accept || !path || !out_tokens) return FA_ERR_NULL;
+    const uintptr_t probs = reinterpret_cast<uintptr_t>(target_probs) | reinterpret_cast<uintptr_t>(draft_probs);
+    const uintptr_t words = reinterpret_cast<uintptr_t>(tokens) | reinterpret_cast<uintptr_t>(parents) | reinterpret_cast<uintptr_t>(tree_lens) |
+                            reinterpret_cast<uintptr_t>(uniforms) | reinterpret_cast<uintptr_t>(noise) | reinterpret_cast<uintptr_t>(n_accept) |
+                            reinterpret_cast<uintptr_t>(path) | reinterpret_cast<uintptr_t>(out_tokens);
+    if ((words & 3u) || (probs & (dtype == FA_DTYPE_FP32 ? 3u : 1u))) return FA_ERR_ALIGN;
+    int sms = 0;
+    if (int rc = check_device(&sms)) return rc;
+    fa::VerifyParams vp;
+    vp.p = target_probs;
+    vp.q = draft_probs;
+    vp.tokens = tokens;
+    vp.parents = parents;
+    vp.tree_lens = tree_lens;
+    vp.uniforms = uniforms;
+    vp.noise = noise;
+    vp.n_accept = n_accept;
+    vp.path = path;
+    vp.out_tokens = out_tokens;
+    vp.T = T;
+    vp.V = V;
+    int cluster = fa::kVerifyMaxCluster;
+    while (cluster > 1 && ((long long)B * cluster > 2ll * sms || V / cluster < 1024)) cluster /= 2;
+    const bool vec = V % 4 == 0 && (probs & (dtype == FA_DTYPE_FP32 ? 15u : 7u)) == 0 && aligned16(noise);
+    using Kernel = void (*)(fa::VerifyParams, int);
+    static const Kernel kernels[3][2] = {{fa::fa_spec_verify_kernel<__half, false>, fa::fa_spec_verify_kernel<__half, true>},
+                                         {fa::fa_spec_verify_kernel<__nv_bfloat16, false>, fa::fa_spec_verify_kernel<__nv_bfloat16, true>},
+                                         {fa::fa_spec_verify_kernel<float, false>, fa::fa_spec_verify_kernel<float, true>}};
+    const cudaError_t e = fa::launch_dependent_clusters(kernels[dtype][vec], dim3(B * cluster), cluster, 1, fa::kVerifyThreads, 0,
+                                                        static_cast<cudaStream_t>(stream), vp, cluster);
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlens_k, const int* tree_lens, const int* path,
+                     const int* n_accept, int* new_lens, int layers, int64_t layer_stride, int B, int T, int Skv_max, int num_pages,
+                     int page_size, int max_pages, int table_stride, int row_bytes, void* stream) {
+    if (B < 0 || T <= 0 || layers < 0 || row_bytes <= 0 || layer_stride < 0) return FA_ERR_SHAPE;
+    if (block_table) {
+        if (num_pages < 0 || max_pages < 0 || page_size <= 0 || table_stride < max_pages) return FA_ERR_SHAPE;
+        if ((long long)max_pages * page_size > 0x7fffffffll) return FA_ERR_SHAPE;
+    } else if (Skv_max < 0) return FA_ERR_SHAPE;
+    if (B > 65535) return FA_ERR_UNSUPPORTED;
+    if (B == 0) return FA_OK;
+    if (!seqlens_k || !path || !n_accept || !new_lens) return FA_ERR_NULL;
+    if (layers > 0 && (!k || !v)) return FA_ERR_NULL;
+    if (row_bytes % 16 || layer_stride % 16 || !aligned16(k) || !aligned16(v)) return FA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(seqlens_k) | reinterpret_cast<uintptr_t>(tree_lens) |
+         reinterpret_cast<uintptr_t>(path) | reinterpret_cast<uintptr_t>(n_accept) | reinterpret_cast<uintptr_t>(new_lens)) & 3u)
+        return FA_ERR_ALIGN;
+    int sms = 0;
+    if (int rc = check_device(&sms)) return rc;
+    fa::CompactParams cp;
+    cp.k = static_cast<char*>(k);
+    cp.v = static_cast<char*>(v);
+    cp.seqlens = seqlens_k;
+    cp.tree_lens = tree_lens;
+    cp.path = path;
+    cp.n_accept = n_accept;
+    cp.new_lens = new_lens;
+    cp.block_table = block_table;
+    cp.B = B;
+    cp.T = T;
+    cp.layers = layers;
+    cp.page_size = block_table ? page_size : 1;
+    cp.table_stride = table_stride;
+    cp.max_rows = block_table ? max_pages * page_size : Skv_max;
+    cp.num_pages = num_pages;
+    cp.row_vecs = row_bytes / 16;
+    cp.layer_stride = layer_stride / 16;
+    const long long blocks = (2ll * layers * cp.row_vecs + fa::kCompactThreads - 1) / fa::kCompactThreads;
+    const long long most = 8ll * sms / B;   // as many as run at once
+    const int grid = (int)(blocks < most ? (blocks > 0 ? blocks : 1) : (most > 0 ? most : 1));
+    const cudaError_t e = fa::launch_dependent(fa::fa_cache_compact_kernel, dim3(grid, B), fa::kCompactThreads, 0, static_cast<cudaStream_t>(stream), cp);
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+// CTAs of the one cluster that looks a pool's reference counts over.
+static int pages_cluster(int num_pages) {
+    int c = 1;
+    while (c < fa::kPagesMaxCluster && (long long)c * fa::kPagesThreads * fa::kPagesPerThread < num_pages) c *= 2;
+    return c;
+}
+
+int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int* n_short, int B, int num_pages, int page_size,
+                    int max_pages, int table_stride, void* stream) {
+    if (B < 0 || num_pages < 0 || page_size <= 0 || max_pages < 0 || table_stride < max_pages) return FA_ERR_SHAPE;
+    if (B > fa::kPagesMaxItems) return FA_ERR_UNSUPPORTED;
+    if (B == 0) return FA_OK;
+    if (!block_table || !held || !refs || !want || !n_short) return FA_ERR_NULL;
+    if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(held) | reinterpret_cast<uintptr_t>(refs) |
+         reinterpret_cast<uintptr_t>(want) | reinterpret_cast<uintptr_t>(n_short)) & 3u)
+        return FA_ERR_ALIGN;
+    if (int rc = check_device()) return rc;
+    fa::ResizeParams rp = {block_table, held, refs, want, n_short, B, max_pages, table_stride, page_size, num_pages};
+    const int cluster = pages_cluster(num_pages);
+    const cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_resize_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, 0,
+                                                        static_cast<cudaStream_t>(stream), rp, cluster);
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k, int* refs, const int* src, const int* dst,
+                  int* n_short, int n, int layers, int64_t layer_stride, int B, int num_pages, int page_size, int max_pages,
+                  int table_stride, int row_bytes, void* stream) {
+    if (n < 0 || B < 0 || layers < 0 || layer_stride < 0 || num_pages < 0 || page_size <= 0 || max_pages < 0 || table_stride < max_pages || row_bytes <= 0)
+        return FA_ERR_SHAPE;
+    if ((long long)max_pages * page_size > 0x7fffffffll || (long long)page_size * (row_bytes / 16) > 0x3fffffffll) return FA_ERR_SHAPE;
+    if (n > fa::kPagesMaxItems || layers > 32767) return FA_ERR_UNSUPPORTED;
+    if (n == 0) return FA_OK;
+    if (!block_table || !held || !seqlens_k || !refs || !src || !dst || !n_short) return FA_ERR_NULL;
+    if (layers > 0 && (!k || !v)) return FA_ERR_NULL;
+    if (row_bytes % 16 || layer_stride % 16 || !aligned16(k) || !aligned16(v)) return FA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(held) | reinterpret_cast<uintptr_t>(seqlens_k) |
+         reinterpret_cast<uintptr_t>(refs) | reinterpret_cast<uintptr_t>(src) | reinterpret_cast<uintptr_t>(dst) |
+         reinterpret_cast<uintptr_t>(n_short)) & 3u)
+        return FA_ERR_ALIGN;
+    if (int rc = check_device()) return rc;
+    fa::ForkParams fp;
+    fp.k = static_cast<uint4*>(k);
+    fp.v = static_cast<uint4*>(v);
+    fp.table = block_table;
+    fp.held = held;
+    fp.seqlens = seqlens_k;
+    fp.refs = refs;
+    fp.src = src;
+    fp.dst = dst;
+    fp.n_short = n_short;
+    fp.n = n;
+    fp.B = B;
+    fp.layers = layers;
+    fp.page_size = page_size;
+    fp.num_pages = num_pages;
+    fp.max_pages = max_pages;
+    fp.table_stride = table_stride;
+    fp.row_vecs = row_bytes / 16;
+    fp.layer_stride = layer_stride / 16;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int cluster = pages_cluster(num_pages);
+    cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_fork_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, 0, st, fp, cluster);
+    if (e != cudaSuccess) return cuda_fail(e);
+    if (layers == 0 || page_size == 1) return FA_OK;   // (a page of one row is never partly filled)
+    e = fa::launch_dependent(fa::fa_pages_fork_copy_kernel, dim3(1, 2 * layers, n), fa::kForkThreads, 0, st, fp);
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
 
 int fa_decode_append(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse,

@@ -1,0 +1,188 @@
+"""The operators of a speculative decoding step on the host: the argument checks of the C entry points (which come before any
+CUDA call), the binding's own, and the pins of the oracle that the GPU tests compare with."""
+import ctypes
+
+import pytest
+import torch
+
+from oracle import speculative as ref
+
+
+@pytest.fixture(scope="module")
+def fa():
+    from paper_2410_16663_b200 import build
+    build.build()
+    from paper_2410_16663_b200 import binding
+    return binding
+
+
+def tree_params(fa, **kw):
+    buf = torch.zeros(1 << 16, dtype=torch.float16)
+    at = (buf.data_ptr() + 15) & ~15
+    p = fa.fa_tree_params()
+    p.q = p.k = p.v = p.o = p.seqlens_k = p.mask = p.workspace = at
+    p.B, p.T, p.Hq, p.Hkv, p.Skv_max, p.d, p.dtype, p.scale = 2, 4, 4, 2, 256, 128, fa.FA_DTYPE_FP16, 0.1
+    p.mask_stride, p.workspace_bytes = 4, 1 << 30
+    for name, value in kw.items():
+        setattr(p, name, at + value[1] if isinstance(value, tuple) else value)
+    p._keep = buf
+    return p
+
+
+def test_tree_attention_refuses_bad_arguments(fa):
+    call = lambda **kw: fa.lib.fa_decode_tree(ctypes.byref(tree_params(fa, **kw)), None)
+    assert fa.lib.fa_decode_tree(None, None) == fa.FA_ERR_NULL
+    assert call(B=0) == fa.FA_OK
+    for kw in (dict(B=-1), dict(T=0), dict(T=-3), dict(Hq=5), dict(Hkv=0), dict(Skv_max=-1), dict(mask_stride=-4), dict(d=0)):
+        assert call(**kw) == fa.FA_ERR_SHAPE, kw
+    for kw in (dict(T=257), dict(T=200, Skv_max=199), dict(d=256), dict(d=96), dict(dtype=fa.FA_DTYPE_FP32), dict(scale=-0.1),
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(B=65536), dict(Hq=70000, Hkv=1)):
+        assert call(**kw) == fa.FA_ERR_UNSUPPORTED, kw
+    for kw in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(mask=None), dict(seqlens_k=None)):
+        assert call(**kw) == fa.FA_ERR_NULL, kw
+    for kw in (dict(q=("at", 2)), dict(k=("at", 8)), dict(v=("at", 8)), dict(o=("at", 4)), dict(workspace=("at", 4)), dict(mask=("at", 2)),
+               dict(tree_lens=("at", 1)), dict(lse=("at", 2)), dict(seqlens_k=("at", 2))):
+        assert call(**kw) == fa.FA_ERR_ALIGN, kw
+    need = fa.fa_decode_tree_workspace_bytes(2, 4, 4, 2, 256, 128)
+    assert need > 0 and fa.fa_decode_tree_workspace_bytes(2, 4, 4, 2, 256, 96) == 0 and fa.fa_decode_tree_workspace_bytes(2, 0, 4, 2, 256, 128) == 0
+    assert call(workspace_bytes=need - 1) == fa.FA_ERR_WORKSPACE and call(workspace=None) == fa.FA_ERR_WORKSPACE
+    paged = dict(block_table=("at", 0), num_pages=8, page_size=64, max_pages=4, table_stride=4)
+    for kw in (dict(page_size=48), dict(page_size=0), dict(table_stride=3), dict(num_pages=-1), dict(num_pages=0),
+               dict(max_pages=1 << 26, table_stride=1 << 26)):
+        assert call(**{**paged, **kw}) == fa.FA_ERR_SHAPE, kw
+    assert call(**{**paged, "block_table": ("at", 2)}) == fa.FA_ERR_ALIGN
+    assert call(**{**paged, "max_pages": 0}) == fa.FA_ERR_UNSUPPORTED        # no room for the tree's own rows
+
+
+def test_verification_refuses_bad_arguments(fa):
+    buf = torch.zeros(4096, dtype=torch.float32)
+    at = (buf.data_ptr() + 15) & ~15
+    names = ["p", "q", "tokens", "parents", "tree_lens", "u", "noise", "n_accept", "path", "out"]
+
+    def call(**kw):
+        a = dict(dict.fromkeys(names, at), B=1, T=2, V=8, dtype=fa.FA_DTYPE_FP32)
+        a.update(kw)
+        return fa.lib.fa_spec_verify(*[a[n] for n in names], a["B"], a["T"], a["V"], a["dtype"], None)
+
+    assert call(B=0) == fa.FA_OK
+    for kw in (dict(B=-1), dict(T=0), dict(V=0)):
+        assert call(**kw) == fa.FA_ERR_SHAPE, kw
+    for kw in (dict(T=257), dict(V=(1 << 30) + 1), dict(B=65536), dict(dtype=3), dict(dtype=-1)):
+        assert call(**kw) == fa.FA_ERR_UNSUPPORTED, kw
+    for n in names:
+        if n not in ("q", "tree_lens"):
+            assert call(**{n: None}) == fa.FA_ERR_NULL, n
+        assert call(**{n: at + 2}) == fa.FA_ERR_ALIGN, n
+    assert call(p=at + 1, dtype=fa.FA_DTYPE_BF16) == fa.FA_ERR_ALIGN
+
+
+def test_cache_operators_refuse_bad_arguments(fa):
+    buf = torch.zeros(4096, dtype=torch.float32)
+    at = (buf.data_ptr() + 15) & ~15
+
+    def compact(**kw):
+        a = dict(k=at, v=at, table=None, lens=at, tree_lens=None, path=at, n=at, new=at, L=1, ls=0, B=1, T=2, S=8, np=0, ps=0, mp=0, ts=0, row=256)
+        a.update(kw)
+        return fa.lib.fa_cache_compact(*a.values(), None)
+
+    assert compact(B=0) == fa.FA_OK
+    paged = dict(table=at, np=4, ps=16, mp=2, ts=2)
+    for kw in (dict(B=-1), dict(T=0), dict(L=-1), dict(row=0), dict(ls=-16), dict(S=-1), {**paged, "ps": 0}, {**paged, "ts": 1},
+               {**paged, "np": -1}, {**paged, "mp": 1 << 28, "ts": 1 << 28}):
+        assert compact(**kw) == fa.FA_ERR_SHAPE, kw
+    assert compact(B=65536) == fa.FA_ERR_UNSUPPORTED
+    for n in ("k", "v", "lens", "path", "n", "new"):
+        assert compact(**{n: None}) == fa.FA_ERR_NULL, n
+    for kw in (dict(row=24), dict(ls=8), dict(k=at + 8), dict(v=at + 4), dict(path=at + 2), dict(new=at + 1), dict(tree_lens=at + 2),
+               {**paged, "table": at + 2}):
+        assert compact(**kw) == fa.FA_ERR_ALIGN, kw
+
+    def resize(**kw):
+        a = dict(table=at, held=at, refs=at, want=at, short=at, B=1, np=8, ps=16, mp=2, ts=2)
+        a.update(kw)
+        return fa.lib.fa_pages_resize(*a.values(), None)
+
+    assert resize(B=0) == fa.FA_OK
+    for kw in (dict(B=-1), dict(np=-1), dict(ps=0), dict(mp=-1), dict(ts=1)):
+        assert resize(**kw) == fa.FA_ERR_SHAPE, kw
+    assert resize(B=4097) == fa.FA_ERR_UNSUPPORTED
+    for n in ("table", "held", "refs", "want", "short"):
+        assert resize(**{n: None}) == fa.FA_ERR_NULL and resize(**{n: at + 2}) == fa.FA_ERR_ALIGN, n
+
+    def fork(**kw):
+        a = dict(k=at, v=at, table=at, held=at, lens=at, refs=at, src=at, dst=at, short=at, n=1, L=1, ls=0, B=2, np=8, ps=16, mp=2, ts=2, row=256)
+        a.update(kw)
+        return fa.lib.fa_pages_fork(*a.values(), None)
+
+    assert fork(n=0) == fa.FA_OK
+    for kw in (dict(n=-1), dict(B=-1), dict(L=-1), dict(ls=-16), dict(np=-1), dict(ps=0), dict(mp=-1), dict(ts=1), dict(row=0),
+               dict(mp=1 << 28, ts=1 << 28)):
+        assert fork(**kw) == fa.FA_ERR_SHAPE, kw
+    for kw in (dict(n=4097), dict(L=32768)):
+        assert fork(**kw) == fa.FA_ERR_UNSUPPORTED, kw
+    for n in ("k", "v", "table", "held", "lens", "refs", "src", "dst", "short"):
+        assert fork(**{n: None}) == fa.FA_ERR_NULL, n
+    for kw in (dict(row=40), dict(ls=8), dict(k=at + 8), dict(v=at + 8), dict(src=at + 2), dict(lens=at + 1), dict(table=at + 2)):
+        assert fork(**kw) == fa.FA_ERR_ALIGN, kw
+
+
+def test_binding_refuses_what_the_library_cannot_see(fa):
+    q = torch.zeros(1, 2, 4, 128, dtype=torch.float16)
+    k = torch.zeros(1, 64, 2, 128, dtype=torch.float16)
+    lens, mask = torch.zeros(1, dtype=torch.int32), torch.zeros(1, 2, 1, dtype=torch.int32)
+    ok = dict(q=q, k=k, v=k, o=q, lse=None, seqlens_k=lens, mask=mask, scale=0.1, workspace=None)
+    for kw in (dict(mask=mask.long()), dict(mask=torch.zeros(1, 2, 2, dtype=torch.int32)), dict(mask=torch.zeros(3, 1, dtype=torch.int32)),
+               dict(k=k.float()), dict(o=q.float()), dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), dict(seqlens_k=lens.long())):
+        with pytest.raises(ValueError):
+            fa.fa_decode_tree(**{**ok, **kw})
+    p = torch.zeros(1, 2, 8)
+    ints, f = torch.zeros(1, 2, dtype=torch.int32), torch.zeros(1, 2)
+    base = [p, p, ints, ints, f, torch.zeros(1, 8), torch.zeros(1, dtype=torch.int32), ints, ints]
+    for i, bad in ((0, p.double()), (1, p.half()), (2, ints.long()), (4, f.double()), (5, torch.zeros(8, 2).T[:1]), (7, ints.long())):
+        args = list(base)
+        args[i] = bad
+        with pytest.raises(ValueError):
+            fa.fa_spec_verify(*args)
+    kk = torch.zeros(2, 4, 16, 2, 64)
+    i1 = torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        fa.fa_cache_compact(kk, kk.half(), i1, ints, i1, i1)
+    with pytest.raises(ValueError):
+        fa.fa_pages_fork(kk, kk, ints, i1, i1, torch.zeros(5, dtype=torch.int32), i1, i1, i1)
+    with pytest.raises(ValueError):
+        fa.fa_pages_resize(ints, i1, torch.zeros(8, dtype=torch.int32)[::2], i1, i1, 16)
+
+
+def test_oracle_verification_draws_from_the_target():
+    """Whatever the draft proposes, the first emitted token is distributed as the target's first row: 6000 trees with two children
+    each over a vocabulary of 5; a frequency of probability p is within 5 sqrt(p (1 - p) / n) of it."""
+    gen = torch.Generator().manual_seed(3)
+    n, V = 6000, 5
+    p = torch.softmax(torch.randn(3, V, generator=gen), -1)
+    for with_q in (True, False):
+        q = torch.softmax(torch.randn(3, V, generator=gen), -1)
+        count = torch.zeros(V, dtype=torch.float64)
+        for _ in range(n):
+            tokens = [0] + (torch.multinomial(q[0], 2, replacement=True, generator=gen).tolist() if with_q else [1, 3])
+            u = torch.rand(3, generator=gen)
+            noise = torch.empty(V).exponential_(generator=gen)
+            _, out = ref.verify(p, q if with_q else None, tokens, [-1, 0, 0], u, noise, 3)
+            count[out[0]] += 1
+        pd = p[0].double()
+        assert ((count / n - pd).abs() <= 5 * (pd * (1 - pd) / n).sqrt()).all(), (with_q, count / n, pd)
+
+
+def test_oracle_tree_attention_of_a_chain_is_causal():
+    import oracle
+    gen = torch.Generator().manual_seed(4)
+    q, k, v = (torch.randn(1, s, h, 64, generator=gen, dtype=torch.float64).half() for s, h in ((6, 4), (19, 2), (19, 2)))
+    see = ref.ancestors([-1, 0, 1, 2, 3, 4])[None]
+    o, lse = ref.tree_attention(q, k, v, [19], see, 0.125)
+    o2, l2 = oracle.attention_full(q, k, v, True, 0.125)
+    assert float((o - o2).abs().max()) < 1e-12 and float((lse - l2).abs().max()) < 1e-12
+
+
+def test_words_of_a_mask():
+    see = torch.zeros(1, 40, dtype=torch.bool)
+    see[0, [0, 31, 32, 39]] = True
+    assert ref.bits_to_words(see).tolist() == [[1 - (1 << 31), 1 + (1 << 7)]]
