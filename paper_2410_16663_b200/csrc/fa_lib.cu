@@ -12,6 +12,7 @@
 #include <mutex>
 
 #include "decode.cuh"
+#include "decode_tree.cuh"
 #include "prefill_pingpong.cuh"
 #include "proj_gemm.cuh"
 #include "prefill_d64.cuh"
@@ -105,9 +106,13 @@ int encode_map_tile(CUtensorMap* tm, const void* base, int B, int S, int H, int6
     return (d == 64 ? encode_map : encode_map_blocks)(tm, base, B, S, H, sb, ss, sh, box_rows, bf16, d);
 }
 
-// Tensor map over a contiguous 16-bit cache [slabs, S, H, d] (d = 128 or 64) with boxes of box_rows keys x all of d.
-int encode_map_cache(CUtensorMap* tm, const void* base, int slabs, int S, int H, int box_rows, bool bf16, int d) {
-    return encode_map_blocks(tm, base, slabs, S, H, (int64_t)S * H * d, (int64_t)H * d, d, box_rows, bf16, d);
+// Tensor map over a contiguous 16-bit cache [slabs, S, H, d] (d = 128 or 64) with boxes of box_rows keys x all of d, or one
+// 64-element block of it.
+int encode_map_cache(CUtensorMap* tm, const void* base, int slabs, int S, int H, int box_rows, bool bf16, int d, bool one_block = false) {
+    const Strides st = legal_strides(slabs, S, H, (int64_t)S * H * d, (int64_t)H * d, d, d);
+    return encode_tiled<5>(tm, type16(bf16), base, {64, (cuuint64_t)S, (cuuint64_t)(d / 64), (cuuint64_t)H, (cuuint64_t)slabs},
+                           {(cuuint64_t)st.s * 2, 128, (cuuint64_t)st.h * 2, (cuuint64_t)st.b * 2},
+                           {64, (cuuint32_t)box_rows, (cuuint32_t)(one_block ? 1 : d / 64), 1, 1});
 }
 
 // Tensor map over a [B, S, H, 128] one-byte tensor, contiguous: a box is box_rows sequence
@@ -980,6 +985,76 @@ int decode_impl(const void* q, const void* k_cache, const void* v_cache, void* o
     return d == 64 ? decode_launch<64>(tk, tv, dp, o, lse, g, bf16, direct, Skv_max > 0, st)
                    : decode_launch<128>(tk, tv, dp, o, lse, g, bf16, direct, Skv_max > 0, st);
 }
+
+// fa_decode_tree with more rows per kv head than the split decode kernel's CTAs have (see decode_tree.cuh).
+constexpr int kTreeFewRows = 16;
+struct TreeBlocks {   // how the rows that share a kv head are cut: blocks of at most two tiles of 128, of equal size in whole warps
+    int blocks, rows;
+    explicit TreeBlocks(int all) : blocks((all + 255) / 256), rows(all) {
+        if (blocks > 1) rows = ((all + blocks - 1) / blocks + 31) / 32 * 32;
+    }
+};
+template <typename T, int D>
+int tree_launch(const CUtensorMap& tk, const CUtensorMap& tv, const fa::TreeParams& tp, int sms, cudaStream_t st) {
+    const bool two = tp.rows > 128;
+    const auto kern = two ? fa::fa_decode_tree_kernel<T, D, 2> : fa::fa_decode_tree_kernel<T, D, 1>;
+    const int smem = two ? fa::TreeShape<D, 2>::kSmem : fa::TreeShape<D, 1>::kSmem, threads = two ? fa::TreeShape<D, 2>::kThreads : fa::TreeShape<D, 1>::kThreads;
+    int sm_count = 0;
+    if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
+    const int grid = sms < fa::kTreeMaxCtas ? sms : fa::kTreeMaxCtas;
+    cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tk, tv, tp);
+    if (e == cudaSuccess && grid > 1)
+        e = fa::launch_dependent(fa::fa_decode_tree_combine_kernel<T, D>, dim3((tp.rows + 1024 / D - 1) / (1024 / D), grid - 1), fa::kTreeCombineThreads, 0, st, tp, grid);
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
+    int rc = decode_check_args(p.q, p.k, p.v, p.o, p.seqlens_k, p.B, p.Hq, p.Hkv, Skv_max, p.d, p.scale, p.T, kTreeMaxNodes);
+    if (rc) return rc;
+    if (p.B == 0) return FA_OK;
+    if (!aligned16(p.workspace)) return FA_ERR_ALIGN;
+    if (!p.workspace || p.workspace_bytes < fa_decode_tree_workspace_bytes(p.B, p.T, p.Hq, p.Hkv, Skv_max, p.d)) return FA_ERR_WORKSPACE;
+    int sms = 0;
+    rc = check_device(&sms);
+    if (rc) return rc;
+    const TreeBlocks tb(p.Hq / p.Hkv * p.T);
+    fa::TreeParams tp;
+    tp.q = p.q;
+    tp.o = p.o;
+    tp.lse = p.lse;
+    tp.seqlens = p.seqlens_k;
+    tp.tree_lens = p.tree_lens;
+    tp.mask = p.mask;
+    tp.block_table = p.block_table;
+    tp.o_part = static_cast<float*>(p.workspace);
+    tp.lse_part = tp.o_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows * p.d;
+    tp.starts = reinterpret_cast<long long*>(tp.lse_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows);
+    tp.mask_stride = p.mask_stride;
+    tp.mask_words = (p.T + 31) / 32;
+    tp.B = p.B;
+    tp.T = p.T;
+    tp.Hq = p.Hq;
+    tp.Hkv = p.Hkv;
+    tp.g = p.Hq / p.Hkv;
+    tp.Smax = Skv_max;
+    tp.rows = tb.rows;
+    tp.blocks = tb.blocks;
+    tp.page_size = p.block_table ? p.page_size : 1;
+    tp.table_stride = p.table_stride;
+    tp.min_tiles = 1;
+    tp.scale_log2 = p.scale * 1.4426950408889634f;
+    const bool bf16 = p.dtype == FA_DTYPE_BF16;
+    const int slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : Skv_max;
+    const bool small = p.block_table && p.page_size < fa::kDecTile;
+    const int box_rows = small ? p.page_size : fa::kDecTile;
+    CUtensorMap tk, tv;
+    rc = encode_map_cache(&tk, p.k, slabs, slab_rows, p.Hkv, box_rows, bf16, p.d, small);
+    if (rc) return rc;
+    rc = encode_map_cache(&tv, p.v, slabs, slab_rows, p.Hkv, box_rows, bf16, p.d);
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p.d == 64) return bf16 ? tree_launch<__nv_bfloat16, 64>(tk, tv, tp, sms, st) : tree_launch<__half, 64>(tk, tv, tp, sms, st);
+    return bf16 ? tree_launch<__nv_bfloat16, 128>(tk, tv, tp, sms, st) : tree_launch<__half, 128>(tk, tv, tp, sms, st);
+}
 }  // namespace
 
 extern "C" {
@@ -1084,7 +1159,10 @@ int fa_decode_ex(const fa_decode_params* p, void* stream) {
 }
 
 size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d) {
-    return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
+    if (B <= 0 || T <= 0 || T > kTreeMaxNodes || Hq <= 0 || Hkv <= 0 || Skv_max <= 0 || (d != 128 && d != 64)) return 0;
+    if ((long long)(Hq / Hkv) * T <= kTreeFewRows) return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
+    const TreeBlocks tb(Hq / Hkv * T);
+    return 2 * (size_t)fa::kTreeMaxCtas * tb.rows * ((size_t)d + 1) * sizeof(float) + ((size_t)B + 1) * sizeof(long long);
 }
 
 int fa_decode_tree(const fa_tree_params* p, void* stream) {
@@ -1100,6 +1178,7 @@ int fa_decode_tree(const fa_tree_params* p, void* stream) {
     if ((reinterpret_cast<uintptr_t>(p->mask) | reinterpret_cast<uintptr_t>(p->tree_lens) | reinterpret_cast<uintptr_t>(p->seqlens_k) |
          reinterpret_cast<uintptr_t>(p->lse)) & 3u)
         return FA_ERR_ALIGN;
+    if (p->Hkv > 0 && (long long)(p->Hq / p->Hkv) * p->T > kTreeFewRows) return tree_impl(*p, Skv_max, stream);
     return decode_impl(p->q, p->k, p->v, p->o, p->lse, p->seqlens_k, p->B, p->Hq, p->Hkv, Skv_max, p->d, p->scale, p->workspace,
                        p->workspace_bytes, stream, p->block_table, p->num_pages, p->block_table ? p->page_size : 0, p->table_stride,
                        p->T, p->dtype == FA_DTYPE_BF16, p);
