@@ -305,6 +305,25 @@ def _int32(what: str, *tensors) -> None:
             raise ValueError(f"{what}: index tensors are int32, not {t.dtype}")
 
 
+def tree_mask(parents):
+    """The mask of ``fa_decode_tree`` for trees given by their parents, int32 [B,T] (or [T]; parents[i] < i, -1 for the root): each
+    node sees itself and the nodes above it.  Made with torch operations on the parents' device, once per step."""
+    T = parents.shape[-1]
+    up = parents.long()
+    see = torch.eye(T, dtype=torch.bool, device=parents.device).expand(*up.shape, T).clone()
+    hop = up.clamp(min=0).unsqueeze(-1)
+    for _ in range(max(1, (T - 1).bit_length())):   # what a node's ancestor sees, twice as far up each time
+        live = (up >= 0).unsqueeze(-1)
+        see = see | (torch.gather(see, -2, hop.expand_as(see)) & live)
+        up = torch.where(up >= 0, torch.gather(up, -1, hop.squeeze(-1)), up)
+        hop = up.clamp(min=0).unsqueeze(-1)
+    W = (T + 31) // 32
+    bits = torch.zeros(*see.shape[:-1], W * 32, dtype=torch.int64, device=see.device)
+    bits[..., :T] = see
+    words = (bits.view(*see.shape[:-1], W, 32) << torch.arange(32, device=see.device)).sum(-1)
+    return torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
+
+
 def fa_decode_tree_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, Skv_max: int, d: int) -> int:
     return int(lib.fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max, d))
 

@@ -15,6 +15,7 @@
 #pragma once
 
 #include "decode.cuh"
+#include "prefill_pingpong.cuh"
 
 namespace fa {
 
@@ -26,7 +27,10 @@ struct TreeShape {
     static constexpr int kTileB = 128 * D * 2;                       // Q, K or V of 128 rows
     static constexpr int kSlots = 7 * 128 / D - kTiles;              // 224 KiB in all
     static constexpr int kSmem = 1024 + (kTiles + kSlots) * kTileB;
-    static constexpr int kThreads = 128 * kTiles + 64;
+    static constexpr int kThreads = 128 * kTiles + 128;
+    // Keys of a softmax step.  A row tile has two score buffers of so many columns: while one is in the softmax, the
+    // tensor cores take the other's probabilities and fill it again.
+    static constexpr int kStep = kTiles == 2 ? 64 : 128;
 };
 
 struct TreeParams {
@@ -39,26 +43,30 @@ struct TreeParams {
     const int* block_table;   // nullptr: contiguous
     float* o_part;            // [2 ctas][D/4][rows][4]
     float* lse_part;          // [2 ctas][rows]
-    long long* starts;        // [B + 1] first tile of each sequence, and of none
+    int* starts;              // [B + 1] first tile of each sequence, and of none
     long long mask_stride;
     int mask_words;
     int B, T, Hq, Hkv, g, Smax;
     int rows;                 // rows per block (at most 128 kTiles), blocks per (sequence, kv head)
     int blocks;
+    int q_boxes;              // 128 rows are the heads of whole nodes, and one box of the tensor map over q
     int page_size, table_stride;
-    int min_tiles;            // tiles a CTA takes at least
     float scale_log2;
 };
 
 // The tiles of item `it` (kv head and row block) of sequence b come behind those of the items before it; CTA c of `ctas` takes the
-// tiles from begin(c) to begin(c + 1).
+// tiles from begin(c) to begin(c + 1): one more than the others in the first `more` CTAs.
 struct TreePlan {
-    long long total;
-    int ctas;
-    __device__ __forceinline__ TreePlan(long long total, int grid, int min_tiles)
-        : total(total), ctas((int)max(1ll, min((long long)grid, total / min_tiles))) {}
-    __device__ __forceinline__ long long begin(int c) const { return c >= ctas ? total : total * c / ctas; }
-    __device__ __forceinline__ int owner(long long tile) const { return (int)(((tile + 1) * ctas - 1) / total); }
+    int total, ctas, each, more;
+    __device__ __forceinline__ TreePlan(int total, int grid) : total(total), ctas(max(1, min(grid, total))) {
+        each = total / ctas;
+        more = total - each * ctas;
+    }
+    __device__ __forceinline__ int begin(int c) const { return c >= ctas ? total : c * each + min(c, more); }
+    __device__ __forceinline__ int owner(int tile) const {   // (of a tile that there is)
+        const int big = more * (each + 1);
+        return tile < big ? tile / (each + 1) : more + (tile - big) / each;
+    }
 };
 __device__ __forceinline__ int tree_seq_len(const TreeParams& p, int b) { return max(0, min(p.seqlens[b], p.Smax)); }
 
@@ -69,21 +77,43 @@ struct TreeSegment {
     int len, live;        // keys and nodes of the sequence
 };
 
+template <int kSlots>
 struct TreeBars {
-    template <int kSlots>
-    struct At {
-        static constexpr int full = 0, empty = kSlots, s_full = 2 * kSlots, p_full = s_full + 2, pv = p_full + 2, q_full = pv + 2,
-                             seg_full = q_full + 2, seg_empty = seg_full + kTreeSegs, count = seg_empty + kTreeSegs;
-    };
+    static constexpr int full = 0, empty = kSlots, s_full = 2 * kSlots, p_full = s_full + 4, pv = p_full + 4, q_full = pv + 4,
+                         q_empty = q_full + 2, seg_full = q_empty + 2, seg_empty = seg_full + kTreeSegs, count = seg_empty + kTreeSegs;
 };
 
-// grid: the SMs; the last two warps load and issue.
+// Every other slot of the ring: K tiles from slot 0 on, V tiles from slot 1.
+template <int N>
+struct TreeRing {
+    uint32_t slot, par;
+    __device__ __forceinline__ void next() {
+        slot += 2;
+        if (slot >= N) {
+            slot -= N;
+            par ^= 1;
+        }
+    }
+};
+
+template <int N>
+__device__ __forceinline__ float tree_row_max(const uint32_t (&s)[N]) {
+    float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m[k] = max3(m[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+    return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+}
+
+// grid: the SMs; the last four warps load K and V, issue the two products and load Q.
 template <typename T, int D, int kTiles>
 __global__ void __launch_bounds__(TreeShape<D, kTiles>::kThreads, 1)
-fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const TreeParams p) {
+fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                      const __grid_constant__ CUtensorMap tm_v, const TreeParams p) {
     using Shape = TreeShape<D, kTiles>;
-    constexpr int kSlots = Shape::kSlots, kTileB = Shape::kTileB;
-    using At = TreeBars::At<kSlots>;
+    constexpr int kSlots = Shape::kSlots, kTileB = Shape::kTileB, kStep = Shape::kStep, kSub = kDecTile / kStep;
+    using At = TreeBars<kSlots>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t sQ = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const uint32_t sRing = sQ + kTiles * kTileB;
@@ -97,19 +127,9 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
-        for (int i = 0; i < kSlots; ++i) {
-            mbar_init(bar(At::full + i), 1);
-            mbar_init(bar(At::empty + i), 1);
-        }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(bar(At::s_full + i), 1);
-            mbar_init(bar(At::p_full + i), 4);
-            mbar_init(bar(At::pv + i), 1);
-            mbar_init(bar(At::q_full + i), 4);
-        }
-        for (int i = 0; i < kTreeSegs; ++i) {
-            mbar_init(bar(At::seg_full + i), 1);
-            mbar_init(bar(At::seg_empty + i), kSoftmaxWarps + 1);
+        for (int i = 0; i < At::count; ++i) {
+            const bool p_full = i >= At::p_full && i < At::p_full + 4, seg_empty = i >= At::seg_empty;
+            mbar_init(bar(i), p_full ? 4 : seg_empty ? kSoftmaxWarps + 3 : 1);
         }
         abort_flag = 0;
         fence_mbar_init();
@@ -124,49 +144,61 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
+    const uint32_t tmem_o = tmem + 2 * kTiles * kStep;   // behind the score buffers
     grid_dep_wait();
 
     const int ps = p.page_size;
     const bool small = p.block_table != nullptr && ps < kDecTile;   // a tile is several pages
     bool ok = true;
+    // segment `ord`, copied; false: a wait gave up
+    auto segment = [&](uint32_t ord, TreeSegment& s) {
+        if (!pp_warp_wait(bar(At::seg_full + ord % kTreeSegs), (ord / kTreeSegs) & 1, &abort_flag, 320)) return false;
+        s = segs[ord % kTreeSegs];
+        return true;
+    };
 
     if (warp == kSoftmaxWarps) {
         // ---------------------------------------------------------------- segments, K and V
         const int items = p.Hkv * p.blocks;
-        // tiles of sequence b's items
-        auto tiles_of = [&](int b) { return b < p.B ? (long long)((tree_seq_len(p, b) + kDecTile - 1) / kDecTile) * items : 0ll; };
-        auto scan = [&](long long x) {
+        // the lengths of 32 sequences at a time, one per lane
+        int chunk = -32, chunk_len = 0;
+        auto lens_at = [&](int b0) {
+            if (b0 != chunk) {
+                chunk = b0;
+                chunk_len = b0 + lane < p.B ? tree_seq_len(p, b0 + lane) : 0;
+            }
+            return chunk_len;
+        };
+        auto len_of = [&](int b) { return __shfl_sync(0xffffffffu, lens_at(b & ~31), b & 31); };
+        auto tiles_at = [&](int b0) { return (lens_at(b0) + kDecTile - 1) / kDecTile * items; };   // of this lane's sequence's items
+        auto scan = [&](int x) {
 #pragma unroll
             for (int sh = 1; sh < 32; sh <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, x, sh);
+                const int y = __shfl_up_sync(0xffffffffu, x, sh);
                 if (lane >= sh) x += y;
             }
             return x;
         };
-        long long total = 0;
+        int total = 0;
         for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const long long mine = tiles_of(b0 + lane), upto = total + scan(mine);
+            const int mine = tiles_at(b0), upto = total + scan(mine);
             if (blockIdx.x == 0 && b0 + lane < p.B) p.starts[b0 + lane] = upto - mine;
             total = __shfl_sync(0xffffffffu, upto, 31);
         }
         if (blockIdx.x == 0 && lane == 0) p.starts[p.B] = total;
-        const TreePlan plan(total, gridDim.x, p.min_tiles);
-        const long long end = plan.begin(blockIdx.x + 1);
-        long long pos = plan.begin(blockIdx.x);
-        if ((int)blockIdx.x >= plan.ctas) pos = end;
+        const TreePlan plan(total, gridDim.x);
+        const int end = plan.begin(blockIdx.x + 1);
+        int pos = plan.begin(blockIdx.x);
         // the sequence of the run's first tile, and that tile's place among the sequence's
-        int b = 0;
-        long long in_seq = 0;
+        int b = 0, in_seq = 0;
         if (pos < end) {
-            long long before = 0;
-            for (int b0 = 0;; b0 += 32) {
-                const long long upto = before + scan(tiles_of(b0 + lane));
+            for (int b0 = 0, before = 0;; b0 += 32) {
+                const int mine = tiles_at(b0), upto = before + scan(mine);
                 const uint32_t past = __ballot_sync(0xffffffffu, upto > pos);
                 if (past) {
                     const int at = __ffs(past) - 1;
                     b = b0 + at;
-                    const long long first = __shfl_up_sync(0xffffffffu, upto, 1);
-                    in_seq = pos - (at > 0 ? __shfl_sync(0xffffffffu, first, at) : before);
+                    in_seq = pos - __shfl_sync(0xffffffffu, upto - mine, at);
                     break;
                 }
                 before = __shfl_sync(0xffffffffu, upto, 31);
@@ -174,23 +206,22 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
         }
         const uint64_t stream_policy = l2_policy_evict_first();   // every tile is read once
         uint32_t ring = 0;   // slots filled
-        int len = pos < end ? tree_seq_len(p, b) : 0, len_next = pos < end && b + 1 < p.B ? tree_seq_len(p, b + 1) : 0;
+        int len = pos < end ? len_of(b) : 0;
         int item = 0, t0 = 0;
         if (pos < end) {
             const int of = (len + kDecTile - 1) / kDecTile;
-            item = (int)(in_seq / of);
-            t0 = (int)(in_seq % of);
+            item = in_seq / of;
+            t0 = in_seq % of;
         }
         for (uint32_t ord = 0; ok; ++ord) {
             const int slot = ord % kTreeSegs;
-            ok = mbar_wait(bar(At::seg_empty + slot), ((ord / kTreeSegs) & 1) ^ 1, &abort_flag, 300);
-            ok = __all_sync(0xffffffffu, ok);
+            ok = pp_warp_wait(bar(At::seg_empty + slot), ((ord / kTreeSegs) & 1) ^ 1, &abort_flag, 300);
             if (!ok) break;
             const int of = (len + kDecTile - 1) / kDecTile;
-            const int n = (int)min((long long)(of - t0), end - pos);
+            const int n = min(of - t0, end - pos);
             const int hk = item / p.blocks;
             if (lane == 0) {
-                segs[slot] = {b, hk, item % p.blocks, t0, n, of, len, tree_nodes(p.tree_lens, b, p.T, len)};
+                segs[slot] = {b, hk, item % p.blocks, t0, n, of, len, n > 0 ? tree_nodes(p.tree_lens, b, p.T, len) : 0};
                 mbar_arrive(bar(At::seg_full + slot));
             }
             if (n <= 0) break;
@@ -232,139 +263,159 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             t0 = 0;
             if (++item == items && pos < end) {   // the next sequence that has keys
                 item = 0;
-                do {
-                    ++b;
-                    len = len_next;
-                    len_next = b + 1 < p.B ? tree_seq_len(p, b + 1) : 0;
-                } while (len == 0);
+                do len = len_of(++b);
+                while (len == 0);
             }
         }
         __syncwarp();
     } else if (warp == kSoftmaxWarps + 1) {
-        // ---------------------------------------------------------------- MMAs
+        // ---------------------------------------------------------------- S = Q K^T
         if (elect_one()) {
-            constexpr uint32_t idesc_qk = instr_desc_f16(kBf16, 128, 128, false, false);
-            constexpr uint32_t idesc_pv = instr_desc_f16(kBf16, 128, D, false, true);
-            uint32_t g = 0;   // tiles begun
-            auto slot_of = [&](uint32_t i) { return i % kSlots; };
-            auto wait_full = [&](uint32_t i) { return mbar_wait(bar(At::full + slot_of(i)), (i / kSlots) & 1, &abort_flag, 310); };
-            // scores of tile i into buffer x: of row tile x, or (one row tile) of every other tile
-            auto scores = [&](uint32_t i, int x) {
-                tc_fence_after();
-                const uint32_t k = sRing + slot_of(2 * i) * kTileB, q = sQ + (kTiles == 2 ? x * kTileB : 0);
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    const uint32_t off = (ks >> 2) * 16384 + (ks & 3) * 32;
-                    mma_ss(tmem + x * 128, smem_desc_sw128(q + off, 16, 1024), smem_desc_sw128(k + off, 16, 1024), idesc_qk, ks > 0);
-                }
-                mma_commit(bar(At::s_full + x));
-            };
-            // a 16-key step of V: its rows lie in one page
-            const uint32_t v_block = small ? (uint32_t)ps * 128u : 16384u;
-            auto output = [&](uint32_t i, int x, bool first) {
-                tc_fence_after();
-                const uint32_t v = sRing + slot_of(2 * i + 1) * kTileB;
-                const uint32_t o = tmem + 256 + (kTiles == 2 ? x * 128 : 0);
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks) {
-                    uint32_t at = ks * 2048u;
-                    if (small && D > 64) at += (D / 64 - 1) * v_block * ((uint32_t)(ks * 16) / (uint32_t)ps);
-                    mma_ts(o, tmem + x * 128 + ks * 8, smem_desc_sw128(v + at, v_block, 1024), idesc_pv, !first || ks > 0);
-                }
-                mma_commit(bar(At::pv + (kTiles == 2 ? x : 0)));
-            };
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kStep, false, false);
+            const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16);
+            TreeRing<kSlots> ring{0, 0};
+            uint32_t s = 0;   // steps begun
             for (uint32_t ord = 0; ok; ++ord) {
                 const int slot = ord % kTreeSegs;
                 if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kTreeSegs) & 1, &abort_flag, 311))) break;
                 const int n = segs[slot].n;
                 mbar_arrive(bar(At::seg_empty + slot));
                 if (n <= 0) break;
+#pragma unroll
                 for (int x = 0; x < kTiles; ++x)
                     if (ok) ok = mbar_wait(bar(At::q_full + x), ord & 1, &abort_flag, 312);
-                if constexpr (kTiles == 2) {
-                    if (ok) ok = wait_full(2 * g);
-                    if (!ok) break;
-                    scores(g, 0);
-                    scores(g, 1);
-                    mma_commit(bar(At::empty + slot_of(2 * g)));
-                    for (int j = 0; j < n; ++j, ++g) {
-                        const bool more = j + 1 < n;
-                        if (!(ok = wait_full(2 * g + 1))) break;
-                        if (!(ok = mbar_wait(bar(At::p_full), g & 1, &abort_flag, 313))) break;
-                        output(g, 0, j == 0);
-                        if (more) {
-                            if (!(ok = wait_full(2 * g + 2))) break;
-                            scores(g + 1, 0);
-                        }
-                        if (!(ok = mbar_wait(bar(At::p_full + 1), g & 1, &abort_flag, 314))) break;
-                        output(g, 1, j == 0);
-                        mma_commit(bar(At::empty + slot_of(2 * g + 1)));
-                        if (more) {
-                            scores(g + 1, 1);
-                            mma_commit(bar(At::empty + slot_of(2 * g + 2)));
+                for (int j = 0; j < n && ok; ++j) {
+                    if (!(ok = mbar_wait(bar(At::full + ring.slot), ring.par, &abort_flag, 310))) break;
+                    const uint32_t kt = k_lo + ring.slot * (kTileB >> 4);
+#pragma unroll
+                    for (int sub = 0; sub < kSub; ++sub, ++s) {
+                        const uint32_t buf = kSub == 2 ? sub : s & 1;
+#pragma unroll
+                        for (int x = 0; x < kTiles; ++x) {
+                            // P V of two steps ago has taken the probabilities that lie there
+                            if (s >= 2 && ok) ok = mbar_wait(bar(At::pv + 2 * x + buf), ((s >> 1) - 1) & 1, &abort_flag, 313);
+                            tc_fence_after();
+                            if (ok) {
+#pragma unroll
+                                for (int ks = 0; ks < D / 16; ++ks) {
+                                    const uint32_t off = ((ks >> 2) * 16384 + (ks & 3) * 32) >> 4;
+                                    mma_ss_lo(tmem + (2 * x + buf) * kStep, q_lo + x * (kTileB >> 4) + off, kt + sub * (kStep * 128 >> 4) + off, idesc, ks > 0);
+                                }
+                                mma_commit(bar(At::s_full + 2 * x + buf));
+                            }
                         }
                     }
-                } else {
-                    for (int j = 0; j < 2 && j < n && ok; ++j) {
-                        if (!(ok = wait_full(2 * (g + j)))) break;
-                        scores(g + j, (g + j) & 1);
-                        mma_commit(bar(At::empty + slot_of(2 * (g + j))));
-                    }
-                    for (int j = 0; j < n && ok; ++j, ++g) {
-                        if (!(ok = mbar_wait(bar(At::p_full + (g & 1)), (g >> 1) & 1, &abort_flag, 313))) break;
-                        if (!(ok = wait_full(2 * g + 1))) break;
-                        output(g, g & 1, j == 0);
-                        mma_commit(bar(At::empty + slot_of(2 * g + 1)));
-                        if (j + 2 < n) {
-                            if (!(ok = wait_full(2 * (g + 2)))) break;
-                            scores(g + 2, g & 1);
-                            mma_commit(bar(At::empty + slot_of(2 * (g + 2))));
-                        }
-                    }
+                    mma_commit(bar(At::empty + ring.slot));
+                    ring.next();
                 }
+                if (ok)
+#pragma unroll
+                    for (int x = 0; x < kTiles; ++x) mma_commit(bar(At::q_empty + x));
             }
             // (what was committed last has arrived before the CTA ends)
-            if (ok && g > 0) ok = mbar_wait(bar(At::empty + slot_of(2 * g - 1)), ((2 * g - 1) / kSlots) & 1, &abort_flag, 315);
+            if (ok && s > 0) {
+                const uint32_t i = 2 * (s / kSub) - 2;
+                ok = mbar_wait(bar(At::empty + i % kSlots), (i / kSlots) & 1, &abort_flag, 314);
+            }
+        }
+        __syncwarp();
+    } else if (warp == kSoftmaxWarps + 2) {
+        // ---------------------------------------------------------------- O += P V
+        if (elect_one()) {
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, D, false, true);
+            // 16 keys of V, which lie in one page: 64-element blocks of its rows
+            const uint32_t block = small ? (uint32_t)ps * 128u : 16384u;
+            const uint32_t v_lo = desc_lo(sRing, block);
+            uint32_t key_off[8];
+#pragma unroll
+            for (int ks = 0; ks < 8; ++ks) key_off[ks] = (ks * 2048u + (small && D > 64 ? (D / 64 - 1) * block * ((uint32_t)(ks * 16) / (uint32_t)ps) : 0u)) >> 4;
+            TreeRing<kSlots> ring{1, 0};
+            uint32_t s = 0;
+            for (uint32_t ord = 0; ok; ++ord) {
+                const int slot = ord % kTreeSegs;
+                if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kTreeSegs) & 1, &abort_flag, 315))) break;
+                const int n = segs[slot].n;
+                mbar_arrive(bar(At::seg_empty + slot));
+                if (n <= 0) break;
+                for (int j = 0; j < n && ok; ++j) {
+                    if (!(ok = mbar_wait(bar(At::full + ring.slot), ring.par, &abort_flag, 316))) break;
+                    const uint32_t vt = v_lo + ring.slot * (kTileB >> 4);
+#pragma unroll
+                    for (int sub = 0; sub < kSub; ++sub, ++s) {
+                        const uint32_t buf = kSub == 2 ? sub : s & 1;
+#pragma unroll
+                        for (int x = 0; x < kTiles; ++x) {
+                            if (ok) ok = mbar_wait(bar(At::p_full + 2 * x + buf), (s >> 1) & 1, &abort_flag, 317 + x);
+                            tc_fence_after();
+                            if (ok) {
+#pragma unroll
+                                for (int ks = 0; ks < kStep / 16; ++ks)
+                                    mma_ts_lo(tmem_o + x * D, tmem + (2 * x + buf) * kStep + ks * 8, vt + key_off[sub * (kStep / 16) + ks], idesc,
+                                              ks > 0 || sub > 0 || j > 0 ? 1u : 0u);
+                                mma_commit(bar(At::pv + 2 * x + buf));
+                            }
+                        }
+                    }
+                    mma_commit(bar(At::empty + ring.slot));
+                    ring.next();
+                }
+            }
+            if (ok && s > 0) {
+                const uint32_t i = 2 * (s / kSub) - 1;
+                ok = mbar_wait(bar(At::empty + i % kSlots), (i / kSlots) & 1, &abort_flag, 319);
+            }
+        }
+        __syncwarp();
+    } else if (warp == kSoftmaxWarps + 3) {
+        // ---------------------------------------------------------------- Q, as soon as the scores of the segment before are there
+        constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;   // 16-byte pieces of a row; rows that the warp loads at a time
+        const int c = lane % kPieces;
+        if (p.q_boxes) tma_prefetch_desc(&tm_q);
+        TreeSegment seg;
+        for (uint32_t ord = 0; ok; ++ord) {
+            if (!(ok = segment(ord, seg))) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(At::seg_empty + ord % kTreeSegs));
+            if (seg.n <= 0) break;
+            const int R0 = seg.block * p.rows, rows = min(p.rows, p.g * p.T - R0);
+            for (int x = 0; x < kTiles; ++x) {
+                if (ord > 0 && !(ok = pp_warp_wait(bar(At::q_empty + x), (ord - 1) & 1, &abort_flag, 330))) break;
+                if (p.q_boxes) {   // 128 rows are whole nodes: one box of their heads
+                    if (lane == 0) {
+                        mbar_expect_tx(bar(At::q_full + x), kTileB);
+                        tma_load_5d(sQ + x * kTileB, &tm_q, bar(At::q_full + x), 0, seg.hk * p.g, (R0 + x * 128) / p.g, 0, seg.b);
+                    }
+                    continue;
+                }
+                int r = lane / kPieces;
+                int token = (R0 + x * 128 + r) / p.g, head = (R0 + x * 128 + r) % p.g;
+                const int n = min(128, rows - x * 128);
+                for (; r < n; r += kAtOnce) {
+                    const T* q = static_cast<const T*>(p.q) + (((long long)seg.b * p.T + token) * p.Hq + seg.hk * p.g + head) * D + 8 * c;
+                    const uint32_t at = sQ + x * kTileB + r * 128 + (c >> 3) * 16384u + (((c & 7) ^ (r & 7)) << 4);
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(q) : "memory");
+                    for (head += kAtOnce; head >= p.g; head -= p.g) ++token;
+                }
+            }
+            if (!ok) break;
+            if (!p.q_boxes) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0)
+                    for (int x = 0; x < kTiles; ++x) mbar_arrive(bar(At::q_full + x));
+            }
         }
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax: a row per thread
         const int x = warp >> 2;                        // row tile
         const int r = tid & 127;                        // row of it
+        const int row = x * 128 + r;                    // row of the block
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t tO = tmem + lanes + 256 + x * 128;
-        uint32_t g = 0;
-        auto wait = [&](int i, uint32_t parity, unsigned int where) {
-            return __all_sync(0xffffffffu, mbar_wait(bar(i), parity, &abort_flag, where));
-        };
-        auto segment = [&](uint32_t ord, TreeSegment& s) {
-            if (!wait(At::seg_full + ord % kTreeSegs, (ord / kTreeSegs) & 1, 320)) return false;
-            s = segs[ord % kTreeSegs];
-            return true;
-        };
-        int row = 0, token = 0, head = 0;   // row of the block; its node and query head
-        bool mine = false;                  // it is a row
-        auto load_q = [&](const TreeSegment& s) {
-            row = x * 128 + r;
-            const int R = s.block * p.rows + row;
-            mine = row < p.rows && R < p.g * p.T;
-            token = R / p.g;
-            head = s.hk * p.g + R % p.g;
-            if (mine) {
-                const uint4* q = reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (((long long)s.b * p.T + token) * p.Hq + head) * D);
-                const uint32_t at = sQ + x * kTileB + r * 128;
-#pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    const uint4 v = q[c];
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (c >> 3) * 16384u + (((c & 7) ^ (r & 7)) << 4)),
-                                 "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-                                 : "memory");
-                }
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(At::q_full + x));
-        };
+        const uint32_t tO = tmem_o + lanes + x * D;
+        uint32_t s = 0;
+        auto wait = [&](int i, uint32_t parity, unsigned int where) { return pp_warp_wait(bar(i), parity, &abort_flag, where); };
         // sequences without keys are nobody's item
         for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
             if (tree_seq_len(p, b) > 0) continue;
@@ -373,29 +424,32 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             if (p.lse)
                 for (long long i = tid; i < n; i += 128 * kTiles) p.lse[at + i] = -INFINITY;
         }
-        TreeSegment seg, next;
-        ok = segment(0, seg);
-        if (ok && seg.n > 0) load_q(seg);
-        for (uint32_t ord = 0; ok && seg.n > 0; ++ord) {
+        TreeSegment seg;
+        for (uint32_t ord = 0;; ++ord) {
+            if (!(ok = segment(ord, seg)) || seg.n <= 0) break;
+            const int R = seg.block * p.rows + row;
+            const bool mine = row < p.rows && R < p.g * p.T;   // it is a row
+            const int token = R / p.g, head = seg.hk * p.g + R % p.g;
             const TreeRow sees(p.mask + seg.b * p.mask_stride, p.mask_words, mine ? token : seg.live, seg.live);
             const int prefix = seg.len - seg.live;
             const bool some = __any_sync(0xffffffffu, mine);   // a warp without rows only keeps step
             float m_run = -INFINITY, l_run = 0.f;
-            for (int j = 0; j < seg.n; ++j, ++g) {
-                const int key0 = (seg.t0 + j) * kDecTile, valid = min(kDecTile, seg.len - key0);
-                const int buf = kTiles == 2 ? x : g & 1;
-                const uint32_t tS = tmem + lanes + buf * 128;
-                const bool masked = key0 + kDecTile > prefix;   // it reaches into the tree, or past the keys
-                uint32_t vis[4];
+            for (int j = 0; j < seg.n * kSub; ++j, ++s) {
+                const int key0 = seg.t0 * kDecTile + j * kStep;
+                const int buf = 2 * x + (s & 1);
+                const uint32_t tS = tmem + lanes + buf * kStep;
+                const bool masked = key0 + kStep > prefix;   // it reaches into the tree, or past the keys
+                uint32_t vis[kStep / 32];
                 if (masked) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) vis[c] = sees.keys(key0 - prefix + 32 * c) & low_bits(valid - 32 * c);
+                    for (int c = 0; c < kStep / 32; ++c) vis[c] = sees.keys(key0 - prefix + 32 * c) & low_bits(seg.len - key0 - 32 * c);
                 }
-                if (!(ok = wait(At::s_full + buf, (kTiles == 2 ? g : g >> 1) & 1, 321))) break;
+                if (!(ok = wait(At::s_full + buf, (s >> 1) & 1, 321))) break;
                 tc_fence_after();
-                if (x == 0 && valid < kDecTile) {
+                if (x == 0 && s % kSub == 0 && seg.len - key0 < kDecTile) {
                     // V rows past the sequence may hold anything, NaN too: they become zeros (their probabilities are)
-                    const uint32_t i = 2 * g + 1, v = sRing + (i % kSlots) * kTileB;
+                    const uint32_t i = 2 * (s / kSub) + 1, v = sRing + (i % kSlots) * kTileB;
+                    const int valid = seg.len - key0;
                     if (!(ok = wait(At::full + i % kSlots, (i / kSlots) & 1, 322))) break;
                     for (int u = r; u < (kDecTile - valid) * (D / 8); u += 128) {
                         const int key = valid + u / (D / 8), c = u % (D / 8);
@@ -406,66 +460,63 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     fence_proxy_async_smem();
                 }
                 if (some) {
-                    uint32_t sr[4][32];
+                    uint32_t sc[kStep];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld_x32(tS + c * 32, sr[c]);
+                    for (int c = 0; c < kStep / 32; ++c) tmem_ld_x32(tS + 32 * c, *reinterpret_cast<uint32_t(*)[32]>(&sc[32 * c]));
                     tmem_wait_ld();
-                    float s[128];
+                    if (masked) {   // hidden scores become -inf, their exponentials exact zeros (the scale is positive)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) s[c * 32 + i] = __uint_as_float(sr[c][i]);
-                    if (masked) {
-#pragma unroll
-                        for (int i = 0; i < 128; ++i)
-                            if (!((vis[i >> 5] >> (i & 31)) & 1u)) s[i] = -INFINITY;
+                        for (int i = 0; i < kStep; ++i)
+                            if (!(vis[i >> 5] & (1u << (i & 31)))) sc[i] = 0xff800000u;
                     }
-                    float m0 = s[0], m1 = s[1], m2 = s[2], m3 = s[3];
-#pragma unroll
-                    for (int i = 4; i < 128; i += 4) {
-                        m0 = fmaxf(m0, s[i]);
-                        m1 = fmaxf(m1, s[i + 1]);
-                        m2 = fmaxf(m2, s[i + 2]);
-                        m3 = fmaxf(m3, s[i + 3]);
-                    }
-                    const float m_tile = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+                    const float m_step = tree_row_max<kStep>(sc);
                     // The reference of the exponentials follows the row's maximum only where that has outgrown it by 2^8: P is at
                     // most 256 then, and O is seldom scaled.
-                    const bool moved = m_tile > m_run && (m_run == -INFINITY || (m_tile - m_run) * p.scale_log2 > 8.f);
-                    const float m_new = moved ? m_tile : m_run, m_use = m_new == -INFINITY ? 0.f : m_new;
-                    const float alpha = !moved ? 1.f : m_run == -INFINITY ? 0.f : fast_exp2((m_run - m_use) * p.scale_log2);
-                    const float neg = -m_use * p.scale_log2;
+                    const bool moved = (m_step - m_run) * p.scale_log2 > kRescaleThreshold;   // (never on -inf)
+                    const float m_new = moved ? m_step : m_run;
+                    const float alpha = moved ? fast_exp2((m_run - m_new) * p.scale_log2) : 1.f;
+                    const float neg = m_new == -INFINITY ? 0.f : -m_new * p.scale_log2;
                     m_run = m_new;
-                    float l0 = 0.f, l1 = 0.f;
+                    const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(neg, neg);
+                    uint64_t la = f2_pack(0.f, 0.f), lb = la;
 #pragma unroll
-                    for (int half = 0; half < 2; ++half) {
-                        uint32_t w[32];
+                    for (int c = 0; c < kStep / 32; ++c) {
+                        uint32_t w[16];
 #pragma unroll
-                        for (int i = 64 * half; i < 64 * half + 64; i += 2) {
-                            float a = fast_exp2(fmaf(s[i], p.scale_log2, neg)), b = fast_exp2(fmaf(s[i + 1], p.scale_log2, neg));
-                            if (masked) {   // hidden keys count nothing, whatever the scale
-                                if (!((vis[i >> 5] >> (i & 31)) & 1u)) a = 0.f;
-                                if (!((vis[i >> 5] >> ((i + 1) & 31)) & 1u)) b = 0.f;
+                        for (int i = 0; i < 32; i += 4) {
+                            float e[4];
+#pragma unroll
+                            for (int k = 0; k < 4; k += 2) {
+                                const int at = 32 * c + i + k;
+                                f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[at]), __uint_as_float(sc[at + 1])), sc2, nm2), e[k], e[k + 1]);
+                                e[k] = fast_exp2(e[k]);
+                                e[k + 1] = fast_exp2(e[k + 1]);
                             }
-                            l0 += a;
-                            l1 += b;
-                            w[(i & 63) >> 1] = pack2<T>(a, b);
+                            la = f2_add(la, f2_pack(e[0], e[1]));
+                            lb = f2_add(lb, f2_pack(e[2], e[3]));
+                            w[i / 2] = pack2<T>(e[0], e[1]);
+                            w[i / 2 + 1] = pack2<T>(e[2], e[3]);
                         }
-                        tmem_st_x32(tS + 32 * half, w);
+                        tmem_st_x16(tS + 16 * c, w);
                     }
-                    l_run = l_run * alpha + (l0 + l1);
+                    {
+                        float a0, a1, b0, b1;
+                        f2_unpack(la, a0, a1);
+                        f2_unpack(lb, b0, b1);
+                        l_run = l_run * alpha + ((a0 + a1) + (b0 + b1));
+                    }
                     if (j > 0 && __any_sync(0xffffffffu, moved)) {
-                        // (two row tiles: the scores came after P V of the tile before)
-                        if (kTiles == 1 && !(ok = wait(At::pv, (g - 1) & 1, 323))) break;
+                        // O holds the sums up to the step before (these scores came after P V of the one before that)
+                        if (!(ok = wait(At::pv + 2 * x + ((s - 1) & 1), ((s - 1) >> 1) & 1, 323))) break;
                         tc_fence_after();
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t o[32];
-                            tmem_ld_x32(tO + 32 * c, o);
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            tmem_ld_x16(tO + 16 * c, o);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st_x32(tO + 32 * c, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st_x16(tO + 16 * c, o);
                         }
                     }
                     tmem_wait_st();
@@ -475,27 +526,24 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                 if (lane == 0) mbar_arrive(bar(At::p_full + buf));
             }
             if (!ok) break;
-            // ---- the next segment's Q (this one's scores are all there), then this one's output
-            const int out_row = row, out_token = token, out_head = head;
-            const bool out = mine;
-            if (!(ok = segment(ord + 1, next))) break;
-            if (next.n > 0) load_q(next);
-            if (!(ok = wait(At::pv + (kTiles == 2 ? x : 0), (g - 1) & 1, 324))) break;
+            // the last two steps' P V (the scores came after those before)
+            if (s >= 2 && !(ok = wait(At::pv + 2 * x + (s & 1), ((s >> 1) - 1) & 1, 324))) break;
+            if (!(ok = wait(At::pv + 2 * x + ((s - 1) & 1), ((s - 1) >> 1) & 1, 325))) break;
             tc_fence_after();
             if (some) {
                 // l_run == 0: a row that sees nothing here.  (A NaN sum makes the row and its log-sum-exp NaN.)  Rows of nodes that are
                 // none have seen the keys before the tree, and give nothing either.
-                const bool none = l_run == 0.f || out_token >= seg.live;
+                const bool none = l_run == 0.f || token >= seg.live;
                 const float inv = none ? 0.f : 1.f / l_run;
                 const float lse = none ? -INFINITY : (m_run * p.scale_log2 + log2f(l_run)) * 0.6931471805599453f;
                 const bool whole = seg.n == seg.of;
                 const long long slot = 2ll * blockIdx.x + (seg.t0 > 0 ? 0 : 1);
-                if (out) {
-                    if (!whole) p.lse_part[slot * p.rows + out_row] = lse;
-                    else if (p.lse) p.lse[((long long)seg.b * p.Hq + out_head) * p.T + out_token] = lse;
+                if (mine) {
+                    if (!whole) p.lse_part[slot * p.rows + row] = lse;
+                    else if (p.lse) p.lse[((long long)seg.b * p.Hq + head) * p.T + token] = lse;
                 }
-                T* o_row = static_cast<T*>(p.o) + (((long long)seg.b * p.T + out_token) * p.Hq + out_head) * D;
-                float4* o_part = reinterpret_cast<float4*>(p.o_part) + slot * (D / 4) * p.rows + out_row;
+                T* o_row = static_cast<T*>(p.o) + (((long long)seg.b * p.T + token) * p.Hq + head) * D;
+                float4* o_part = reinterpret_cast<float4*>(p.o_part) + slot * (D / 4) * p.rows + row;
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
                     uint32_t o[32];
@@ -504,7 +552,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
                     float f[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(o[i]) * inv;
-                    if (!out) continue;
+                    if (!mine) continue;
                     if (whole) {
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
@@ -519,7 +567,6 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(At::seg_empty + ord % kTreeSegs));
-            seg = next;
         }
         __syncwarp();
     }
@@ -530,76 +577,89 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_con
     if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
-// Merge of the rows that several CTAs have worked on (the recurrence of decode.cuh's merge).  Where the run of CTA c begins inside an
-// item, and is the first to, blocks (.., c - 1) merge the item.  A thread owns four columns of a row; a warp eight such
-// pieces of each of four rows, so that both what it reads and what it writes come in runs of 64 bytes.
-// grid: (rows / (1024 / D), CTAs of the kernel before - 1)
+// Merge of the rows that several CTAs have worked on (the recurrence of decode.cuh's merge).  A thread owns four columns of a row; a
+// warp eight such pieces of each of four rows, so that both what it reads and what it writes come in runs of 64 bytes.
+// grid: (parts of a block's rows, y).  kItems: y is an item, where there are no more of them than CTAs; otherwise the run of CTA y + 1
+// begins inside an item and, if it is the first to, the blocks merge that item.  Few items have many parts, and more blocks to share them.
 constexpr int kTreeCombineThreads = 256;
-template <typename T, int D>
+template <bool kItems>
+constexpr int kTreeCombineRows = kItems ? 8 : 32;
+template <typename T, int D, bool kItems>
 __global__ void __launch_bounds__(kTreeCombineThreads) fa_decode_tree_combine_kernel(const TreeParams p, int grid) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kWarpsPerRow = D / 32;
     const int piece = (warp % kWarpsPerRow) * 8 + (lane & 7);
-    const int row = blockIdx.x * (1024 / D) + (warp / kWarpsPerRow) * 4 + (lane >> 3);
     grid_dep_wait();
-    const long long total = p.starts[p.B];
-    const TreePlan plan(total, grid, p.min_tiles);
-    const int c = blockIdx.y + 1;
-    if (c >= plan.ctas) return;
-    const long long cut = plan.begin(c);
-    int b = 0;
-    for (int hi = p.B; hi - b > 1;) {   // the last sequence that starts at or before the cut, 32 places at a time
-        const int step = (hi - b + 31) / 32, at = b + lane * step;
-        const int n = __popc(__ballot_sync(0xffffffffu, at < hi && p.starts[at] <= cut));
-        b += (n - 1) * step;
-        hi = min(hi, b + step);
-    }
+    const TreePlan plan(p.starts[p.B], grid);
     const int items = p.Hkv * p.blocks;
-    const long long seq = p.starts[b], tiles = (p.starts[b + 1] - seq) / items;
-    const int item = (int)((cut - seq) / tiles), hk = item / p.blocks;
-    const long long first = seq + item * tiles;
+    int b = 0, item, first, tiles;
+    if constexpr (kItems) {
+        b = blockIdx.y / items;
+        item = blockIdx.y % items;
+        const int seq = p.starts[b];
+        tiles = (p.starts[b + 1] - seq) / items;
+        if (tiles == 0) return;
+        first = seq + item * tiles;
+    } else {
+        const int cut = plan.begin(blockIdx.y + 1);
+        if ((int)blockIdx.y + 1 >= plan.ctas) return;
+        for (int hi = p.B; hi - b > 1;) {   // the last sequence that starts at or before the cut, 32 places at a time
+            const int step = (hi - b + 31) / 32, at = b + lane * step;
+            const int n = __popc(__ballot_sync(0xffffffffu, at < hi && p.starts[at] <= cut));
+            b += (n - 1) * step;
+            hi = min(hi, b + step);
+        }
+        const int seq = p.starts[b];
+        tiles = (p.starts[b + 1] - seq) / items;
+        item = (cut - seq) / tiles;
+        first = seq + item * tiles;
+        if (cut == first || (int)blockIdx.y != plan.owner(first)) return;
+    }
     const int c0 = plan.owner(first), c1 = plan.owner(first + tiles - 1);
-    if (cut == first || c != c0 + 1) return;
-    const int R = item % p.blocks * p.rows + row;
-    if (row >= p.rows || R >= p.g * p.T) return;
-    const int token = R / p.g, head = hk * p.g + R % p.g;
-    float M = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    constexpr int kN = 4;
-    for (int at = c0; at <= c1; at += kN) {
-        float l[kN], m = M;
-        float4 v[kN];
+    if (c0 == c1) return;   // its only part is where it belongs
+    const int hk = item / p.blocks, R0 = item % p.blocks * p.rows;
+    constexpr int kRows = kTreeCombineRows<kItems>;
+    const int end = min(min(p.rows, (int)(blockIdx.x + 1) * kRows), p.g * p.T - R0);
+    for (int row = blockIdx.x * kRows + (warp / kWarpsPerRow) * 4 + (lane >> 3); row < end; row += 1024 / D) {
+        const int token = (R0 + row) / p.g, head = hk * p.g + (R0 + row) % p.g;
+        float M = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+        constexpr int kN = kItems ? 8 : 4;
+        for (int at = c0; at <= c1; at += kN) {
+            float l[kN], m = M;
+            float4 v[kN];
 #pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            l[i] = -INFINITY;
-            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (at + i <= c1) {
-                const long long slot = 2ll * (at + i) + (at + i == c0 ? 1 : 0);   // (the first part begins the item)
-                l[i] = p.lse_part[slot * p.rows + row];
-                v[i] = reinterpret_cast<const float4*>(p.o_part)[(slot * (D / 4) + piece) * p.rows + row];
+            for (int i = 0; i < kN; ++i) {
+                l[i] = -INFINITY;
+                v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (at + i <= c1) {
+                    const long long slot = 2ll * (at + i) + (at + i == c0 ? 1 : 0);   // (the first part begins the item)
+                    l[i] = p.lse_part[slot * p.rows + row];
+                    v[i] = reinterpret_cast<const float4*>(p.o_part)[(slot * (D / 4) + piece) * p.rows + row];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kN; ++i) m = fmaxf(m, l[i]);
+            const float ref = m == -INFINITY ? 0.f : m, keep = __expf(M - ref);
+            sum *= keep;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) acc[k] *= keep;
+            M = m;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                if (l[i] == -INFINITY) continue;   // (a part that the row sees nothing of; a NaN gets through)
+                const float w = __expf(l[i] - ref);
+                sum += w;
+                acc[0] = fmaf(w, v[i].x, acc[0]);
+                acc[1] = fmaf(w, v[i].y, acc[1]);
+                acc[2] = fmaf(w, v[i].z, acc[2]);
+                acc[3] = fmaf(w, v[i].w, acc[3]);
             }
         }
-#pragma unroll
-        for (int i = 0; i < kN; ++i) m = fmaxf(m, l[i]);
-        const float ref = m == -INFINITY ? 0.f : m, keep = __expf(M - ref);
-        sum *= keep;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) acc[k] *= keep;
-        M = m;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-            if (l[i] == -INFINITY) continue;   // (a part that the row sees nothing of; a NaN gets through)
-            const float w = __expf(l[i] - ref);
-            sum += w;
-            acc[0] = fmaf(w, v[i].x, acc[0]);
-            acc[1] = fmaf(w, v[i].y, acc[1]);
-            acc[2] = fmaf(w, v[i].z, acc[2]);
-            acc[3] = fmaf(w, v[i].w, acc[3]);
-        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + (((long long)b * p.T + token) * p.Hq + head) * D + 4 * piece) =
+            make_uint2(pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv));
+        if (p.lse && piece == 0) p.lse[((long long)b * p.Hq + head) * p.T + token] = sum == 0.f ? -INFINITY : M + logf(sum);
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + (((long long)b * p.T + token) * p.Hq + head) * D + 4 * piece) =
-        make_uint2(pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv));
-    if (p.lse && piece == 0) p.lse[((long long)b * p.Hq + head) * p.T + token] = sum == 0.f ? -INFINITY : M + logf(sum);
 }
 
 }  // namespace fa

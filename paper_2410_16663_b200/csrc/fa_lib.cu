@@ -988,23 +988,32 @@ int decode_impl(const void* q, const void* k_cache, const void* v_cache, void* o
 
 // fa_decode_tree with more rows per kv head than the split decode kernel's CTAs have (see decode_tree.cuh).
 constexpr int kTreeFewRows = 16;
-struct TreeBlocks {   // how the rows that share a kv head are cut: blocks of at most two tiles of 128, of equal size in whole warps
+// How the rows that share a kv head are cut: blocks of at most two tiles of 128, of equal size in whole warps -- and in whole nodes,
+// where a tile is, so that Q is loaded by boxes.
+struct TreeBlocks {
     int blocks, rows;
-    explicit TreeBlocks(int all) : blocks((all + 255) / 256), rows(all) {
-        if (blocks > 1) rows = ((all + blocks - 1) / blocks + 31) / 32 * 32;
+    bool boxes;
+    TreeBlocks(int g, int T) : blocks((g * T + 255) / 256), rows(g * T), boxes(128 % g == 0) {
+        const int unit = boxes && g > 32 ? g : 32;
+        if (blocks > 1) rows = ((rows + blocks - 1) / blocks + unit - 1) / unit * unit;
     }
 };
 template <typename T, int D>
-int tree_launch(const CUtensorMap& tk, const CUtensorMap& tv, const fa::TreeParams& tp, int sms, cudaStream_t st) {
+int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const fa::TreeParams& tp, int sms, cudaStream_t st) {
     const bool two = tp.rows > 128;
     const auto kern = two ? fa::fa_decode_tree_kernel<T, D, 2> : fa::fa_decode_tree_kernel<T, D, 1>;
     const int smem = two ? fa::TreeShape<D, 2>::kSmem : fa::TreeShape<D, 1>::kSmem, threads = two ? fa::TreeShape<D, 2>::kThreads : fa::TreeShape<D, 1>::kThreads;
     int sm_count = 0;
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
     const int grid = sms < fa::kTreeMaxCtas ? sms : fa::kTreeMaxCtas;
-    cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tk, tv, tp);
-    if (e == cudaSuccess && grid > 1)
-        e = fa::launch_dependent(fa::fa_decode_tree_combine_kernel<T, D>, dim3((tp.rows + 1024 / D - 1) / (1024 / D), grid - 1), fa::kTreeCombineThreads, 0, st, tp, grid);
+    cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tp);
+    const long long items = (long long)tp.B * tp.Hkv * tp.blocks;
+    if (e == cudaSuccess && items < grid)
+        e = fa::launch_dependent(fa::fa_decode_tree_combine_kernel<T, D, true>, dim3((tp.rows + fa::kTreeCombineRows<true> - 1) / fa::kTreeCombineRows<true>, (int)items),
+                                 fa::kTreeCombineThreads, 0, st, tp, grid);
+    else if (e == cudaSuccess && grid > 1)
+        e = fa::launch_dependent(fa::fa_decode_tree_combine_kernel<T, D, false>, dim3((tp.rows + fa::kTreeCombineRows<false> - 1) / fa::kTreeCombineRows<false>, grid - 1),
+                                 fa::kTreeCombineThreads, 0, st, tp, grid);
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
 int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
@@ -1016,7 +1025,9 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     int sms = 0;
     rc = check_device(&sms);
     if (rc) return rc;
-    const TreeBlocks tb(p.Hq / p.Hkv * p.T);
+    const TreeBlocks tb(p.Hq / p.Hkv, p.T);
+    const long long tiles = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile;
+    if (tiles * p.B * p.Hkv * tb.blocks > 0x7fffffffll) return FA_ERR_UNSUPPORTED;   // (they are counted in 32 bits)
     fa::TreeParams tp;
     tp.q = p.q;
     tp.o = p.o;
@@ -1027,7 +1038,7 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     tp.block_table = p.block_table;
     tp.o_part = static_cast<float*>(p.workspace);
     tp.lse_part = tp.o_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows * p.d;
-    tp.starts = reinterpret_cast<long long*>(tp.lse_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows);
+    tp.starts = reinterpret_cast<int*>(tp.lse_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows);
     tp.mask_stride = p.mask_stride;
     tp.mask_words = (p.T + 31) / 32;
     tp.B = p.B;
@@ -1040,20 +1051,27 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     tp.blocks = tb.blocks;
     tp.page_size = p.block_table ? p.page_size : 1;
     tp.table_stride = p.table_stride;
-    tp.min_tiles = 1;
-    tp.scale_log2 = p.scale * 1.4426950408889634f;
+    tp.scale_log2 = fmaxf(p.scale * 1.4426950408889634f, 1e-30f);   // (positive, as in dense_fwd_params)
     const bool bf16 = p.dtype == FA_DTYPE_BF16;
     const int slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : Skv_max;
     const bool small = p.block_table && p.page_size < fa::kDecTile;
     const int box_rows = small ? p.page_size : fa::kDecTile;
-    CUtensorMap tk, tv;
+    CUtensorMap tq, tk, tv;
     rc = encode_map_cache(&tk, p.k, slabs, slab_rows, p.Hkv, box_rows, bf16, p.d, small);
     if (rc) return rc;
+    tq = tk;
+    tp.q_boxes = tb.boxes ? 1 : 0;
+    if (tb.boxes) {   // a box: the g heads of 128 / g nodes, all of d
+        const cuuint64_t d = p.d, hq = p.Hq, nodes = p.T;
+        rc = encode_tiled<5>(&tq, type16(bf16), p.q, {64, hq, nodes, d / 64, (cuuint64_t)p.B}, {d * 2, hq * d * 2, 128, nodes * hq * d * 2},
+                             {64, (cuuint32_t)tp.g, (cuuint32_t)(128 / tp.g), (cuuint32_t)(d / 64), 1});
+        if (rc) return rc;
+    }
     rc = encode_map_cache(&tv, p.v, slabs, slab_rows, p.Hkv, box_rows, bf16, p.d);
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (p.d == 64) return bf16 ? tree_launch<__nv_bfloat16, 64>(tk, tv, tp, sms, st) : tree_launch<__half, 64>(tk, tv, tp, sms, st);
-    return bf16 ? tree_launch<__nv_bfloat16, 128>(tk, tv, tp, sms, st) : tree_launch<__half, 128>(tk, tv, tp, sms, st);
+    if (p.d == 64) return bf16 ? tree_launch<__nv_bfloat16, 64>(tq, tk, tv, tp, sms, st) : tree_launch<__half, 64>(tq, tk, tv, tp, sms, st);
+    return bf16 ? tree_launch<__nv_bfloat16, 128>(tq, tk, tv, tp, sms, st) : tree_launch<__half, 128>(tq, tk, tv, tp, sms, st);
 }
 }  // namespace
 
@@ -1161,8 +1179,8 @@ int fa_decode_ex(const fa_decode_params* p, void* stream) {
 size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d) {
     if (B <= 0 || T <= 0 || T > kTreeMaxNodes || Hq <= 0 || Hkv <= 0 || Skv_max <= 0 || (d != 128 && d != 64)) return 0;
     if ((long long)(Hq / Hkv) * T <= kTreeFewRows) return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
-    const TreeBlocks tb(Hq / Hkv * T);
-    return 2 * (size_t)fa::kTreeMaxCtas * tb.rows * ((size_t)d + 1) * sizeof(float) + ((size_t)B + 1) * sizeof(long long);
+    const TreeBlocks tb(Hq / Hkv, T);
+    return 2 * (size_t)fa::kTreeMaxCtas * tb.rows * ((size_t)d + 1) * sizeof(float) + ((size_t)B + 1) * sizeof(int);
 }
 
 int fa_decode_tree(const fa_tree_params* p, void* stream) {

@@ -311,3 +311,23 @@ def sample_rows(cfg: PrefillConfig, n_random: int, seed: int, pairs=None, tile: 
             mine.update(int(x) for x in torch.randint(0, cfg.Sq, (n_random,), generator=gen))
         rows.extend((b, h, i) for i in sorted(mine))
     return rows
+
+
+def tree_inputs(B: int, T: int, Hq: int, Hkv: int, Smax: int, d: int, dtype: str, page: int, device, seed: int = 0):
+    """Inputs of tree attention on the device: q [B,T,Hq,d], caches [B,Smax,Hkv,d] or pools [pages,page,Hkv,d], lengths (uniform in
+    [Smax/8, Smax], with the tree's rows), parents [B,T] (a node hangs off one of the eight before it), block table or None."""
+    gen = torch.Generator(device=device)
+    gen.manual_seed(int(seed))
+    dt = torch.float16 if dtype == "fp16" else torch.bfloat16
+    new = lambda *s: torch.empty(*s, dtype=dt, device=device).normal_(generator=gen)
+    lens = torch.randint(max(T, Smax // 8), max(T, Smax) + 1, (B,), generator=gen, device=device).to(torch.int32)
+    node = torch.arange(T, device=device)
+    low = (node - 8).clamp(min=0)
+    parents = low + (torch.rand(B, T, generator=gen, device=device) * (node - low)).long()
+    parents = torch.where(node == 0, -1, torch.minimum(parents, (node - 1).clamp(min=0))).to(torch.int32)
+    table, shape = None, (B, Smax, Hkv, d)
+    if page:
+        per = -(-Smax // page)
+        table = torch.randperm(B * per, generator=gen, device=device).view(B, per).to(torch.int32)
+        shape = (B * per, page, Hkv, d)
+    return new(B, T, Hq, d), new(*shape), new(*shape), lens, parents, table

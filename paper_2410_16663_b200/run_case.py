@@ -6,6 +6,7 @@ Meant for profilers (ncu wraps this command) and quick timing:
   python -m paper_2410_16663_b200.run_case decode  --B 16 --H 32 --Hkv 8 --Smax 16384 --d 64    (head dimension 64)
   python -m paper_2410_16663_b200.run_case prefill --B 1 --H 32 --S 8192 --fp8           (8-bit operands)
   python -m paper_2410_16663_b200.run_case proj    --B 4 --H 32 --S 2048 --fused 1       (attention + projection)
+  python -m paper_2410_16663_b200.run_case tree    --B 8 --H 32 --Hkv 8 --Smax 8192 --T 64 --page 64   (a tree of T drafted tokens)
 """
 from __future__ import annotations
 
@@ -20,13 +21,15 @@ from . import inputs as synth
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("kind", choices=["prefill", "decode", "proj"])
+    ap.add_argument("kind", choices=["prefill", "decode", "proj", "tree"])
     ap.add_argument("--B", type=int, default=1)
     ap.add_argument("--H", type=int, default=32)
     ap.add_argument("--Hkv", type=int, default=0)
     ap.add_argument("--S", type=int, default=8192)
     ap.add_argument("--Skv", type=int, default=0)
     ap.add_argument("--Smax", type=int, default=16384)
+    ap.add_argument("--T", type=int, default=64, help="tree: nodes")
+    ap.add_argument("--page", type=int, default=0, help="tree: page size (0: contiguous caches)")
     ap.add_argument("--d", type=int, default=128, choices=[64, 128, 256], help="head dimension (prefill: 64, 128, 256; decode: 64, 128)")
     ap.add_argument("--dtype", default="fp16", choices=["fp16", "bf16"])
     ap.add_argument("--noncausal", action="store_true")
@@ -63,6 +66,14 @@ def main():
         ws = torch.empty(max(4, fa.fa_forward_proj_workspace_bytes(cfg.B, cfg.Sq)), dtype=torch.uint8, device=dev)
         run = lambda: fa.fa_forward_proj(q, k, v, w, o, lse, out, cfg.causal, cfg.scale, bool(a.fused), ws)
         work, unit = (cfg.flops() + 2.0 * cfg.B * cfg.Sq * K * K) / 1e12, "TFLOPS"
+    elif a.kind == "tree":
+        q, k, v, sl, parents, table = synth.tree_inputs(a.B, a.T, a.H, hkv, a.Smax, a.d, a.dtype, a.page, dev, seed=9)
+        mask = fa.tree_mask(parents)
+        o, lse = torch.empty_like(q), torch.empty(a.B, a.H, a.T, dtype=torch.float32, device=dev)
+        most = a.Smax if table is None else table.shape[1] * a.page
+        ws = torch.empty(max(16, fa.fa_decode_tree_workspace_bytes(a.B, a.T, a.H, hkv, most, a.d)), dtype=torch.uint8, device=dev)
+        run = lambda: fa.fa_decode_tree(q, k, v, o, lse, sl, mask, 1.0 / math.sqrt(a.d), ws, block_table=table)
+        work, unit = float(sl.sum()) * hkv * a.d * 4 / 1e9, "GB/s"
     else:
         if a.d == 256 or (a.fp8 and a.d != 128):
             raise SystemExit("decode takes d = 128 or 64 (the 8-bit cache form d = 128 only)")
