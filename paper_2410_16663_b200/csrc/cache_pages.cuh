@@ -86,38 +86,49 @@ constexpr int kPagesMaxCluster = 8;
 
 struct PagesShared {
     int upto[kPagesMaxItems];     // pages wanted by the items up to and including this one
+    int entry[kPagesMaxItems];    // where an item's first page goes in its row of the table
     int warp_sum[32];
-    int carry;
     int count[2];                 // free pages of this CTA's part, of two looks in turn
 };
 
-// Inclusive prefix sums of count(i) over i < n into s.upto; every thread of the CTA calls this.
-template <typename Count>
-__device__ __forceinline__ void pages_prefix(PagesShared& s, int n, Count count) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) s.carry = 0;
-    for (int i0 = 0; i0 < n; i0 += kPagesThreads) {
-        const int i = i0 + tid;
-        int x = i < n ? count(i) : 0;
+// Inclusive prefix sum of x over the threads of the CTA, and the sum of all; every thread calls this.
+__device__ __forceinline__ int pages_scan(PagesShared& s, int x, int& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    auto scan = [&](int v) {
 #pragma unroll
         for (int sh = 1; sh < 32; sh <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, x, sh);
-            if (lane >= sh) x += y;
+            const int y = __shfl_up_sync(0xffffffffu, v, sh);
+            if (lane >= sh) v += y;
         }
-        if (lane == 31) s.warp_sum[warp] = x;
-        __syncthreads();
-        int before = s.carry;
-        for (int w = 0; w < warp; ++w) before += s.warp_sum[w];
-        if (i < n) s.upto[i] = before + x;
-        __syncthreads();
-        if (tid == kPagesThreads - 1) s.carry = before + x;
+        return v;
+    };
+    x = scan(x);
+    __syncthreads();   // (the sums of the scan before have been read)
+    if (lane == 31) s.warp_sum[warp] = x;
+    __syncthreads();
+    const int sums = scan(s.warp_sum[lane]);
+    all = __shfl_sync(0xffffffffu, sums, 31);
+    const int before = __shfl_sync(0xffffffffu, sums, warp > 0 ? warp - 1 : 0);
+    return warp > 0 ? before + x : x;
+}
+// Prefix sums of count(i) over i < n into s.upto, entry(i) into s.entry.
+template <typename Count, typename Entry>
+__device__ __forceinline__ void pages_prefix(PagesShared& s, int n, Count count, Entry entry) {
+    int carry = 0, all;
+    for (int i0 = 0; i0 < n; i0 += kPagesThreads) {
+        const int i = i0 + threadIdx.x;
+        const int upto = pages_scan(s, i < n ? count(i) : 0, all);
+        if (i < n) {
+            s.upto[i] = carry + upto;
+            s.entry[i] = entry(i);
+        }
+        carry += all;
     }
     __syncthreads();
 }
 
 // This thread's pages of round `round` as bits (set: free), and how many free ones come before them in the round's part of this CTA.
 __device__ __forceinline__ uint32_t pages_look(PagesShared& s, const int* refs, int num_pages, long long first, int slot, int& before) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t free_bits = 0;
     int r[kPagesPerThread];
     if (first + kPagesPerThread <= num_pages && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
@@ -133,23 +144,14 @@ __device__ __forceinline__ uint32_t pages_look(PagesShared& s, const int* refs, 
 #pragma unroll
     for (int j = 0; j < kPagesPerThread; ++j) free_bits |= (r[j] == 0 ? 1u : 0u) << j;
     const int mine = __popc(free_bits);
-    int x = mine;
-#pragma unroll
-    for (int sh = 1; sh < 32; sh <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, sh);
-        if (lane >= sh) x += y;
-    }
-    __syncthreads();   // (warp_sum of the round before has been read)
-    if (lane == 31) s.warp_sum[warp] = x;
-    __syncthreads();
-    before = x - mine;
-    for (int w = 0; w < warp; ++w) before += s.warp_sum[w];
-    if (tid == kPagesThreads - 1) s.count[slot] = before + mine;
+    int all;
+    before = pages_scan(s, mine, all) - mine;
+    if (threadIdx.x == 0) s.count[slot] = all;
     return free_bits;
 }
 
 // Free pages in all and their distribution: for every free page whose rank is below `total` and whose request can be served in
-// full, give(item, how many of the item's pages come before it, page).  Returns the number of free pages, or some number >= total.
+// full, give(item, entry in its row of the table, page).  Returns the number of free pages, or some number >= total.
 // Every thread of every CTA of the cluster calls this.
 template <typename Give>
 __device__ __forceinline__ int pages_distribute(PagesShared& s, const int* refs, int num_pages, int n_items, int rank, int cluster, Give give) {
@@ -180,14 +182,16 @@ __device__ __forceinline__ int pages_distribute(PagesShared& s, const int* refs,
         const int all = rounds > 1 ? look(r, base) : found;
         int at = seen + base + before;
         const int first = (int)(r * per_round + ((long long)rank * kPagesThreads + threadIdx.x) * kPagesPerThread);
-        for (uint32_t left = bits; left != 0 && at < total; left &= left - 1, ++at) {
-            int lo = 0, hi = n_items - 1;      // the first item whose range ends past `at`
-            while (lo < hi) {
+        int lo = 0;      // the first item whose range ends past `at`
+        if (bits != 0 && at < total)
+            for (int hi = n_items - 1; lo < hi;) {
                 const int mid = (lo + hi) >> 1;
                 if (s.upto[mid] > at) hi = mid;
                 else lo = mid + 1;
             }
-            if (s.upto[lo] <= found) give(lo, at - (lo > 0 ? s.upto[lo - 1] : 0), first + __ffs(left) - 1);
+        for (uint32_t left = bits; left != 0 && at < total; left &= left - 1, ++at) {
+            while (s.upto[lo] <= at) ++lo;
+            if (s.upto[lo] <= found) give(lo, s.entry[lo] + at - (lo > 0 ? s.upto[lo - 1] : 0), first + __ffs(left) - 1);
         }
         seen += all;
     }
@@ -220,12 +224,12 @@ __global__ void __launch_bounds__(kPagesThreads) fa_pages_resize_kernel(const Re
             row[e] = -1;
         }
     }
-    pages_prefix(s, p.B, [&](int b) { return need(b) > p.max_pages ? 0 : max(need(b) - had(b), 0); });
+    pages_prefix(s, p.B, [&](int b) { return need(b) > p.max_pages ? 0 : max(need(b) - had(b), 0); }, had);
     if (tid == 0) shorts = 0;
     __threadfence();
     cluster_sync_all();
-    const int found = pages_distribute(s, p.refs, p.num_pages, p.B, rank, cluster, [&](int b, int i, int page) {
-        p.table[(long long)b * p.table_stride + had(b) + i] = page;
+    const int found = pages_distribute(s, p.refs, p.num_pages, p.B, rank, cluster, [&](int b, int e, int page) {
+        p.table[(long long)b * p.table_stride + e] = page;
         p.refs[page] = 1;
     });
     cluster_sync_all();   // held has been read, and so have the others' counts
@@ -265,10 +269,11 @@ __global__ void __launch_bounds__(kPagesThreads) fa_pages_fork_kernel(const Fork
     grid_dep_wait();
     auto ok_pair = [&](int i) { return p.src[i] >= 0 && p.src[i] < p.B && p.dst[i] >= 0 && p.dst[i] < p.B; };
     auto rows = [&](int i) { return (int)max(0ll, min((long long)p.seqlens[p.src[i]], (long long)p.max_pages * p.page_size)); };
-    pages_prefix(s, p.n, [&](int i) { return ok_pair(i) && rows(i) % p.page_size != 0 ? 1 : 0; });
+    pages_prefix(s, p.n, [&](int i) { return ok_pair(i) && rows(i) % p.page_size != 0 ? 1 : 0; },
+                 [&](int i) { return ok_pair(i) ? rows(i) / p.page_size : 0; });
     if (tid == 0) shorts = 0;
-    const int found = pages_distribute(s, p.refs, p.num_pages, p.n, rank, cluster, [&](int i, int, int page) {
-        p.table[(long long)p.dst[i] * p.table_stride + rows(i) / p.page_size] = page;
+    const int found = pages_distribute(s, p.refs, p.num_pages, p.n, rank, cluster, [&](int i, int e, int page) {
+        p.table[(long long)p.dst[i] * p.table_stride + e] = page;
         p.refs[page] = 1;
     });
     for (int i = rank * 32 + (tid >> 5); i < p.n; i += cluster * 32) {   // a warp per pair
@@ -303,13 +308,13 @@ __global__ void __launch_bounds__(kPagesThreads) fa_pages_fork_kernel(const Fork
     if (tid == 0) *p.n_short = shorts;
 }
 
-// The rows of a fork: the filled rows of each last page, in every plane.  They lie one after the other.
-// grid: (parts, planes, pairs)
+// The rows of a fork: the filled rows of each last page, in every plane.  They lie one after the other.  grid: (pairs, planes): pairs
+// that share a prompt copy the same rows of a plane at about the same time, and L2 has them.
 constexpr int kForkThreads = 256;
 constexpr int kForkBatch = 8;
 __global__ void __launch_bounds__(kForkThreads) fa_pages_fork_copy_kernel(const ForkParams p) {
     grid_dep_wait();
-    const int i = blockIdx.z, a = p.src[i], b = p.dst[i];
+    const int i = blockIdx.x, a = p.src[i], b = p.dst[i];
     if (a < 0 || a >= p.B || b < 0 || b >= p.B) return;
     const int len = p.seqlens[b];          // (0 where it was not served)
     const int rows = len % p.page_size, e = len / p.page_size;
@@ -321,7 +326,7 @@ __global__ void __launch_bounds__(kForkThreads) fa_pages_fork_copy_kernel(const 
     const uint4* x = base + from * page_vecs;
     uint4* y = base + to * page_vecs;
     const int n = rows * p.row_vecs;
-    for (int u0 = blockIdx.x * kForkThreads * kForkBatch; u0 < n; u0 += gridDim.x * kForkThreads * kForkBatch) {
+    for (int u0 = 0; u0 < n; u0 += kForkThreads * kForkBatch) {
         uint4 r[kForkBatch];
 #pragma unroll
         for (int j = 0; j < kForkBatch; ++j) {

@@ -1349,7 +1349,7 @@ int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k,
     cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_fork_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, 0, st, fp, cluster);
     if (e != cudaSuccess) return cuda_fail(e);
     if (layers == 0 || page_size == 1) return FA_OK;   // (a page of one row is never partly filled)
-    e = fa::launch_dependent(fa::fa_pages_fork_copy_kernel, dim3(1, 2 * layers, n), fa::kForkThreads, 0, st, fp);
+    e = fa::launch_dependent(fa::fa_pages_fork_copy_kernel, dim3(n, 2 * layers), fa::kForkThreads, 0, st, fp);
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
 

@@ -57,7 +57,7 @@ __device__ __forceinline__ float load1(const __nv_bfloat16* x) { return __bfloat
 
 // kVec: V is a multiple of four and the arrays are aligned, so that rows are read four entries at a time.
 template <typename T, bool kVec>
-__global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const VerifyParams p, int cluster) {
+__global__ void __launch_bounds__(kVerifyThreads, 2) fa_spec_verify_kernel(const VerifyParams p, int cluster) {
     __shared__ float px[kVerifyMaxNodes], qx[kVerifyMaxNodes], uni[kVerifyMaxNodes];
     __shared__ int tok[kVerifyMaxNodes], gone[kVerifyMaxNodes];
     __shared__ short par[kVerifyMaxNodes], walk[kVerifyMaxNodes + 1];
@@ -86,30 +86,21 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
     }
     __syncthreads();
 
-    // every warp has all parents and tokens, eight per lane
-    int up[kVerifyMaxNodes / 32], said[kVerifyMaxNodes / 32];
-#pragma unroll
-    for (int w = 0; w < kVerifyMaxNodes / 32; ++w) {
-        const bool there = 32 * w + lane < live;
-        up[w] = there ? par[32 * w + lane] : -1;
-        said[w] = there ? tok[32 * w + lane] : -1;
-    }
-    // the next child of `node` past node `after`, or `live`
+    // the next child of `node` past node `after`, or `live` (32 nodes at a time, the whole warp)
     auto child = [&](int node, int after) {
-        int found = live;
-#pragma unroll
-        for (int w = kVerifyMaxNodes / 32 - 1; w >= 0; --w) {
-            const uint32_t m = __ballot_sync(0xffffffffu, up[w] == node && 32 * w + lane > after);
-            if (m) found = 32 * w + __ffs(m) - 1;
+        for (int i0 = (after + 1) & ~31; i0 < live; i0 += 32) {
+            const int i = i0 + lane;
+            const uint32_t m = __ballot_sync(0xffffffffu, i < live && i > after && par[i] == node);
+            if (m) return i0 + __ffs(m) - 1;
         }
-        return found;
+        return live;
     };
 
-    // entries v of this CTA, several at a time: f(v, p(v), q(v), E(v))
-    auto each = [&](const T* pr, const T* qr, const float* er, auto f) {
+    // entries v of this CTA, some at a time: f(v, p(v), q(v), E(v))
+    auto each = [&](const T* pr, const T* qr, const float* er, auto at_once, auto f) {
         if constexpr (kVec) {
             const int groups = p.V / 4, step = cluster * kVerifyThreads;
-            constexpr int kN = 4;
+            constexpr int kN = decltype(at_once)::value;
             for (int g0 = rank * kVerifyThreads + tid; g0 < groups; g0 += kN * step) {
                 float a[kN][4], c[kN][4], e[kN][4];
 #pragma unroll
@@ -131,7 +122,7 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
             }
         } else {
             const int step = cluster * kVerifyThreads;
-            constexpr int kN = 8;
+            constexpr int kN = 2 * decltype(at_once)::value;
             for (int v0 = rank * kVerifyThreads + tid; v0 < p.V; v0 += kN * step) {
                 float a[kN], c[kN], e[kN];
 #pragma unroll
@@ -161,8 +152,7 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
         float r = fmaxf(__fsub_rn(px[i], __fmul_rn(s, Q ? qi : 0.f)), 0.f);
         if (!Q) {
             bool again = false;   // an earlier child had the same token
-#pragma unroll
-            for (int w = 0; w < kVerifyMaxNodes / 32; ++w) again |= up[w] == cur && 32 * w + lane < i && said[w] == tok[i];
+            for (int k = lane; k < i; k += 32) again |= par[k] == cur && tok[k] == tok[i];
             if (__any_sync(0xffffffffu, again)) r = 0.f;
         }
         if (__fmul_rn(__fmul_rn(u, Z), qi) < r) {
@@ -179,17 +169,18 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
         i = child(cur, i);
         if (Q && i < live) {   // another child: the mass of what is left
             float sum = 0.f;
-            each(P + (long long)cur * p.V, Q + (long long)cur * p.V, static_cast<const float*>(nullptr),
+            each(P + (long long)cur * p.V, Q + (long long)cur * p.V, static_cast<const float*>(nullptr), std::integral_constant<int, 4>(),
                  [&](int, float a, float c, float) { sum += fmaxf(__fsub_rn(a, __fmul_rn(s, c)), 0.f); });
 #pragma unroll
             for (int sh = 16; sh > 0; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
             __syncthreads();
             if (lane == 0) warp_sum[warp] = sum;
             __syncthreads();
-            if (tid == 0) {
-                float all = 0.f;
-                for (int w = 0; w < kVerifyThreads / 32; ++w) all += warp_sum[w];
-                z_slot[turn] = all;
+            if (warp == 0) {
+                float all = lane < kVerifyThreads / 32 ? warp_sum[lane] : 0.f;
+#pragma unroll
+                for (int sh = 8; sh > 0; sh >>= 1) all += __shfl_xor_sync(0xffffffffu, all, sh);
+                if (lane == 0) z_slot[turn] = all;
             }
             cluster_sync_all();
             Z = 0.f;
@@ -198,14 +189,11 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
         }
     }
     int rejected = 0;   // tokens of cur's children: none of them stands
-    if (!Q) {
-#pragma unroll
-        for (int w = 0; w < kVerifyMaxNodes / 32; ++w) {
-            const uint32_t m = __ballot_sync(0xffffffffu, up[w] == cur);
-            if (warp == 0 && up[w] == cur) gone[rejected + __popc(m & ((1u << lane) - 1u))] = said[w];
-            rejected += __popc(m);
+    if (!Q)
+        for (int i = child(cur, cur); i < live; i = child(cur, i)) {
+            if (tid == 0) gone[rejected] = tok[i];
+            ++rejected;
         }
-    }
     __syncthreads();
 
     // ---- the token after the last node: largest score, then lowest index, as one number (scores are positive)
@@ -214,7 +202,7 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
         float top = 0.f, most = 0.f;   // most: a little less than top
         int at = 0;
         const float sub = pass == 0 ? s : 0.f;
-        each(P + (long long)cur * p.V, pass == 0 && Q ? Q + (long long)cur * p.V : nullptr, E, [&](int v, float a, float c, float e) {
+        each(P + (long long)cur * p.V, pass == 0 && Q ? Q + (long long)cur * p.V : nullptr, E, std::integral_constant<int, 2>(), [&](int v, float a, float c, float e) {
             const float r = __fsub_rn(a, __fmul_rn(sub, c));
             if (!(r > 0.f) || !(r >= most * e)) return;   // (nearly all, without a division)
             const float score = __fdiv_rn(r, e);
@@ -234,9 +222,14 @@ __global__ void __launch_bounds__(kVerifyThreads) fa_spec_verify_kernel(const Ve
         }
         if (lane == 0) warp_best[warp] = key;
         __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < kVerifyThreads / 32; ++w) key = warp_best[w] > key ? warp_best[w] : key;
-            best_slot[pass] = key;
+        if (warp == 0) {
+            key = lane < kVerifyThreads / 32 ? warp_best[lane] : 0ull;
+#pragma unroll
+            for (int sh = 8; sh > 0; sh >>= 1) {
+                const unsigned long long o = __shfl_xor_sync(0xffffffffu, key, sh);
+                key = o > key ? o : key;
+            }
+            if (lane == 0) best_slot[pass] = key;
         }
         cluster_sync_all();
         for (int c = 0; c < cluster; ++c) {
