@@ -1304,7 +1304,10 @@ int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int
     if (int rc = check_device()) return rc;
     fa::ResizeParams rp = {block_table, held, refs, want, n_short, B, max_pages, table_stride, page_size, num_pages};
     const int cluster = pages_cluster(num_pages);
-    const cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_resize_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, 0,
+    int sm_count = 0;
+    if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(fa::fa_pages_resize_kernel), sizeof(fa::PagesShared), &sm_count))
+        return cuda_fail(static_cast<cudaError_t>(ce));
+    const cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_resize_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, sizeof(fa::PagesShared),
                                                         static_cast<cudaStream_t>(stream), rp, cluster);
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
@@ -1346,7 +1349,10 @@ int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k,
     fp.layer_stride = layer_stride / 16;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int cluster = pages_cluster(num_pages);
-    cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_fork_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, 0, st, fp, cluster);
+    int sm_count = 0;
+    if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(fa::fa_pages_fork_kernel), sizeof(fa::PagesShared), &sm_count))
+        return cuda_fail(static_cast<cudaError_t>(ce));
+    cudaError_t e = fa::launch_dependent_clusters(fa::fa_pages_fork_kernel, dim3(cluster), cluster, 1, fa::kPagesThreads, sizeof(fa::PagesShared), st, fp, cluster);
     if (e != cudaSuccess) return cuda_fail(e);
     if (layers == 0 || page_size == 1) return FA_OK;   // (a page of one row is never partly filled)
     e = fa::launch_dependent(fa::fa_pages_fork_copy_kernel, dim3(n, 2 * layers), fa::kForkThreads, 0, st, fp);

@@ -180,6 +180,9 @@ __device__ __forceinline__ int clc_answer(uint32_t src) {
 __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
+// The two halves of a meeting that orders nothing that the threads have written.
+__device__ __forceinline__ void cluster_arrive_relaxed() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 // The address of another CTA's copy of a shared-memory variable, and a load from it.
 __device__ __forceinline__ uint32_t cluster_map(uint32_t addr, uint32_t rank) {
     uint32_t r;
