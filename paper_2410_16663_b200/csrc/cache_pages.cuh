@@ -76,18 +76,21 @@ __global__ void __launch_bounds__(kCompactThreads) fa_cache_compact_kernel(const
 }
 
 // ---------------------------------------------------------------------------------------
-// Pages of a pool.  One cluster looks the reference counts over, 16 pages per thread at a time; each CTA has the requests (pages
-// wanted, in order) as inclusive prefix sums in its shared memory, and a free page of rank r goes to the request whose
-// range r falls into.
+// Pages of a pool.  One cluster looks the reference counts over, 16 pages per thread at a time, and each CTA lists the free ones of its
+// part; it has the requests (pages wanted, in order) as inclusive prefix sums in shared memory, and a free page of rank r goes
+// to the request whose range r falls into.  (Through the list, neighbouring ranks are written by neighbouring threads: their
+// entries of the table lie next to each other.)
 constexpr int kPagesThreads = 1024;
 constexpr int kPagesPerThread = 16;
 constexpr int kPagesMaxItems = 4096;   // sequences of a resize, pairs of a fork
 constexpr int kPagesMaxCluster = 8;
+constexpr int kPagesBatch = 8;         // a lane's entries that are read before the first is written
 
 struct PagesShared {
     int upto[kPagesMaxItems];     // pages wanted by the items up to and including this one
     int entry[kPagesMaxItems];    // where an item's first page goes in its row of the table
-    int need[kPagesMaxItems];     // resize: entries that a sequence is to have
+    int need[kPagesMaxItems];     // resize: entries that a sequence is to have; fork: rows of a last page that is partly filled
+    unsigned short list[kPagesThreads * kPagesPerThread];   // free pages of this CTA's part of a round
     int warp_sum[32];
     int shorts;
     int count[2];                 // free pages of this CTA's part, of two looks in turn
@@ -127,42 +130,64 @@ __device__ __forceinline__ void pages_prefix(PagesShared& s, int n, Count count)
     __syncthreads();
 }
 
-// This thread's pages of round `round` as bits (set: free), and how many free ones come before them in the round's part of this CTA.
-__device__ __forceinline__ uint32_t pages_look(PagesShared& s, const int* refs, int num_pages, long long first, int slot, int& before) {
-    uint32_t free_bits = 0;
-    int r[kPagesPerThread];
-    if (first + kPagesPerThread <= num_pages && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
+// The free pages of this CTA's part of a round, in order, as places in the part (s.list), and how many they are.  A warp reads its 512
+// counts in four runs of 512 bytes; a lane has four neighbouring ones of each.
+__device__ __forceinline__ int pages_look(PagesShared& s, const int* refs, int num_pages, long long first) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kRuns = kPagesPerThread / 4;
+    const long long at = first + warp * (32 * kPagesPerThread) + lane * 4;
+    int r[kRuns][4];
 #pragma unroll
-        for (int j = 0; j < kPagesPerThread / 4; ++j) {
-            const int4 x = __ldcg(reinterpret_cast<const int4*>(refs + first) + j);
-            r[4 * j] = x.x, r[4 * j + 1] = x.y, r[4 * j + 2] = x.z, r[4 * j + 3] = x.w;
+    for (int k = 0; k < kRuns; ++k) {
+        if (at + 128 * k + 4 <= num_pages && (reinterpret_cast<uintptr_t>(refs) & 15u) == 0) {
+            const int4 x = __ldcg(reinterpret_cast<const int4*>(refs + at + 128 * k));
+            r[k][0] = x.x, r[k][1] = x.y, r[k][2] = x.z, r[k][3] = x.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[k][j] = at + 128 * k + j < num_pages ? __ldcg(refs + at + 128 * k + j) : 1;
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < kPagesPerThread; ++j) r[j] = first + j < num_pages ? __ldcg(refs + first + j) : 1;
     }
+    // how many are free, a byte per run (at most 128 in a warp)
+    uint32_t mine = 0;
 #pragma unroll
-    for (int j = 0; j < kPagesPerThread; ++j) free_bits |= (r[j] == 0 ? 1u : 0u) << j;
-    const int mine = __popc(free_bits);
-    int all;
-    before = pages_scan(s, mine, all) - mine;
-    if (threadIdx.x == 0) s.count[slot] = all;
-    return free_bits;
+    for (int k = 0; k < kRuns; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mine += (r[k][j] == 0 ? 1u : 0u) << (8 * k);
+    uint32_t upto = mine;
+#pragma unroll
+    for (int sh = 1; sh < 32; sh <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, upto, sh);
+        if (lane >= sh) upto += y;
+    }
+    const uint32_t runs = __shfl_sync(0xffffffffu, upto, 31);
+    int sum = 0, all;
+#pragma unroll
+    for (int k = 0; k < kRuns; ++k) sum += runs >> (8 * k) & 255u;
+    int before = __shfl_sync(0xffffffffu, pages_scan(s, lane == 31 ? sum : 0, all), 31) - sum;   // of the warps before
+#pragma unroll
+    for (int k = 0; k < kRuns; ++k) {
+        int to = before + (int)((upto - mine) >> (8 * k) & 255u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (r[k][j] == 0) s.list[to++] = (unsigned short)(warp * (32 * kPagesPerThread) + 128 * k + lane * 4 + j);
+        before += runs >> (8 * k) & 255u;
+    }
+    __syncthreads();
+    return all;
 }
 
 // Free pages in all and their distribution: for every free page whose rank is below `total` and whose request can be served in
-// full, give(item, entry in its row of the table, page).  Returns the number of free pages, or some number >= total.
-// Every thread of every CTA of the cluster calls this.
+// full, give(item, entry in its row of the table, page), neighbouring ranks by neighbouring threads.  Returns the number of
+// free pages, or some number >= total.  Every thread of every CTA of the cluster calls this.
 template <typename Give>
 __device__ __forceinline__ int pages_distribute(PagesShared& s, const int* refs, int num_pages, int n_items, int rank, int cluster, Give give) {
     const int total = n_items > 0 ? s.upto[n_items - 1] : 0;
-    const long long per_round = (long long)cluster * kPagesThreads * kPagesPerThread;
+    const long long part = kPagesThreads * kPagesPerThread, per_round = cluster * part;
     const uint32_t count_at = smem_u32(s.count);
-    int found = 0, rounds = 0, before = 0, turn = 0;
-    uint32_t bits = 0;
-    auto look = [&](int round, int& base) {   // base: free pages in the round before this CTA's part; returns those of the round
-        const long long first = round * per_round + ((long long)rank * kPagesThreads + threadIdx.x) * kPagesPerThread;
-        bits = pages_look(s, refs, num_pages, first, turn, before);
+    int found = 0, rounds = 0, turn = 0, mine = 0, base = 0;
+    auto look = [&](int round) {   // mine: free pages of this CTA's part, base: of the parts before it; returns those of the round
+        mine = pages_look(s, refs, num_pages, round * per_round + rank * part);
+        if (threadIdx.x == 0) s.count[turn] = mine;
         cluster_sync_all();
         int all = 0;
         base = 0;
@@ -174,26 +199,25 @@ __device__ __forceinline__ int pages_distribute(PagesShared& s, const int* refs,
         turn ^= 1;   // (a count is written again only after another meeting, by when all have read it)
         return all;
     };
-    int base = 0;
-    for (; rounds * per_round < num_pages && found < total; ++rounds) found += look(rounds, base);
-    // (one round, the usual case: its bits are still there; otherwise the counts are looked over again, in L2)
+    for (; rounds * per_round < num_pages && found < total; ++rounds) found += look(rounds);
+    // (one round, the usual case: its list is still there; otherwise the counts are looked over again, in L2)
     int seen = 0;
     for (int r = 0; r < rounds && seen < total; ++r) {
-        const int all = rounds > 1 ? look(r, base) : found;
-        int at = seen + base + before;
-        const int first = (int)(r * per_round + ((long long)rank * kPagesThreads + threadIdx.x) * kPagesPerThread);
-        int lo = 0;      // the first item whose range ends past `at`
-        if (bits != 0 && at < total)
+        const int all = rounds > 1 ? look(r) : found;
+        const long long first = r * per_round + rank * part;
+        const int n = min(mine, total - seen - base);
+        for (int i = threadIdx.x; i < n; i += kPagesThreads) {
+            const int at = seen + base + i;
+            int lo = 0;      // the first item whose range ends past `at`
             for (int hi = n_items - 1; lo < hi;) {
                 const int mid = (lo + hi) >> 1;
                 if (s.upto[mid] > at) hi = mid;
                 else lo = mid + 1;
             }
-        for (uint32_t left = bits; left != 0 && at < total; left &= left - 1, ++at) {
-            while (s.upto[lo] <= at) ++lo;
-            if (s.upto[lo] <= found) give(lo, s.entry[lo] + at - (lo > 0 ? s.upto[lo - 1] : 0), first + __ffs(left) - 1);
+            if (s.upto[lo] <= found) give(lo, s.entry[lo] + at - (lo > 0 ? s.upto[lo - 1] : 0), (int)(first + s.list[i]));
         }
         seen += all;
+        if (rounds > 1) __syncthreads();   // (the list is written anew)
     }
     return found;
 }
@@ -209,10 +233,10 @@ struct ResizeParams {
 
 // Sequence b is to hold ceil(want[b] / page_size) pages.  grid: one cluster.  (What the sequences hold and want is read once, so that
 // the CTAs meet only behind what is given back and for the counts, and at the end wait for no writes.  512 sequences on 131072 pages
-// 14 -> 7 us a call.)
+// 14 -> 9.5 us a call, with the list.)
 __global__ void __launch_bounds__(kPagesThreads) fa_pages_resize_kernel(const ResizeParams p, int cluster) {
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    PagesShared& s = *reinterpret_cast<PagesShared*>(smem_raw);
+    extern __shared__ __align__(16) uint8_t pages_smem[];
+    PagesShared& s = *reinterpret_cast<PagesShared*>(pages_smem);
     const int tid = threadIdx.x, rank = blockIdx.x, lane = tid & 31;
     grid_dep_wait();
     for (int b = tid; b < p.B; b += kPagesThreads) {
@@ -226,10 +250,15 @@ __global__ void __launch_bounds__(kPagesThreads) fa_pages_resize_kernel(const Re
     for (int b = rank * 32 + (tid >> 5); b < p.B; b += cluster * 32) {
         int* row = p.table + (long long)b * p.table_stride;
         const int held = s.entry[b];
-        for (int e = s.need[b] + lane; e < held; e += 32) {
-            const int page = row[e];
-            if (page >= 0 && page < p.num_pages) atomicSub(p.refs + page, 1);
-            row[e] = -1;
+        for (int e0 = s.need[b] + lane; e0 < held; e0 += 32 * kPagesBatch) {
+            int page[kPagesBatch];
+#pragma unroll
+            for (int k = 0; k < kPagesBatch; ++k) page[k] = e0 + 32 * k < held ? row[e0 + 32 * k] : -1;
+#pragma unroll
+            for (int k = 0; k < kPagesBatch; ++k) {
+                if (page[k] >= 0 && page[k] < p.num_pages) atomicSub(p.refs + page[k], 1);
+                if (e0 + 32 * k < held) row[e0 + 32 * k] = -1;
+            }
         }
     }
     pages_prefix(s, p.B, [&](int b) { return s.need[b] > p.max_pages ? 0 : max(s.need[b] - s.entry[b], 0); });
@@ -272,8 +301,8 @@ struct ForkParams {
 
 // The tables of a fork: dst[i] gets src[i]'s full pages, and a fresh one for a last page that is partly filled.  grid: one cluster.
 __global__ void __launch_bounds__(kPagesThreads) fa_pages_fork_kernel(const ForkParams p, int cluster) {
-    extern __shared__ __align__(16) uint8_t smem_raw[];
-    PagesShared& s = *reinterpret_cast<PagesShared*>(smem_raw);
+    extern __shared__ __align__(16) uint8_t pages_smem[];
+    PagesShared& s = *reinterpret_cast<PagesShared*>(pages_smem);
     const int tid = threadIdx.x, rank = blockIdx.x, lane = tid & 31;
     grid_dep_wait();
     auto ok_pair = [&](int i) { return p.src[i] >= 0 && p.src[i] < p.B && p.dst[i] >= 0 && p.dst[i] < p.B; };
@@ -299,13 +328,15 @@ __global__ void __launch_bounds__(kPagesThreads) fa_pages_fork_kernel(const Fork
         const bool part = s.need[i] != 0, served = !part || s.upto[i] <= found;
         const int* from = p.table + (long long)p.src[i] * p.table_stride;
         int* to = p.table + (long long)p.dst[i] * p.table_stride;
-        for (int e = lane; e < p.max_pages; e += 32) {
-            if (served && e < full) {
-                const int page = from[e];
-                to[e] = page;
-                if (page >= 0 && page < p.num_pages) atomicAdd(p.refs + page, 1);
-            } else if (!(served && part && e == full)) {
-                to[e] = -1;
+        for (int e0 = lane; e0 < p.max_pages; e0 += 32 * kPagesBatch) {
+            int page[kPagesBatch];
+#pragma unroll
+            for (int k = 0; k < kPagesBatch; ++k) page[k] = served && e0 + 32 * k < full ? from[e0 + 32 * k] : -1;
+#pragma unroll
+            for (int k = 0; k < kPagesBatch; ++k) {
+                const int e = e0 + 32 * k;
+                if (page[k] >= 0 && page[k] < p.num_pages) atomicAdd(p.refs + page[k], 1);
+                if (e < p.max_pages && !(served && part && e == full)) to[e] = page[k];
             }
         }
         if (lane == 0) {
