@@ -27,6 +27,9 @@ struct TreeShape {
     static constexpr int kSlots = 7 * 128 / D - kTiles;              // 224 KiB in all
     static constexpr int kSmem = 1024 + (kTiles + kSlots) * kTileB;
     static constexpr int kThreads = 128 * kTiles + 64 + 64 * kTiles;
+    // K and V tiles: groups of eight keys, each with its 64-element blocks one after the other (eight rows of 128 swizzled
+    // bytes): a page of any size is one box, and all 128 keys are one operand of regular strides.
+    static constexpr int kGroupB = 1024 * (D / 64);
     // Keys of a softmax step.  A row tile has two score buffers of so many columns: while one is in the softmax, the
     // tensor cores take the other's probabilities and fill it again.
     static constexpr int kStep = kTiles == 2 ? 64 : 128;
@@ -42,19 +45,22 @@ struct TreeParams {
     const int* block_table;   // nullptr: contiguous
     float* o_part;            // [2 ctas][D/4][rows][4]
     float* lse_part;          // [2 ctas][rows]
-    int* starts;              // [B + 1] first tile of each sequence, and of none
+    int* starts;              // [B + 1] first unit of each sequence, and of none
     long long mask_stride;
     int mask_words;
     int B, T, Hq, Hkv, g, Smax;
     int rows;                 // rows per block (at most 128 kTiles), blocks per (sequence, kv head)
     int blocks;
     int q_boxes;              // 128 rows are the heads of whole nodes, and one box of the tensor map over q
-    int page_size, table_stride;
+    int page_size, table_stride, num_pages;
     float scale_log2;
 };
 
-// The tiles of item `it` (kv head and row block) of sequence b come behind those of the items before it; CTA c of `ctas` takes the
-// tiles from begin(c) to begin(c + 1): one more than the others in the first `more` CTAs.
+// The work is dealt out in units: an item is kTreeItemCost of them, for what its beginning and its end take, and one for each tile.
+// (Items of nine tiles on 16-key pages, eight kv heads: a CTA that got ten of them took 148 thousand clocks, the median 104.)
+// Those of item `it` (kv head and row block) of sequence b come behind those of the items before it; CTA c of `ctas` has the units
+// from begin(c) to begin(c + 1): one more than the others in the first `more` CTAs.
+constexpr int kTreeItemCost = 1;
 struct TreePlan {
     int total, ctas, each, more;
     __device__ __forceinline__ TreePlan(int total, int grid) : total(total), ctas(max(1, min(grid, total))) {
@@ -62,11 +68,12 @@ struct TreePlan {
         more = total - each * ctas;
     }
     __device__ __forceinline__ int begin(int c) const { return c >= ctas ? total : c * each + min(c, more); }
-    __device__ __forceinline__ int owner(int tile) const {   // (of a tile that there is)
+    __device__ __forceinline__ int owner(int unit) const {   // (of a unit that there is)
         const int big = more * (each + 1);
-        return tile < big ? tile / (each + 1) : more + (tile - big) / each;
+        return unit < big ? unit / (each + 1) : more + (unit - big) / each;
     }
 };
+__device__ __forceinline__ int tree_item_units(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile + kTreeItemCost : 0; }
 __device__ __forceinline__ int tree_seq_len(const TreeParams& p, int b) { return max(0, min(p.seqlens[b], p.Smax)); }
 
 // A run of tiles of one item; n == 0: no more.
@@ -81,6 +88,28 @@ struct TreeBars {
     static constexpr int full = 0, empty = kSlots, s_full = 2 * kSlots, p_full = s_full + 4, pv = p_full + 4, q_full = pv + 4,
                          q_empty = q_full + 2, seg_full = q_empty + 2, seg_empty = seg_full + kTreeSegs, count = seg_empty + kTreeSegs;
 };
+
+// Products as in prefill_pipelined.cuh, with the upper half of a descriptor by the bytes from one group of eight rows to the next.
+__host__ __device__ constexpr uint32_t tree_desc_hi(uint32_t group_bytes) { return (group_bytes >> 4) | (1u << 14) | (2u << 29); }
+__device__ __forceinline__ void tree_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %6};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(a_hi), "r"(b_hi)
+        : "memory");
+}
+__device__ __forceinline__ void tree_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(b_hi)
+        : "memory");
+}
 
 // Every other slot of the ring: K tiles from slot 0 on, V tiles from slot 1.
 template <int N>
@@ -109,7 +138,8 @@ __device__ __forceinline__ float tree_row_max(const uint32_t (&s)[N]) {
 template <typename T, int D, int kTiles>
 __global__ void __launch_bounds__(TreeShape<D, kTiles>::kThreads, 1)
 fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                      const __grid_constant__ CUtensorMap tm_v, const TreeParams p) {
+                      const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_k8,
+                      const __grid_constant__ CUtensorMap tm_v8, const TreeParams p) {
     using Shape = TreeShape<D, kTiles>;
     constexpr int kSlots = Shape::kSlots, kTileB = Shape::kTileB, kStep = Shape::kStep, kSub = kDecTile / kStep;
     using At = TreeBars<kSlots>;
@@ -139,12 +169,59 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         tmem_alloc(smem_u32(&tmem_holder), 512);
         tmem_relinquish();
     }
+    // The loading warp finds the CTA's run meanwhile: its first and last unit, and the sequence and the place in it of the first.  (As
+    // little code as can be: it runs once, and fetching its instructions takes longer than executing them.)
+    const int items = p.Hkv * p.blocks;
+    int pos = 0, end = 0, b = 0, in_seq = 0, chunk = 0, chunk_len = 0;
+    auto lens_at = [&](int b0) {   // the lengths of 32 sequences, one per lane
+        if (b0 != chunk) {
+            chunk = b0;
+            chunk_len = b0 + lane < p.B ? tree_seq_len(p, b0 + lane) : 0;
+        }
+        return chunk_len;
+    };
+    auto len_of = [&](int b) { return __shfl_sync(0xffffffffu, lens_at(b & ~31), b & 31); };
+    if (warp == kSoftmaxWarps) {
+        grid_dep_wait();
+        chunk = -1;
+        int total = 0, mine = 0, upto = 0;   // units of this lane's sequence of a chunk, and with those of all before it
+        auto scan = [&](int b0, int before) {
+            mine = tree_item_units(lens_at(b0)) * items;
+            upto = mine;
+#pragma unroll 1
+            for (int sh = 1; sh < 32; sh <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, sh);
+                if (lane >= sh) upto += y;
+            }
+            upto += before;
+            return __shfl_sync(0xffffffffu, upto, 31);
+        };
+#pragma unroll 1
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            total = scan(b0, total);
+            if (blockIdx.x == 0 && b0 + lane < p.B) p.starts[b0 + lane] = upto - mine;
+        }
+        if (blockIdx.x == 0 && lane == 0) p.starts[p.B] = total;
+        const TreePlan plan(total, gridDim.x);
+        pos = plan.begin(blockIdx.x);
+        end = plan.begin(blockIdx.x + 1);
+#pragma unroll 1
+        for (int b0 = p.B > 32 ? 0 : -32, before = 0; pos < end; b0 += 32) {   // (one chunk: it has been scanned)
+            if (b0 >= 0) before = scan(b0, before);
+            const uint32_t past = __ballot_sync(0xffffffffu, upto > pos);
+            if (past) {
+                const int at = __ffs(past) - 1;
+                b = max(b0, 0) + at;
+                in_seq = pos - __shfl_sync(0xffffffffu, upto - mine, at);
+                break;
+            }
+        }
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
     const uint32_t tmem_o = tmem + 2 * kTiles * kStep;   // behind the score buffers
-
     grid_dep_wait();
 
     const int ps = p.page_size;
@@ -159,69 +236,35 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 
     if (warp == kSoftmaxWarps) {
         // ---------------------------------------------------------------- segments, K and V
-        const int items = p.Hkv * p.blocks;
-        // the lengths of 32 sequences at a time, one per lane
-        int chunk = -32, chunk_len = 0;
-        auto lens_at = [&](int b0) {
-            if (b0 != chunk) {
-                chunk = b0;
-                chunk_len = b0 + lane < p.B ? tree_seq_len(p, b0 + lane) : 0;
-            }
-            return chunk_len;
-        };
-        auto len_of = [&](int b) { return __shfl_sync(0xffffffffu, lens_at(b & ~31), b & 31); };
-        auto tiles_at = [&](int b0) { return (lens_at(b0) + kDecTile - 1) / kDecTile * items; };   // of this lane's sequence's items
-        auto scan = [&](int x) {
-#pragma unroll
-            for (int sh = 1; sh < 32; sh <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, x, sh);
-                if (lane >= sh) x += y;
-            }
-            return x;
-        };
-        int total = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const int mine = tiles_at(b0), upto = total + scan(mine);
-            if (blockIdx.x == 0 && b0 + lane < p.B) p.starts[b0 + lane] = upto - mine;
-            total = __shfl_sync(0xffffffffu, upto, 31);
-        }
-        if (blockIdx.x == 0 && lane == 0) p.starts[p.B] = total;
-        const TreePlan plan(total, gridDim.x);
-        const int end = plan.begin(blockIdx.x + 1);
-        int pos = plan.begin(blockIdx.x);
-        // the sequence of the run's first tile, and that tile's place among the sequence's
-        int b = 0, in_seq = 0;
-        if (pos < end) {
-            for (int b0 = 0, before = 0;; b0 += 32) {
-                const int mine = tiles_at(b0), upto = before + scan(mine);
-                const uint32_t past = __ballot_sync(0xffffffffu, upto > pos);
-                if (past) {
-                    const int at = __ffs(past) - 1;
-                    b = b0 + at;
-                    in_seq = pos - __shfl_sync(0xffffffffu, upto - mine, at);
-                    break;
-                }
-                before = __shfl_sync(0xffffffffu, upto, 31);
-            }
-        }
         const uint64_t stream_policy = l2_policy_evict_first();   // every tile is read once
+        const int last_row = p.B * p.Smax - kDecTile;   // of the caches that a whole tile can start at (pages: unused)
         uint32_t ring = 0;   // slots filled
-        int len = pos < end ? len_of(b) : 0;
-        int item = 0, t0 = 0;
-        if (pos < end) {
-            const int of = (len + kDecTile - 1) / kDecTile;
-            item = in_seq / of;
-            t0 = in_seq % of;
-        }
+        int next_len = pos < end ? len_of(b) : 0, units = tree_item_units(next_len), next_b = b;
+        int item = pos < end ? in_seq / units : 0, unit = in_seq - item * units;   // the next item, and the next of its units
         for (uint32_t ord = 0; ok; ++ord) {
+            int t0 = 0, n = 0, hk = 0, block = 0, len = 0;
+            while (pos < end && n == 0) {   // (a run may have an item's first units alone, and no tile)
+                const int last = min(units, unit + end - pos);
+                b = next_b;
+                len = next_len;
+                t0 = max(0, unit - kTreeItemCost);
+                n = max(0, last - kTreeItemCost) - t0;
+                hk = item / p.blocks;
+                block = item - hk * p.blocks;
+                pos += last - unit;
+                unit = 0;
+                if (pos < end && ++item == items) {   // the next sequence that has keys
+                    item = 0;
+                    do next_len = len_of(++next_b);
+                    while (next_len == 0);
+                    units = tree_item_units(next_len);
+                }
+            }
             const int slot = ord % kTreeSegs;
             ok = pp_warp_wait(bar(At::seg_empty + slot), ((ord / kTreeSegs) & 1) ^ 1, &abort_flag, 300);
             if (!ok) break;
-            const int of = (len + kDecTile - 1) / kDecTile;
-            const int n = min(of - t0, end - pos);
-            const int hk = item / p.blocks;
             if (lane == 0) {
-                segs[slot] = {b, hk, item % p.blocks, t0, n, of, len, n > 0 ? tree_nodes(p.tree_lens, b, p.T, len) : 0};
+                segs[slot] = {b, hk, block, t0, n, (len + kDecTile - 1) / kDecTile, len, n > 0 ? tree_nodes(p.tree_lens, b, p.T, len) : 0};
                 mbar_arrive(bar(At::seg_full + slot));
             }
             if (n <= 0) break;
@@ -232,39 +275,27 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             };
             int page_next = lookup(t0 * kDecTile);
             for (int j = 0; j < n; ++j) {
-                const int key0 = (t0 + j) * kDecTile, page = page_next;
+                const int key0 = (t0 + j) * kDecTile, page = (unsigned)page_next < (unsigned)p.num_pages ? page_next : -1;   // (none: zeros)
                 if (j + 1 < n) page_next = lookup(key0 + kDecTile);
-                const int pages = small ? min(kDecTile / ps, (len - key0 + ps - 1) / ps) : 1;   // that hold keys
-                const uint32_t bytes = small ? (uint32_t)(pages * ps) * (2u * D) : (uint32_t)kTileB;
+                // A tile is one box, or one for each of its pages that hold keys; where its rows would reach past the caches' last,
+                // one for each eight keys, by a map that knows where a slab ends.
+                const int row = table ? page * ps + (small ? 0 : key0 % ps) : b * p.Smax + key0;
+                const bool at_end = !table && row > last_row;
+                const int box = at_end ? 8 : small ? ps : kDecTile, boxes = (min(len - key0, kDecTile) + box - 1) / box;
 #pragma unroll
                 for (int kv = 0; kv < 2; ++kv, ++ring) {
                     const uint32_t at = ring % kSlots;
                     if (lane == 0) ok = mbar_wait(bar(At::empty + at), ((ring / kSlots) & 1) ^ 1, &abort_flag, 301);
                     if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; break; }
-                    const uint32_t dst = sRing + at * kTileB, full = bar(At::full + at);
-                    if (lane == 0) mbar_expect_tx(full, bytes);
+                    const uint32_t dst = sRing + at * kTileB + (uint32_t)(lane * box) * (2u * D), full = bar(At::full + at);
+                    if (lane == 0) mbar_expect_tx(full, (uint32_t)(boxes * box) * (2u * D));
                     __syncwarp();
-                    const CUtensorMap* tm = kv ? &tm_v : &tm_k;
-                    if (small) {
-                        // V: a page is one box, 64-element blocks of its rows; K: a box per block, as all 128 keys are one operand
-                        if (lane < pages) {
-                            if (kv || D == 64) tma_load_5d_hint(dst + (uint32_t)(lane * ps) * (2u * D), tm, full, 0, 0, 0, hk, page, stream_policy);
-                            else
-                                for (int c = 0; c < D / 64; ++c)
-                                    tma_load_5d_hint(dst + c * 16384u + (uint32_t)(lane * ps) * 128u, tm, full, 0, 0, c, hk, page, stream_policy);
-                        }
-                    } else if (lane == 0) {
-                        tma_load_5d_hint(dst, tm, full, 0, table ? key0 % ps : key0, 0, hk, table ? page : b, stream_policy);
+                    if (lane < boxes) {
+                        if (at_end) tma_load_5d_hint(dst, kv ? &tm_v8 : &tm_k8, full, 0, key0 + 8 * lane, 0, hk, b, stream_policy);
+                        else tma_load_5d_hint(dst, kv ? &tm_v : &tm_k, full, 0, 0, 0, 0, row * p.Hkv + hk, stream_policy);
                     }
                 }
                 if (!ok) break;
-            }
-            pos += n;
-            t0 = 0;
-            if (++item == items && pos < end) {   // the next sequence that has keys
-                item = 0;
-                do len = len_of(++b);
-                while (len == 0);
             }
         }
         __syncwarp();
@@ -274,6 +305,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kStep, false, false);
             const int x = warp - (kSoftmaxWarps + 2);
             const uint32_t q_lo = desc_lo(sQ + x * kTileB, 16), k_lo = desc_lo(sRing, 16), scores = tmem + 2 * x * kStep;
+            constexpr uint32_t q_hi = tree_desc_hi(1024), k_hi = tree_desc_hi(Shape::kGroupB);
             TreeRing<kSlots> ring{0, 0};
             uint32_t s = 0;   // steps begun
             for (uint32_t ord = 0; ok; ++ord) {
@@ -294,8 +326,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                         tc_fence_after();
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks) {
-                            const uint32_t off = ((ks >> 2) * 16384 + (ks & 3) * 32) >> 4;
-                            mma_ss_lo(scores + buf * kStep, q_lo + off, kt + sub * (kStep * 128 >> 4) + off, idesc, ks > 0);
+                            const uint32_t q_off = ((ks >> 2) * 16384 + (ks & 3) * 32) >> 4, k_off = ((ks >> 2) * 1024 + (ks & 3) * 32) >> 4;
+                            tree_mma_ss(scores + buf * kStep, q_lo + q_off, q_hi, kt + sub * (kStep / 8 * Shape::kGroupB >> 4) + k_off, k_hi, idesc, ks > 0);
                         }
                         mma_commit(bar(At::s_full + 2 * x + buf));
                     }
@@ -316,12 +348,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, D, false, true);
             const int x = warp - (kSoftmaxWarps + 2 + kTiles);
-            // 16 keys of V, which lie in one page: 64-element blocks of its rows
-            const uint32_t block = small ? (uint32_t)ps * 128u : 16384u;
-            const uint32_t v_lo = desc_lo(sRing, block), probs = tmem + 2 * x * kStep, out = tmem_o + x * D;
-            uint32_t key_off[8];
-#pragma unroll
-            for (int ks = 0; ks < 8; ++ks) key_off[ks] = (ks * 2048u + (small && D > 64 ? (D / 64 - 1) * block * ((uint32_t)(ks * 16) / (uint32_t)ps) : 0u)) >> 4;
+            const uint32_t v_lo = desc_lo(sRing, 1024), probs = tmem + 2 * x * kStep, out = tmem_o + x * D;
+            constexpr uint32_t v_hi = tree_desc_hi(Shape::kGroupB);
             TreeRing<kSlots> ring{1, 0};
             uint32_t s = 0;
             for (uint32_t ord = 0; ok; ++ord) {
@@ -340,7 +368,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                         tc_fence_after();
 #pragma unroll
                         for (int ks = 0; ks < kStep / 16; ++ks)
-                            mma_ts_lo(out, probs + buf * kStep + ks * 8, vt + key_off[sub * (kStep / 16) + ks], idesc, ks > 0 || sub > 0 || j > 0 ? 1u : 0u);
+                            tree_mma_ts(out, probs + buf * kStep + ks * 8, vt + ((sub * (kStep / 16) + ks) * 2 * Shape::kGroupB >> 4), v_hi, idesc,
+                                        ks > 0 || sub > 0 || j > 0 ? 1u : 0u);
                         mma_commit(bar(At::pv + 2 * x + buf));
                     }
                     mma_commit(bar(At::empty + ring.slot));
@@ -418,6 +447,14 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             const bool mine = row < p.rows && R < p.g * p.T;   // it is a row
             const int token = R / p.g, head = seg.hk * p.g + R % p.g;
             const TreeRow sees(p.mask + seg.b * p.mask_stride, p.mask_words, mine ? token : seg.live, seg.live);
+            // the first 64 bits of its row of the mask, read ahead of the tile that they are for
+            const uint32_t node0 = mine && token < seg.live ? sees.word(0) : 0u, node32 = mine && token < seg.live ? sees.word(1) : 0u;
+            auto visible = [&](int first) {   // 32 keys, as TreeRow::keys
+                if (p.mask_words > 2 || first <= -32 || sees.words == nullptr) return sees.keys(first);
+                const int w = first >> 5;
+                auto word = [&](int i) { return i < 0 ? 0xffffffffu : i == 0 ? node0 : i == 1 ? node32 : 0u; };
+                return __funnelshift_r(word(w), word(w + 1), (uint32_t)first & 31u);
+            };
             const int prefix = seg.len - seg.live;
             const bool some = __any_sync(0xffffffffu, mine);   // a warp without rows only keeps step
             float m_run = -INFINITY, l_run = 0.f;
@@ -429,7 +466,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 uint32_t vis[kStep / 32];
                 if (masked) {
 #pragma unroll
-                    for (int c = 0; c < kStep / 32; ++c) vis[c] = sees.keys(key0 - prefix + 32 * c) & low_bits(seg.len - key0 - 32 * c);
+                    for (int c = 0; c < kStep / 32; ++c) vis[c] = visible(key0 - prefix + 32 * c) & low_bits(seg.len - key0 - 32 * c);
                 }
                 if (!(ok = wait(At::s_full + buf, (s >> 1) & 1, 321))) break;
                 tc_fence_after();
@@ -441,9 +478,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     if (!(ok = wait(At::full + i % kSlots, (i / kSlots) & 1, 322))) break;
                     for (int u = r; u < (kDecTile - valid) * (D / 8); u += 128) {
                         const int key = valid + u / (D / 8), c = u % (D / 8);
-                        const uint32_t base = small ? (uint32_t)(key / ps * ps) * (2u * D) + (uint32_t)(key % ps) * 128u + (c >> 3) * (uint32_t)ps * 128u
-                                                    : (uint32_t)key * 128u + (c >> 3) * 16384u;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(v + base + (((c & 7) ^ (key & 7)) << 4)), "r"(0u) : "memory");
+                        const uint32_t at = v + (uint32_t)(key >> 3) * Shape::kGroupB + (c >> 3) * 1024u + (uint32_t)(key & 7) * 128u;
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + ((c & 7) << 4)), "r"(0u) : "memory");   // (a row is a row, swizzled or not)
                     }
                     fence_proxy_async_smem();
                 }
@@ -533,22 +569,21 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 T* o_row = static_cast<T*>(p.o) + (((long long)seg.b * p.T + token) * p.Hq + head) * D;
                 float4* o_part = reinterpret_cast<float4*>(p.o_part) + slot * (D / 4) * p.rows + row;
 #pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld_x32(tO + 32 * c, o);
+                for (int c = 0; c < D / 64; ++c) {
+                    uint32_t o[64];
+                    tmem_ld_x32(tO + 64 * c, *reinterpret_cast<uint32_t(*)[32]>(&o[0]));
+                    tmem_ld_x32(tO + 64 * c + 32, *reinterpret_cast<uint32_t(*)[32]>(&o[32]));
                     tmem_wait_ld();
-                    float f[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = none ? 0.f : __uint_as_float(o[i]) * inv;
+                    auto f = [&](int i) { return none ? 0.f : __uint_as_float(o[i]) * inv; };
                     if (!mine) continue;
                     if (whole) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8)
-                            *reinterpret_cast<uint4*>(o_row + 32 * c + i) = make_uint4(pack2<T>(f[i], f[i + 1]), pack2<T>(f[i + 2], f[i + 3]),
-                                                                                      pack2<T>(f[i + 4], f[i + 5]), pack2<T>(f[i + 6], f[i + 7]));
+                        for (int i = 0; i < 64; i += 8)
+                            *reinterpret_cast<uint4*>(o_row + 64 * c + i) = make_uint4(pack2<T>(f(i), f(i + 1)), pack2<T>(f(i + 2), f(i + 3)),
+                                                                                      pack2<T>(f(i + 4), f(i + 5)), pack2<T>(f(i + 6), f(i + 7)));
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) o_part[(long long)(8 * c + i / 4) * p.rows] = make_float4(f[i], f[i + 1], f[i + 2], f[i + 3]);
+                        for (int i = 0; i < 64; i += 4) o_part[(long long)(16 * c + i / 4) * p.rows] = make_float4(f(i), f(i + 1), f(i + 2), f(i + 3));
                     }
                 }
             }
@@ -578,14 +613,14 @@ __global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm) fa_dec
     grid_dep_wait();
     const TreePlan plan(p.starts[p.B], grid);
     const int items = p.Hkv * p.blocks;
-    int b = 0, item, first, tiles;
+    int b = 0, item, first, tiles;   // first: the unit of the item's first tile
     if constexpr (kItems) {
         b = blockIdx.y / items;
         item = blockIdx.y % items;
-        const int seq = p.starts[b];
-        tiles = (p.starts[b + 1] - seq) / items;
-        if (tiles == 0) return;
-        first = seq + item * tiles;
+        const int seq = p.starts[b], units = (p.starts[b + 1] - seq) / items;
+        if (units == 0) return;
+        tiles = units - kTreeItemCost;
+        first = seq + item * units + kTreeItemCost;
     } else {
         const int cut = plan.begin(blockIdx.y + 1);
         if ((int)blockIdx.y + 1 >= plan.ctas) return;
@@ -595,11 +630,11 @@ __global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm) fa_dec
             b += (n - 1) * step;
             hi = min(hi, b + step);
         }
-        const int seq = p.starts[b];
-        tiles = (p.starts[b + 1] - seq) / items;
-        item = (cut - seq) / tiles;
-        first = seq + item * tiles;
-        if (cut == first || (int)blockIdx.y != plan.owner(first)) return;
+        const int seq = p.starts[b], units = (p.starts[b + 1] - seq) / items;
+        item = (cut - seq) / units;
+        tiles = units - kTreeItemCost;
+        first = seq + item * units + kTreeItemCost;
+        if (cut <= first || (int)blockIdx.y != plan.owner(first)) return;
     }
     const int c0 = plan.owner(first), c1 = plan.owner(first + tiles - 1);
     if (c0 == c1) return;   // its only part is where it belongs

@@ -106,13 +106,9 @@ int encode_map_tile(CUtensorMap* tm, const void* base, int B, int S, int H, int6
     return (d == 64 ? encode_map : encode_map_blocks)(tm, base, B, S, H, sb, ss, sh, box_rows, bf16, d);
 }
 
-// Tensor map over a contiguous 16-bit cache [slabs, S, H, d] (d = 128 or 64) with boxes of box_rows keys x all of d, or one
-// 64-element block of it.
-int encode_map_cache(CUtensorMap* tm, const void* base, int slabs, int S, int H, int box_rows, bool bf16, int d, bool one_block = false) {
-    const Strides st = legal_strides(slabs, S, H, (int64_t)S * H * d, (int64_t)H * d, d, d);
-    return encode_tiled<5>(tm, type16(bf16), base, {64, (cuuint64_t)S, (cuuint64_t)(d / 64), (cuuint64_t)H, (cuuint64_t)slabs},
-                           {(cuuint64_t)st.s * 2, 128, (cuuint64_t)st.h * 2, (cuuint64_t)st.b * 2},
-                           {64, (cuuint32_t)box_rows, (cuuint32_t)(one_block ? 1 : d / 64), 1, 1});
+// Tensor map over a contiguous 16-bit cache [slabs, S, H, d] (d = 128 or 64) with boxes of box_rows keys x all of d.
+int encode_map_cache(CUtensorMap* tm, const void* base, int slabs, int S, int H, int box_rows, bool bf16, int d) {
+    return encode_map_blocks(tm, base, slabs, S, H, (int64_t)S * H * d, (int64_t)H * d, d, box_rows, bf16, d);
 }
 
 // Tensor map over a [B, S, H, 128] one-byte tensor, contiguous: a box is box_rows sequence
@@ -999,14 +995,14 @@ struct TreeBlocks {
     }
 };
 template <typename T, int D>
-int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const fa::TreeParams& tp, int sms, cudaStream_t st) {
+int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tk8, const CUtensorMap& tv8, const fa::TreeParams& tp, int sms, cudaStream_t st) {
     const bool two = tp.rows > 128;
     const auto kern = two ? fa::fa_decode_tree_kernel<T, D, 2> : fa::fa_decode_tree_kernel<T, D, 1>;
     const int smem = two ? fa::TreeShape<D, 2>::kSmem : fa::TreeShape<D, 1>::kSmem, threads = two ? fa::TreeShape<D, 2>::kThreads : fa::TreeShape<D, 1>::kThreads;
     int sm_count = 0;
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
     const int grid = sms < fa::kTreeMaxCtas ? sms : fa::kTreeMaxCtas;
-    cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tp);
+    cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tk8, tv8, tp);
     if (e == cudaSuccess && grid > 1) {
         // one round of blocks, as many to an item (or a CTA's beginning) as there is room for
         const long long items = (long long)tp.B * tp.Hkv * tp.blocks;
@@ -1026,8 +1022,8 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     rc = check_device(&sms);
     if (rc) return rc;
     const TreeBlocks tb(p.Hq / p.Hkv, p.T);
-    const long long tiles = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile;
-    if (tiles * p.B * p.Hkv * tb.blocks > 0x7fffffffll) return FA_ERR_UNSUPPORTED;   // (they are counted in 32 bits)
+    const long long units = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile + fa::kTreeItemCost;
+    if (units * p.B * p.Hkv * tb.blocks > 0x7fffffffll) return FA_ERR_UNSUPPORTED;   // (they are counted in 32 bits)
     fa::TreeParams tp;
     tp.q = p.q;
     tp.o = p.o;
@@ -1051,14 +1047,25 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     tp.blocks = tb.blocks;
     tp.page_size = p.block_table ? p.page_size : 1;
     tp.table_stride = p.table_stride;
+    tp.num_pages = p.num_pages;
     tp.scale_log2 = fmaxf(p.scale * 1.4426950408889634f, 1e-30f);   // (positive, as in dense_fwd_params)
     const bool bf16 = p.dtype == FA_DTYPE_BF16;
+    // K and V: the dimensions are (64 elements of d, 8 rows, 64-element blocks of d, groups of 8 rows, heads of all rows one after the
+    // other), so that a box lands group by group and may begin at any row; it is a tile, or a page if that is smaller.  Such
+    // a map only knows where a box begins: all its rows have to exist, and the tile that ends past the caches' last row comes by
+    // the other two, in boxes of eight rows, whose dimensions are those of the caches.
     const int slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : Skv_max;
-    const bool small = p.block_table && p.page_size < fa::kDecTile;
-    const int box_rows = small ? p.page_size : fa::kDecTile;
-    CUtensorMap tq, tk, tv;
-    rc = encode_map_cache(&tk, p.k, slabs, slab_rows, p.Hkv, box_rows, bf16, p.d, small);
-    if (rc) return rc;
+    const int box_rows = p.block_table && p.page_size < fa::kDecTile ? p.page_size : fa::kDecTile;
+    const cuuint64_t head = (cuuint64_t)p.d * 2, row = head * p.Hkv, heads = (cuuint64_t)slabs * slab_rows * p.Hkv, blocks = p.d / 64;
+    if (heads > 0x7fffffffull) return FA_ERR_UNSUPPORTED;   // (coordinates are 32 bits)
+    CUtensorMap tq, tk, tv, tk8, tv8;
+    for (int i = 0; i < 2; ++i) {
+        rc = encode_tiled<5>(i ? &tv : &tk, type16(bf16), i ? p.v : p.k, {64, 8, blocks, (cuuint64_t)box_rows / 8, heads}, {row, 128, 8 * row, head},
+                             {64, 8, (cuuint32_t)blocks, (cuuint32_t)box_rows / 8, 1});
+        if (rc) return rc;
+        rc = encode_map_cache(i ? &tv8 : &tk8, i ? p.v : p.k, slabs, slab_rows, p.Hkv, 8, bf16, p.d);
+        if (rc) return rc;
+    }
     tq = tk;
     tp.q_boxes = tb.boxes ? 1 : 0;
     if (tb.boxes) {   // a box: the g heads of 128 / g nodes, all of d
@@ -1067,11 +1074,9 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
                              {64, (cuuint32_t)tp.g, (cuuint32_t)(128 / tp.g), (cuuint32_t)(d / 64), 1});
         if (rc) return rc;
     }
-    rc = encode_map_cache(&tv, p.v, slabs, slab_rows, p.Hkv, box_rows, bf16, p.d);
-    if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (p.d == 64) return bf16 ? tree_launch<__nv_bfloat16, 64>(tq, tk, tv, tp, sms, st) : tree_launch<__half, 64>(tq, tk, tv, tp, sms, st);
-    return bf16 ? tree_launch<__nv_bfloat16, 128>(tq, tk, tv, tp, sms, st) : tree_launch<__half, 128>(tq, tk, tv, tp, sms, st);
+    if (p.d == 64) return bf16 ? tree_launch<__nv_bfloat16, 64>(tq, tk, tv, tk8, tv8, tp, sms, st) : tree_launch<__half, 64>(tq, tk, tv, tk8, tv8, tp, sms, st);
+    return bf16 ? tree_launch<__nv_bfloat16, 128>(tq, tk, tv, tk8, tv8, tp, sms, st) : tree_launch<__half, 128>(tq, tk, tv, tk8, tv8, tp, sms, st);
 }
 }  // namespace
 

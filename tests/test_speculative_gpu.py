@@ -197,6 +197,44 @@ def test_tree_pages_past_32_bits(fa, T):
     assert_close_to_oracle(o, lse, o_ref, l_ref)
 
 
+@pytest.mark.parametrize("T", [4, 40])
+@pytest.mark.parametrize("page", [16, 128])
+def test_tree_pages_that_are_none(fa, T, page):
+    # table entries outside the pool read as zeros, whatever they are
+    gen = torch.Generator().manual_seed(12)
+    H, d, n = 2, 64, 4 * page
+    k, v = torch.randn(4, page, H, d, generator=gen).half(), torch.randn(4, page, H, d, generator=gen).half()
+    q = torch.randn(1, T, 8, d, generator=gen).half()
+    see = ref.ancestors(random_tree(T, random.Random(2)))[None]
+    for bad in (-1, 4, 1 << 30, -(1 << 31), (1 << 31) - 1, (1 << 28) + 1):
+        kz, vz = k.clone(), v.clone()
+        kz[1], vz[1] = 0, 0
+        o_ref, l_ref = ref.tree_attention(q, kz.view(1, n, H, d), vz.view(1, n, H, d), [n], see, 0.125)
+        o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 8, T, device=DEV)
+        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 8, H, n, d), dtype=torch.uint8, device=DEV)
+        fa.fa_decode_tree(q.to(DEV), k.to(DEV), v.to(DEV), o, lse, ints([n]), ref.bits_to_words(see).to(DEV), 0.125, ws, block_table=ints([[0, bad, 2, 3]]))
+        assert_close_to_oracle(o, lse, o_ref, l_ref)
+
+
+@pytest.mark.parametrize("smax", [40, 127, 128, 129, 200, 1001])
+def test_tree_at_the_end_of_the_caches(fa, smax):
+    # the last sequence ends with the caches' last row; other rows of the allocation hold NaN
+    for T, hq, hkv, d in ((20, 8, 1, 128), (33, 4, 4, 64), (40, 8, 1, 64)):
+        B, gen = 2, torch.Generator().manual_seed(smax)
+        lens = [max(T, smax // 2), smax]
+        q = torch.randn(B, T, hq, d, generator=gen).half()
+        k, check_k = guard_alloc((B, smax, hkv, d), torch.float16, DEV, pad=64 * hkv * d)
+        v, check_v = guard_alloc((B, smax, hkv, d), torch.float16, DEV, pad=64 * hkv * d)
+        k.copy_(torch.randn(k.shape, generator=gen)), v.copy_(torch.randn(v.shape, generator=gen))
+        see = torch.stack([ref.ancestors(random_tree(T, random.Random(b))) for b in range(B)])
+        o_ref, l_ref = ref.tree_attention(q, k.cpu(), v.cpu(), lens, see, 0.1)
+        o, lse = torch.empty_like(q, device=DEV), torch.empty(B, hq, T, device=DEV)
+        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(B, T, hq, hkv, smax, d), dtype=torch.uint8, device=DEV)
+        fa.fa_decode_tree(q.to(DEV), k, v, o, lse, ints(lens), ref.bits_to_words(see).to(DEV), 0.1, ws)
+        assert_close_to_oracle(o, lse, o_ref, l_ref)
+        check_k(), check_v()
+
+
 # ------------------------------------------------------------------ verification
 def check_verify(fa, B, T, V, dtype, draft, seed, trees=None, live=None, p=None, q=None, tokens=None, u=None, noise=None):
     gen, rng = torch.Generator().manual_seed(seed), random.Random(seed)
