@@ -278,8 +278,8 @@ size_t fa_decode_append_workspace_bytes(int B, int Sq, int Hq, int Hkv, int Skv_
  *   sequences have one tree.
  *   Cache rows past a sequence's end may hold anything.  Inside it, the KEY of a node that a row does not see may be
  *   anything (NaN too); its VALUE must be finite, as it is multiplied by zero.
- *   workspace: fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max or max_pages * page_size, d) bytes, 16-byte aligned.
- * Errors: as fa_decode_ex; FA_ERR_UNSUPPORTED also for T > 256 or T > Skv_max, FA_ERR_NULL without a mask, FA_ERR_SHAPE for a
+ *   workspace: fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max or max_pages * page_size, d, variant) bytes, 16-byte aligned.
+ * Errors: as fa_decode_ex; FA_ERR_UNSUPPORTED also for T > 256, T > Skv_max or another variant, FA_ERR_NULL without a mask, FA_ERR_SHAPE for a
  * negative mask_stride.
  */
 typedef struct fa_tree_params {
@@ -295,13 +295,15 @@ typedef struct fa_tree_params {
     int B, T, Hq, Hkv, Skv_max, d;
     int dtype;              /* FA_DTYPE_FP16 or FA_DTYPE_BF16 */
     int num_pages, page_size, max_pages, table_stride;
+    int variant;            /* 0 = default, by the sizes; others force one kernel, for A/B timing and tests: 1 = the split decode kernel,
+                               2 = the kernel for many rows per kv head */
     int64_t mask_stride;    /* words */
     float scale;
     void* workspace;
     size_t workspace_bytes;
 } fa_tree_params;
 int fa_decode_tree(const fa_tree_params* p, void* stream);
-size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d);
+size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d, int variant);
 
 /*
  * Verification of a tree of drafted tokens (speculative decoding) against the target's probabilities, from given random

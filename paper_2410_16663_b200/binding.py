@@ -66,18 +66,18 @@ lib.fa_decode_ex.argtypes = [ctypes.POINTER(fa_decode_params), _p]
 class fa_tree_params(ctypes.Structure):
     _fields_ = [("q", _p), ("k", _p), ("v", _p), ("o", _p), ("lse", _p), ("seqlens_k", _p), ("tree_lens", _p), ("mask", _p),
                 ("block_table", _p), ("B", _i), ("T", _i), ("Hq", _i), ("Hkv", _i), ("Skv_max", _i), ("d", _i), ("dtype", _i),
-                ("num_pages", _i), ("page_size", _i), ("max_pages", _i), ("table_stride", _i), ("mask_stride", ctypes.c_int64),
+                ("num_pages", _i), ("page_size", _i), ("max_pages", _i), ("table_stride", _i), ("variant", _i), ("mask_stride", ctypes.c_int64),
                 ("scale", _f), ("workspace", _p), ("workspace_bytes", _sz)]
 
 
 lib.fa_decode_tree.restype = _i
 lib.fa_decode_tree.argtypes = [_p, _p]   # (an fa_tree_params by reference, or its bytes)
-_TREE = struct.Struct("@9P11iqfPN")      # fa_tree_params
+_TREE = struct.Struct("@9P12iqfPN")      # fa_tree_params
 assert _TREE.size == ctypes.sizeof(fa_tree_params)
 _FA16 = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16}
 _FA_PROBS = {**_FA16, torch.float32: FA_DTYPE_FP32}
 lib.fa_decode_tree_workspace_bytes.restype = _sz
-lib.fa_decode_tree_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i]
+lib.fa_decode_tree_workspace_bytes.argtypes = [_i, _i, _i, _i, _i, _i, _i]
 lib.fa_spec_verify.restype = _i
 lib.fa_spec_verify.argtypes = [_p] * 10 + [_i, _i, _i, _i, _p]
 lib.fa_cache_compact.restype = _i
@@ -348,12 +348,12 @@ def tree_mask(parents):
     return torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32)
 
 
-def fa_decode_tree_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, Skv_max: int, d: int) -> int:
-    return int(lib.fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max, d))
+def fa_decode_tree_workspace_bytes(B: int, T: int, Hq: int, Hkv: int, Skv_max: int, d: int, variant: int = 0) -> int:
+    return int(lib.fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max, d, variant))
 
 
 def fa_decode_tree(q, k, v, o, lse, seqlens_k, mask, scale: float, workspace, tree_lens=None, block_table=None,
-                   max_pages: int = None, raise_on_error: bool = True) -> int:
+                   max_pages: int = None, variant: int = 0, raise_on_error: bool = True) -> int:
     """``fa_decode_tree``: q, o [B,T,Hq,d], the nodes of each sequence's tree, whose rows end its cache; mask int32
     [B,T,ceil(T/32)], or [T,ceil(T/32)] for one tree (see ``tree_mask``); k, v, block_table as for ``fa_decode_ex``; seqlens_k
     int32 [B] with the tree's rows, tree_lens int32 [B] or None."""
@@ -375,7 +375,7 @@ def fa_decode_tree(q, k, v, o, lse, seqlens_k, mask, scale: float, workspace, tr
     else:
         sizes = (0, d, _FA16[dt], slabs, rows, block_table.shape[1] if max_pages is None else max_pages, _table("fa_decode_tree", block_table))
     p = _TREE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), seqlens_k.data_ptr(), _ptr(tree_lens), mask.data_ptr(),
-                   _ptr(block_table), B, T, Hq, Hkv, *sizes, 0 if len(seen) == 2 else T * seen[2], scale, _ptr(workspace),
+                   _ptr(block_table), B, T, Hq, Hkv, *sizes, variant, 0 if len(seen) == 2 else T * seen[2], scale, _ptr(workspace),
                    0 if workspace is None else workspace.numel() * workspace.element_size())
     return _check(lib.fa_decode_tree(p, _stream()), "fa_decode_tree", raise_on_error)
 

@@ -1,11 +1,11 @@
 // Attention for a tree of drafted tokens over a cache, for more rows than one warp-level MMA has.
 //
-// The T nodes of a sequence times the g query heads of a kv head are R = g T rows that read the same keys.  Up to 16 of them
-// the split decode kernel (decode.cuh) takes; it would read, and widen into fragments, every key once per 16 rows.  Here a CTA
+// The T nodes of a sequence times the g query heads of a kv head are R = g T rows that read the same keys.  The split
+// decode kernel (decode.cuh) reads every key once per 16 of them, which is as good while that is few keys.  Here a CTA
 // holds one or two tiles of 128 rows, S = Q K^T and O += P V are tcgen05 instructions with a row per lane of tensor memory, and
 // a tile of 128 keys is read once for all of them.  An item is a block of rows of one (sequence, kv head); the tiles of all
-// items, one after the other, are dealt out in equal runs to as many CTAs as there are SMs, whatever the lengths
-// (TreePlan).  A run's first and last item may be shared with other CTAs: their rows go to the workspace, with their log-sum-exps, and
+// items, one after the other, are dealt out in equal runs to as many CTAs as run at once, whatever the
+// lengths (TreePlan).  A run's first and last item may be shared with other CTAs: their rows go to the workspace, with their log-sum-exps, and
 // a second kernel merges them; every other row is written where it belongs.
 //
 // Roles: a warp that looks up the run's segments (one per item) and loads K and V tiles into a ring; one that loads Q; and for each row
@@ -18,21 +18,31 @@
 
 namespace fa {
 
-constexpr int kTreeMaxCtas = 160;     // the workspace has room for the partial results of so many
+constexpr int kTreeMaxSms = 160;      // the workspace has room for the partial results of so many
 constexpr int kTreeSegs = 4;          // segments between the loading warp and the others
+
+// Head dimension 64: half the bytes per key and the same softmax, so that one CTA's four softmax warps would be what bounds it
+// (64 sequences of 1000 to 2048 keys, 16 rows per kv head: 65 us, 31 for the bytes): two CTAs to an SM, of one row tile each.
+template <int D>
+constexpr int kTreeCtasPerSm = D == 64 ? 2 : 1;
 
 template <int D, int kTiles>
 struct TreeShape {
     static constexpr int kTileB = 128 * D * 2;                       // Q, K or V of 128 rows
-    static constexpr int kSlots = 7 * 128 / D - kTiles;              // 224 KiB in all
+    static constexpr int kSlots = D == 64 ? 5 : 7 - kTiles;          // 224 KiB in all, or 96
     static constexpr int kSmem = 1024 + (kTiles + kSlots) * kTileB;
     static constexpr int kThreads = 128 * kTiles + 64 + 64 * kTiles;
     // K and V tiles: groups of eight keys, each with its 64-element blocks one after the other (eight rows of 128 swizzled
     // bytes): a page of any size is one box, and all 128 keys are one operand of regular strides.
     static constexpr int kGroupB = 1024 * (D / 64);
-    // Keys of a softmax step.  A row tile has two score buffers of so many columns: while one is in the softmax, the
-    // tensor cores take the other's probabilities and fill it again.
-    static constexpr int kStep = kTiles == 2 ? 64 : 128;
+    // Keys of a softmax step, and a row tile's score buffers of so many columns.  With two, the tensor cores take one's probabilities
+    // and fill it again while the other is in the softmax; with one (all that two CTAs have room for), the other CTA is at work.
+    static constexpr int kStep = kTiles == 2 ? 64 : 128, kBufs = D == 64 ? 1 : 2;
+    static constexpr int kTmemCols = D == 64 ? 256 : 512;
+    static_assert(kTiles * (kStep * kBufs + D) <= kTmemCols && kTmemCols * kTreeCtasPerSm<D> <= 512 && (D == 128 || kTiles == 1), "tensor memory");
+    // Two CTAs leave 128 registers a thread, which the softmax warps share out anew.
+    static constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
+    static_assert(kSoftmaxRegs + kOtherRegs <= 2 * 128, "setmaxnreg.inc would wait for registers nobody releases");
 };
 
 struct TreeParams {
@@ -134,14 +144,14 @@ __device__ __forceinline__ float tree_row_max(const uint32_t (&s)[N]) {
     return fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
 }
 
-// grid: the SMs; behind the softmax warps one that loads K and V, one that loads Q, and for each row tile one for each product.
+// grid: as many as run at once; behind the softmax warps one that loads K and V, one that loads Q, and for each row tile one for each product.
 template <typename T, int D, int kTiles>
-__global__ void __launch_bounds__(TreeShape<D, kTiles>::kThreads, 1)
+__global__ void __launch_bounds__(TreeShape<D, kTiles>::kThreads, kTreeCtasPerSm<D>)
 fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_k8,
                       const __grid_constant__ CUtensorMap tm_v8, const TreeParams p) {
     using Shape = TreeShape<D, kTiles>;
-    constexpr int kSlots = Shape::kSlots, kTileB = Shape::kTileB, kStep = Shape::kStep, kSub = kDecTile / kStep;
+    constexpr int kSlots = Shape::kSlots, kTileB = Shape::kTileB, kStep = Shape::kStep, kSub = kDecTile / kStep, kBufs = Shape::kBufs;
     using At = TreeBars<kSlots>;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t sQ = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -166,7 +176,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         tma_prefetch_desc(&tm_v);
     }
     if (warp == 0) {
-        tmem_alloc(smem_u32(&tmem_holder), 512);
+        tmem_alloc(smem_u32(&tmem_holder), Shape::kTmemCols);
         tmem_relinquish();
     }
     // The loading warp finds the CTA's run meanwhile: its first and last unit, and the sequence and the place in it of the first.  (As
@@ -221,7 +231,9 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
-    const uint32_t tmem_o = tmem + 2 * kTiles * kStep;   // behind the score buffers
+    const uint32_t tmem_o = tmem + kTiles * kBufs * kStep;   // behind the score buffers
+    auto buf_of = [](uint32_t step) { return kBufs == 2 ? step & 1 : 0u; };
+    auto phase_of = [](uint32_t step) { return kBufs == 2 ? step >> 1 : step; };   // of a buffer's barriers
     grid_dep_wait();
 
     const int ps = p.page_size;
@@ -234,6 +246,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         return true;
     };
 
+    if (warp >= kSoftmaxWarps) {
+    if constexpr (D == 64) setmaxnreg_dec<Shape::kOtherRegs>();
     if (warp == kSoftmaxWarps) {
         // ---------------------------------------------------------------- segments, K and V
         const uint64_t stream_policy = l2_policy_evict_first();   // every tile is read once
@@ -304,7 +318,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kStep, false, false);
             const int x = warp - (kSoftmaxWarps + 2);
-            const uint32_t q_lo = desc_lo(sQ + x * kTileB, 16), k_lo = desc_lo(sRing, 16), scores = tmem + 2 * x * kStep;
+            const uint32_t q_lo = desc_lo(sQ + x * kTileB, 16), k_lo = desc_lo(sRing, 16), scores = tmem + x * kBufs * kStep;
             constexpr uint32_t q_hi = tree_desc_hi(1024), k_hi = tree_desc_hi(Shape::kGroupB);
             TreeRing<kSlots> ring{0, 0};
             uint32_t s = 0;   // steps begun
@@ -320,9 +334,9 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     const uint32_t kt = k_lo + ring.slot * (kTileB >> 4);
 #pragma unroll
                     for (int sub = 0; sub < kSub; ++sub, ++s) {
-                        const uint32_t buf = kSub == 2 ? sub : s & 1;
-                        // P V of two steps ago has taken the probabilities that lie there
-                        if (s >= 2 && !(ok = mbar_wait(bar(At::pv + 2 * x + buf), ((s >> 1) - 1) & 1, &abort_flag, 313))) break;
+                        const uint32_t buf = buf_of(s);
+                        // P V has taken the probabilities that lie there
+                        if (s >= kBufs && !(ok = mbar_wait(bar(At::pv + 2 * x + buf), (phase_of(s) - 1) & 1, &abort_flag, 313))) break;
                         tc_fence_after();
 #pragma unroll
                         for (int ks = 0; ks < D / 16; ++ks) {
@@ -348,7 +362,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, D, false, true);
             const int x = warp - (kSoftmaxWarps + 2 + kTiles);
-            const uint32_t v_lo = desc_lo(sRing, 1024), probs = tmem + 2 * x * kStep, out = tmem_o + x * D;
+            const uint32_t v_lo = desc_lo(sRing, 1024), probs = tmem + x * kBufs * kStep, out = tmem_o + x * D;
             constexpr uint32_t v_hi = tree_desc_hi(Shape::kGroupB);
             TreeRing<kSlots> ring{1, 0};
             uint32_t s = 0;
@@ -363,8 +377,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                     const uint32_t vt = v_lo + ring.slot * (kTileB >> 4);
 #pragma unroll
                     for (int sub = 0; sub < kSub; ++sub, ++s) {
-                        const uint32_t buf = kSub == 2 ? sub : s & 1;
-                        if (!(ok = mbar_wait(bar(At::p_full + 2 * x + buf), (s >> 1) & 1, &abort_flag, 317))) break;
+                        const uint32_t buf = buf_of(s);
+                        if (!(ok = mbar_wait(bar(At::p_full + 2 * x + buf), phase_of(s) & 1, &abort_flag, 317))) break;
                         tc_fence_after();
 #pragma unroll
                         for (int ks = 0; ks < kStep / 16; ++ks)
@@ -423,8 +437,10 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             }
         }
         __syncwarp();
+    }
     } else {
         // ---------------------------------------------------------------- softmax: a row per thread
+        if constexpr (D == 64) setmaxnreg_inc<Shape::kSoftmaxRegs>();
         const int x = warp >> 2;                        // row tile
         const int r = tid & 127;                        // row of it
         const int row = x * 128 + r;                    // row of the block
@@ -460,15 +476,15 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             float m_run = -INFINITY, l_run = 0.f;
             for (int j = 0; j < seg.n * kSub; ++j, ++s) {
                 const int key0 = seg.t0 * kDecTile + j * kStep;
-                const int buf = 2 * x + (s & 1);
-                const uint32_t tS = tmem + lanes + buf * kStep;
+                const int buf = 2 * x + buf_of(s);   // (of the barriers)
+                const uint32_t tS = tmem + lanes + (x * kBufs + buf_of(s)) * kStep;
                 const bool masked = key0 + kStep > prefix;   // it reaches into the tree, or past the keys
                 uint32_t vis[kStep / 32];
                 if (masked) {
 #pragma unroll
                     for (int c = 0; c < kStep / 32; ++c) vis[c] = visible(key0 - prefix + 32 * c) & low_bits(seg.len - key0 - 32 * c);
                 }
-                if (!(ok = wait(At::s_full + buf, (s >> 1) & 1, 321))) break;
+                if (!(ok = wait(At::s_full + buf, phase_of(s) & 1, 321))) break;
                 tc_fence_after();
                 if (s % kSub == 0 && seg.len - key0 < kDecTile) {
                     // V rows past the sequence may hold anything, NaN too: they become zeros (their probabilities are).  Each row tile's
@@ -530,8 +546,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                         l_run = l_run * alpha + ((a0 + a1) + (b0 + b1));
                     }
                     if (j > 0 && __any_sync(0xffffffffu, moved)) {
-                        // O holds the sums up to the step before (these scores came after P V of the one before that)
-                        if (!(ok = wait(At::pv + 2 * x + ((s - 1) & 1), ((s - 1) >> 1) & 1, 323))) break;
+                        // O holds the sums up to the step before.  (One buffer: the scores came after those; two: after the sums before.)
+                        if (kBufs == 2 && !(ok = wait(At::pv + 2 * x + buf_of(s - 1), phase_of(s - 1) & 1, 323))) break;
                         tc_fence_after();
 #pragma unroll 1
                         for (int c = 0; c < D / 16; ++c) {
@@ -550,9 +566,9 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
                 if (lane == 0) mbar_arrive(bar(At::p_full + buf));
             }
             if (!ok) break;
-            // the last two steps' P V (the scores came after those before)
-            if (s >= 2 && !(ok = wait(At::pv + 2 * x + (s & 1), ((s >> 1) - 1) & 1, 324))) break;
-            if (!(ok = wait(At::pv + 2 * x + ((s - 1) & 1), ((s - 1) >> 1) & 1, 325))) break;
+            // P V of the last step, and of the one before it where the last scores did not wait for that
+            if (kBufs == 2 && s >= 2 && !(ok = wait(At::pv + 2 * x + buf_of(s - 2), phase_of(s - 2) & 1, 324))) break;
+            if (!(ok = wait(At::pv + 2 * x + buf_of(s - 1), phase_of(s - 1) & 1, 325))) break;
             tc_fence_after();
             if (some) {
                 // l_run == 0: a row that sees nothing here.  (A NaN sum makes the row and its log-sum-exp NaN.)  Rows of nodes that are
@@ -597,7 +613,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 0) tmem_dealloc(tmem, 512);
+    if (warp == 0) tmem_dealloc(tmem, Shape::kTmemCols);
 }
 
 // Merge of the rows that several CTAs have worked on (the recurrence of decode.cuh's merge).  A thread owns four columns of a row; a

@@ -982,26 +982,40 @@ int decode_impl(const void* q, const void* k_cache, const void* v_cache, void* o
                    : decode_launch<128>(tk, tv, dp, o, lse, g, bf16, direct, Skv_max > 0, st);
 }
 
-// fa_decode_tree with more rows per kv head than the split decode kernel's CTAs have (see decode_tree.cuh).
-constexpr int kTreeFewRows = 16;
-// How the rows that share a kv head are cut: blocks of at most two tiles of 128, of equal size in whole warps -- and in whole nodes,
-// where a tile is, so that Q is loaded by boxes.
+// Which kernel takes a tree: the split decode kernel, whose CTAs have 16 of the rows that share a kv head and each read all keys, or the
+// one for many rows (decode_tree.cuh), which takes some 4 us more to begin and to merge.  By the blocks of 16 rows and the
+// tiles of 128 keys per SM if all sequences were as long as they may be (us, split / many rows, 32/8 heads unless said; d = 128:
+// 16 rows 64 x 1000-2048 keys 68 / 74, 64 x 100-500 on 16-key pages 30 / 43; 32 rows 4 x 1000-2048 13.2 / 15.2, 16 x 400-512 15.3 / 17.2, 16 x
+// 1000-2048 31.7 / 27.6, 64 x 400-512 52.2 / 48.8; 64 rows 1 x 512 6.5 / 10.3, 1 x 8192 19.3 / 18.7, 4 x 512 13.6 / 12.3, 4 x 1000-2048 27.0 / 16.4;
+// 128 rows 1 x 2048 12.9 / 13.3, 4 x 512 25.2 / 14.1; 256 rows 1 x 512 12.9 / 13.7.  d = 64, half the bytes and twice the CTAs: 32 rows 16 x
+// 1000-2048 16.5 / 22.0, 16 x 8/8 heads, 20 rows, 1000-4096 28.1 / 29.7; 64 rows 4 x 1000-2048 11.0 / 13.7, 64 x 400-512 44.4 / 39.3, 16 x 1000-8192 74.7 /
+// 44.7; 128 rows 4 x 512 13.0 / 11.8.)  The SMs are counted as 148, so that the workspace is of one size on every device.
+bool tree_takes_many_rows(int B, int T, int Hq, int Hkv, int Skv_max, int d, int variant) {
+    if (variant != 0) return variant == 2;
+    const long long blocks = ((long long)(Hq / Hkv) * T + 15) / 16, tiles = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile * B * Hkv;
+    return d == 64 ? blocks >= 3 && tiles * blocks > 24ll * 148 : blocks >= 2 && tiles * blocks > 8ll * 148;
+}
+// How the rows that share a kv head are cut: blocks of at most two tiles of 128 (one with d = 64), of equal size in whole warps -- and in
+// whole nodes, where a tile is, so that Q is loaded by boxes.
 struct TreeBlocks {
-    int blocks, rows;
+    int most, blocks, rows;
     bool boxes;
-    TreeBlocks(int g, int T) : blocks((g * T + 255) / 256), rows(g * T), boxes(128 % g == 0) {
+    TreeBlocks(int g, int T, int d) : most(d == 64 ? 128 : 256), blocks((g * T + most - 1) / most), rows(g * T), boxes(128 % g == 0) {
         const int unit = boxes && g > 32 ? g : 32;
         if (blocks > 1) rows = ((rows + blocks - 1) / blocks + unit - 1) / unit * unit;
     }
+    // partial results that a call may have: two for each CTA
+    size_t slots(int d) const { return 2 * (size_t)fa::kTreeMaxSms * (d == 64 ? fa::kTreeCtasPerSm<64> : fa::kTreeCtasPerSm<128>); }
 };
 template <typename T, int D>
 int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tk8, const CUtensorMap& tv8, const fa::TreeParams& tp, int sms, cudaStream_t st) {
-    const bool two = tp.rows > 128;
-    const auto kern = two ? fa::fa_decode_tree_kernel<T, D, 2> : fa::fa_decode_tree_kernel<T, D, 1>;
-    const int smem = two ? fa::TreeShape<D, 2>::kSmem : fa::TreeShape<D, 1>::kSmem, threads = two ? fa::TreeShape<D, 2>::kThreads : fa::TreeShape<D, 1>::kThreads;
+    auto kern = fa::fa_decode_tree_kernel<T, D, 1>;
+    int smem = fa::TreeShape<D, 1>::kSmem, threads = fa::TreeShape<D, 1>::kThreads;
+    if constexpr (D == 128)
+        if (tp.rows > 128) kern = fa::fa_decode_tree_kernel<T, D, 2>, smem = fa::TreeShape<D, 2>::kSmem, threads = fa::TreeShape<D, 2>::kThreads;
     int sm_count = 0;
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
-    const int grid = sms < fa::kTreeMaxCtas ? sms : fa::kTreeMaxCtas;
+    const int grid = (sms < fa::kTreeMaxSms ? sms : fa::kTreeMaxSms) * fa::kTreeCtasPerSm<D>;
     cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tk8, tv8, tp);
     if (e == cudaSuccess && grid > 1) {
         // one round of blocks, as many to an item (or a CTA's beginning) as there is room for
@@ -1017,11 +1031,11 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     if (rc) return rc;
     if (p.B == 0) return FA_OK;
     if (!aligned16(p.workspace)) return FA_ERR_ALIGN;
-    if (!p.workspace || p.workspace_bytes < fa_decode_tree_workspace_bytes(p.B, p.T, p.Hq, p.Hkv, Skv_max, p.d)) return FA_ERR_WORKSPACE;
+    if (!p.workspace || p.workspace_bytes < fa_decode_tree_workspace_bytes(p.B, p.T, p.Hq, p.Hkv, Skv_max, p.d, 2)) return FA_ERR_WORKSPACE;
     int sms = 0;
     rc = check_device(&sms);
     if (rc) return rc;
-    const TreeBlocks tb(p.Hq / p.Hkv, p.T);
+    const TreeBlocks tb(p.Hq / p.Hkv, p.T, p.d);
     const long long units = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile + fa::kTreeItemCost;
     if (units * p.B * p.Hkv * tb.blocks > 0x7fffffffll) return FA_ERR_UNSUPPORTED;   // (they are counted in 32 bits)
     fa::TreeParams tp;
@@ -1033,8 +1047,8 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     tp.mask = p.mask;
     tp.block_table = p.block_table;
     tp.o_part = static_cast<float*>(p.workspace);
-    tp.lse_part = tp.o_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows * p.d;
-    tp.starts = reinterpret_cast<int*>(tp.lse_part + (size_t)2 * fa::kTreeMaxCtas * tb.rows);
+    tp.lse_part = tp.o_part + tb.slots(p.d) * tb.rows * p.d;
+    tp.starts = reinterpret_cast<int*>(tp.lse_part + tb.slots(p.d) * tb.rows);
     tp.mask_stride = p.mask_stride;
     tp.mask_words = (p.T + 31) / 32;
     tp.B = p.B;
@@ -1181,16 +1195,17 @@ int fa_decode_ex(const fa_decode_params* p, void* stream) {
                        p->workspace, p->workspace_bytes, stream, nullptr, 0, 0, 0, Sq, p->dtype == FA_DTYPE_BF16);
 }
 
-size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d) {
+size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d, int variant) {
     if (B <= 0 || T <= 0 || T > kTreeMaxNodes || Hq <= 0 || Hkv <= 0 || Skv_max <= 0 || (d != 128 && d != 64)) return 0;
-    if ((long long)(Hq / Hkv) * T <= kTreeFewRows) return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
-    const TreeBlocks tb(Hq / Hkv, T);
-    return 2 * (size_t)fa::kTreeMaxCtas * tb.rows * ((size_t)d + 1) * sizeof(float) + ((size_t)B + 1) * sizeof(int);
+    if (!tree_takes_many_rows(B, T, Hq, Hkv, Skv_max, d, variant)) return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
+    const TreeBlocks tb(Hq / Hkv, T, d);
+    return tb.slots(d) * tb.rows * ((size_t)d + 1) * sizeof(float) + ((size_t)B + 1) * sizeof(int);
 }
 
 int fa_decode_tree(const fa_tree_params* p, void* stream) {
     if (!p) return FA_ERR_NULL;
     if (p->dtype != FA_DTYPE_FP16 && p->dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    if (p->variant < 0 || p->variant > 2) return FA_ERR_UNSUPPORTED;
     int Skv_max = p->Skv_max;
     if (p->block_table) {
         if (int rc = check_table(p->num_pages, p->page_size, p->max_pages, p->table_stride, p->block_table)) return rc;
@@ -1201,7 +1216,7 @@ int fa_decode_tree(const fa_tree_params* p, void* stream) {
     if ((reinterpret_cast<uintptr_t>(p->mask) | reinterpret_cast<uintptr_t>(p->tree_lens) | reinterpret_cast<uintptr_t>(p->seqlens_k) |
          reinterpret_cast<uintptr_t>(p->lse)) & 3u)
         return FA_ERR_ALIGN;
-    if (p->Hkv > 0 && (long long)(p->Hq / p->Hkv) * p->T > kTreeFewRows) return tree_impl(*p, Skv_max, stream);
+    if (p->Hkv > 0 && tree_takes_many_rows(p->B, p->T, p->Hq, p->Hkv, Skv_max, p->d, p->variant)) return tree_impl(*p, Skv_max, stream);
     return decode_impl(p->q, p->k, p->v, p->o, p->lse, p->seqlens_k, p->B, p->Hq, p->Hkv, Skv_max, p->d, p->scale, p->workspace,
                        p->workspace_bytes, stream, p->block_table, p->num_pages, p->block_table ? p->page_size : 0, p->table_stride,
                        p->T, p->dtype == FA_DTYPE_BF16, p);

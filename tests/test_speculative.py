@@ -36,7 +36,7 @@ def test_tree_attention_refuses_bad_arguments(fa):
     for kw in (dict(B=-1), dict(T=0), dict(T=-3), dict(Hq=5), dict(Hkv=0), dict(Skv_max=-1), dict(mask_stride=-4), dict(d=0)):
         assert call(**kw) == fa.FA_ERR_SHAPE, kw
     for kw in (dict(T=257), dict(T=200, Skv_max=199), dict(d=256), dict(d=96), dict(dtype=fa.FA_DTYPE_FP32), dict(scale=-0.1),
-               dict(scale=float("nan")), dict(scale=float("inf")), dict(B=65536), dict(Hq=70000, Hkv=1)):
+               dict(scale=float("nan")), dict(scale=float("inf")), dict(B=65536), dict(Hq=70000, Hkv=1), dict(variant=3), dict(variant=-1)):
         assert call(**kw) == fa.FA_ERR_UNSUPPORTED, kw
     for kw in (dict(q=None), dict(k=None), dict(v=None), dict(o=None), dict(mask=None), dict(seqlens_k=None)):
         assert call(**kw) == fa.FA_ERR_NULL, kw
@@ -46,6 +46,10 @@ def test_tree_attention_refuses_bad_arguments(fa):
     need = fa.fa_decode_tree_workspace_bytes(2, 4, 4, 2, 256, 128)
     assert need > 0 and fa.fa_decode_tree_workspace_bytes(2, 4, 4, 2, 256, 96) == 0 and fa.fa_decode_tree_workspace_bytes(2, 0, 4, 2, 256, 128) == 0
     assert call(workspace_bytes=need - 1) == fa.FA_ERR_WORKSPACE and call(workspace=None) == fa.FA_ERR_WORKSPACE
+    for d in (128, 64):
+        more = fa.fa_decode_tree_workspace_bytes(2, 40, 4, 2, 256, d, 2)
+        assert more > 0 and call(T=40, d=d, variant=2, workspace_bytes=more - 1) == fa.FA_ERR_WORKSPACE
+        assert fa.fa_decode_tree_workspace_bytes(64, 64, 32, 8, 8192, d) == fa.fa_decode_tree_workspace_bytes(64, 64, 32, 8, 8192, d, 2)
     paged = dict(block_table=("at", 0), num_pages=8, page_size=64, max_pages=4, table_stride=4)
     for kw in (dict(page_size=48), dict(page_size=0), dict(table_stride=3), dict(num_pages=-1), dict(num_pages=0),
                dict(max_pages=1 << 26, table_stride=1 << 26)):

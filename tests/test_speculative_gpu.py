@@ -69,18 +69,19 @@ def check_tree(fa, B, T, Hq, Hkv, d, dtype, lens, page=0, tree_lens=None, see=No
     lse, check_l = guard_alloc((B, Hq, T), torch.float32, DEV) if with_lse else (None, lambda: None)
     tab = dev(table)
     skv = S if table is None else table.shape[1] * page
-    need = fa.fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, skv, d)
-    ws = torch.full((need + 256,), 0xff, dtype=torch.uint8, device=DEV)
-    fa.fa_decode_tree(dev(q), dev(k), dev(v), o, lse, ints(lens), dev(words), scale, ws[:need],
-                      tree_lens=None if tree_lens is None else ints(tree_lens), block_table=tab)
-    torch.cuda.synchronize()
-    assert fa.fa_device_status()[0] == 0
-    check_o(), check_l()
-    assert (ws[need:] == 0xff).all(), "workspace overrun"
-    assert_close_to_oracle(o, lse if with_lse else l_ref, o_ref, l_ref, stored_bf16=dtype == torch.bfloat16, p_absv=absv)
-    for b in range(B):
-        assert not o[b, live[b]:].float().any()
-    return o, lse
+    for variant in (0, 1, 2):     # by the sizes, and each of the two kernels
+        need = fa.fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, skv, d, variant)
+        ws = torch.full((need + 256,), 0xff, dtype=torch.uint8, device=DEV)
+        o.fill_(float("nan"))
+        fa.fa_decode_tree(dev(q), dev(k), dev(v), o, lse, ints(lens), dev(words), scale, ws[:need],
+                          tree_lens=None if tree_lens is None else ints(tree_lens), block_table=tab, variant=variant)
+        torch.cuda.synchronize()
+        assert fa.fa_device_status()[0] == 0
+        check_o(), check_l()
+        assert (ws[need:] == 0xff).all(), "workspace overrun"
+        assert_close_to_oracle(o, lse if with_lse else l_ref, o_ref, l_ref, stored_bf16=dtype == torch.bfloat16, p_absv=absv, what=f"variant {variant}")
+        for b in range(B):
+            assert not o[b, live[b]:].float().any()
 
 
 HEADS = [(4, 4), (8, 2), (8, 1), (10, 2), (7, 1), (16, 2)]
@@ -117,10 +118,11 @@ def test_tree_lengths_that_do_not_fit(fa):
     lens, mask = ints([100000, -5]), ref.bits_to_words(torch.ones(2, 4, 4, dtype=torch.bool)).to(DEV)
     q, k = torch.randn(2, 4, 4, 64, device=DEV).half(), torch.randn(2, 50, 4, 64, device=DEV).half()
     o, lse = torch.empty_like(q), torch.empty(2, 4, 4, device=DEV)
-    ws = torch.empty(fa.fa_decode_tree_workspace_bytes(2, 4, 4, 4, 50, 64), dtype=torch.uint8, device=DEV)
-    fa.fa_decode_tree(q, k, k, o, lse, lens, mask, 0.125, ws)
     o_ref, l_ref = ref.tree_attention(q.cpu(), k.cpu(), k.cpu(), [50, 0], torch.ones(2, 4, 4, dtype=torch.bool), 0.125)
-    assert_close_to_oracle(o, lse, o_ref, l_ref)
+    for variant in (1, 2):
+        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(2, 4, 4, 4, 50, 64, variant), dtype=torch.uint8, device=DEV)
+        fa.fa_decode_tree(q, k, k, o, lse, lens, mask, 0.125, ws, variant=variant)
+        assert_close_to_oracle(o, lse, o_ref, l_ref)
 
 
 @pytest.mark.parametrize("T,hq,hkv", [(9, 4, 2), (50, 8, 2), (90, 8, 2)])
@@ -154,10 +156,11 @@ def test_tree_scores_far_apart(fa):
         k, v = (torch.randn(1, 1200, 2, 128, generator=gen) * 4).half(), torch.randn(1, 1200, 2, 128, generator=gen).half()
         see = ref.ancestors(random_tree(T, random.Random(seed)))[None]
         o_ref, l_ref = ref.tree_attention(q, k, v, [1200], see, 0.3)
-        o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 4, T, device=DEV)
-        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 4, 2, 1200, 128), dtype=torch.uint8, device=DEV)
-        fa.fa_decode_tree(q.to(DEV), k.to(DEV), v.to(DEV), o, lse, ints([1200]), ref.bits_to_words(see).to(DEV), 0.3, ws)
-        assert_close_to_oracle(o, lse, o_ref, l_ref, stored_fp16_ulp=True)
+        for variant in (1, 2):
+            o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 4, T, device=DEV)
+            ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 4, 2, 1200, 128, variant), dtype=torch.uint8, device=DEV)
+            fa.fa_decode_tree(q.to(DEV), k.to(DEV), v.to(DEV), o, lse, ints([1200]), ref.bits_to_words(see).to(DEV), 0.3, ws, variant=variant)
+            assert_close_to_oracle(o, lse, o_ref, l_ref, stored_fp16_ulp=True)
 
 
 def test_tree_of_a_chain_is_the_append(fa):
@@ -168,11 +171,12 @@ def test_tree_of_a_chain_is_the_append(fa):
     lens = ints([700, 8, 300])
     mask = ref.bits_to_words(torch.tril(torch.ones(T, T, dtype=torch.bool))).to(DEV)
     a, b = torch.empty_like(q), torch.empty_like(q)
-    ws = torch.empty(fa.fa_decode_tree_workspace_bytes(B, T, 8, 2, S, 128), dtype=torch.uint8, device=DEV)
-    fa.fa_decode_tree(q, k, v, a, None, lens, mask, 128 ** -0.5, ws)
     ws2 = torch.empty(fa.fa_decode_append_workspace_bytes(B, T, 8, 2, S, 128), dtype=torch.uint8, device=DEV)
     fa.fa_decode_ex(q, k, v, b, None, lens, 128 ** -0.5, ws2)
-    assert float((a.double() - b.double()).abs().max()) <= 4e-3
+    for variant in (1, 2):
+        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(B, T, 8, 2, S, 128, variant), dtype=torch.uint8, device=DEV)
+        fa.fa_decode_tree(q, k, v, a, None, lens, mask, 128 ** -0.5, ws, variant=variant)
+        assert float((a.double() - b.double()).abs().max()) <= 4e-3
 
 
 @pytest.mark.parametrize("T", [3, 40])
@@ -191,10 +195,11 @@ def test_tree_pages_past_32_bits(fa, T):
     q = torch.randn(1, T, 16, d, generator=gen).half()
     see = ref.ancestors(random_tree(T, random.Random(1)))[None]
     o_ref, l_ref = ref.tree_attention(q, k.reshape(1, -1, H, d), v.reshape(1, -1, H, d), [n], see, 0.1)
-    o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 16, T, device=DEV)
-    ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 16, H, 7 * page, d), dtype=torch.uint8, device=DEV)
-    fa.fa_decode_tree(q.to(DEV), pool_k, pool_v, o, lse, ints([n]), ref.bits_to_words(see).to(DEV), 0.1, ws, block_table=ints([ids]))
-    assert_close_to_oracle(o, lse, o_ref, l_ref)
+    for variant in (1, 2):
+        o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 16, T, device=DEV)
+        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 16, H, 7 * page, d, variant), dtype=torch.uint8, device=DEV)
+        fa.fa_decode_tree(q.to(DEV), pool_k, pool_v, o, lse, ints([n]), ref.bits_to_words(see).to(DEV), 0.1, ws, block_table=ints([ids]), variant=variant)
+        assert_close_to_oracle(o, lse, o_ref, l_ref)
 
 
 @pytest.mark.parametrize("T", [4, 40])
@@ -210,10 +215,12 @@ def test_tree_pages_that_are_none(fa, T, page):
         kz, vz = k.clone(), v.clone()
         kz[1], vz[1] = 0, 0
         o_ref, l_ref = ref.tree_attention(q, kz.view(1, n, H, d), vz.view(1, n, H, d), [n], see, 0.125)
-        o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 8, T, device=DEV)
-        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 8, H, n, d), dtype=torch.uint8, device=DEV)
-        fa.fa_decode_tree(q.to(DEV), k.to(DEV), v.to(DEV), o, lse, ints([n]), ref.bits_to_words(see).to(DEV), 0.125, ws, block_table=ints([[0, bad, 2, 3]]))
-        assert_close_to_oracle(o, lse, o_ref, l_ref)
+        for variant in (1, 2):
+            o, lse = torch.empty_like(q, device=DEV), torch.empty(1, 8, T, device=DEV)
+            ws = torch.empty(fa.fa_decode_tree_workspace_bytes(1, T, 8, H, n, d, variant), dtype=torch.uint8, device=DEV)
+            fa.fa_decode_tree(q.to(DEV), k.to(DEV), v.to(DEV), o, lse, ints([n]), ref.bits_to_words(see).to(DEV), 0.125, ws,
+                              block_table=ints([[0, bad, 2, 3]]), variant=variant)
+            assert_close_to_oracle(o, lse, o_ref, l_ref)
 
 
 @pytest.mark.parametrize("smax", [40, 127, 128, 129, 200, 1001])
@@ -228,10 +235,11 @@ def test_tree_at_the_end_of_the_caches(fa, smax):
         k.copy_(torch.randn(k.shape, generator=gen)), v.copy_(torch.randn(v.shape, generator=gen))
         see = torch.stack([ref.ancestors(random_tree(T, random.Random(b))) for b in range(B)])
         o_ref, l_ref = ref.tree_attention(q, k.cpu(), v.cpu(), lens, see, 0.1)
-        o, lse = torch.empty_like(q, device=DEV), torch.empty(B, hq, T, device=DEV)
-        ws = torch.empty(fa.fa_decode_tree_workspace_bytes(B, T, hq, hkv, smax, d), dtype=torch.uint8, device=DEV)
-        fa.fa_decode_tree(q.to(DEV), k, v, o, lse, ints(lens), ref.bits_to_words(see).to(DEV), 0.1, ws)
-        assert_close_to_oracle(o, lse, o_ref, l_ref)
+        for variant in (1, 2):
+            o, lse = torch.empty_like(q, device=DEV), torch.empty(B, hq, T, device=DEV)
+            ws = torch.empty(fa.fa_decode_tree_workspace_bytes(B, T, hq, hkv, smax, d, variant), dtype=torch.uint8, device=DEV)
+            fa.fa_decode_tree(q.to(DEV), k, v, o, lse, ints(lens), ref.bits_to_words(see).to(DEV), 0.1, ws, variant=variant)
+            assert_close_to_oracle(o, lse, o_ref, l_ref)
         check_k(), check_v()
 
 
