@@ -408,10 +408,7 @@ def _planes(what: str, k, v):
     if not k.is_contiguous():
         _contiguous(what, k[0])
     size = k.element_size()
-    row = size
-    for n in shape[3:]:
-        row *= n
-    return shape[0], shape[1], shape[2], stride[0] * size, row
+    return shape[0], shape[1], shape[2], stride[0] * size, stride[2] * size
 
 
 def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, block_table=None, max_pages: int = None,
@@ -420,7 +417,8 @@ def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, 
     [L,num_pages,page_size,Hkv,d] (any element type); path int32 [B,T], n_accept int32 [B] as ``fa_spec_verify`` writes
     them; writes new_lens int32 [B]."""
     layers, slabs, rows, stride, row = _planes("fa_cache_compact", k, v)
-    if not (_good(seqlens_k) and _good(path) and _good(n_accept) and _good(new_lens) and _good(tree_lens)):
+    if not (seqlens_k.dtype is _INT and path.dtype is _INT and n_accept.dtype is _INT and new_lens.dtype is _INT and path.is_contiguous()
+            and seqlens_k.is_contiguous() and n_accept.is_contiguous() and new_lens.is_contiguous() and (tree_lens is None or _good(tree_lens))):
         _contiguous("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
         _int32("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
     B, T = path.shape
@@ -436,7 +434,8 @@ def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, 
 def fa_pages_resize(block_table, held, refs, want, n_short, page_size: int, raise_on_error: bool = True) -> int:
     """``fa_pages_resize``: block_table int32 [B,max_pages], held int32 [B], refs int32 [num_pages], want int32 [B] (rows);
     n_short int32 [1] counts the sequences that could not be served."""
-    if not (_good(held) and _good(refs) and _good(want) and _good(n_short)):
+    if not (held.dtype is _INT and refs.dtype is _INT and want.dtype is _INT and n_short.dtype is _INT and held.is_contiguous()
+            and refs.is_contiguous() and want.is_contiguous() and n_short.is_contiguous()):
         _contiguous("fa_pages_resize", held, refs, want, n_short)
         _int32("fa_pages_resize", held, refs, want, n_short)
     B, pages = block_table.shape

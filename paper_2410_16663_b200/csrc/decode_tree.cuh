@@ -55,7 +55,8 @@ struct TreeParams {
     const int* block_table;   // nullptr: contiguous
     float* o_part;            // [2 ctas][D/4][rows][4]
     float* lse_part;          // [2 ctas][rows]
-    int* starts;              // [B + 1] first unit of each sequence, and of none
+    int4* merges;             // what there is to merge: (sequence, item, first CTA, last CTA), one CTA: nothing
+    int by_item;              // an entry for each item, where they are fewer than the CTAs; otherwise for each CTA but the first
     long long mask_stride;
     int mask_words;
     int B, T, Hq, Hkv, g, Smax;
@@ -182,6 +183,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
     // The loading warp finds the CTA's run meanwhile: its first and last unit, and the sequence and the place in it of the first.  (As
     // little code as can be: it runs once, and fetching its instructions takes longer than executing them.)
     const int items = p.Hkv * p.blocks;
+    TreePlan plan(1, 1);
     int pos = 0, end = 0, b = 0, in_seq = 0, chunk = 0, chunk_len = 0;
     auto lens_at = [&](int b0) {   // the lengths of 32 sequences, one per lane
         if (b0 != chunk) {
@@ -209,10 +211,8 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 #pragma unroll 1
         for (int b0 = 0; b0 < p.B; b0 += 32) {
             total = scan(b0, total);
-            if (blockIdx.x == 0 && b0 + lane < p.B) p.starts[b0 + lane] = upto - mine;
         }
-        if (blockIdx.x == 0 && lane == 0) p.starts[p.B] = total;
-        const TreePlan plan(total, gridDim.x);
+        plan = TreePlan(total, gridDim.x);
         pos = plan.begin(blockIdx.x);
         end = plan.begin(blockIdx.x + 1);
 #pragma unroll 1
@@ -256,8 +256,10 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
         int next_len = pos < end ? len_of(b) : 0, units = tree_item_units(next_len), next_b = b;
         int item = pos < end ? in_seq / units : 0, unit = in_seq - item * units;   // the next item, and the next of its units
         for (uint32_t ord = 0; ok; ++ord) {
-            int t0 = 0, n = 0, hk = 0, block = 0, len = 0;
+            int t0 = 0, n = 0, hk = 0, block = 0, len = 0, first = 0, last_tile = 0;   // units of the item's first and last tile
             while (pos < end && n == 0) {   // (a run may have an item's first units alone, and no tile)
+                first = pos - unit + kTreeItemCost;
+                last_tile = pos - unit + units - 1;
                 const int last = min(units, unit + end - pos);
                 b = next_b;
                 len = next_len;
@@ -278,6 +280,13 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             ok = pp_warp_wait(bar(At::seg_empty + slot), ((ord / kTreeSegs) & 1) ^ 1, &abort_flag, 300);
             if (!ok) break;
             if (lane == 0) {
+                // The merge of a shared item is entered by who has its first tile, or by who comes next.
+                if (p.by_item) {
+                    if (n > 0 && t0 == 0) p.merges[b * items + hk * p.blocks + block] = make_int4(b, hk * p.blocks + block, blockIdx.x, plan.owner(last_tile));
+                } else if (ord == 0 && blockIdx.x > 0) {
+                    const bool mine = n > 0 && t0 > 0 && plan.owner(first) + 1 == (int)blockIdx.x;
+                    p.merges[blockIdx.x - 1] = make_int4(b, hk * p.blocks + block, blockIdx.x - 1, mine ? plan.owner(last_tile) : 0);
+                }
                 segs[slot] = {b, hk, block, t0, n, (len + kDecTile - 1) / kDecTile, len, n > 0 ? tree_nodes(p.tree_lens, b, p.T, len) : 0};
                 mbar_arrive(bar(At::seg_full + slot));
             }
@@ -455,6 +464,7 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             for (long long i = tid; i < n * (D / 8); i += 128 * kTiles) reinterpret_cast<uint4*>(p.o)[at * (D / 8) + i] = make_uint4(0u, 0u, 0u, 0u);
             if (p.lse)
                 for (long long i = tid; i < n; i += 128 * kTiles) p.lse[at + i] = -INFINITY;
+            for (int i = tid; p.by_item && i < items; i += 128 * kTiles) p.merges[b * items + i] = make_int4(0, 0, 0, 0);
         }
         TreeSegment seg;
         for (uint32_t ord = 0;; ++ord) {
@@ -618,48 +628,24 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
 
 // Merge of the rows that several CTAs have worked on (the recurrence of decode.cuh's merge).  A thread owns four columns of a row; a
 // warp eight such pieces of each of four rows, so that both what it reads and what it writes come in runs of 64 bytes.
-// grid: (blocks that share an item's rows, y).  kItems: y is an item, where there are no more of them than CTAs; otherwise the run of CTA
-// y + 1 begins inside an item and, if it is the first to, the blocks merge that item.
-constexpr int kTreeCombineThreads = 256, kTreeCombinePerSm = 6;
+// grid: (blocks that share an item's rows, entries of TreeParams::merges).  kItems: an entry for each item: few, of many parts.
+constexpr int kTreeCombineThreads = 256;
+template <bool kItems>
+constexpr int kTreeCombinePerSm = kItems ? 3 : 6;
 template <typename T, int D, bool kItems>
-__global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm) fa_decode_tree_combine_kernel(const TreeParams p, int grid) {
+__global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm<kItems>) fa_decode_tree_combine_kernel(const TreeParams p) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr int kWarpsPerRow = D / 32;
     const int piece = (warp % kWarpsPerRow) * 8 + (lane & 7);
     grid_dep_wait();
-    const TreePlan plan(p.starts[p.B], grid);
-    const int items = p.Hkv * p.blocks;
-    int b = 0, item, first, tiles;   // first: the unit of the item's first tile
-    if constexpr (kItems) {
-        b = blockIdx.y / items;
-        item = blockIdx.y % items;
-        const int seq = p.starts[b], units = (p.starts[b + 1] - seq) / items;
-        if (units == 0) return;
-        tiles = units - kTreeItemCost;
-        first = seq + item * units + kTreeItemCost;
-    } else {
-        const int cut = plan.begin(blockIdx.y + 1);
-        if ((int)blockIdx.y + 1 >= plan.ctas) return;
-        for (int hi = p.B; hi - b > 1;) {   // the last sequence that starts at or before the cut, 32 places at a time
-            const int step = (hi - b + 31) / 32, at = b + lane * step;
-            const int n = __popc(__ballot_sync(0xffffffffu, at < hi && p.starts[at] <= cut));
-            b += (n - 1) * step;
-            hi = min(hi, b + step);
-        }
-        const int seq = p.starts[b], units = (p.starts[b + 1] - seq) / items;
-        item = (cut - seq) / units;
-        tiles = units - kTreeItemCost;
-        first = seq + item * units + kTreeItemCost;
-        if (cut <= first || (int)blockIdx.y != plan.owner(first)) return;
-    }
-    const int c0 = plan.owner(first), c1 = plan.owner(first + tiles - 1);
-    if (c0 == c1) return;   // its only part is where it belongs
+    const int4 merge = p.merges[blockIdx.y];
+    const int b = merge.x, item = merge.y, c0 = merge.z, c1 = merge.w;
+    if (c1 <= c0) return;   // its only part is where it belongs
     const int hk = item / p.blocks, R0 = item % p.blocks * p.rows;
     const int end = min(p.rows, p.g * p.T - R0);
     for (int row = blockIdx.x * (1024 / D) + (warp / kWarpsPerRow) * 4 + (lane >> 3); row < end; row += gridDim.x * (1024 / D)) {
-        const int token = (R0 + row) / p.g, head = hk * p.g + (R0 + row) % p.g;
         float M = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int kN = 4;
+        constexpr int kN = kItems ? 8 : 4;
         for (int at = c0; at <= c1; at += kN) {
             float l[kN], m = M;
             float4 v[kN];
@@ -692,6 +678,7 @@ __global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm) fa_dec
             }
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int token = (R0 + row) / p.g, head = hk * p.g + (R0 + row) % p.g;
         *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + (((long long)b * p.T + token) * p.Hq + head) * D + 4 * piece) =
             make_uint2(pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv));
         if (p.lse && piece == 0) p.lse[((long long)b * p.Hq + head) * p.T + token] = sum == 0.f ? -INFINITY : M + logf(sum);

@@ -1008,7 +1008,7 @@ struct TreeBlocks {
     size_t slots(int d) const { return 2 * (size_t)fa::kTreeMaxSms * (d == 64 ? fa::kTreeCtasPerSm<64> : fa::kTreeCtasPerSm<128>); }
 };
 template <typename T, int D>
-int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tk8, const CUtensorMap& tv8, const fa::TreeParams& tp, int sms, cudaStream_t st) {
+int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tk8, const CUtensorMap& tv8, fa::TreeParams& tp, int sms, cudaStream_t st) {
     auto kern = fa::fa_decode_tree_kernel<T, D, 1>;
     int smem = fa::TreeShape<D, 1>::kSmem, threads = fa::TreeShape<D, 1>::kThreads;
     if constexpr (D == 128)
@@ -1016,13 +1016,14 @@ int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap&
     int sm_count = 0;
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
     const int grid = (sms < fa::kTreeMaxSms ? sms : fa::kTreeMaxSms) * fa::kTreeCtasPerSm<D>;
+    tp.by_item = (long long)tp.B * tp.Hkv * tp.blocks < grid ? 1 : 0;
     cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tk8, tv8, tp);
     if (e == cudaSuccess && grid > 1) {
-        // one round of blocks, as many to an item (or a CTA's beginning) as there is room for
-        const long long items = (long long)tp.B * tp.Hkv * tp.blocks;
-        const int y = items < grid ? (int)items : grid - 1, parts = (tp.rows + 1024 / D - 1) / (1024 / D), room = fa::kTreeCombinePerSm * sms / y;
-        const auto combine = items < grid ? fa::fa_decode_tree_combine_kernel<T, D, true> : fa::fa_decode_tree_combine_kernel<T, D, false>;
-        e = fa::launch_dependent(combine, dim3(parts < room ? parts : room, y), fa::kTreeCombineThreads, 0, st, tp, grid);
+        // one round of blocks, as many to an entry as there is room for
+        const int y = tp.by_item ? tp.B * tp.Hkv * tp.blocks : grid - 1, parts = (tp.rows + 1024 / D - 1) / (1024 / D);
+        const int room = (tp.by_item ? fa::kTreeCombinePerSm<true> : fa::kTreeCombinePerSm<false>) * sms / y;
+        const auto combine = tp.by_item ? fa::fa_decode_tree_combine_kernel<T, D, true> : fa::fa_decode_tree_combine_kernel<T, D, false>;
+        e = fa::launch_dependent(combine, dim3(parts < room ? parts : room > 0 ? room : 1, y), fa::kTreeCombineThreads, 0, st, tp);
     }
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
@@ -1048,7 +1049,7 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
     tp.block_table = p.block_table;
     tp.o_part = static_cast<float*>(p.workspace);
     tp.lse_part = tp.o_part + tb.slots(p.d) * tb.rows * p.d;
-    tp.starts = reinterpret_cast<int*>(tp.lse_part + tb.slots(p.d) * tb.rows);
+    tp.merges = reinterpret_cast<int4*>(tp.lse_part + tb.slots(p.d) * tb.rows);   // (slots is a multiple of four)
     tp.mask_stride = p.mask_stride;
     tp.mask_words = (p.T + 31) / 32;
     tp.B = p.B;
@@ -1199,7 +1200,7 @@ size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max
     if (B <= 0 || T <= 0 || T > kTreeMaxNodes || Hq <= 0 || Hkv <= 0 || Skv_max <= 0 || (d != 128 && d != 64)) return 0;
     if (!tree_takes_many_rows(B, T, Hq, Hkv, Skv_max, d, variant)) return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
     const TreeBlocks tb(Hq / Hkv, T, d);
-    return tb.slots(d) * tb.rows * ((size_t)d + 1) * sizeof(float) + ((size_t)B + 1) * sizeof(int);
+    return tb.slots(d) * tb.rows * ((size_t)d + 1) * sizeof(float) + tb.slots(d) * sizeof(int4) / 2;
 }
 
 int fa_decode_tree(const fa_tree_params* p, void* stream) {
