@@ -524,3 +524,43 @@ def test_a_step_in_a_graph_and_on_a_side_stream(fa):
         assert all(torch.equal(first[n], second[n]) for n in ("table", "held", "refs", "k", "v"))
         assert z["new_lens"].tolist() == [a - T + 1 + b for a, b in zip(lens, z["n"].tolist())] and z["short"].tolist() == [0]
     assert fa.fa_device_status()[0] == 0
+
+
+def test_steps_of_a_serving_loop(fa):
+    """The example's loop: forked sequences decode some steps; the pages' counts, tables and lengths agree with one another at the end,
+    and the cache holds the rows of exactly the tokens that stand, with the attention's own inputs written again."""
+    from paper_2410_16663_b200 import speculate
+    samples, prompt, nodes, steps, page = 5, 333, 13, 4, 16
+    said, cache = speculate.run(samples, prompt, nodes, steps, layers=2, vocab=512, page=page)
+    torch.cuda.synchronize()
+    assert fa.fa_device_status()[0] == 0 and int(cache.short) == 0
+    lens, held, table, refs = (t.tolist() for t in (cache.lens, cache.held, cache.table, cache.refs))
+    gained = [sum(1 + int(n[b]) for _, n in said) for b in range(samples)]
+    assert lens == [prompt + g for g in gained]
+    assert held == [-(-x // page) for x in lens]
+    count = [0] * len(refs)
+    for b in range(samples):
+        assert all(e >= 0 for e in table[b][:held[b]]) and all(e == -1 for e in table[b][held[b]:])
+        for e in table[b][:held[b]]:
+            count[e] += 1
+    assert count == refs and max(refs) == samples and sum(r == samples for r in refs) == prompt // page
+    for out, n in said:
+        for b in range(samples):
+            k = int(n[b])
+            assert (out[b, :k + 1] >= 0).all() and (out[b, k + 1:] == -1).all()
+    # layer 0's keys depend on the tokens alone: the last token's row of every step stands first in its tree, the accepted ones follow
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(0)
+    model = speculate.Model(2, 8, 2, 128, 512, torch.bfloat16, DEV, gen)
+    for b in range(samples):
+        tokens = []
+        for i, (out, n) in enumerate(said):
+            k = int(n[b])
+            first = int(said[i - 1][0][b, int(said[i - 1][1][b])]) if i else None
+            tokens += [first] + out[b, :k].tolist()
+        rows = torch.arange(prompt, lens[b], device=DEV)
+        got = cache.k[0, cache.table[b, rows // page].long(), rows % page]
+        known = [i for i, t in enumerate(tokens) if t is not None]
+        x = model.embed[torch.tensor([tokens[i] for i in known], device=DEV)][None]
+        want = model.project(x, 0)[1][0]
+        assert torch.allclose(got[known].float(), want.float(), rtol=2e-2, atol=2e-2)
