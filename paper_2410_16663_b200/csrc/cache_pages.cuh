@@ -27,10 +27,10 @@ struct CompactParams {
     int row_vecs;            // 16-byte pieces of a row
     long long layer_stride;  // 16-byte pieces between layers
 };
-constexpr int kCompactThreads = 256;
-constexpr int kCompactBatch = 8;     // rows in flight per thread
+constexpr int kCompactThreads = 256, kCompactPerSm = 4;
+constexpr int kCompactBatch = 4, kCompactUnits = 2;     // rows and pieces in flight per thread
 
-__global__ void __launch_bounds__(kCompactThreads) fa_cache_compact_kernel(const CompactParams p) {
+__global__ void __launch_bounds__(kCompactThreads, kCompactPerSm) fa_cache_compact_kernel(const CompactParams p) {
     grid_dep_wait();
     const int b = blockIdx.y;
     const int len = max(0, min(p.seqlens[b], p.max_rows));
@@ -40,14 +40,14 @@ __global__ void __launch_bounds__(kCompactThreads) fa_cache_compact_kernel(const
     if (blockIdx.x == 0 && threadIdx.x == 0) p.new_lens[b] = live > 0 ? prefix + 1 + n : len;
     const int* path = p.path + (long long)b * p.T;
     const int* table = p.block_table ? p.block_table + (long long)b * p.table_stride : nullptr;
-    // row `row` of the sequence in pieces from its plane's start; -1: not a row of the pool
+    // row `row` of the sequence among the rows of its plane; -1: not a row of the pool
     auto place = [&](int row) -> long long {
-        if (!table) return ((long long)b * p.max_rows + row) * p.row_vecs;
+        if (!table) return (long long)b * p.max_rows + row;
         const int page = table[row / p.page_size];
         if (page < 0 || page >= p.num_pages) return -1;
-        return ((long long)page * p.page_size + row % p.page_size) * p.row_vecs;
+        return (long long)page * p.page_size + row % p.page_size;
     };
-    const long long units = 2ll * p.layers * p.row_vecs;   // (plane, piece)
+    const int units = 2 * p.layers * p.row_vecs, stride = gridDim.x * kCompactThreads;   // (plane, piece)
     for (int i0 = 1; i0 <= n; i0 += kCompactBatch) {
         long long from[kCompactBatch], to[kCompactBatch];
 #pragma unroll
@@ -57,20 +57,26 @@ __global__ void __launch_bounds__(kCompactThreads) fa_cache_compact_kernel(const
             if (i > n) continue;
             const int x = path[i];
             if (x <= i || x >= live) continue;   // (it is there already; or no node)
-            from[j] = place(prefix + x);
-            to[j] = place(prefix + i);
+            from[j] = place(prefix + x) * p.row_vecs;
+            to[j] = place(prefix + i) * p.row_vecs;
             if (to[j] < 0) from[j] = -1;
         }
-        for (long long u = (long long)blockIdx.x * kCompactThreads + threadIdx.x; u < units; u += (long long)gridDim.x * kCompactThreads) {
-            const int plane = (int)(u / p.row_vecs), piece = (int)(u % p.row_vecs);
-            uint4* base = reinterpret_cast<uint4*>(plane & 1 ? p.v : p.k) + (long long)(plane >> 1) * p.layer_stride + piece;
-            uint4 x[kCompactBatch];
+        for (int u0 = blockIdx.x * kCompactThreads + threadIdx.x; u0 < units; u0 += kCompactUnits * stride) {
+            uint4 x[kCompactUnits][kCompactBatch];
+            uint4* base[kCompactUnits];
 #pragma unroll
-            for (int j = 0; j < kCompactBatch; ++j)
-                if (from[j] >= 0) x[j] = base[from[j]];
+            for (int k = 0; k < kCompactUnits; ++k) {
+                const int u = u0 + k * stride, plane = u / p.row_vecs;
+                base[k] = reinterpret_cast<uint4*>(plane & 1 ? p.v : p.k) + (long long)(plane >> 1) * p.layer_stride + (u - plane * p.row_vecs);
 #pragma unroll
-            for (int j = 0; j < kCompactBatch; ++j)
-                if (from[j] >= 0) base[to[j]] = x[j];
+                for (int j = 0; j < kCompactBatch; ++j)
+                    if (from[j] >= 0 && u < units) x[k][j] = base[k][from[j]];
+            }
+#pragma unroll
+            for (int k = 0; k < kCompactUnits; ++k)
+#pragma unroll
+                for (int j = 0; j < kCompactBatch; ++j)
+                    if (from[j] >= 0 && u0 + k * stride < units) base[k][to[j]] = x[k][j];
         }
     }
 }

@@ -1078,7 +1078,8 @@ int tree_impl(const fa_tree_params& p, int Skv_max, void* stream) {
         rc = encode_tiled<5>(i ? &tv : &tk, type16(bf16), i ? p.v : p.k, {64, 8, blocks, (cuuint64_t)box_rows / 8, heads}, {row, 128, 8 * row, head},
                              {64, 8, (cuuint32_t)blocks, (cuuint32_t)box_rows / 8, 1});
         if (rc) return rc;
-        rc = encode_map_cache(i ? &tv8 : &tk8, i ? p.v : p.k, slabs, slab_rows, p.Hkv, 8, bf16, p.d);
+        if (p.block_table) (i ? tv8 : tk8) = i ? tv : tk;   // (a page's rows all exist)
+        else rc = encode_map_cache(i ? &tv8 : &tk8, i ? p.v : p.k, slabs, slab_rows, p.Hkv, 8, bf16, p.d);
         if (rc) return rc;
     }
     tq = tk;
@@ -1299,8 +1300,9 @@ int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlen
     cp.num_pages = num_pages;
     cp.row_vecs = row_bytes / 16;
     cp.layer_stride = layer_stride / 16;
+    if (2ll * layers * cp.row_vecs > 0x3fffffffll) return FA_ERR_UNSUPPORTED;
     const long long blocks = (2ll * layers * cp.row_vecs + fa::kCompactThreads - 1) / fa::kCompactThreads;
-    const long long most = 8ll * sms / B;   // as many as run at once
+    const long long most = (long long)fa::kCompactPerSm * sms / B;   // as many as run at once
     const int grid = (int)(blocks < most ? (blocks > 0 ? blocks : 1) : (most > 0 ? most : 1));
     const cudaError_t e = fa::launch_dependent(fa::fa_cache_compact_kernel, dim3(grid, B), fa::kCompactThreads, 0, static_cast<cudaStream_t>(stream), cp);
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
