@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(kVerifyThreads, 2) fa_spec_verify_kernel(const
         float top = 0.f, most = 0.f;   // most: a little less than top
         int at = 0;
         const float sub = pass == 0 ? s : 0.f;
-        each(P + (long long)cur * p.V, pass == 0 && Q ? Q + (long long)cur * p.V : nullptr, E, std::integral_constant<int, kVec ? 4 : 3>(), [&](int v, float a, float c, float e) {
+        each(P + (long long)cur * p.V, pass == 0 && Q ? Q + (long long)cur * p.V : nullptr, E, std::integral_constant<int, 2>(), [&](int v, float a, float c, float e) {
             const float r = __fsub_rn(a, __fmul_rn(sub, c));
             if (!(r > 0.f) || !(r >= most * e)) return;   // (nearly all, without a division)
             const float score = __fdiv_rn(r, e);
