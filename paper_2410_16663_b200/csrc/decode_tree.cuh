@@ -486,31 +486,33 @@ fa_decode_tree_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_con
             const int prefix = seg.len - seg.live;
             const bool some = __any_sync(0xffffffffu, mine);   // a warp without rows only keeps step
             float m_run = -INFINITY, l_run = 0.f;
+            // V rows past the sequence may hold anything, NaN too: they become zeros (their probabilities are).  Each row tile's
+            // warps see to it themselves, before their own P V.
+            auto clear_v = [&](int valid) {
+                const uint32_t i = 2 * (s / kSub) + 1, v = sRing + (i % kSlots) * kTileB;
+                if (!wait(At::full + i % kSlots, (i / kSlots) & 1, 322)) return false;
+                for (int u = r; u < (kDecTile - valid) * (D / 8); u += 128) {
+                    const int key = valid + u / (D / 8), c = u % (D / 8);
+                    const uint32_t at = v + (uint32_t)(key >> 3) * Shape::kGroupB + (c >> 3) * 1024u + (uint32_t)(key & 7) * 128u;
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + ((c & 7) << 4)), "r"(0u) : "memory");   // (a row is a row, swizzled or not)
+                }
+                fence_proxy_async_smem();
+                return true;
+            };
             for (int j = 0; j < seg.n * kSub; ++j, ++s) {
                 const int key0 = seg.t0 * kDecTile + j * kStep;
                 const int buf = 2 * x + buf_of(s);   // (of the barriers)
                 const uint32_t tS = tmem + lanes + (x * kBufs + buf_of(s)) * kStep;
-                const bool masked = key0 + kStep > prefix;   // it reaches into the tree, or past the keys
+                // its tile reaches into the tree, or past the keys (one test for all that this asks for: a branch is 30 clocks)
+                const bool masked = (seg.t0 + j / kSub + 1) * kDecTile > prefix;
                 uint32_t vis[kStep / 32];
                 if (masked) {
 #pragma unroll
                     for (int c = 0; c < kStep / 32; ++c) vis[c] = visible(key0 - prefix + 32 * c) & low_bits(seg.len - key0 - 32 * c);
+                    if (s % kSub == 0 && seg.len - key0 < kDecTile && !(ok = clear_v(seg.len - key0))) break;
                 }
                 if (!(ok = wait(At::s_full + buf, phase_of(s) & 1, 321))) break;
                 tc_fence_after();
-                if (s % kSub == 0 && seg.len - key0 < kDecTile) {
-                    // V rows past the sequence may hold anything, NaN too: they become zeros (their probabilities are).  Each row tile's
-                    // warps see to it themselves, before their own P V.
-                    const uint32_t i = 2 * (s / kSub) + 1, v = sRing + (i % kSlots) * kTileB;
-                    const int valid = seg.len - key0;
-                    if (!(ok = wait(At::full + i % kSlots, (i / kSlots) & 1, 322))) break;
-                    for (int u = r; u < (kDecTile - valid) * (D / 8); u += 128) {
-                        const int key = valid + u / (D / 8), c = u % (D / 8);
-                        const uint32_t at = v + (uint32_t)(key >> 3) * Shape::kGroupB + (c >> 3) * 1024u + (uint32_t)(key & 7) * 128u;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + ((c & 7) << 4)), "r"(0u) : "memory");   // (a row is a row, swizzled or not)
-                    }
-                    fence_proxy_async_smem();
-                }
                 if (some) {
                     uint32_t sc[kStep];
 #pragma unroll
