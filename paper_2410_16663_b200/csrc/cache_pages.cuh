@@ -13,7 +13,9 @@ namespace fa {
 // ---------------------------------------------------------------------------------------
 // Compaction: row prefix + i of sequence b <- row prefix + path[b][i], i = 1 .. n_accept[b], in every plane (a layer's K or V).
 // A thread owns 16 bytes of a row in some planes and moves them in the order of i, several rows' loads ahead of the
-// first store: as path[i] >= i and the path ascends, a row that is still to be read has not been written.
+// first store: as path[i] >= i and the path ascends, a row that is still to be read has not been written.  Few bytes move; what
+// bounds it is the chain of length, path, table and row, which a thread follows once for all of its pieces.  64 sequences, 32 layers, 8 x 128
+// fp16 on 16-key pages, 17 MB: 8.0 us (9.1 with eight rows of one piece in flight, two CTAs to an SM); 1 sequence 2.3.
 struct CompactParams {
     char* k;
     char* v;
@@ -359,7 +361,8 @@ __global__ void __launch_bounds__(kPagesThreads) fa_pages_fork_kernel(const Fork
 }
 
 // The rows of a fork: the filled rows of each last page, in every plane.  They lie one after the other.  grid: (pairs, planes): pairs
-// that share a prompt copy the same rows of a plane at about the same time, and L2 has them.
+// that share a prompt copy the same rows of a plane at about the same time, and L2 has them (64 of 16 prompts, 32 layers, 260 MB
+// written: with the tables 65 us, 102 with a pair's planes next to each other).  HBM bounds it.
 constexpr int kForkThreads = 256;
 constexpr int kForkBatch = 8;
 __global__ void __launch_bounds__(kForkThreads) fa_pages_fork_copy_kernel(const ForkParams p) {

@@ -1252,6 +1252,8 @@ int fa_spec_verify(const void* target_probs, const void* draft_probs, const int*
     vp.out_tokens = out_tokens;
     vp.T = T;
     vp.V = V;
+    // as many CTAs to a sequence as run at once, two to an SM, with two entries of the vocabulary for each thread at least (32 sequences of 131072
+    // tokens: 23.6 us with 8, 23.8 with up to 16; one of 32000: 5.6 with 8, 6.5 with 16)
     int cluster = fa::kVerifyMaxCluster;
     while (cluster > 1 && ((long long)B * cluster > 2ll * sms || V / cluster < 1024)) cluster /= 2;
     const bool vec = V % 4 == 0 && (probs & (dtype == FA_DTYPE_FP32 ? 15u : 7u)) == 0 && aligned16(noise);
