@@ -270,8 +270,8 @@ size_t fa_decode_append_workspace_bytes(int B, int Sq, int Hq, int Hkv, int Skv_
  * len = seqlens_k[b] keys, the tree's rows INCLUDED, node j's key and value are cache row len - n + j, and query row t sees
  *     every key before the tree (rows below len - n), and
  *     node j (0 <= j < n) iff bit j % 32 of mask[b * mask_stride + t * ceil(T / 32) + j / 32] is set
- * (the mask holds ancestors, not parents, and each node's own bit; it need not be a tree's).  Rows t >= n, and rows that
- * see nothing, give O = 0 and LSE = -inf.
+ * (the mask holds ancestors, not parents, and each node's own bit; it need not be a tree's).  Rows t >= n (whose q may be
+ * anything), and rows that see nothing, give O = 0 and LSE = -inf.
  *   q, o [B,T,Hq,d], lse [B,Hq,T] float or NULL, 1 <= T <= 256; d = 128 or 64; fp16 or bf16; q, o and the caches contiguous.
  *   Caches and block table as for fa_decode_ex.  seqlens_k, tree_lens, mask: int32 on the DEVICE; lengths are clamped to
  *   [0, Skv_max], tree_lens to [0, min(T, len)]; mask_stride: words from one sequence's mask to the next, 0 = all

@@ -59,6 +59,7 @@ def check_tree(fa, B, T, Hq, Hkv, d, dtype, lens, page=0, tree_lens=None, see=No
     absv = ref.tree_attention(q, k, v, lens, see_b, scale, tree_lens, abs_v=True)[0] if dtype == torch.bfloat16 else None
     for b in range(B):
         k[b, lens[b]:], v[b, lens[b]:] = float("nan"), float("nan")
+        q[b, live[b]:] = float("nan")                 # queries of no node
     table = None
     if page:
         k, table = paged_copy(k, lens, page, torch.Generator().manual_seed(seed + 1), wide=wide)
