@@ -340,9 +340,11 @@ int fa_spec_verify(const void* target_probs, const void* draft_probs, const int*
  * (A sequence without tree rows keeps its length.)  Rows past the new length keep what they had or hold what was moved.
  *   k, v: contiguous caches [layers,B,Skv_max,row] (block_table == NULL), or pools [layers,num_pages,page_size,row] behind
  *   block_table [B,table_stride], page_size any positive number; row: row_bytes bytes, a multiple of 16 (Hkv * d elements of any
- *   type); layer_stride: bytes from one layer to the next, a multiple of 16.  new_lens must not be seqlens_k.
+ *   type); layer_stride: bytes from one layer to the next, a multiple of 16.  new_lens shares no memory with seqlens_k or another input:
+ *   it is written while they are read (FA_ERR_UNSUPPORTED).
  *   Nodes outside (i, n) in path[b][i] and pages outside [0, num_pages) are skipped.
- * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (B > 65535, rows of 8 GiB and more over all layers), FA_ERR_NULL, FA_ERR_ALIGN.
+ * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (B > 65535, rows of 8 GiB and more over all layers, new_lens among the inputs), FA_ERR_NULL,
+ * FA_ERR_ALIGN.
  */
 int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlens_k, const int* tree_lens, const int* path,
                      const int* n_accept, int* new_lens, int layers, int64_t layer_stride, int B, int T, int Skv_max, int num_pages,

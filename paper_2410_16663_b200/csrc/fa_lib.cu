@@ -129,6 +129,12 @@ int encode_map_matrix(CUtensorMap* tm, const void* base, int rows, int cols, boo
 // a page holds a multiple of the 128-key tile, or 16, 32 or 64 keys (several pages per tile)
 bool page_size_ok(int ps) { return ps > 0 && (ps % fa::kDecTile == 0 || ps == 16 || ps == 32 || ps == 64); }
 
+// Arrays of 32-bit words that share memory.
+bool words_overlap(const int* a, long long na, const int* b, long long nb) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a && b && x < y + 4 * (uintptr_t)nb && y < x + 4 * (uintptr_t)na;
+}
+
 // A block table's sizes, of the decode forms that take a parameter block.
 int check_table(int num_pages, int page_size, int max_pages, int table_stride, const int* block_table) {
     if (num_pages < 0 || max_pages < 0 || !page_size_ok(page_size)) return FA_ERR_SHAPE;
@@ -1282,6 +1288,11 @@ int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlen
     if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(seqlens_k) | reinterpret_cast<uintptr_t>(tree_lens) |
          reinterpret_cast<uintptr_t>(path) | reinterpret_cast<uintptr_t>(n_accept) | reinterpret_cast<uintptr_t>(new_lens)) & 3u)
         return FA_ERR_ALIGN;
+    // a sequence's new length is written by one of its CTAs while others may still have to read what they work from
+    if (words_overlap(new_lens, B, seqlens_k, B) || words_overlap(new_lens, B, tree_lens, B) || words_overlap(new_lens, B, n_accept, B) ||
+        words_overlap(new_lens, B, path, (long long)B * T) ||
+        (block_table && words_overlap(new_lens, B, block_table, (long long)(B - 1) * table_stride + max_pages)))
+        return FA_ERR_UNSUPPORTED;
     int sms = 0;
     if (int rc = check_device(&sms)) return rc;
     fa::CompactParams cp;

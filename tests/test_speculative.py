@@ -190,3 +190,28 @@ def test_words_of_a_mask():
     see = torch.zeros(1, 40, dtype=torch.bool)
     see[0, [0, 31, 32, 39]] = True
     assert ref.bits_to_words(see).tolist() == [[1 - (1 << 31), 1 + (1 << 7)]]
+
+
+def test_compaction_refuses_new_lengths_among_its_inputs(fa):
+    """new_lens[b] is written while other CTAs may still have to read b's length, tree, path and table entries: in place, rows would
+    move at a wrong prefix.  Next to them it may lie (what is behind the check, the device, then answers)."""
+    B, T, pages = 3, 4, 2
+    buf = torch.zeros(4096, dtype=torch.int32)
+    at = (buf.data_ptr() + 15) & ~15
+    words = lambda i: at + 4 * i
+    a = dict(k=at, v=at, table=None, lens=words(100), tree_lens=words(200), path=words(300), n=words(400), new=words(500), L=1, ls=0, B=B, T=T, S=8,
+             np=4, ps=16, mp=pages, ts=pages + 3, row=256)
+    call = lambda **kw: fa.lib.fa_cache_compact(*{**a, **kw}.values(), None)
+    if torch.cuda.is_available():
+        pytest.skip("a device would take host pointers")
+    free = call()
+    assert free in (fa.FA_ERR_DEVICE, fa.FA_ERR_CUDA)
+    for name, n in (("lens", B), ("tree_lens", B), ("n", B), ("path", B * T)):
+        for new in (a[name], a[name] + 4 * (n - 1), a[name] - 4 * (B - 1)):
+            assert call(new=new) == fa.FA_ERR_UNSUPPORTED, name
+        for new in (a[name] + 4 * n, a[name] - 4 * B):
+            assert call(new=new) == free, name
+    table = words(600)
+    end = table + 4 * ((B - 1) * (pages + 3) + pages)
+    assert call(table=table, new=end - 4) == fa.FA_ERR_UNSUPPORTED and call(table=table, new=end) == free
+    assert call(tree_lens=None) == free
