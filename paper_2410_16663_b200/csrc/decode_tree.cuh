@@ -61,6 +61,7 @@ struct TreeParams {
     float* lse_part;          // [2 ctas][rows]
     int4* merges;             // what there is to merge: (sequence, item, first CTA, last CTA), one CTA: nothing
     int by_item;              // an entry for each item, where they are fewer than the CTAs; otherwise for each CTA but the first
+    int ctas;                 // of the grid
     long long mask_stride;
     int mask_words;
     int B, T, Hq, Hkv, g, Smax;
@@ -78,18 +79,25 @@ struct TreeParams {
 constexpr int kTreeItemCost = 1;
 struct TreePlan {
     int total, ctas, each, more;
-    __device__ __forceinline__ TreePlan(int total, int grid) : total(total), ctas(max(1, min(grid, total))) {
+    __host__ __device__ __forceinline__ TreePlan(int total, int grid) : total(total), ctas(grid < total ? grid : total) {
+        if (ctas < 1) ctas = 1;
         each = total / ctas;
         more = total - each * ctas;
     }
-    __device__ __forceinline__ int begin(int c) const { return c >= ctas ? total : c * each + min(c, more); }
-    __device__ __forceinline__ int owner(int unit) const {   // (of a unit that there is)
+    __host__ __device__ __forceinline__ int begin(int c) const { return c >= ctas ? total : c * each + (c < more ? c : more); }
+    __host__ __device__ __forceinline__ int owner(int unit) const {   // (of a unit that there is)
         const int big = more * (each + 1);
         return unit < big ? unit / (each + 1) : more + (unit - big) / each;
     }
 };
 __device__ __forceinline__ int tree_item_units(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile + kTreeItemCost : 0; }
 __device__ __forceinline__ int tree_seq_len(const TreeParams& p, int b) { return max(0, min(p.seqlens[b], p.Smax)); }
+
+// An entry of TreeParams::merges that says to merge something, and nothing that is not there.  A loading warp whose wait gave up leaves its
+// later entries as it found them, and the workspace may have held anything.
+__host__ __device__ __forceinline__ bool tree_merge_there(const int4& m, int B, int items, int ctas) {
+    return m.x >= 0 && m.x < B && m.y >= 0 && m.y < items && m.z >= 0 && m.z < m.w && m.w < ctas;
+}
 
 // A run of tiles of one item; n == 0: no more.
 struct TreeSegment {
@@ -648,7 +656,7 @@ __global__ void __launch_bounds__(kTreeCombineThreads, kTreeCombinePerSm<kItems>
     grid_dep_wait();
     const int4 merge = p.merges[blockIdx.y];
     const int b = merge.x, item = merge.y, c0 = merge.z, c1 = merge.w;
-    if (c1 <= c0) return;   // its only part is where it belongs
+    if (!tree_merge_there(merge, p.B, p.Hkv * p.blocks, p.ctas)) return;   // (an item's only part is where it belongs)
     const int hk = item / p.blocks, R0 = item % p.blocks * p.rows;
     const int end = min(p.rows, p.g * p.T - R0);
     for (int row = blockIdx.x * (1024 / D) + (warp / kWarpsPerRow) * 4 + (lane >> 3); row < end; row += gridDim.x * (1024 / D)) {

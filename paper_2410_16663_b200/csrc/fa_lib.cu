@@ -1023,6 +1023,7 @@ int tree_launch(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap&
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
     const int grid = (sms < fa::kTreeMaxSms ? sms : fa::kTreeMaxSms) * fa::kTreeCtasPerSm<D>;
     tp.by_item = (long long)tp.B * tp.Hkv * tp.blocks < grid ? 1 : 0;
+    tp.ctas = grid;
     cudaError_t e = fa::launch_dependent(kern, dim3(grid), threads, smem, st, tq, tk, tv, tk8, tv8, tp);
     if (e == cudaSuccess && grid > 1) {
         // one round of blocks, as many to an entry as there is room for
