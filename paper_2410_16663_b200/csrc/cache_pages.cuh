@@ -105,6 +105,14 @@ struct PagesShared {
 };
 static_assert(sizeof(PagesShared) <= 100 * 1024, "dynamic shared memory of the kernels below");
 
+// Sums of numbers of pages: all wants together may pass 32 bits (4096 sequences of a table of a million entries), and end at a
+// number that no pool has free (num_pages < kPagesNever), so that whoever comes behind is not served.
+constexpr int kPagesNever = 0x7fffffff;
+__host__ __device__ __forceinline__ int pages_add(int a, int b) {   // (of 0 .. kPagesNever)
+    const unsigned sum = (unsigned)a + (unsigned)b;
+    return sum < (unsigned)kPagesNever ? (int)sum : kPagesNever;
+}
+
 // Inclusive prefix sum of x over the threads of the CTA, and the sum of all; every thread calls this.
 __device__ __forceinline__ int pages_scan(PagesShared& s, int x, int& all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -112,7 +120,7 @@ __device__ __forceinline__ int pages_scan(PagesShared& s, int x, int& all) {
 #pragma unroll
         for (int sh = 1; sh < 32; sh <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, v, sh);
-            if (lane >= sh) v += y;
+            if (lane >= sh) v = pages_add(v, y);
         }
         return v;
     };
@@ -123,7 +131,7 @@ __device__ __forceinline__ int pages_scan(PagesShared& s, int x, int& all) {
     const int sums = scan(s.warp_sum[lane]);
     all = __shfl_sync(0xffffffffu, sums, 31);
     const int before = __shfl_sync(0xffffffffu, sums, warp > 0 ? warp - 1 : 0);
-    return warp > 0 ? before + x : x;
+    return warp > 0 ? pages_add(before, x) : x;
 }
 // Prefix sums of count(i) over i < n into s.upto.
 template <typename Count>
@@ -132,8 +140,8 @@ __device__ __forceinline__ void pages_prefix(PagesShared& s, int n, Count count)
     for (int i0 = 0; i0 < n; i0 += kPagesThreads) {
         const int i = i0 + threadIdx.x;
         const int upto = pages_scan(s, i < n ? count(i) : 0, all);
-        if (i < n) s.upto[i] = carry + upto;
-        carry += all;
+        if (i < n) s.upto[i] = pages_add(carry, upto);
+        carry = pages_add(carry, all);
     }
     __syncthreads();
 }

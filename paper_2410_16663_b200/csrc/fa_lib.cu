@@ -1332,7 +1332,7 @@ static int pages_cluster(int num_pages) {
 int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int* n_short, int B, int num_pages, int page_size,
                     int max_pages, int table_stride, void* stream) {
     if (B < 0 || num_pages < 0 || page_size <= 0 || max_pages < 0 || table_stride < max_pages) return FA_ERR_SHAPE;
-    if (B > fa::kPagesMaxItems) return FA_ERR_UNSUPPORTED;
+    if (B > fa::kPagesMaxItems || num_pages >= fa::kPagesNever) return FA_ERR_UNSUPPORTED;
     if (B == 0) return FA_OK;
     if (!block_table || !held || !refs || !want || !n_short) return FA_ERR_NULL;
     if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(held) | reinterpret_cast<uintptr_t>(refs) |
@@ -1355,7 +1355,7 @@ int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k,
     if (n < 0 || B < 0 || layers < 0 || layer_stride < 0 || num_pages < 0 || page_size <= 0 || max_pages < 0 || table_stride < max_pages || row_bytes <= 0)
         return FA_ERR_SHAPE;
     if ((long long)max_pages * page_size > 0x7fffffffll || (long long)page_size * (row_bytes / 16) > 0x3fffffffll) return FA_ERR_SHAPE;
-    if (n > fa::kPagesMaxItems || layers > 32767) return FA_ERR_UNSUPPORTED;
+    if (n > fa::kPagesMaxItems || layers > 32767 || num_pages >= fa::kPagesNever) return FA_ERR_UNSUPPORTED;
     if (n == 0) return FA_OK;
     if (!block_table || !held || !seqlens_k || !refs || !src || !dst || !n_short) return FA_ERR_NULL;
     if (layers > 0 && (!k || !v)) return FA_ERR_NULL;

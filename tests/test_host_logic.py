@@ -42,6 +42,11 @@ def test_a_merge_takes_nothing_from_its_table_that_is_not_there(tmp_path):
     run_host_check("tree_merge_check", tmp_path)
 
 
+@needs_nvcc
+def test_sums_of_wanted_pages_end_at_a_number_that_no_pool_has(tmp_path):
+    run_host_check("pages_sum_check", tmp_path)
+
+
 def test_kernels_read_nothing_through_the_non_coherent_path():
     """A kernel launched as a programmatic dependent lives while the one before it still writes, so its
     inputs are not read-only for its lifetime, which __ldg and ld.global.nc require."""

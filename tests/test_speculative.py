@@ -215,3 +215,10 @@ def test_compaction_refuses_new_lengths_among_its_inputs(fa):
     end = table + 4 * ((B - 1) * (pages + 3) + pages)
     assert call(table=table, new=end - 4) == fa.FA_ERR_UNSUPPORTED and call(table=table, new=end) == free
     assert call(tree_lens=None) == free
+
+
+def test_pages_refuse_a_pool_past_their_sums(fa):
+    buf = torch.zeros(64, dtype=torch.int32)
+    at = (buf.data_ptr() + 15) & ~15
+    assert fa.lib.fa_pages_resize(at, at, at, at, at, 1, (1 << 31) - 1, 16, 2, 2, None) == fa.FA_ERR_UNSUPPORTED
+    assert fa.lib.fa_pages_fork(at, at, at, at, at, at, at, at, at, 1, 1, 0, 2, (1 << 31) - 1, 16, 2, 2, 256, None) == fa.FA_ERR_UNSUPPORTED

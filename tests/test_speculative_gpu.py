@@ -430,6 +430,29 @@ def test_resize_many_sequences(fa):
     check_resize(fa, table, held, refs, [rng.randint(0, 64) for _ in range(B)], 16)
 
 
+def test_resize_wants_past_32_bits(fa):
+    # 4096 sequences that together want 2^31 - 2 to some more than 2^31 pages, of a pool of 3000: the first two have what they want,
+    # nobody else gets or is said to hold a page
+    if torch.cuda.mem_get_info()[0] < 24e9:
+        pytest.skip("needs 24 GB")
+    B, most, num_pages = 4096, (1 << 19) + 1024, 3000
+    table = torch.full((B, most), -1, dtype=torch.int32, device=DEV)
+    held, refs, short = ints([0] * B), ints([0] * num_pages), ints([-9])
+    for total in ((1 << 31) - 2, (1 << 31) - 1, 1 << 31, (B - 2) * most + 1200):
+        left, want = total - 1200, [1000, 200]
+        for i in range(2, B):
+            want.append(min(most, left - (B - 1 - i)))           # (everybody wants a page)
+            left -= want[-1]
+        assert sum(want) == total and min(want) > 0
+        fa.fa_pages_resize(table, held, refs, ints(want), short, 1)
+        assert short.tolist() == [B - 2]
+        assert held.tolist() == [1000, 200] + [0] * (B - 2)
+        assert table[0, :1000].tolist() == list(range(1000)) and table[1, :200].tolist() == list(range(1000, 1200))
+        assert int((table >= 0).sum()) == 1200 and refs.tolist() == [1] * 1200 + [0] * 1800
+        fa.fa_pages_resize(table, held, refs, ints([0] * B), short, 1)
+        assert short.tolist() == [0] and not refs.any()
+
+
 @pytest.mark.parametrize("page,num_pages,n", [(16, 60, 9), (1, 400, 5), (64, 17000, 3), (7, 13, 12), (128, 30, 1), (16, 150000, 40)])
 def test_fork(fa, page, num_pages, n):
     gen, rng = torch.Generator().manual_seed(page), random.Random(page)
