@@ -1205,7 +1205,7 @@ int fa_decode_ex(const fa_decode_params* p, void* stream) {
 }
 
 size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max, int d, int variant) {
-    if (B <= 0 || T <= 0 || T > kTreeMaxNodes || Hq <= 0 || Hkv <= 0 || Skv_max <= 0 || (d != 128 && d != 64)) return 0;
+    if (B <= 0 || T <= 0 || T > kTreeMaxNodes || Hq <= 0 || Hq > 65535 || Hkv <= 0 || Hq % Hkv || Skv_max <= 0 || (d != 128 && d != 64)) return 0;
     if (!tree_takes_many_rows(B, T, Hq, Hkv, Skv_max, d, variant)) return fa_decode_append_workspace_bytes(B, T, Hq, Hkv, Skv_max, d);
     const TreeBlocks tb(Hq / Hkv, T, d);
     return tb.slots(d) * tb.rows * ((size_t)d + 1) * sizeof(float) + tb.slots(d) * sizeof(int4) / 2;

@@ -1,6 +1,9 @@
 """The operators of a speculative decoding step on the host: the argument checks of the C entry points (which come before any
 CUDA call), the binding's own, and the pins of the oracle that the GPU tests compare with."""
 import ctypes
+import os
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -222,3 +225,14 @@ def test_pages_refuse_a_pool_past_their_sums(fa):
     at = (buf.data_ptr() + 15) & ~15
     assert fa.lib.fa_pages_resize(at, at, at, at, at, 1, (1 << 31) - 1, 16, 2, 2, None) == fa.FA_ERR_UNSUPPORTED
     assert fa.lib.fa_pages_fork(at, at, at, at, at, at, at, at, at, 1, 1, 0, 2, (1 << 31) - 1, 16, 2, 2, 256, None) == fa.FA_ERR_UNSUPPORTED
+
+
+def test_tree_workspace_of_heads_that_do_not_divide(fa):
+    """Sizes that the call refuses need no workspace, and asking for it ends in an answer (in a process of its own: fewer query heads
+    than kv heads would be a division by zero)."""
+    ask = "from paper_2410_16663_b200 import binding as fa\nprint([fa.fa_decode_tree_workspace_bytes(1, 4, hq, hkv, 256, 128, v) " \
+          "for hq, hkv in ((2, 4), (5, 2), (1 << 30, 1)) for v in (0, 1, 2)])"
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", ask], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0, (out.returncode, out.stderr[-500:])
+    assert out.stdout.split() == str([0] * 9).split()
