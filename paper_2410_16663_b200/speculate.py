@@ -2,7 +2,7 @@
 
 A prompt's rows are in a page pool of every layer; ``fa_pages_fork`` makes more sequences of it, which share its full pages.
 Then each step drafts a tree of tokens for every sequence and
-  1. ``fa_pages_resize``    makes room for the tree's rows,
+  1. ``fa_pages_resize``    makes room for the tree's rows (who gets none sits the step out),
   2. the model writes their keys and values and, layer by layer, ``fa_decode_tree`` attends over cache and tree,
   3. ``fa_spec_verify``     decides which tokens stand, and draws the one after them,
   4. ``fa_cache_compact``   moves the accepted rows together, in all layers,
@@ -23,33 +23,45 @@ from . import binding as fa
 
 
 class PagedCache:
-    """Page pools of all layers and the state that ``fa_pages_resize`` and ``fa_pages_fork`` keep."""
+    """Page pools of all layers and the state that ``fa_pages_resize`` and ``fa_pages_fork`` keep.  ``short`` counts the
+    sequences that were not served, over all calls.  Behind the pools' pages lies one that is nobody's."""
 
     def __init__(self, layers, pages, page, Hkv, d, sequences, rows, dtype, device):
-        self.page = page
-        self.k = torch.zeros(layers, pages, page, Hkv, d, dtype=dtype, device=device)
-        self.v = torch.zeros_like(self.k)
+        self.page, self.pages = page, pages
+        self.all_k = torch.zeros(layers, pages + 1, page, Hkv, d, dtype=dtype, device=device)
+        self.all_v = torch.zeros_like(self.all_k)
+        self.k, self.v = self.all_k[:, :pages], self.all_v[:, :pages]
         ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device=device)
         self.table = torch.full((sequences, -(-rows // page)), -1, dtype=torch.int32, device=device)
-        self.held, self.lens, self.refs, self.short = ints(sequences), ints(sequences), ints(pages), ints(1)
+        self.held, self.lens, self.refs, self.short, self.missed = ints(sequences), ints(sequences), ints(pages), ints(1), ints(1)
 
     def resize(self, rows):
-        fa.fa_pages_resize(self.table, self.held, self.refs, rows, self.short, self.page)
+        fa.fa_pages_resize(self.table, self.held, self.refs, rows, self.missed, self.page)
+        self.short += self.missed
+
+    def reserve(self, n):
+        """Room for n more rows of every sequence; returns who has it, [B] truth values."""
+        rows = self.lens + n
+        self.resize(rows)
+        return self.held * self.page >= rows
 
     def fork(self, src, dst):
-        fa.fa_pages_fork(self.k, self.v, self.table, self.held, self.lens, self.refs, src, dst, self.short)
+        fa.fa_pages_fork(self.k, self.v, self.table, self.held, self.lens, self.refs, src, dst, self.missed)
+        self.short += self.missed
 
-    def write(self, layer, first, k, v):
-        """Rows k, v [B,n,Hkv,d] of every sequence, from row first [B] on."""
+    def write(self, layer, first, k, v, served):
+        """Rows k, v [B,n,Hkv,d] of the sequences that ``served`` [B] says, from row first [B] on.  (The others' go to the page that is
+        nobody's: an index of -1 would be the pool's last page, and leaving rows out would wait for the GPU to count them.)"""
         rows = first[:, None] + torch.arange(k.shape[1], device=k.device)[None, :]
-        pages = torch.gather(self.table, 1, rows // self.page).long()
-        self.k[layer, pages, rows % self.page] = k
-        self.v[layer, pages, rows % self.page] = v
+        entries = (rows // self.page).clamp(max=self.table.shape[1] - 1)
+        pages = torch.where(served[:, None], torch.gather(self.table, 1, entries), self.pages).long()
+        self.all_k[layer, pages, rows % self.page] = k
+        self.all_v[layer, pages, rows % self.page] = v
 
-    def compact(self, path, n_accept):
+    def compact(self, path, n_accept, tree_lens):
         """The accepted rows of each sequence's tree, which end its cache, move together; the lengths follow."""
         new = torch.empty_like(self.lens)
-        fa.fa_cache_compact(self.k, self.v, self.lens, path, n_accept, new, block_table=self.table)
+        fa.fa_cache_compact(self.k, self.v, self.lens, path, n_accept, new, tree_lens=tree_lens, block_table=self.table)
         self.lens = new
 
 
@@ -72,18 +84,21 @@ class Model:
 
 def step(model, cache, tokens, parents, draft, gen, ws):
     """One step: tokens, parents int32 [B,T], draft [B,T,V] the draft's distributions after each node.  Returns (out_tokens, n_accept,
-    the target's distributions)."""
+    the target's distributions).  A sequence for whose tree the pool has no pages keeps its rows and says nothing: its out_tokens
+    are -1 and its n_accept is 0."""
     B, T = tokens.shape
-    cache.resize(cache.lens + T)                                   # room for the tree
+    served = cache.reserve(T)                                      # room for the tree
     first = cache.lens
-    cache.lens = cache.lens + T
+    live = torch.where(served, T, 0).to(torch.int32)
+    cache.lens = cache.lens + live
     mask = fa.tree_mask(parents)
     x = model.embed[tokens.long()]
     for layer in range(len(model.w)):
         q, k, v = model.project(x, layer)
-        cache.write(layer, first, k, v)
+        cache.write(layer, first, k, v, served)
         o = torch.empty_like(q)
-        fa.fa_decode_tree(q, cache.k[layer], cache.v[layer], o, None, cache.lens, mask, 1.0 / math.sqrt(model.d), ws, block_table=cache.table)
+        fa.fa_decode_tree(q, cache.k[layer], cache.v[layer], o, None, cache.lens, mask, 1.0 / math.sqrt(model.d), ws, tree_lens=live,
+                          block_table=cache.table)
         x = x + o.view(B, T, -1)
     target = model.probabilities(x)
     dev = tokens.device
@@ -91,10 +106,10 @@ def step(model, cache, tokens, parents, draft, gen, ws):
     path, out = torch.empty(B, T, dtype=torch.int32, device=dev), torch.empty(B, T, dtype=torch.int32, device=dev)
     uniforms = torch.rand(B, T, device=dev, generator=gen)
     noise = torch.empty(B, target.shape[-1], device=dev).exponential_(generator=gen).clamp_(min=1e-20)
-    fa.fa_spec_verify(target, draft, tokens, parents, uniforms, noise, n_accept, path, out)
-    cache.compact(path, n_accept)                                  # the accepted rows, in all layers
+    fa.fa_spec_verify(target, draft, tokens, parents, uniforms, noise, n_accept, path, out, tree_lens=live)
+    cache.compact(path, n_accept, live)                            # the accepted rows, in all layers
     cache.resize(cache.lens)                                       # and the pages behind them
-    return out, n_accept, target
+    return torch.where(served[:, None], out, -1), torch.where(served, n_accept, 0), target
 
 
 def random_trees(B, T, gen, device):
@@ -138,7 +153,8 @@ def run(samples=4, prompt=1000, nodes=24, steps=4, layers=4, Hq=8, Hkv=2, d=128,
         tokens = torch.multinomial(draft.view(-1, vocab), 1, generator=gen).view(samples, nodes)
         tokens[:, :1] = last
         out, n_accept, _ = step(model, cache, tokens.to(torch.int32), random_trees(samples, nodes, gen, device), draft, gen, ws)
-        last = torch.gather(out, 1, n_accept[:, None].long())       # the token after the last that stands
+        new = torch.gather(out, 1, n_accept[:, None].long())        # the token after the last that stands
+        last = torch.where(new >= 0, new, last)
         said.append((out, n_accept))
     return said, cache
 
