@@ -7,8 +7,8 @@ Then each step drafts a tree of tokens for every sequence and
   3. ``fa_spec_verify``     decides which tokens stand, and draws the one after them,
   4. ``fa_cache_compact``   moves the accepted rows together, in all layers,
   5. ``fa_pages_resize``    gives back the pages past the new length.
-The model here is a stand-in of random weights (one matrix per layer for each of Q, K and V, and the vocabulary's), and so is
-the draft, which is the target's distribution with noise.  Nothing in a step waits for the GPU.
+The model here is a stand-in of random weights (embeddings, one matrix per layer for each of Q, K and V, and one for the vocabulary),
+and so is the draft, which is the same model without the attention and with noise.  Nothing in a step waits for the GPU.
 
   python -m paper_2410_16663_b200.speculate --samples 8 --prompt 1000 --nodes 24 --steps 5
 """
@@ -66,20 +66,22 @@ class PagedCache:
 
 
 class Model:
-    """A stand-in: embeddings, a matrix for each of Q, K and V per layer, and the vocabulary's matrix again at the end."""
+    """A stand-in: embeddings, a matrix for each of Q, K and V per layer, and one for the vocabulary at the end.  (Not the embeddings
+    again: a token of a random model would then be followed by itself, with certainty.)"""
 
     def __init__(self, layers, Hq, Hkv, d, vocab, dtype, device, gen):
         new = lambda *s: torch.empty(*s, dtype=dtype, device=device).normal_(0.0, 1.0, generator=gen)
         self.Hq, self.Hkv, self.d, width = Hq, Hkv, d, Hq * d
         self.embed = new(vocab, width)
         self.w = [[new(width, h * d) / math.sqrt(width) for h in (Hq, Hkv, Hkv)] for _ in range(layers)]
+        self.head = new(vocab, width)
 
     def project(self, x, layer):
         return [(x @ w).view(*x.shape[:2], -1, self.d) for w in self.w[layer]]
 
     def probabilities(self, x):
         x = x / x.float().square().mean(-1, keepdim=True).sqrt().to(x.dtype)
-        return torch.softmax((x @ self.embed.T).float() / math.sqrt(x.shape[-1]) * 3.0, -1)
+        return torch.softmax((x @ self.head.T).float() / math.sqrt(x.shape[-1]) * 3.0, -1)
 
 
 def step(model, cache, tokens, parents, draft, gen, ws):
@@ -120,6 +122,24 @@ def random_trees(B, T, gen, device):
     return torch.where(node == 0, -1, torch.minimum(up, (node - 1).clamp(min=0))).to(torch.int32)
 
 
+def draft_trees(model, last, parents, gen):
+    """A tree of drafted tokens for every sequence: node 0 is the token ``last`` [B,1], every other node is drawn from the draft's
+    distribution after its parent.  Returns tokens int32 [B,T] and the distributions [B,T,V]."""
+    B, T = parents.shape
+    tokens, row = last.repeat(1, T), torch.arange(B, device=last.device)
+
+    def after(x):
+        x = model.embed[x]
+        return model.probabilities(x + torch.empty_like(x).normal_(0.0, 0.3, generator=gen))
+
+    draft = [after(last[:, 0])]
+    for i in range(1, T):
+        up = torch.stack(draft, 1)[row, parents[:, i].long()]
+        tokens[:, i] = torch.multinomial(up, 1, generator=gen)[:, 0]
+        draft.append(after(tokens[:, i]))
+    return tokens.to(torch.int32), torch.stack(draft, 1)
+
+
 def run(samples=4, prompt=1000, nodes=24, steps=4, layers=4, Hq=8, Hkv=2, d=128, vocab=4096, page=16, dtype=torch.bfloat16, seed=0,
         device="cuda"):
     """Forks ``samples`` sequences off one prompt and decodes ``steps`` steps of each.  Returns (emitted tokens per step and
@@ -147,12 +167,9 @@ def run(samples=4, prompt=1000, nodes=24, steps=4, layers=4, Hq=8, Hkv=2, d=128,
     last = torch.randint(0, vocab, (samples, 1), device=device, generator=gen)
     said = []
     for _ in range(steps):
-        # the draft: one distribution for all of a sequence's nodes, near what the target says after the last token
-        x = model.embed[last.long()]
-        draft = model.probabilities(x + torch.empty_like(x).normal_(0.0, 0.3, generator=gen)).expand(samples, nodes, vocab).contiguous()
-        tokens = torch.multinomial(draft.view(-1, vocab), 1, generator=gen).view(samples, nodes)
-        tokens[:, :1] = last
-        out, n_accept, _ = step(model, cache, tokens.to(torch.int32), random_trees(samples, nodes, gen, device), draft, gen, ws)
+        parents = random_trees(samples, nodes, gen, device)
+        tokens, draft = draft_trees(model, last, parents, gen)
+        out, n_accept, _ = step(model, cache, tokens, parents, draft, gen, ws)
         new = torch.gather(out, 1, n_accept[:, None].long())        # the token after the last that stands
         last = torch.where(new >= 0, new, last)
         said.append((out, n_accept))

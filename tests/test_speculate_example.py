@@ -117,3 +117,65 @@ def test_a_loop_of_a_pool_that_is_too_small(loop):
         said = [s + int((o >= 0).sum()) for s, o in zip(said, out)]
     assert cache.lens.tolist() == [5 + s for s in said] and max(said) >= 5 and int(cache.short) > 0
     assert int(cache.refs.max()) == 1 and int(cache.refs.sum()) == int(cache.held.sum())
+
+
+# ------------------------------------------------------------------ what the example's check of its cache can see
+SAMPLES, PROMPT, NODES, STEPS, PAGE = 5, 41, 13, 5, 16
+
+
+def run_and_check(loop, check):
+    said, cache = loop.run(SAMPLES, PROMPT, NODES, STEPS, layers=2, Hq=4, Hkv=2, d=16, vocab=64, page=PAGE, dtype=torch.float32, device="cpu")
+    model = loop.Model(2, 4, 2, 16, 64, torch.float32, "cpu", torch.Generator().manual_seed(0))
+    return said, cache, check(said, cache, model, PROMPT)
+
+
+def rows_that_differ(said, cache, model, prompt):
+    """Rows of layer 0's keys, which depend on the tokens alone, that are not those of the tokens that stand."""
+    bad = 0
+    for b in range(len(said[0][1])):
+        tokens = []
+        for i, (out, n) in enumerate(said):
+            tokens += [int(said[i - 1][0][b, int(said[i - 1][1][b])]) if i else None] + out[b, :int(n[b])].tolist()
+        known = [i for i, t in enumerate(tokens) if t is not None]
+        got = ref.gather_rows(cache.k[0], cache.table, b, int(cache.lens[b]))[prompt:]
+        assert len(got) == len(tokens)
+        want = model.project(model.embed[torch.tensor([tokens[i] for i in known])][None], 0)[1][0]
+        bad += int(((got[known] - want).abs().amax((1, 2)) > 1e-3).sum())
+    return bad
+
+
+def test_the_loop_accepts_rejects_and_moves(loop):
+    """A loop whose every token is the same, or whose drafts all stand, would show nothing of verification and compaction."""
+    said, cache, bad = run_and_check(loop, rows_that_differ)
+    assert bad == 0 and int(cache.short) == 0
+    lib = loop.fa
+    accepted = torch.stack([n for _, n in lib.log])
+    assert (accepted == 0).any() and (accepted >= 2).any() and 0.3 < float(accepted.float().mean()) < NODES / 2
+    moved = sum(int(path[b, i]) > i for path, n in lib.log for b in range(SAMPLES) for i in range(1, int(n[b]) + 1))
+    assert moved >= 10
+    for b in range(SAMPLES):
+        assert len({t for out, n in said for t in out[b, :int(n[b]) + 1].tolist()}) >= 5
+
+
+@pytest.mark.parametrize("mistake", ["nothing moves", "the next row", "a path backwards"])
+def test_the_check_of_the_cache_sees_a_compaction_that_is_wrong(loop, monkeypatch, mistake):
+    right = ref.compact
+
+    def wrong(k, v, lens, path, n, tree_lens=None, table=None, T=None):
+        if mistake == "nothing moves":
+            return right(k.clone(), v.clone(), lens, path, n, tree_lens, table, T)
+        if mistake == "the next row":
+            return right(k, v, lens, [[min(int(x) + (i > 0), T - 1) for i, x in enumerate(row)] for row in path], n, tree_lens, table, T)
+        return right(k, v, lens, [[int(row[0])] + [int(x) for x in row[1:1 + int(m)]][::-1] + [-1] * (T - 1 - int(m)) for row, m in zip(path, n)], n, tree_lens, table, T)
+
+    monkeypatch.setattr(ref, "compact", wrong)
+    assert run_and_check(loop, rows_that_differ)[2] > 0
+
+
+def test_the_example_model_is_not_certain(loop):
+    """At the sizes of the GPU test: what follows a token is spread over several, and another for another token."""
+    gen = torch.Generator().manual_seed(0)
+    model = loop.Model(2, 8, 2, 128, 512, torch.bfloat16, "cpu", gen)
+    p = model.probabilities(model.embed[torch.arange(64)])
+    assert float(p.amax(-1).mean()) < 0.6 and float((p * p).sum(-1).reciprocal().mean()) > 3
+    assert int((p.argmax(-1) == torch.arange(64)).sum()) <= 4 and p.argmax(-1).unique().numel() > 30

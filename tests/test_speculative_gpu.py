@@ -588,3 +588,35 @@ def test_steps_of_a_serving_loop(fa):
         x = model.embed[torch.tensor([tokens[i] for i in known], device=DEV)][None]
         want = model.project(x, 0)[1][0]
         assert torch.allclose(got[known].float(), want.float(), rtol=2e-2, atol=2e-2)
+
+
+def test_steps_of_a_serving_loop_that_rejects_and_moves(fa, monkeypatch):
+    """The example's loop once more, with what its calls decided: drafts are rejected and stand, accepted rows move, every sequence says
+    several tokens, and layer 0's keys and values are those of the tokens that stand."""
+    from paper_2410_16663_b200 import speculate
+    log, compact = [], fa.fa_cache_compact
+
+    def logged(k, v, lens, path, n, new, **kw):
+        log.append((path.clone(), n.clone()))
+        return compact(k, v, lens, path, n, new, **kw)
+
+    monkeypatch.setattr(fa, "fa_cache_compact", logged)
+    samples, prompt, nodes, steps, page = 5, 333, 13, 6, 16
+    said, cache = speculate.run(samples, prompt, nodes, steps, layers=2, vocab=512, page=page, seed=1)
+    assert fa.fa_device_status()[0] == 0 and int(cache.short) == 0
+    accepted = torch.stack([n for _, n in log])
+    assert (accepted == 0).any() and (accepted >= 2).any()
+    assert sum(int(path[b, i]) > i for path, n in log for b in range(samples) for i in range(1, int(n[b]) + 1)) >= 10
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(1)
+    model = speculate.Model(2, 8, 2, 128, 512, torch.bfloat16, DEV, gen)
+    for b in range(samples):
+        tokens = []
+        for i, (out, n) in enumerate(said):
+            tokens += [int(said[i - 1][0][b, int(said[i - 1][1][b])]) if i else -1] + out[b, :int(n[b])].tolist()
+        assert len(set(tokens)) >= 5
+        rows = torch.arange(prompt + 1, int(cache.lens[b]), device=DEV)
+        x = model.embed[torch.tensor(tokens[1:], device=DEV)][None]
+        for pool, part in ((cache.k, 1), (cache.v, 2)):
+            got = pool[0, cache.table[b, rows // page].long(), rows % page]
+            assert torch.allclose(got.float(), model.project(x, 0)[part][0].float(), rtol=2e-2, atol=2e-2)
