@@ -331,9 +331,11 @@ def _table(what: str, t) -> int:
 
 def tree_mask(parents):
     """The mask of ``fa_decode_tree`` for trees given by their parents, int32 [B,T] (or [T]; parents[i] < i, -1 for the root): each
-    node sees itself and the nodes above it.  Made with torch operations on the parents' device, once per step."""
+    node sees itself and the nodes above it.  A number outside [0, i) is no parent, as for ``fa_spec_verify`` (entries past a tree's
+    length may hold anything).  Made with torch operations on the parents' device, once per step."""
     T = parents.shape[-1]
     up = parents.long()
+    up = torch.where(up < torch.arange(T, device=up.device), up, -1)
     see = torch.eye(T, dtype=torch.bool, device=parents.device).expand(*up.shape, T).clone()
     hop = up.clamp(min=0).unsqueeze(-1)
     for _ in range(max(1, (T - 1).bit_length())):   # what a node's ancestor sees, twice as far up each time

@@ -236,3 +236,16 @@ def test_tree_workspace_of_heads_that_do_not_divide(fa):
     out = subprocess.run([sys.executable, "-c", ask], cwd=root, capture_output=True, text=True, timeout=300)
     assert out.returncode == 0, (out.returncode, out.stderr[-500:])
     assert out.stdout.split() == str([0] * 9).split()
+
+
+def test_mask_of_parents_that_are_none(fa):
+    """Entries past a tree's length may hold anything: no index outside the tree is followed, nor a node that comes later."""
+    for T in (1, 5, 33, 70):
+        parents = [-1] + [(i - 1) // 2 for i in range(1, T)]
+        assert torch.equal(fa.tree_mask(torch.tensor(parents, dtype=torch.int32)), ref.bits_to_words(ref.ancestors(parents)))
+        for none in (T, T - 1, T + 7, (1 << 31) - 1, -(1 << 31), -2):
+            odd = parents[:T // 2] + [none] * (T - T // 2)
+            clean = parents[:T // 2] + [none if 0 <= none < i else -1 for i in range(T // 2, T)]
+            want = ref.bits_to_words(ref.ancestors(clean))
+            assert torch.equal(fa.tree_mask(torch.tensor(odd, dtype=torch.int32)), want)
+            assert torch.equal(fa.tree_mask(torch.tensor([parents, odd], dtype=torch.int32))[1], want)
