@@ -297,7 +297,8 @@ def fa_decode_ex(q, k, v, o, lse, seqlens_k, scale: float, workspace, block_tabl
     return _check(rc, "fa_decode_ex", raise_on_error)
 
 
-# The checks of the calls below: what the library cannot see of its pointers.  (A step's calls are short, and bound by what the host
+# The checks of the calls below: what the library cannot see of its pointers.  Types, layouts and sizes, as a tensor that is too
+# small would be read or written past its end; vectors [B] may be longer than the batch.  (A step's calls are short, and bound by what the host
 # does for them: a call first asks in one expression whether all is well, and looks for what is wrong only if not; parameter
 # blocks are packed, not filled field by field.  fa_decode_tree 6.7 -> 3.8 us before the library, fa_cache_compact 10.3 -> 5.7.)
 _INT, _HALF, _BF16, _FLOAT = torch.int32, torch.float16, torch.bfloat16, torch.float32
@@ -316,9 +317,10 @@ def _int32(what: str, *tensors) -> None:
             raise ValueError(f"{what}: index tensors are int32, not {t.dtype}")
 
 
-def _good(t) -> bool:
-    """An index tensor as the library reads it, or none."""
-    return t is None or (t.dtype is _INT and t.is_contiguous())
+def _shapes(what: str, **tensors) -> None:
+    """The call's tensors do not go together: says how."""
+    given = ", ".join(f"{name} {tuple(t.shape)}" for name, t in tensors.items() if t is not None)
+    raise ValueError(f"{what}: shapes that do not go together, {given}")
 
 
 def _table(what: str, t) -> int:
@@ -362,24 +364,32 @@ def fa_decode_tree(q, k, v, o, lse, seqlens_k, mask, scale: float, workspace, tr
     dt = q.dtype
     if not (k.dtype is dt and v.dtype is dt and o.dtype is dt and (dt is _HALF or dt is _BF16)):
         raise ValueError("fa_decode_tree: q, k, v and o share one 16-bit type")
-    if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous() and _good(seqlens_k) and _good(mask) and _good(tree_lens)
+    if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous() and seqlens_k.dtype is _INT
+            and seqlens_k.is_contiguous() and mask.dtype is _INT and mask.is_contiguous()
+            and (tree_lens is None or (tree_lens.dtype is _INT and tree_lens.is_contiguous()))
             and (lse is None or (lse.is_contiguous() and lse.dtype is _FLOAT))):
         _contiguous("fa_decode_tree", q, k, v, o, lse, seqlens_k, mask, tree_lens)
         _int32("fa_decode_tree", seqlens_k, mask, tree_lens)
         raise ValueError("fa_decode_tree: lse is float32")
-    B, T, Hq, d = q.shape
-    slabs, rows, Hkv, _ = k.shape
+    B, T, Hq, d = shape = q.shape
+    slabs, rows, Hkv, width = cache = k.shape
     seen = mask.shape
     if seen != (B, T, (T + 31) // 32) and seen != (T, (T + 31) // 32):
         raise ValueError(f"fa_decode_tree: a mask of shape {tuple(seen)} for T = {T}")
     if block_table is None:
-        sizes = (rows, d, _FA16[dt], 0, 0, 0, 0)
+        tables, sizes = slabs, (rows, d, _FA16[dt], 0, 0, 0, 0)
     else:
-        sizes = (0, d, _FA16[dt], slabs, rows, block_table.shape[1] if max_pages is None else max_pages, _table("fa_decode_tree", block_table))
-    p = _TREE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), _ptr(lse), seqlens_k.data_ptr(), _ptr(tree_lens), mask.data_ptr(),
-                   _ptr(block_table), B, T, Hq, Hkv, *sizes, variant, 0 if len(seen) == 2 else T * seen[2], scale, _ptr(workspace),
-                   0 if workspace is None else workspace.numel() * workspace.element_size())
-    return _check(lib.fa_decode_tree(p, _stream()), "fa_decode_tree", raise_on_error)
+        tables, pages = block_table.shape
+        sizes = (0, d, _FA16[dt], slabs, rows, pages if max_pages is None else max_pages, _table("fa_decode_tree", block_table))
+    if not (o.shape == shape and v.shape == cache and width == d and tables >= B and seqlens_k.numel() >= B
+            and (tree_lens is None or tree_lens.numel() >= B) and (lse is None or lse.numel() >= B * Hq * T)):
+        _shapes("fa_decode_tree", q=q, o=o, k=k, v=v, seqlens_k=seqlens_k, tree_lens=tree_lens, lse=lse, block_table=block_table)
+    p = _TREE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), 0 if lse is None else lse.data_ptr(), seqlens_k.data_ptr(),
+                   0 if tree_lens is None else tree_lens.data_ptr(), mask.data_ptr(), 0 if block_table is None else block_table.data_ptr(),
+                   B, T, Hq, Hkv, *sizes, variant, 0 if len(seen) == 2 else T * seen[2], scale,
+                   0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
+    rc = lib.fa_decode_tree(p, _stream())
+    return _check(rc, "fa_decode_tree", raise_on_error) if rc else rc
 
 
 def fa_spec_verify(target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens=None,
@@ -392,14 +402,20 @@ def fa_spec_verify(target_probs, draft_probs, tokens, parents, uniforms, noise, 
     if uniforms.dtype is not _FLOAT or noise.dtype is not _FLOAT:
         raise ValueError("fa_spec_verify: random numbers are float32")
     if not (target_probs.is_contiguous() and (draft_probs is None or draft_probs.is_contiguous()) and uniforms.is_contiguous() and noise.is_contiguous()
-            and _good(tokens) and _good(parents) and _good(n_accept) and _good(path) and _good(out_tokens) and _good(tree_lens)):
+            and tokens.dtype is _INT and tokens.is_contiguous() and parents.dtype is _INT and parents.is_contiguous() and path.dtype is _INT
+            and path.is_contiguous() and out_tokens.dtype is _INT and out_tokens.is_contiguous() and n_accept.dtype is _INT
+            and n_accept.is_contiguous() and (tree_lens is None or (tree_lens.dtype is _INT and tree_lens.is_contiguous()))):
         _contiguous("fa_spec_verify", target_probs, draft_probs, tokens, parents, uniforms, noise, n_accept, path, out_tokens, tree_lens)
         _int32("fa_spec_verify", tokens, parents, n_accept, path, out_tokens, tree_lens)
-    B, T, V = target_probs.shape
-    rc = lib.fa_spec_verify(target_probs.data_ptr(), _ptr(draft_probs), tokens.data_ptr(), parents.data_ptr(), _ptr(tree_lens),
-                            uniforms.data_ptr(), noise.data_ptr(), n_accept.data_ptr(), path.data_ptr(), out_tokens.data_ptr(), B, T, V,
-                            _FA_PROBS[dt], _stream())
-    return _check(rc, "fa_spec_verify", raise_on_error)
+    B, T, V = shape = target_probs.shape
+    if not (tokens.numel() == parents.numel() == uniforms.numel() == path.numel() == out_tokens.numel() == B * T and noise.numel() == B * V
+            and n_accept.numel() >= B and (draft_probs is None or draft_probs.shape == shape) and (tree_lens is None or tree_lens.numel() >= B)):
+        _shapes("fa_spec_verify", target_probs=target_probs, draft_probs=draft_probs, tokens=tokens, parents=parents, uniforms=uniforms, noise=noise,
+                n_accept=n_accept, path=path, out_tokens=out_tokens, tree_lens=tree_lens)
+    rc = lib.fa_spec_verify(target_probs.data_ptr(), 0 if draft_probs is None else draft_probs.data_ptr(), tokens.data_ptr(), parents.data_ptr(),
+                            0 if tree_lens is None else tree_lens.data_ptr(), uniforms.data_ptr(), noise.data_ptr(), n_accept.data_ptr(),
+                            path.data_ptr(), out_tokens.data_ptr(), B, T, V, _FA_PROBS[dt], _stream())
+    return _check(rc, "fa_spec_verify", raise_on_error) if rc else rc
 
 
 def _planes(what: str, k, v):
@@ -420,17 +436,22 @@ def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, 
     them; writes new_lens int32 [B]."""
     layers, slabs, rows, stride, row = _planes("fa_cache_compact", k, v)
     if not (seqlens_k.dtype is _INT and path.dtype is _INT and n_accept.dtype is _INT and new_lens.dtype is _INT and path.is_contiguous()
-            and seqlens_k.is_contiguous() and n_accept.is_contiguous() and new_lens.is_contiguous() and (tree_lens is None or _good(tree_lens))):
+            and seqlens_k.is_contiguous() and n_accept.is_contiguous() and new_lens.is_contiguous()
+            and (tree_lens is None or (tree_lens.dtype is _INT and tree_lens.is_contiguous()))):
         _contiguous("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
         _int32("fa_cache_compact", seqlens_k, path, n_accept, new_lens, tree_lens)
     B, T = path.shape
     if block_table is None:
-        args = (rows, 0, 0, 0, 0)
+        tables, args = slabs, (rows, 0, 0, 0, 0)
     else:
-        args = (0, slabs, rows, block_table.shape[1] if max_pages is None else max_pages, _table("fa_cache_compact", block_table))
-    rc = lib.fa_cache_compact(k.data_ptr(), v.data_ptr(), _ptr(block_table), seqlens_k.data_ptr(), _ptr(tree_lens), path.data_ptr(),
-                              n_accept.data_ptr(), new_lens.data_ptr(), layers, stride, B, T, *args, row, _stream())
-    return _check(rc, "fa_cache_compact", raise_on_error)
+        tables, pages = block_table.shape
+        args = (0, slabs, rows, pages if max_pages is None else max_pages, _table("fa_cache_compact", block_table))
+    if not (tables >= B and seqlens_k.numel() >= B and n_accept.numel() >= B and new_lens.numel() >= B and (tree_lens is None or tree_lens.numel() >= B)):
+        _shapes("fa_cache_compact", k=k, path=path, seqlens_k=seqlens_k, n_accept=n_accept, new_lens=new_lens, tree_lens=tree_lens, block_table=block_table)
+    rc = lib.fa_cache_compact(k.data_ptr(), v.data_ptr(), 0 if block_table is None else block_table.data_ptr(), seqlens_k.data_ptr(),
+                              0 if tree_lens is None else tree_lens.data_ptr(), path.data_ptr(), n_accept.data_ptr(), new_lens.data_ptr(),
+                              layers, stride, B, T, *args, row, _stream())
+    return _check(rc, "fa_cache_compact", raise_on_error) if rc else rc
 
 
 def fa_pages_resize(block_table, held, refs, want, n_short, page_size: int, raise_on_error: bool = True) -> int:
@@ -441,25 +462,31 @@ def fa_pages_resize(block_table, held, refs, want, n_short, page_size: int, rais
         _contiguous("fa_pages_resize", held, refs, want, n_short)
         _int32("fa_pages_resize", held, refs, want, n_short)
     B, pages = block_table.shape
+    if not (held.numel() >= B and want.numel() >= B and n_short.numel() >= 1):
+        _shapes("fa_pages_resize", block_table=block_table, held=held, want=want, n_short=n_short)
     rc = lib.fa_pages_resize(block_table.data_ptr(), held.data_ptr(), refs.data_ptr(), want.data_ptr(), n_short.data_ptr(), B, refs.numel(),
                              page_size, pages, _table("fa_pages_resize", block_table), _stream())
-    return _check(rc, "fa_pages_resize", raise_on_error)
+    return _check(rc, "fa_pages_resize", raise_on_error) if rc else rc
 
 
 def fa_pages_fork(k, v, block_table, held, seqlens_k, refs, src, dst, n_short, raise_on_error: bool = True) -> int:
     """``fa_pages_fork``: pools k, v [L,num_pages,page_size,Hkv,d] with the state of ``fa_pages_resize`` and seqlens_k int32
     [B]; sequence dst[i] becomes a copy of src[i] (int32 [n] each); n_short int32 [1] counts the pairs that got no page."""
     layers, slabs, rows, stride, row = _planes("fa_pages_fork", k, v)
-    if not (_good(held) and _good(seqlens_k) and _good(refs) and _good(src) and _good(dst) and _good(n_short)):
+    if not (held.dtype is _INT and held.is_contiguous() and seqlens_k.dtype is _INT and seqlens_k.is_contiguous() and refs.dtype is _INT
+            and refs.is_contiguous() and src.dtype is _INT and src.is_contiguous() and dst.dtype is _INT and dst.is_contiguous()
+            and n_short.dtype is _INT and n_short.is_contiguous()):
         _contiguous("fa_pages_fork", held, seqlens_k, refs, src, dst, n_short)
         _int32("fa_pages_fork", held, seqlens_k, refs, src, dst, n_short)
     if refs.numel() != slabs:
         raise ValueError("fa_pages_fork: refs has an entry for each of the pool's pages")
     B, pages = block_table.shape
+    if not (held.numel() >= B and seqlens_k.numel() >= B and src.numel() == dst.numel() and n_short.numel() >= 1):
+        _shapes("fa_pages_fork", block_table=block_table, held=held, seqlens_k=seqlens_k, src=src, dst=dst, n_short=n_short)
     rc = lib.fa_pages_fork(k.data_ptr(), v.data_ptr(), block_table.data_ptr(), held.data_ptr(), seqlens_k.data_ptr(), refs.data_ptr(),
                            src.data_ptr(), dst.data_ptr(), n_short.data_ptr(), src.numel(), layers, stride, B, slabs, rows, pages,
                            _table("fa_pages_fork", block_table), row, _stream())
-    return _check(rc, "fa_pages_fork", raise_on_error)
+    return _check(rc, "fa_pages_fork", raise_on_error) if rc else rc
 
 
 def fa_decode_append_workspace_bytes(B: int, Sq: int, Hq: int, Hkv: int, Skv_max: int, d: int) -> int:

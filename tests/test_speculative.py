@@ -249,3 +249,60 @@ def test_mask_of_parents_that_are_none(fa):
             want = ref.bits_to_words(ref.ancestors(clean))
             assert torch.equal(fa.tree_mask(torch.tensor(odd, dtype=torch.int32)), want)
             assert torch.equal(fa.tree_mask(torch.tensor([parents, odd], dtype=torch.int32))[1], want)
+
+
+class Recorder:
+    """Takes the place of the library: what the binding passes on."""
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.last = (name, args)
+            return 0
+        return call
+
+
+@pytest.fixture
+def calls(fa, monkeypatch):
+    recorder = Recorder()
+    monkeypatch.setattr(fa, "lib", recorder)
+    monkeypatch.setattr(fa, "_stream", lambda: 0)
+    return recorder
+
+
+def refused(call, right, **wrong):
+    """``right`` goes through; every replacement of one argument is refused before anything is passed on."""
+    call(**right)
+    for name, values in wrong.items():
+        for value in values:
+            with pytest.raises(ValueError):
+                call(**{**right, name: value})
+
+
+def test_binding_refuses_sizes_that_do_not_go_together(fa, calls):
+    """A tensor that is smaller than the call takes it for would be read or written past its end."""
+    half, i32, f32 = (lambda *s, t=t: torch.zeros(*s, dtype=t) for t in (torch.float16, torch.int32, torch.float32))
+    B, T, Hq, Hkv, d, S = 3, 5, 4, 2, 64, 20
+    tree = dict(q=half(B, T, Hq, d), k=half(B, S, Hkv, d), v=half(B, S, Hkv, d), o=half(B, T, Hq, d), lse=f32(B, Hq, T), seqlens_k=i32(B),
+                mask=i32(B, T, 1), scale=0.1, workspace=None, tree_lens=i32(B))
+    refused(fa.fa_decode_tree, tree, k=[half(B, S, Hkv, 128), half(B, S + 1, Hkv, d)], v=[half(B, S, Hkv, 128), half(B, S, 1, d), half(B - 1, S, Hkv, d)],
+            o=[half(B, T, Hq, 128), half(B, T - 1, Hq, d)], lse=[f32(B, Hq, T - 1)], seqlens_k=[i32(B - 1)], tree_lens=[i32(1)])
+    few = {**tree, "k": half(B - 1, S, Hkv, d), "v": half(B - 1, S, Hkv, d)}        # fewer caches than sequences
+    with pytest.raises(ValueError):
+        fa.fa_decode_tree(**few)
+    paged = {**few, "block_table": i32(B, 2)}
+    refused(fa.fa_decode_tree, paged, block_table=[i32(B - 1, 2)])
+    fa.fa_decode_tree(**{**tree, "seqlens_k": i32(B + 4), "tree_lens": None, "lse": None})          # vectors may be longer
+    p = f32(B, T, 9)
+    verify = dict(target_probs=p, draft_probs=p, tokens=i32(B, T), parents=i32(B, T), uniforms=f32(B, T), noise=f32(B, 9), n_accept=i32(B), path=i32(B, T),
+                  out_tokens=i32(B, T), tree_lens=i32(B))
+    less = [i32(B, T - 1), i32(B - 1, T), i32(B, T + 1)]
+    refused(fa.fa_spec_verify, verify, draft_probs=[f32(B, T, 8), f32(B, T - 1, 9), f32(1, T, 9)], tokens=less, parents=less, path=less, out_tokens=less,
+            uniforms=[f32(B, T - 1)], noise=[f32(B, 8), f32(1, 9)], n_accept=[i32(B - 1)], tree_lens=[i32(B - 1)])
+    kv = half(2, B, S, Hkv, d)
+    compact = dict(k=kv, v=kv, seqlens_k=i32(B), path=i32(B, T), n_accept=i32(B), new_lens=i32(B), tree_lens=i32(B))
+    refused(fa.fa_cache_compact, compact, path=[i32(B + 1, T)], seqlens_k=[i32(B - 1)], n_accept=[i32(B - 1)], new_lens=[i32(B - 1)], tree_lens=[i32(B - 1)],
+            block_table=[i32(B - 1, 2)])
+    refused(fa.fa_pages_resize, dict(block_table=i32(B, 4), held=i32(B), refs=i32(7), want=i32(B), n_short=i32(1), page_size=16), held=[i32(B - 1)],
+            want=[i32(B - 1)], n_short=[i32(0)])
+    refused(fa.fa_pages_fork, dict(k=kv, v=kv, block_table=i32(4, 4), held=i32(4), seqlens_k=i32(4), refs=i32(B), src=i32(2), dst=i32(2), n_short=i32(1)),
+            held=[i32(3)], seqlens_k=[i32(3)], src=[i32(1)], dst=[i32(1)], n_short=[i32(0)], refs=[i32(B + 1)])
