@@ -7,6 +7,7 @@ missing or fails to load, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import struct
 
@@ -426,7 +427,10 @@ def _planes(what: str, k, v):
     if not k.is_contiguous():
         _contiguous(what, k[0])
     size = k.element_size()
-    return shape[0], shape[1], shape[2], stride[0] * size, stride[2] * size
+    # (the stride of an extent of 1 may be any number)
+    layer = stride[0] if shape[0] > 1 else 0
+    row = stride[2] if shape[2] > 1 else math.prod(shape[3:])
+    return shape[0], shape[1], shape[2], layer * size, row * size
 
 
 def fa_cache_compact(k, v, seqlens_k, path, n_accept, new_lens, tree_lens=None, block_table=None, max_pages: int = None,

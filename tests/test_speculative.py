@@ -306,3 +306,17 @@ def test_binding_refuses_sizes_that_do_not_go_together(fa, calls):
             want=[i32(B - 1)], n_short=[i32(0)])
     refused(fa.fa_pages_fork, dict(k=kv, v=kv, block_table=i32(4, 4), held=i32(4), seqlens_k=i32(4), refs=i32(B), src=i32(2), dst=i32(2), n_short=i32(1)),
             held=[i32(3)], seqlens_k=[i32(3)], src=[i32(1)], dst=[i32(1)], n_short=[i32(0)], refs=[i32(B + 1)])
+
+
+def test_binding_reads_no_stride_of_an_extent_of_one(fa, calls):
+    """torch calls a tensor contiguous whatever the strides of its extents of 1 are: a page of one row, one layer."""
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    B, T = 2, 3
+    for k, layer, row in ((torch.zeros(3, 2, 7, 2, 64).half(), 7 * 2 * 2 * 64 * 2, 256), (torch.zeros(1, 3, 7, 2, 64).half().movedim(0, 2), 7 * 2 * 64 * 2, 256),
+                          (torch.zeros(2, 5, 2, 64).half().as_strided((1, 2, 5, 2, 64), (3, 640, 128, 64, 1)), 0, 256)):
+        fa.fa_cache_compact(k, k, i32(B), i32(B, T), i32(B), i32(B), block_table=i32(B, 4))
+        name, args = calls.last
+        assert name == "fa_cache_compact" and (args[8], args[9], args[17]) == (k.shape[0], layer, row)
+        fa.fa_pages_fork(k, k, i32(B, 4), i32(B), i32(B), i32(k.shape[1]), i32(1), i32(1), i32(1))
+        name, args = calls.last
+        assert name == "fa_pages_fork" and (args[10], args[11], args[17]) == (k.shape[0], layer, row)
