@@ -358,7 +358,7 @@ int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlen
  *   then pages are taken, in the order of the sequences and of their entries, the free ones of lowest index first (refs = 1).
  * A sequence gets its pages iff the free pages suffice for all that it and the sequences before it ask for; if not, or if it asks
  * for more than max_pages, it keeps what it holds and is counted in n_short [1].
- *   B <= 4096 in a call, num_pages < 2^31 - 1.  The cache itself is not touched.
+ *   B <= 4096 in a call, num_pages < 2^31 - 1.  The cache itself is not touched.  With B == 0 nothing is done: n_short keeps what it held.
  * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (B, num_pages), FA_ERR_NULL, FA_ERR_ALIGN.
  */
 int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int* n_short, int B, int num_pages, int page_size,
@@ -371,7 +371,8 @@ int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int
  * the pairs -- so that a page with room is never shared and both sequences can append.  held and seqlens_k of dst follow, entries of its table row
  * past its pages become -1.  A pair for which no free page is left is counted in n_short [1]; its dst then has no rows and no pages.
  *   k, v, layers, layer_stride, row_bytes: as for fa_cache_compact (pools).  dst[i] holds no pages before the call (fa_pages_resize
- *   to 0 rows), occurs once, and is no src of the same call.  n <= 4096.  Indices outside [0, B) are skipped.
+ *   to 0 rows), occurs once, and is no src of the same call.  n <= 4096.  Indices outside [0, B) are skipped.  With n == 0 nothing is
+ *   done: n_short keeps what it held.
  * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (n > 4096, layers > 32767, num_pages = 2^31 - 1), FA_ERR_NULL, FA_ERR_ALIGN.
  */
 int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k, int* refs, const int* src, const int* dst,

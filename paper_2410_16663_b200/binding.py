@@ -468,6 +468,8 @@ def fa_pages_resize(block_table, held, refs, want, n_short, page_size: int, rais
     B, pages = block_table.shape
     if not (held.numel() >= B and want.numel() >= B and n_short.numel() >= 1):
         _shapes("fa_pages_resize", block_table=block_table, held=held, want=want, n_short=n_short)
+    if B == 0:   # (a call of the library that has nothing to do writes nothing)
+        n_short.zero_()
     rc = lib.fa_pages_resize(block_table.data_ptr(), held.data_ptr(), refs.data_ptr(), want.data_ptr(), n_short.data_ptr(), B, refs.numel(),
                              page_size, pages, _table("fa_pages_resize", block_table), _stream())
     return _check(rc, "fa_pages_resize", raise_on_error) if rc else rc
@@ -487,6 +489,8 @@ def fa_pages_fork(k, v, block_table, held, seqlens_k, refs, src, dst, n_short, r
     B, pages = block_table.shape
     if not (held.numel() >= B and seqlens_k.numel() >= B and src.numel() == dst.numel() and n_short.numel() >= 1):
         _shapes("fa_pages_fork", block_table=block_table, held=held, seqlens_k=seqlens_k, src=src, dst=dst, n_short=n_short)
+    if src.numel() == 0:
+        n_short.zero_()
     rc = lib.fa_pages_fork(k.data_ptr(), v.data_ptr(), block_table.data_ptr(), held.data_ptr(), seqlens_k.data_ptr(), refs.data_ptr(),
                            src.data_ptr(), dst.data_ptr(), n_short.data_ptr(), src.numel(), layers, stride, B, slabs, rows, pages,
                            _table("fa_pages_fork", block_table), row, _stream())

@@ -320,3 +320,14 @@ def test_binding_reads_no_stride_of_an_extent_of_one(fa, calls):
         fa.fa_pages_fork(k, k, i32(B, 4), i32(B), i32(B), i32(k.shape[1]), i32(1), i32(1), i32(1))
         name, args = calls.last
         assert name == "fa_pages_fork" and (args[10], args[11], args[17]) == (k.shape[0], layer, row)
+
+
+def test_nobody_is_short_where_there_is_nothing_to_do(fa, monkeypatch):
+    """An empty batch and an empty list of pairs: the count of an earlier call does not stand (the library itself leaves it, and says so)."""
+    monkeypatch.setattr(fa, "_stream", lambda: 0)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    short, kv = i32(1) + 7, torch.zeros(1, 3, 16, 1, 64).half()
+    assert fa.lib.fa_pages_resize(None, None, None, None, short.data_ptr(), 0, 3, 16, 2, 2, None) == fa.FA_OK and short.tolist() == [7]
+    assert fa.fa_pages_resize(i32(0, 2), i32(0), i32(3), i32(0), short, 16) == fa.FA_OK and short.tolist() == [0]
+    short += 7
+    assert fa.fa_pages_fork(kv, kv, i32(2, 2), i32(2), i32(2), i32(3), i32(0), i32(0), short) == fa.FA_OK and short.tolist() == [0]
