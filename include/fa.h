@@ -279,6 +279,8 @@ size_t fa_decode_append_workspace_bytes(int B, int Sq, int Hq, int Hkv, int Skv_
  *   Cache rows past a sequence's end may hold anything.  Inside it, the KEY of a node that a row does not see may be
  *   anything (NaN too); its VALUE must be finite, as it is multiplied by zero.
  *   workspace: fa_decode_tree_workspace_bytes(B, T, Hq, Hkv, Skv_max or max_pages * page_size, d, variant) bytes, 16-byte aligned.
+ *   Which of two kernels takes the call goes by the sizes, with every sequence as long as Skv_max (max_pages * page_size) allows: a caller
+ *   that knows a bound of its lengths passes max_pages by it, as a table far wider than that may cost a short call some microseconds.
  * Errors: as fa_decode_ex; FA_ERR_UNSUPPORTED also for T > 256, T > Skv_max or another variant, FA_ERR_NULL without a mask, FA_ERR_SHAPE for a
  * negative mask_stride.
  */

@@ -989,17 +989,34 @@ int decode_impl(const void* q, const void* k_cache, const void* v_cache, void* o
 }
 
 // Which kernel takes a tree: the split decode kernel, whose CTAs have 16 of the rows that share a kv head and each read all keys, or the
-// one for many rows (decode_tree.cuh), which takes some 4 us more to begin and to merge.  By the blocks of 16 rows and the
-// tiles of 128 keys per SM if all sequences were as long as they may be (us, split / many rows, 32/8 heads unless said; d = 128:
-// 16 rows 64 x 1000-2048 keys 68 / 74, 64 x 100-500 on 16-key pages 30 / 43; 32 rows 4 x 1000-2048 13.2 / 15.2, 16 x 400-512 15.3 / 17.2, 16 x
-// 1000-2048 31.7 / 27.6, 64 x 400-512 52.2 / 48.8; 64 rows 1 x 512 6.5 / 10.3, 1 x 8192 19.3 / 18.7, 4 x 512 13.6 / 12.3, 4 x 1000-2048 27.0 / 16.4;
-// 128 rows 1 x 2048 12.9 / 13.3, 4 x 512 25.2 / 14.1; 256 rows 1 x 512 12.9 / 13.7.  d = 64, half the bytes and twice the CTAs: 32 rows 16 x
-// 1000-2048 16.5 / 22.0, 16 x 8/8 heads, 20 rows, 1000-4096 28.1 / 29.7; 64 rows 4 x 1000-2048 11.0 / 13.7, 64 x 400-512 44.4 / 39.3, 16 x 1000-8192 74.7 /
-// 44.7; 128 rows 4 x 512 13.0 / 11.8.)  The SMs are counted as 148, so that the workspace is of one size on every device.
+// one for many rows (decode_tree.cuh), which takes some 4 us more to begin and to merge.
+// The split kernel's work is its CTAs (16-row blocks x kv heads x sequences) times their tiles of 128 keys, if all sequences were as long
+// as they may be; what a tile of work costs goes by how it cuts the call (decode_plan): a cluster of CTAs per block, which they share; whole
+// sequences; or chunks that a second kernel merges, whose length does not go by the blocks and is short where there are few sequences.
+// So the many-rows kernel takes a call from so many tiles of work per SM on, by how it would be cut and, where a sequence is
+// whole and with d = 64 (half the bytes, two CTAs to an SM), by the blocks.  Both sides (tiles per SM: us, split / many rows; 32/8 heads, B x nodes, keys):
+//   d = 128, cluster        6.9: 1 x 32, 2048 12.9 / 13.2; 8.9: 2 x 6, 5133 15.2 / 17.3;   9.8: 1 x 26, 3235 17.4 / 15.9; 13.9: 1 x 8, 16491 24.7 / 21.3
+//            whole, 2 blocks  6.9: 16 x 8, 512 15.2 / 16.9; 12.1: 16 x 8, 812 17.6 / 19.9;  19: 16 x 8, 1285 23.4 / 21.8; 22.5: 16 x 6, 1543 31.0 / 25.9
+//            whole, 3 and more  3.2: 6 x 20, 250 10.7 / 12.8;                               4.3: 8 x 20, 153 15.8 / 14.1; 6.9: 8 x 32, 236 20.6 / 15.3
+//            cut              1.6: 1 x 40, 349 11.4 / 12.8;                                 3.5: 4 x 16, 512 13.8 / 11.9; 6.9: 4 x 32, 512 25.6 / 14.9
+//   d = 64, 2 blocks: cluster 59: 2 x 6, 34601 31.8 / 36.3; 108: 4 x 5, 31842 56.9 / 46.3.  whole 69: 64 x 5, 1161 34.8 / 43.5, 80: 32 x 8, 2917
+//     39.5 / 38.9.  cut 17: 12 x 6, 1601 15.7 / 17.6; 47: 12 x 6, 4560 31.3 / 24.5
+//   3 blocks: cluster 34: 3 x 10, 8707 19.3 / 19.5; 72: 6 x 10, 9403 51.6 / 33.1.  whole 47: 32 x 10, 1151 30.6 / 31.9; 75: 16 x 10, 3711 38.6 / 29.2
+//   4 and more: cluster 14: 4 x 16, 2048 11.6 / 14.6, 21: 1 x 32, 6183 15.4 / 19.5; 32: 3 x 20, 4995 24.4 / 17.8.  whole 8.6: 8 x 40, 208 11.7 / 13.4;
+//     20.8: 16 x 48, 247 25.4 / 17.6.  cut 3.2: 2 x 40, 279 8.1 / 10.8; 6.9: 4 x 32, 512 13.2 / 11.5
+// 1500 calls of drawn sizes: 17 take 10 % longer than by the other kernel (153 by the product of blocks and tiles alone), 0.3 % in the geometric mean (3.3).
+// Knowingly given away: one or two kv heads in all over 10000 keys and more (2 x 8/1 heads, 13 nodes, 12445 keys 15.2 / 25.5: an item in 74 parts), and
+// sequences of one tile (8 x 32/2, 48 nodes, 128 keys 24.9 / 13.3).  The SMs are counted as 148, and 74 clusters of two of them, so that
+// the workspace is of one size on every device.
 bool tree_takes_many_rows(int B, int T, int Hq, int Hkv, int Skv_max, int d, int variant) {
     if (variant != 0) return variant == 2;
-    const long long blocks = ((long long)(Hq / Hkv) * T + 15) / 16, tiles = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile * B * Hkv;
-    return d == 64 ? blocks >= 3 && tiles * blocks > 24ll * 148 : blocks >= 2 && tiles * blocks > 8ll * 148;
+    const long long blocks = ((long long)(Hq / Hkv) * T + 15) / 16, tiles = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile, ctas = blocks * B * Hkv;
+    if (blocks < 2) return false;
+    // by head dimension; 2, 3 or more blocks; cluster, whole, cut
+    constexpr int kNever = 1 << 30;
+    static const int from[2][3][3] = {{{9, 14, 2}, {9, 4, 2}, {9, 4, 2}}, {{85, kNever, 24}, {40, 50, 8}, {28, 12, 6}}};
+    const bool cluster = tiles > 1 && ctas <= (d == 64 ? 148 : 74), whole = Skv_max <= decode_chunk(B, Hkv, Skv_max, true);
+    return ctas * tiles > 148ll * from[d == 64][(blocks < 4 ? blocks : 4) - 2][cluster ? 0 : whole ? 1 : 2];
 }
 // How the rows that share a kv head are cut: blocks of at most two tiles of 128 (one with d = 64), of equal size in whole warps -- and in
 // whole nodes, where a tile is, so that Q is loaded by boxes.

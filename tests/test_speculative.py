@@ -331,3 +331,23 @@ def test_nobody_is_short_where_there_is_nothing_to_do(fa, monkeypatch):
     assert fa.fa_pages_resize(i32(0, 2), i32(0), i32(3), i32(0), short, 16) == fa.FA_OK and short.tolist() == [0]
     short += 7
     assert fa.fa_pages_fork(kv, kv, i32(2, 2), i32(2), i32(2), i32(3), i32(0), i32(0), short) == fa.FA_OK and short.tolist() == [0]
+
+
+@pytest.mark.parametrize("d,B,T,hq,hkv,keys,kernel", [
+    # one cluster per row block
+    (128, 1, 8, 32, 8, 512, 1), (128, 1, 32, 32, 8, 2048, 1), (128, 2, 6, 32, 8, 5133, 1), (128, 1, 26, 32, 8, 3235, 2), (128, 1, 16, 32, 8, 8192, 2),
+    # whole sequences per CTA, two row blocks and more
+    (128, 16, 8, 32, 8, 512, 1), (128, 16, 8, 32, 8, 812, 1), (128, 16, 6, 32, 8, 1543, 2), (128, 64, 8, 32, 8, 512, 2), (128, 6, 20, 32, 8, 250, 1),
+    (128, 8, 20, 32, 8, 153, 2), (128, 8, 32, 32, 8, 236, 2),
+    # cut into chunks that are merged
+    (128, 1, 40, 32, 8, 349, 1), (128, 4, 16, 32, 8, 512, 2), (128, 4, 32, 32, 8, 512, 2), (128, 2, 40, 64, 8, 289, 2), (128, 8, 8, 32, 2, 989, 2),
+    # 16 rows per kv head: one row block
+    (128, 64, 4, 32, 8, 2048, 1), (64, 64, 4, 32, 8, 2048, 1),
+    (64, 2, 6, 32, 8, 34601, 1), (64, 4, 5, 32, 8, 31842, 2), (64, 64, 5, 32, 8, 1161, 1), (64, 12, 6, 32, 8, 1601, 1), (64, 12, 6, 32, 8, 4560, 2),
+    (64, 3, 10, 32, 8, 8707, 1), (64, 6, 10, 32, 8, 9403, 2), (64, 32, 10, 32, 8, 1151, 1), (64, 16, 10, 32, 8, 3711, 2),
+    (64, 4, 16, 32, 8, 2048, 1), (64, 1, 32, 32, 8, 6183, 1), (64, 3, 20, 32, 8, 4995, 2), (64, 8, 40, 32, 8, 208, 1), (64, 16, 48, 32, 8, 247, 2),
+    (64, 2, 40, 32, 8, 279, 1), (64, 4, 32, 32, 8, 512, 2), (64, 3, 61, 40, 5, 7951, 2), (64, 3, 80, 32, 8, 837, 2)])
+def test_the_tree_kernel_is_the_faster_one_where_both_were_timed(fa, d, B, T, hq, hkv, keys, kernel):
+    """The default's choice, seen by the workspace that it asks for, at sizes on both sides of each line that the rule's comment gives times for."""
+    sizes = [fa.fa_decode_tree_workspace_bytes(B, T, hq, hkv, keys, d, variant) for variant in (0, 1, 2)]
+    assert sizes[1] != sizes[2] and sizes[0] == sizes[kernel]
