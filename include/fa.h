@@ -327,7 +327,8 @@ size_t fa_decode_tree_workspace_bytes(int B, int T, int Hq, int Hkv, int Skv_max
  * (Sums are fp32, comparisons with NaN fail.)
  *   n_accept int32 [B]: drafted tokens that stand; path int32 [B,T]: the nodes that stand, from node 0 on, then -1;
  *   out_tokens int32 [B,T]: their tokens without node 0's, the last token, then -1.
- *   T <= 256, V <= 2^30; all contiguous and aligned to their elements.  A token outside [0, V) is never accepted.
+ *   T <= 256, V <= 2^30; all contiguous and aligned to their elements.  A token outside [0, V) is never accepted.  n_accept, path and
+ *   out_tokens share no memory with the inputs.
  * Errors: FA_ERR_SHAPE, FA_ERR_UNSUPPORTED (T, V, dtype, B > 65535), FA_ERR_NULL, FA_ERR_ALIGN.
  */
 int fa_spec_verify(const void* target_probs, const void* draft_probs, const int* tokens, const int* parents,
@@ -370,8 +371,9 @@ int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int
  * Sequences that go on from the same rows (parallel sampling, beams): for i = 0 .. n-1 sequence dst[i] becomes a copy of src[i], with
  * the state of fa_pages_resize and seqlens_k [B] on the device.  Full pages are shared (refs + 1); of a last page that is
  * partly filled, the filled rows are copied, K and V, all layers, to a fresh page -- the free ones of lowest index, in the order of
- * the pairs -- so that a page with room is never shared and both sequences can append.  held and seqlens_k of dst follow, entries of its table row
- * past its pages become -1.  A pair for which no free page is left is counted in n_short [1]; its dst then has no rows and no pages.
+ * the pairs -- so that a page with room is not shared and both sequences can append.  (A sequence that is later cut back into a page that
+ * others hold, fa_pages_resize to rows that end inside it, must not append there: their rows would change.)  held and seqlens_k of dst
+ * follow, entries of its table row past its pages become -1.  A pair for which no free page is left is counted in n_short [1]; its dst then has no rows and no pages.
  *   k, v, layers, layer_stride, row_bytes: as for fa_cache_compact (pools).  dst[i] holds no pages before the call (fa_pages_resize
  *   to 0 rows), occurs once, and is no src of the same call.  n <= 4096.  Indices outside [0, B) are skipped.  With n == 0 nothing is
  *   done: n_short keeps what it held.

@@ -13,9 +13,10 @@ namespace fa {
 // ---------------------------------------------------------------------------------------
 // Compaction: row prefix + i of sequence b <- row prefix + path[b][i], i = 1 .. n_accept[b], in every plane (a layer's K or V).
 // A thread owns 16 bytes of a row in some planes and moves them in the order of i, several rows' loads ahead of the
-// first store: as path[i] >= i and the path ascends, a row that is still to be read has not been written.  Few bytes move; what
-// bounds it is the chain of length, path, table and row, which a thread follows once for all of its pieces.  64 sequences, 32 layers, 8 x 128
-// fp16 on 16-key pages, 17 MB: 8.0 us (9.1 with eight rows of one piece in flight, two CTAs to an SM); 1 sequence 2.3.
+// first store: a row moves down (path[i] > i), and what has been written by then are rows up to i.  Few bytes move.  One sequence takes 2.3 us, the
+// chain of length, path, table and row, which a thread follows once for all of its pieces.  64 sequences, 32 layers, 8 x 128 fp16 on
+// 16-key pages, 17 MB: 8.0 us (9.1 with eight rows of one piece in flight, two CTAs to an SM), as each has nine CTAs whatever it moves: 28 of
+// them move no row, and the threads of 28 others, with one or two, have two to four loads in flight of eight.
 struct CompactParams {
     char* k;
     char* v;

@@ -11,9 +11,11 @@
 // Roles: a warp that looks up the run's segments (one per item) and loads K and V tiles into a ring; one that loads Q; and for each row
 // tile four warps for softmax and output, a row per thread, and a thread for each product.  A row tile has two score buffers,
 // whose probabilities overlay the scores: the tensor cores are at work on one while the other is in the softmax.
-// What bounds it: with one row tile HBM (16 sequences of 100 to 8000 keys on 16-key pages, 104 rows per kv head: 64 us, 265 MB, 4.1 TB/s with the
-// merge, which takes 8), with two the softmax warps and the power limit (32 sequences of 1024 to 16384 keys, 256 rows: 318 us, 3.0 TB/s and
-// 740 TFLOPS at 1.40 GHz).
+// What bounds it: the softmax warps, each of which goes one after the other through loading the scores, maximum, exponentials, storing and
+// handing over.  One row tile has one such warp per scheduler and takes 3300 clocks for 128 keys, where HBM takes 2550 and no unit is near
+// its limit (16 sequences of 100 to 8000 keys on 16-key pages, 104 rows per kv head: 64 us, 265 MB, 4.1 TB/s with the merge, which takes 8);
+// two have two per scheduler, 2200 clocks for 64 keys, and the power limit (32 sequences of 1024 to 16384 keys, 256 rows: 307 us,
+// 3.1 TB/s and 760 TFLOPS at 1.40 GHz).
 #pragma once
 
 #include "decode.cuh"
