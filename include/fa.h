@@ -55,6 +55,7 @@ extern "C" {
 #define FA_DTYPE_FP16 0
 #define FA_DTYPE_BF16 1
 #define FA_DTYPE_FP32 2 /* only as fa_params.o_dtype */
+#define FA_DTYPE_E4M3 3 /* only as fa_append_params.cache_dtype */
 
 /*
  * Prefill / general forward, fp16 inputs and output (Section 5.1 operator; Section 4.1 method).
@@ -382,6 +383,66 @@ int fa_pages_resize(int* block_table, int* held, int* refs, const int* want, int
 int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k, int* refs, const int* src, const int* dst,
                   int* n_short, int n, int layers, int64_t layer_stride, int B, int num_pages, int page_size, int max_pages,
                   int table_stride, int row_bytes, void* stream);
+
+/*
+ * Position rotation (no counterpart in the paper, whose models rotate queries and keys ahead of the attention): of every head x of a token at
+ * position pos, the rot_dim columns from rot_offset on are turned pair by pair,
+ *     (a, b)  ->  factor * (a cos w - b sin w, a sin w + b cos w),      w = 2 pi * frac(pos * turns[i] / 2^64),   i < rot_dim / 2,
+ * with (a, b) the columns i and rot_dim / 2 + i of them (interleaved == 0), or 2 i and 2 i + 1; the other columns are copied.
+ *   turns [rot_dim / 2] on the DEVICE: what a position adds to pair i's angle, as a share of a full turn in 64-bit fixed point (for
+ *   frequencies f_i in radians: f_i / 2 pi * 2^64, modulo 2^64), so that no position loses any of the angle.  Frequencies scaled for long
+ *   contexts are just other turns; their negatives turn back.  factor: any finite number (1, or what a scaled context asks for).
+ *   x, out [n,H,d] of dtype (FA_DTYPE_FP16 or FA_DTYPE_BF16), d contiguous, strides in elements from one token and head to the next;
+ *   out may be x with its strides, and shares no memory with it otherwise.  positions int32 [n] on the DEVICE.  The arithmetic is in 32 bits, the
+ *   results are rounded once.
+ *   d a multiple of 16 up to 1024, rot_dim a multiple of 16 up to min(d, 512), rot_offset a multiple of 8 with rot_offset + rot_dim <= d.
+ * Errors: FA_ERR_SHAPE (negative sizes, rotated columns outside the head, strides that are negative or not multiples of 8), FA_ERR_UNSUPPORTED (those
+ * sizes, dtype, a factor that is not finite), FA_ERR_NULL, FA_ERR_ALIGN (x and out 16 bytes, turns 8).
+ */
+int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turns, int n, int H, int d, int rot_dim, int rot_offset,
+            int interleaved, float factor, int64_t x_token_stride, int64_t x_head_stride, int64_t out_token_stride,
+            int64_t out_head_stride, int dtype, void* stream);
+
+/*
+ * New tokens' rows for the caches that the decode calls read: keys are turned as by fa_rope and written to their rows, values are
+ * written as they are, and the tokens' queries are turned on the way.  The n tokens are those of B sequences one after the other, sequence b's
+ * from cu_seqlens[b] to cu_seqlens[b + 1] (int32 [B + 1] on the DEVICE), or T each where cu_seqlens is NULL (n = B * T).  Token t
+ * of sequence b gets row first_rows[b] + t of its cache, and its position is positions[token], or that row where positions is NULL.
+ *   q, q_out [n,Hq,d] (NULL: no queries), k [n,Hkv,d], v [n,Hkv,dv] (NULL: keys alone): of dtype, with strides in elements from one
+ *   token and head to the next; q_out may be q with its strides.  turns == NULL: nothing is turned (queries are copied).
+ *   Caches of cache_dtype: dtype, or FA_DTYPE_E4M3, where what is written is x / k_scale and x / v_scale, rounded to the nearest
+ *   and at most 448.  A row holds Hkv * d (v: Hkv * dv) contiguous elements; k_cache_stride, v_cache_stride: elements from one slab to the next
+ *   and from one row to the next, where a slab is a sequence (block_table == NULL: slabs of Skv_max rows) or a page of page_size rows (any
+ *   positive number) behind block_table [B,table_stride].  So both caches may be parts of one row: of latent attention's cache
+ *   (fa_decode_latent) the vectors' rotated ends are "keys" of one head of 64, and the vectors are its "values", of 512.
+ *   counts int32 [B] (NULL: all): only the first counts[b] tokens of sequence b are written.  Rows outside the cache, and pages outside
+ *   [0, num_pages), are passed over.  Tokens behind the last sequence (cu_seqlens[B] < n) are nobody's: nothing of theirs is written.  No two tokens may have one row.
+ *   d, dv multiples of 16 up to 1024; rotation as for fa_rope; caches and their strides in whole 16 bytes.  Outputs share no memory with the inputs otherwise.
+ * Errors: as fa_rope; FA_ERR_SHAPE also for n != B * T, table_stride < max_pages; FA_ERR_UNSUPPORTED for a k_scale or v_scale that is not positive and finite.
+ */
+typedef struct fa_append_params {
+    const void* q;
+    void* q_out;
+    const void* k;
+    const void* v;
+    void* k_cache;
+    void* v_cache;
+    const uint64_t* turns;
+    const int* positions;
+    const int* first_rows;
+    const int* counts;
+    const int* cu_seqlens;
+    const int* block_table;
+    int64_t q_stride[2], q_out_stride[2], k_stride[2], v_stride[2]; /* token, head */
+    int64_t k_cache_stride[2], v_cache_stride[2];                   /* slab, row */
+    int n, B, T, Hq, Hkv, d, dv;
+    int rot_dim, rot_offset, interleaved;
+    int dtype;       /* FA_DTYPE_FP16 or FA_DTYPE_BF16 */
+    int cache_dtype; /* dtype or FA_DTYPE_E4M3 */
+    int Skv_max, num_pages, page_size, max_pages, table_stride;
+    float factor, k_scale, v_scale;
+} fa_append_params;
+int fa_cache_append(const fa_append_params* p, void* stream);
 
 /*
  * Decode over an 8-bit cache (Appendix D.2 evaluates the operator with 8-bit operands; in the

@@ -16,7 +16,7 @@ import torch
 FA_OK = 0
 FA_ERR_NULL, FA_ERR_SHAPE, FA_ERR_UNSUPPORTED, FA_ERR_ALIGN = -1, -2, -3, -4
 FA_ERR_WORKSPACE, FA_ERR_DEVICE, FA_ERR_CUDA, FA_ERR_TIMEOUT = -5, -6, -7, -8
-FA_DTYPE_FP16, FA_DTYPE_BF16, FA_DTYPE_FP32 = 0, 1, 2
+FA_DTYPE_FP16, FA_DTYPE_BF16, FA_DTYPE_FP32, FA_DTYPE_E4M3 = 0, 1, 2, 3
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libfa.so")
 if not os.path.exists(_LIB_PATH):
@@ -75,6 +75,21 @@ lib.fa_decode_tree.restype = _i
 lib.fa_decode_tree.argtypes = [_p, _p]   # (an fa_tree_params by reference, or its bytes)
 _TREE = struct.Struct("@9P12iqfPN")      # fa_tree_params
 assert _TREE.size == ctypes.sizeof(fa_tree_params)
+class fa_append_params(ctypes.Structure):
+    _fields_ = [(name, _p) for name in ("q", "q_out", "k", "v", "k_cache", "v_cache", "turns", "positions", "first_rows", "counts",
+                                        "cu_seqlens", "block_table")]
+    _fields_ += [(name + "_stride", ctypes.c_int64 * 2) for name in ("q", "q_out", "k", "v", "k_cache", "v_cache")]
+    _fields_ += [(name, _i) for name in ("n", "B", "T", "Hq", "Hkv", "d", "dv", "rot_dim", "rot_offset", "interleaved", "dtype",
+                                         "cache_dtype", "Skv_max", "num_pages", "page_size", "max_pages", "table_stride")]
+    _fields_ += [("factor", _f), ("k_scale", _f), ("v_scale", _f)]
+
+
+lib.fa_rope.restype = _i
+lib.fa_rope.argtypes = [_p] * 4 + [_i] * 6 + [_f] + [ctypes.c_int64] * 4 + [_i, _p]
+lib.fa_cache_append.restype = _i
+lib.fa_cache_append.argtypes = [_p, _p]     # (an fa_append_params by reference, or its bytes)
+_APPEND = struct.Struct("@12P12q17i3f")     # fa_append_params
+assert _APPEND.size == ctypes.sizeof(fa_append_params)
 _FA16 = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16}
 _FA_PROBS = {**_FA16, torch.float32: FA_DTYPE_FP32}
 lib.fa_decode_tree_workspace_bytes.restype = _sz
@@ -128,7 +143,7 @@ FA_DECODE_NOALLOC_BYTES = 4 << 20
 
 EXPORTS = ["fa_forward", "fa_forward_bf16", "fa_forward_ex", "fa_forward_fp8", "fa_forward_proj", "fa_forward_proj_workspace_bytes", "fa_decode", "fa_decode_workspace_bytes",
            "fa_decode_noalloc", "fa_decode_paged", "fa_forward_varlen", "fa_decode_fp8", "fa_decode_fp8_paged", "fa_decode_fp8_bf16", "fa_decode_fp8_paged_bf16", "fa_decode_append", "fa_decode_append_workspace_bytes", "fa_decode_ex", "fa_forward_varlen_paged",
-           "fa_decode_tree", "fa_decode_tree_workspace_bytes", "fa_spec_verify", "fa_cache_compact", "fa_pages_resize", "fa_pages_fork",
+           "fa_decode_tree", "fa_decode_tree_workspace_bytes", "fa_spec_verify", "fa_cache_compact", "fa_pages_resize", "fa_pages_fork", "fa_rope", "fa_cache_append",
            "fa_forward_host", "fa_forward_host_staging_bytes", "fa_device_status", "fa_selftest_wait", "fa_selftest_decode_cut", "fa_strerror",
            "fa_version", "fa_last_cuda_error"]
 
@@ -498,6 +513,138 @@ def fa_pages_fork(k, v, block_table, held, seqlens_k, refs, src, dst, n_short, r
                            src.data_ptr(), dst.data_ptr(), n_short.data_ptr(), src.numel(), layers, stride, B, slabs, rows, pages,
                            _table("fa_pages_fork", block_table), row, _stream())
     return _check(rc, "fa_pages_fork", raise_on_error) if rc else rc
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, stretch: float = 1.0, trained: int = 0, slow: float = 1.0, fast: float = 32.0,
+                     device="cuda"):
+    """Radians per position of each pair of ``rot_dim`` rotated columns, float64: base^(-2 i / rot_dim).  ``stretch`` > 1 scales them for
+    contexts so many times longer: all alike (positions drawn together), or, with ``trained`` the context a model was trained on,
+    by parts: pairs that turn less than ``slow`` times over it are slowed down by stretch, those that turn more than ``fast`` times
+    stay, in between it is a mixture of both, linear in the turns.  (A larger base is given as such.)"""
+    w = float(base) ** (-torch.arange(0, rot_dim, 2, dtype=torch.float64, device=device) / rot_dim)
+    if stretch == 1.0:
+        return w
+    if not trained:
+        return w / stretch
+    keep = ((trained * w / (2.0 * math.pi) - slow) / (fast - slow)).clamp(0.0, 1.0)
+    return w * (keep + (1.0 - keep) / stretch)
+
+
+def rope_turns(frequencies):
+    """The ``turns`` of ``fa_rope`` and ``fa_cache_append`` for frequencies in radians per position (float64 [rot_dim / 2], see
+    ``rope_frequencies``): shares of a full turn in 64-bit fixed point, int64 (its bits are what counts).  Made once for a model."""
+    if frequencies.dtype is not torch.float64 or frequencies.dim() != 1:
+        raise ValueError("rope_turns: frequencies are float64 [rot_dim / 2] (32 bits lose the angles of far positions)")
+    share = frequencies / (2.0 * math.pi)
+    share = share - share.round()
+    return torch.where(share >= 0.5, share - 1.0, share).mul(2.0 ** 64).to(torch.int64)   # (half a turn either way is the same)
+
+
+def _turns(what: str, t) -> int:
+    if t.dtype is not torch.int64 or not t.is_contiguous() or t.dim() != 1:
+        raise ValueError(f"{what}: turns are int64 [rot_dim / 2], contiguous (see rope_turns)")
+    return 2 * t.shape[0]
+
+
+def fa_rope(x, out, positions, turns, offset: int = 0, interleaved: bool = False, factor: float = 1.0, raise_on_error: bool = True) -> int:
+    """``fa_rope``: x, out [n,H,d] (out may be x), fp16 or bf16, any strides of tokens and heads; positions int32 [n]; turns from
+    ``rope_turns``, for the 2 * len(turns) columns of each head from ``offset`` on."""
+    dt = x.dtype
+    if not (out.dtype is dt and (dt is _HALF or dt is _BF16)):
+        raise ValueError("fa_rope: x and out share one 16-bit type")
+    n, H, d = x.shape
+    rot = _turns("fa_rope", turns)
+    xt, xh, xd = x.stride()
+    ot, oh, od = out.stride()
+    if out.shape != x.shape or xd != 1 or od != 1 or positions.numel() < n or positions.dtype is not _INT or not positions.is_contiguous():
+        _contiguous("fa_rope", positions)
+        _int32("fa_rope", positions)
+        if xd != 1 or od != 1:
+            raise ValueError("fa_rope: the columns of a head are contiguous")
+        _shapes("fa_rope", x=x, out=out, positions=positions)
+    # (the stride of an extent of 1 may be any number)
+    rc = lib.fa_rope(x.data_ptr(), out.data_ptr(), positions.data_ptr(), turns.data_ptr(), n, H, d, rot, offset, 1 if interleaved else 0, factor,
+                     xt if n > 1 else 0, xh if H > 1 else 0, ot if n > 1 else 0, oh if H > 1 else 0, _FA16[dt], _stream())
+    return _check(rc, "fa_rope", raise_on_error) if rc else rc
+
+
+def _tokens(what: str, t):
+    """(tokens, heads, width, stride of a token, stride of a head) of [n,H,d] or [B,T,H,d]."""
+    shape, stride = t.shape, t.stride()
+    if stride[-1] != 1 and shape[-1] != 1:
+        raise ValueError(f"{what}: the columns of a head are contiguous")
+    H, d = shape[-2:]
+    head = stride[-2] if H > 1 else 0
+    if len(shape) == 3:
+        return shape[0], H, d, stride[0] if shape[0] > 1 else 0, head
+    B, T = shape[:2]
+    if B > 1 and T > 1 and stride[0] != T * stride[1]:
+        raise ValueError(f"{what}: the tokens of [B,T,H,d] are as far apart from one sequence to the next as inside it")
+    return B * T, H, d, (stride[1] if T > 1 else stride[0]) if B * T > 1 else 0, head
+
+
+def _rows(what: str, cache, Hkv: int, d: int):
+    """(slabs, rows of a slab, stride of a slab, stride of a row) of a cache [slabs,rows,Hkv,d], or [slabs,rows,d] for one head."""
+    shape, stride = cache.shape, cache.stride()
+    if shape[2:] != (Hkv, d) and not (Hkv == 1 and shape[2:] == (d,)):
+        raise ValueError(f"{what}: a cache of shape {tuple(shape)} for {Hkv} heads of {d}")
+    if stride[-1] != 1 or (Hkv > 1 and stride[2] != d):
+        raise ValueError(f"{what}: a row of a cache is contiguous, not of strides {stride[2:]}")
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0
+
+
+def fa_cache_append(q, q_out, k, v, k_cache, v_cache, first_rows, turns=None, positions=None, counts=None, cu_seqlens=None,
+                    block_table=None, max_pages: int = None, offset: int = 0, interleaved: bool = False, factor: float = 1.0,
+                    k_scale: float = 1.0, v_scale: float = 1.0, raise_on_error: bool = True) -> int:
+    """``fa_cache_append``: q, q_out [n,Hq,d] (or None), k [n,Hkv,d], v [n,Hkv,dv] (or None), packed by cu_seqlens int32 [B+1], or
+    without it [B,T,H,d] or the same tokens as [n,H,d]; first_rows int32 [B]; caches [B,Smax,Hkv,d] and [B,Smax,Hkv,dv], or with a block table
+    [num_pages,page_size,...], of the inputs' type or FP8 e4m3 (``torch.float8_e4m3fn`` or uint8 bit patterns) with one factor
+    each; turns from ``rope_turns`` (None: no rotation); positions int32 [n], counts int32 [B] or None."""
+    what, dt = "fa_cache_append", k.dtype
+    if not ((dt is _HALF or dt is _BF16) and (v is None or v.dtype is dt) and (q is None or (q.dtype is dt and q_out.dtype is dt))):
+        raise ValueError(f"{what}: q, q_out, k and v share one 16-bit type")
+    ct = k_cache.dtype
+    f8 = ct is torch.float8_e4m3fn or ct is torch.uint8
+    if not (f8 or ct is dt) or (v is not None and v_cache.dtype is not ct):
+        raise ValueError(f"{what}: caches are of the inputs' type or e4m3, both of one type")
+    for t in (first_rows, positions, counts, cu_seqlens):
+        if t is not None and not (t.dtype is _INT and t.is_contiguous()):
+            _int32(what, t)
+            _contiguous(what, t)
+    n, Hkv, d, kt, kh = _tokens(what, k)
+    slabs, rows, ks, kr = _rows(what, k_cache, Hkv, d)
+    fits = True
+    Hq = qt = qh = ot = oh = dv = vt = vh = vs = vr = 0
+    if q is not None:
+        nq, Hq, dq, qt, qh = _tokens(what, q)
+        no, ho, do, ot, oh = _tokens(what, q_out)
+        fits = nq == no == n and ho == Hq and dq == do == d
+    if v is not None:
+        nv, hv, dv, vt, vh = _tokens(what, v)
+        slabs_v, rows_v, vs, vr = _rows(what, v_cache, Hkv, dv)
+        fits = fits and nv == n and hv == Hkv and slabs_v == slabs and rows_v == rows
+    B = first_rows.numel() if cu_seqlens is None else cu_seqlens.numel() - 1
+    if cu_seqlens is None and k.dim() == 4:
+        B = k.shape[0]
+    T = 0 if cu_seqlens is not None or B == 0 else n // B
+    if block_table is None:
+        tables, sizes = slabs, (rows, 0, 0, 0, 0)
+    else:
+        tables, pages = block_table.shape
+        sizes = (0, slabs, rows, pages if max_pages is None else max_pages, _table(what, block_table))
+    if not (fits and tables >= B and first_rows.numel() >= B and (counts is None or counts.numel() >= B)
+            and (positions is None or positions.numel() >= n) and (cu_seqlens is not None or B * T == n)):
+        _shapes(what, q=q, q_out=q_out, k=k, v=v, k_cache=k_cache, v_cache=v_cache, first_rows=first_rows, positions=positions, counts=counts,
+                cu_seqlens=cu_seqlens, block_table=block_table)
+    rot = 0 if turns is None else _turns(what, turns)
+    p = _APPEND.pack(0 if q is None else q.data_ptr(), 0 if q is None else q_out.data_ptr(), k.data_ptr(), 0 if v is None else v.data_ptr(),
+                     k_cache.data_ptr(), 0 if v is None else v_cache.data_ptr(), 0 if turns is None else turns.data_ptr(),
+                     0 if positions is None else positions.data_ptr(), first_rows.data_ptr(), 0 if counts is None else counts.data_ptr(),
+                     0 if cu_seqlens is None else cu_seqlens.data_ptr(), 0 if block_table is None else block_table.data_ptr(),
+                     qt, qh, ot, oh, kt, kh, vt, vh, ks, kr, vs, vr, n, B, T, Hq, Hkv, d, dv, rot, offset if rot else 0, 1 if interleaved else 0,
+                     _FA16[dt], FA_DTYPE_E4M3 if f8 else _FA16[dt], *sizes, factor, k_scale, v_scale)
+    rc = lib.fa_cache_append(p, _stream())
+    return _check(rc, what, raise_on_error) if rc else rc
 
 
 def fa_decode_append_workspace_bytes(B: int, Sq: int, Hq: int, Hkv: int, Skv_max: int, d: int) -> int:

@@ -22,6 +22,7 @@
 #include "decode_fp8.cuh"
 #include "prefill_pipelined.cuh"
 #include "prefill_simple.cuh"
+#include "rope_append.cuh"
 #include "spec_verify.cuh"
 
 namespace {
@@ -1337,6 +1338,144 @@ int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlen
     const int grid = (int)(blocks < most ? (blocks > 0 ? blocks : 1) : (most > 0 ? most : 1));
     const cudaError_t e = fa::launch_dependent(fa::fa_cache_compact_kernel, dim3(grid, B), fa::kCompactThreads, 0, static_cast<cudaStream_t>(stream), cp);
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+}  // extern "C"
+
+namespace {
+
+bool finite_positive(float x) { return x > 0.f && !isinf(x); }
+
+// Strides of [tokens, heads, width] in elements.
+bool token_strides_ok(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && !(s[0] & 7) && !(s[1] & 7) && s[0] < (1ll << 38) && s[1] < (1ll << 38); }
+
+// What a rotation asks of its sizes.
+int check_rotation(int d, int rot, int offset, float factor) {
+    if (rot < 0 || offset < 0 || (long long)offset + rot > d) return FA_ERR_SHAPE;
+    if (d % 16 || d > 1024 || rot % 16 || rot > 512 || offset % 8 || !isfinite(factor)) return FA_ERR_UNSUPPORTED;
+    return FA_OK;
+}
+
+int rope_launch(fa::RopeParams& rp, bool bf16, bool f8, cudaStream_t st) {
+    int sms = 0;
+    if (int rc = check_device(&sms)) return rc;
+    const int half = rp.turns ? rp.rot / 2 : 1;
+    // Few tokens: a token's heads are shared by CTAs, a vector pair to a thread.  Many: several tokens to a CTA, a warp each to look up.
+    int split = 1;
+    rp.tokens = 1;
+    if (rp.n < 2 * sms) {
+        split = (rp.units + fa::kRopeThreads - 1) / fa::kRopeThreads;
+        const int room = 4 * sms / rp.n > 0 ? 4 * sms / rp.n : 1;
+        if (split > room) split = room;
+    } else {
+        while (2 * rp.tokens <= 4 && 2 * rp.tokens * half <= fa::kRopeMostAngles && (long long)rp.n >= 8ll * sms * rp.tokens) rp.tokens *= 2;
+    }
+    rp.by_units.set(rp.units);
+    const auto kern = bf16 ? (f8 ? fa::fa_rope_append_kernel<__nv_bfloat16, true> : fa::fa_rope_append_kernel<__nv_bfloat16, false>)
+                           : (f8 ? fa::fa_rope_append_kernel<__half, true> : fa::fa_rope_append_kernel<__half, false>);
+    const cudaError_t e = fa::launch_dependent(kern, dim3((rp.n + rp.tokens - 1) / rp.tokens, split), fa::kRopeThreads, 0, st, rp);
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+}  // namespace
+
+extern "C" {
+
+int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turns, int n, int H, int d, int rot_dim, int rot_offset,
+            int interleaved, float factor, int64_t x_token_stride, int64_t x_head_stride, int64_t out_token_stride,
+            int64_t out_head_stride, int dtype, void* stream) {
+    if (n < 0 || H <= 0 || d <= 0) return FA_ERR_SHAPE;
+    if (int rc = check_rotation(d, rot_dim, rot_offset, factor)) return rc;
+    if (dtype != FA_DTYPE_FP16 && dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    const int64_t xs[2] = {x_token_stride, x_head_stride}, os[2] = {out_token_stride, out_head_stride};
+    if (!token_strides_ok(xs) || !token_strides_ok(os)) return FA_ERR_SHAPE;
+    if ((long long)H * d > (1 << 24)) return FA_ERR_UNSUPPORTED;
+    if (n == 0) return FA_OK;
+    if (!x || !out || !positions || (rot_dim > 0 && !turns)) return FA_ERR_NULL;
+    if (!aligned16(x) || !aligned16(out) || (reinterpret_cast<uintptr_t>(turns) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u))
+        return FA_ERR_ALIGN;
+    fa::RopeParams rp = {};
+    rp.q = x;
+    rp.q_out = out;
+    rp.turns = rot_dim > 0 ? reinterpret_cast<const unsigned long long*>(turns) : nullptr;
+    rp.positions = positions;
+    rp.q_st = xs[0]; rp.q_sh = xs[1]; rp.o_st = os[0]; rp.o_sh = os[1];
+    rp.n = n; rp.d = d; rp.dv = d;
+    rp.rot = rot_dim; rp.offset = rot_offset; rp.interleaved = interleaved != 0;
+    rp.q_units = rp.k_units = rp.units = H * (d / 16);
+    rp.by_d.set(d / 16);
+    rp.by_dv.set(d / 16);
+    rp.by_T.set(1);
+    rp.factor = factor;
+    return rope_launch(rp, dtype == FA_DTYPE_BF16, false, static_cast<cudaStream_t>(stream));
+}
+
+int fa_cache_append(const fa_append_params* pp, void* stream) {
+    if (!pp) return FA_ERR_NULL;
+    const fa_append_params& p = *pp;
+    if (p.n < 0 || p.B < 0 || p.Hkv <= 0 || p.d <= 0 || (p.q && p.Hq <= 0) || (p.v && p.dv <= 0)) return FA_ERR_SHAPE;
+    if (!p.cu_seqlens && (p.T < 0 || (long long)p.B * p.T != p.n)) return FA_ERR_SHAPE;
+    const bool turned = p.turns && p.rot_dim > 0, f8 = p.cache_dtype == FA_DTYPE_E4M3;
+    if (int rc = check_rotation(p.d, p.rot_dim, p.rot_offset, p.factor)) return rc;
+    if (p.v && (p.dv % 16 || p.dv > 1024)) return FA_ERR_UNSUPPORTED;
+    if (p.dtype != FA_DTYPE_FP16 && p.dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    if (!f8 && p.cache_dtype != p.dtype) return FA_ERR_UNSUPPORTED;
+    if (f8 && (!finite_positive(p.k_scale) || (p.v && !finite_positive(p.v_scale)))) return FA_ERR_UNSUPPORTED;
+    if (p.block_table) {
+        if (p.num_pages < 0 || p.max_pages < 0 || p.page_size <= 0 || p.table_stride < p.max_pages) return FA_ERR_SHAPE;
+        if ((long long)p.max_pages * p.page_size > 0x7fffffffll) return FA_ERR_SHAPE;
+    } else if (p.Skv_max < 0) return FA_ERR_SHAPE;
+    if (!token_strides_ok(p.k_stride) || (p.v && !token_strides_ok(p.v_stride)) || (p.q && (!token_strides_ok(p.q_stride) || !token_strides_ok(p.q_out_stride))))
+        return FA_ERR_SHAPE;
+    const int64_t unit = f8 ? 15 : 7;   // 16 bytes
+    for (int i = 0; i < 2; ++i) {
+        if (p.k_cache_stride[i] < 0 || p.k_cache_stride[i] >= (1ll << 42) || (p.k_cache_stride[i] & unit)) return FA_ERR_SHAPE;
+        if (p.v && (p.v_cache_stride[i] < 0 || p.v_cache_stride[i] >= (1ll << 42) || (p.v_cache_stride[i] & unit))) return FA_ERR_SHAPE;
+    }
+    const long long width = (p.q ? (long long)p.Hq * p.d : 0) + (long long)p.Hkv * p.d + (p.v ? (long long)p.Hkv * p.dv : 0);
+    if (width > (1 << 24)) return FA_ERR_UNSUPPORTED;
+    if (p.n == 0 || p.B == 0) return FA_OK;
+    if (!p.k || !p.k_cache || !p.first_rows || (p.q && !p.q_out) || (p.v && !p.v_cache)) return FA_ERR_NULL;
+    if (!aligned16(p.q) || !aligned16(p.q_out) || !aligned16(p.k) || !aligned16(p.v) || !aligned16(p.k_cache) || !aligned16(p.v_cache) ||
+        (reinterpret_cast<uintptr_t>(p.turns) & 7u))
+        return FA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(p.positions) | reinterpret_cast<uintptr_t>(p.first_rows) | reinterpret_cast<uintptr_t>(p.counts) |
+         reinterpret_cast<uintptr_t>(p.cu_seqlens) | reinterpret_cast<uintptr_t>(p.block_table)) & 3u)
+        return FA_ERR_ALIGN;
+    fa::RopeParams rp = {};
+    rp.q = p.q;
+    rp.q_out = p.q_out;
+    rp.k = p.k;
+    rp.v = p.v;
+    rp.k_cache = static_cast<char*>(p.k_cache);
+    rp.v_cache = static_cast<char*>(p.v_cache);
+    rp.turns = turned ? reinterpret_cast<const unsigned long long*>(p.turns) : nullptr;
+    rp.positions = p.positions;
+    rp.first = p.first_rows;
+    rp.counts = p.counts;
+    rp.cu = p.cu_seqlens;
+    rp.block_table = p.block_table;
+    rp.q_st = p.q_stride[0]; rp.q_sh = p.q_stride[1]; rp.o_st = p.q_out_stride[0]; rp.o_sh = p.q_out_stride[1];
+    rp.k_st = p.k_stride[0]; rp.k_sh = p.k_stride[1]; rp.v_st = p.v_stride[0]; rp.v_sh = p.v_stride[1];
+    const int size = f8 ? 1 : 2;
+    rp.kc_slab = p.k_cache_stride[0] * size; rp.kc_row = p.k_cache_stride[1] * size;
+    rp.vc_slab = p.v_cache_stride[0] * size; rp.vc_row = p.v_cache_stride[1] * size;
+    rp.n = p.n; rp.B = p.B; rp.T = p.T; rp.d = p.d; rp.dv = p.v ? p.dv : 16;
+    rp.rot = p.rot_dim; rp.offset = p.rot_offset; rp.interleaved = p.interleaved != 0;
+    rp.q_units = p.q ? p.Hq * (p.d / 16) : 0;
+    rp.k_units = rp.q_units + p.Hkv * (p.d / 16);
+    rp.units = rp.k_units + (p.v ? p.Hkv * (p.dv / 16) : 0);
+    rp.max_rows = p.block_table ? p.max_pages * p.page_size : p.Skv_max;
+    rp.page_size = p.block_table ? p.page_size : 1;
+    rp.table_stride = p.table_stride;
+    rp.num_pages = p.num_pages;
+    rp.by_d.set(p.d / 16);
+    rp.by_dv.set(rp.dv / 16);
+    rp.by_T.set(p.cu_seqlens || p.T < 1 ? 1 : p.T);
+    rp.factor = p.factor;
+    rp.k_scale = p.k_scale;
+    rp.v_scale = p.v_scale;
+    return rope_launch(rp, p.dtype == FA_DTYPE_BF16, f8, static_cast<cudaStream_t>(stream));
 }
 
 // CTAs of the one cluster that looks a pool's reference counts over.
