@@ -445,6 +445,38 @@ typedef struct fa_append_params {
 int fa_cache_append(const fa_append_params* p, void* stream);
 
 /*
+ * Latent attention (no counterpart in the paper): a token's keys and values of all heads come from one latent vector l_j, and one rotated vector
+ * r_j that the heads share is the end of every head's key.  Two forms, for prompts and for new tokens:
+ *
+ * fa_forward_latent, the expanded form: keys and values of each head have been formed from the latent vectors (a matrix product), and
+ *     O[i,h,:] = sum_j softmax_j( scale * (<q[i,h,:], k[j,h,:]> + <q_rope[i,h,:], k_rope[j,:]>) + mask(i,j) ) * v[j,h,:]
+ * over a packed batch as in fa_forward_varlen (cu_seqlens_q, cu_seqlens_k, max_seqlen_q, max_seqlen_k, the bottom-right aligned mask, rows that
+ * see no key, what is read of the next sequence: all as there).
+ *   q [total_q,H,128], q_rope [total_q,H,64], k, v [total_k,H,128], k_rope [total_k,64], o [total_q,H,128], lse [H,total_q] float or NULL, of dtype.
+ *   The last dimension is contiguous; strides in elements from one token and head to the next, multiples of 8, so that q and q_rope may be parts of one
+ *   tensor, k and v of another, and k_rope the ends of the latent cache's rows; o is contiguous.  d must be 128 and d_rope 64.
+ * Errors: as fa_forward_varlen.
+ */
+typedef struct fa_latent_params {
+    const void* q;
+    const void* q_rope;
+    const void* k;
+    const void* k_rope;
+    const void* v;
+    void* o;
+    float* lse; /* may be NULL */
+    const int* cu_seqlens_q; /* [B + 1], device */
+    const int* cu_seqlens_k;
+    int64_t q_stride[2], q_rope_stride[2], k_stride[2], v_stride[2]; /* token, head */
+    int64_t k_rope_stride;                                           /* token */
+    int B, H, total_q, total_k, max_seqlen_q, max_seqlen_k;
+    int d, d_rope;
+    int causal, dtype;
+    float scale;
+} fa_latent_params;
+int fa_forward_latent(const fa_latent_params* p, void* stream);
+
+/*
  * Decode over an 8-bit cache (Appendix D.2 evaluates the operator with 8-bit operands; in the
  * decode stage the cache dominates the traffic, so here it is the cached K and V that are 8-bit):
  * the computation of fa_decode with K = k_scale * k_cache and V = v_scale * v_cache, where

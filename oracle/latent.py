@@ -44,12 +44,12 @@ def append_places(n, B, T, cu, first, counts, rows, table=None, page=0, pages=0)
 
 
 def attention(q, k, v, scale, causal):
-    """q [n,dk], k [m,dk], v [m,dv]: (o [n,dv], lse [n]); causal: the n queries are the last of the m positions.  A row that sees
-    nothing gives zeros and -inf."""
+    """q [n,dk], k [m,dk], v [m,dv]: (o [n,dv], lse [n], sum P |V| [n,dv], sum |V| [dv]); causal: the n queries are the last of the m
+    positions.  A row that sees nothing gives zeros and -inf."""
     n, m = q.shape[0], k.shape[0]
     s = q.double() @ k.double().T * scale
     if causal:
         s = s.masked_fill(torch.arange(m)[None, :] > torch.arange(m - n, m)[:, None], -math.inf)
     lse = torch.logsumexp(s, 1) if m else torch.full((n,), -math.inf, dtype=torch.float64)
     p = torch.where(torch.isneginf(lse)[:, None], torch.zeros_like(s), torch.exp(s - lse.clamp(min=-1e300)[:, None]))
-    return p @ v.double(), lse, p @ v.double().abs()
+    return p @ v.double(), lse, p @ v.double().abs(), v.double().abs().sum(0)

@@ -90,6 +90,17 @@ lib.fa_cache_append.restype = _i
 lib.fa_cache_append.argtypes = [_p, _p]     # (an fa_append_params by reference, or its bytes)
 _APPEND = struct.Struct("@12P12q17i3f")     # fa_append_params
 assert _APPEND.size == ctypes.sizeof(fa_append_params)
+class fa_latent_params(ctypes.Structure):
+    _fields_ = [(name, _p) for name in ("q", "q_rope", "k", "k_rope", "v", "o", "lse", "cu_seqlens_q", "cu_seqlens_k")]
+    _fields_ += [(name + "_stride", ctypes.c_int64 * 2) for name in ("q", "q_rope", "k", "v")] + [("k_rope_stride", ctypes.c_int64)]
+    _fields_ += [(name, _i) for name in ("B", "H", "total_q", "total_k", "max_seqlen_q", "max_seqlen_k", "d", "d_rope", "causal", "dtype")]
+    _fields_ += [("scale", _f)]
+
+
+lib.fa_forward_latent.restype = _i
+lib.fa_forward_latent.argtypes = [_p, _p]   # (an fa_latent_params by reference, or its bytes)
+_LATENT = struct.Struct("@9P9q10if0q")      # fa_latent_params
+assert _LATENT.size == ctypes.sizeof(fa_latent_params)
 _FA16 = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16}
 _FA_PROBS = {**_FA16, torch.float32: FA_DTYPE_FP32}
 lib.fa_decode_tree_workspace_bytes.restype = _sz
@@ -143,7 +154,7 @@ FA_DECODE_NOALLOC_BYTES = 4 << 20
 
 EXPORTS = ["fa_forward", "fa_forward_bf16", "fa_forward_ex", "fa_forward_fp8", "fa_forward_proj", "fa_forward_proj_workspace_bytes", "fa_decode", "fa_decode_workspace_bytes",
            "fa_decode_noalloc", "fa_decode_paged", "fa_forward_varlen", "fa_decode_fp8", "fa_decode_fp8_paged", "fa_decode_fp8_bf16", "fa_decode_fp8_paged_bf16", "fa_decode_append", "fa_decode_append_workspace_bytes", "fa_decode_ex", "fa_forward_varlen_paged",
-           "fa_decode_tree", "fa_decode_tree_workspace_bytes", "fa_spec_verify", "fa_cache_compact", "fa_pages_resize", "fa_pages_fork", "fa_rope", "fa_cache_append",
+           "fa_decode_tree", "fa_decode_tree_workspace_bytes", "fa_spec_verify", "fa_cache_compact", "fa_pages_resize", "fa_pages_fork", "fa_rope", "fa_cache_append", "fa_forward_latent",
            "fa_forward_host", "fa_forward_host_staging_bytes", "fa_device_status", "fa_selftest_wait", "fa_selftest_decode_cut", "fa_strerror",
            "fa_version", "fa_last_cuda_error"]
 
@@ -644,6 +655,33 @@ def fa_cache_append(q, q_out, k, v, k_cache, v_cache, first_rows, turns=None, po
                      qt, qh, ot, oh, kt, kh, vt, vh, ks, kr, vs, vr, n, B, T, Hq, Hkv, d, dv, rot, offset if rot else 0, 1 if interleaved else 0,
                      _FA16[dt], FA_DTYPE_E4M3 if f8 else _FA16[dt], *sizes, factor, k_scale, v_scale)
     rc = lib.fa_cache_append(p, _stream())
+    return _check(rc, what, raise_on_error) if rc else rc
+
+
+def fa_forward_latent(q, q_rope, k, k_rope, v, o, lse, cu_seqlens_q, cu_seqlens_k, max_seqlen_q: int, max_seqlen_k: int, causal: bool, scale: float,
+                      raise_on_error: bool = True) -> int:
+    """``fa_forward_latent``: a packed batch, q [total_q,H,128] and q_rope [total_q,H,64], k, v [total_k,H,128], k_rope [total_k,64] shared
+    by the heads, all with any strides of tokens and heads; o [total_q,H,128] contiguous, lse [H,total_q] or None; cu_seqlens_* int32 [B+1]."""
+    what, dt = "fa_forward_latent", q.dtype
+    if not ((dt is _HALF or dt is _BF16) and all(t.dtype is dt for t in (q_rope, k, k_rope, v, o))):
+        raise ValueError(f"{what}: q, q_rope, k, k_rope, v and o share one 16-bit type")
+    if lse is not None and lse.dtype is not _FLOAT:
+        raise ValueError(f"{what}: lse is float32")
+    _int32(what, cu_seqlens_q, cu_seqlens_k)
+    _contiguous(what, o, lse, cu_seqlens_q, cu_seqlens_k)
+    n, H, d, qt, qh = _tokens(what, q)
+    nr, hr, rope, rt, rh = _tokens(what, q_rope)
+    m, hk, dk, kt, kh = _tokens(what, k)
+    mv, hv, dv, vt, vh = _tokens(what, v)
+    if not (nr == n and hr == hk == hv == H and dk == dv == d and mv == m and k_rope.shape == (m, rope) and o.shape == (n, H, d)
+            and (lse is None or lse.numel() == H * n) and cu_seqlens_k.numel() == cu_seqlens_q.numel() >= 1):
+        _shapes(what, q=q, q_rope=q_rope, k=k, k_rope=k_rope, v=v, o=o, lse=lse, cu_seqlens_q=cu_seqlens_q, cu_seqlens_k=cu_seqlens_k)
+    if k_rope.stride(1) != 1:
+        raise ValueError(f"{what}: the columns of k_rope are contiguous")
+    p = _LATENT.pack(q.data_ptr(), q_rope.data_ptr(), k.data_ptr(), k_rope.data_ptr(), v.data_ptr(), o.data_ptr(), 0 if lse is None else lse.data_ptr(),
+                     cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), qt, qh, rt, rh, kt, kh, vt, vh, k_rope.stride(0) if m > 1 else 0,
+                     cu_seqlens_q.numel() - 1, H, n, m, max_seqlen_q, max_seqlen_k, d, rope, 1 if causal else 0, _FA16[dt], scale)
+    rc = lib.fa_forward_latent(p, _stream())
     return _check(rc, what, raise_on_error) if rc else rc
 
 

@@ -742,30 +742,10 @@ int fa_forward_ex(const fa_params* p, void* stream) {
 
 // Packed batch; K and V packed too (block_table == nullptr: k, v [total_k,Hkv,d], cu_seqlens_k) or in
 // pages (k, v [num_pages,page_size,Hkv,d], seqlens_k and the block table; total_k = num_pages * page_size).
-static int varlen_impl(const void* q, const void* k, const void* v, void* o, float* lse, const int* cu_seqlens_q,
-                       const int* cu_seqlens_k, int B, int Hq, int Hkv, int total_q, int total_k, int max_seqlen_q,
-                       int max_seqlen_k, int d, int causal, float scale, int dtype, void* stream,
-                       const int* block_table, int num_pages, int page_size, int table_stride) {
-    if (B < 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || total_k < 0 || max_seqlen_q < 0 || max_seqlen_k < 0 || d <= 0)
-        return FA_ERR_SHAPE;
-    if (Hq % Hkv) return FA_ERR_SHAPE;
-    if (max_seqlen_q > total_q || (!block_table && max_seqlen_k > total_k)) return FA_ERR_SHAPE;
-    if (d != 128 && d != 64) return FA_ERR_UNSUPPORTED;
-    if (dtype != FA_DTYPE_FP16 && dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
-    if (!(scale >= 0.f) || isinf(scale)) return FA_ERR_UNSUPPORTED;
-    if (Hq > 65535 || B > 65535) return FA_ERR_UNSUPPORTED;
-    if (B == 0 || total_q == 0 || max_seqlen_q == 0) return FA_OK;
-    if (!q || !o || !cu_seqlens_q || !cu_seqlens_k) return FA_ERR_NULL;
-    if (total_k > 0 && (!k || !v)) return FA_ERR_NULL;
-    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return FA_ERR_ALIGN;
-    if ((reinterpret_cast<uintptr_t>(cu_seqlens_q) | reinterpret_cast<uintptr_t>(cu_seqlens_k) |
-         reinterpret_cast<uintptr_t>(lse)) & 3u)
-        return FA_ERR_ALIGN;
-    int rc = check_device();
-    if (rc) return rc;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool bf16 = dtype == FA_DTYPE_BF16;
-
+// Kernel parameters of a packed batch, from validated arguments.
+static fa::FwdParams packed_fwd_params(void* o, float* lse, const int* cu_seqlens_q, const int* cu_seqlens_k, int B, int Hq, int Hkv, int total_q,
+                                       int max_seqlen_q, int max_seqlen_k, int d, int causal, float scale, const int* block_table, int page_size,
+                                       int table_stride) {
     fa::FwdParams fp;
     fp.o = o;
     fp.lse = lse;
@@ -796,18 +776,48 @@ static int varlen_impl(const void* q, const void* k, const void* v, void* o, flo
     fp.table_stride = table_stride;
     fp.page_size = block_table ? page_size : 1;
     fp.by_tiles_per_page.set(block_table ? page_size / fa::kTile : 1);
+    return fp;
+}
 
-    if (total_k == 0 || max_seqlen_k == 0) {
-        // no keys anywhere: O = 0, LSE = -inf over the packed rows, seen as one sequence
-        fa::FwdParams fe = fp;
-        fe.B = 1; fe.Sq = total_q;
-        const long long rows = (long long)total_q * Hq;
-        const int blocks = (int)((rows + 127) / 128 < 4096 ? (rows + 127) / 128 : 4096);
-        if (bf16) fa::fa_fill_empty_kernel<__nv_bfloat16><<<blocks, 128, 0, st>>>(fe);
-        else fa::fa_fill_empty_kernel<__half><<<blocks, 128, 0, st>>>(fe);
-        cudaError_t e = cudaGetLastError();
-        return e == cudaSuccess ? FA_OK : cuda_fail(e);
-    }
+// No keys anywhere: O = 0, LSE = -inf over the packed rows, seen as one sequence.
+static int fill_packed(const fa::FwdParams& fp, bool bf16, cudaStream_t st) {
+    fa::FwdParams fe = fp;
+    fe.B = 1; fe.Sq = fp.total_q;
+    const long long rows = (long long)fp.total_q * fp.Hq;
+    const int blocks = (int)((rows + 127) / 128 < 4096 ? (rows + 127) / 128 : 4096);
+    if (bf16) fa::fa_fill_empty_kernel<__nv_bfloat16><<<blocks, 128, 0, st>>>(fe);
+    else fa::fa_fill_empty_kernel<__half><<<blocks, 128, 0, st>>>(fe);
+    cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+static int varlen_impl(const void* q, const void* k, const void* v, void* o, float* lse, const int* cu_seqlens_q,
+                       const int* cu_seqlens_k, int B, int Hq, int Hkv, int total_q, int total_k, int max_seqlen_q,
+                       int max_seqlen_k, int d, int causal, float scale, int dtype, void* stream,
+                       const int* block_table, int num_pages, int page_size, int table_stride) {
+    if (B < 0 || Hq <= 0 || Hkv <= 0 || total_q < 0 || total_k < 0 || max_seqlen_q < 0 || max_seqlen_k < 0 || d <= 0)
+        return FA_ERR_SHAPE;
+    if (Hq % Hkv) return FA_ERR_SHAPE;
+    if (max_seqlen_q > total_q || (!block_table && max_seqlen_k > total_k)) return FA_ERR_SHAPE;
+    if (d != 128 && d != 64) return FA_ERR_UNSUPPORTED;
+    if (dtype != FA_DTYPE_FP16 && dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    if (!(scale >= 0.f) || isinf(scale)) return FA_ERR_UNSUPPORTED;
+    if (Hq > 65535 || B > 65535) return FA_ERR_UNSUPPORTED;
+    if (B == 0 || total_q == 0 || max_seqlen_q == 0) return FA_OK;
+    if (!q || !o || !cu_seqlens_q || !cu_seqlens_k) return FA_ERR_NULL;
+    if (total_k > 0 && (!k || !v)) return FA_ERR_NULL;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o)) return FA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(cu_seqlens_q) | reinterpret_cast<uintptr_t>(cu_seqlens_k) |
+         reinterpret_cast<uintptr_t>(lse)) & 3u)
+        return FA_ERR_ALIGN;
+    int rc = check_device();
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool bf16 = dtype == FA_DTYPE_BF16;
+
+    const fa::FwdParams fp = packed_fwd_params(o, lse, cu_seqlens_q, cu_seqlens_k, B, Hq, Hkv, total_q, max_seqlen_q, max_seqlen_k, d, causal, scale,
+                                               block_table, page_size, table_stride);
+    if (total_k == 0 || max_seqlen_k == 0) return fill_packed(fp, bf16, st);
     // the packed tensors as one batch entry; a sequence's rows are reached through the prefix sums
     CUtensorMap tq, tk, tv, to;
     rc = encode_map_tile(&tq, q, 1, total_q, Hq, (int64_t)total_q * Hq * d, (int64_t)Hq * d, d, 128, bf16, d);
@@ -848,6 +858,48 @@ int fa_forward_varlen_paged(const void* q, const void* k_pages, const void* v_pa
     return varlen_impl(q, k_pages, v_pages, o, lse, cu_seqlens_q, seqlens_k, B, Hq, Hkv, total_q, num_pages * page_size,
                        max_seqlen_q, max_seqlen_k, d, causal, scale, dtype, stream, block_table, num_pages, page_size,
                        table_stride);
+}
+
+int fa_forward_latent(const fa_latent_params* pp, void* stream) {
+    if (!pp) return FA_ERR_NULL;
+    const fa_latent_params& p = *pp;
+    if (p.B < 0 || p.H <= 0 || p.total_q < 0 || p.total_k < 0 || p.max_seqlen_q < 0 || p.max_seqlen_k < 0 || p.d <= 0 || p.d_rope <= 0)
+        return FA_ERR_SHAPE;
+    if (p.max_seqlen_q > p.total_q || p.max_seqlen_k > p.total_k) return FA_ERR_SHAPE;
+    if (p.d != 128 || p.d_rope != 64) return FA_ERR_UNSUPPORTED;
+    if (p.dtype != FA_DTYPE_FP16 && p.dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    if (!(p.scale >= 0.f) || isinf(p.scale)) return FA_ERR_UNSUPPORTED;
+    if (p.H > 65535 || p.B > 65535) return FA_ERR_UNSUPPORTED;
+    const int64_t* strides[4] = {p.q_stride, p.q_rope_stride, p.k_stride, p.v_stride};
+    for (int i = 0; i < 4; ++i) {
+        const int64_t s[3] = {0, strides[i][0], strides[i][1]};
+        if (!strides_ok(s, 1, i < 2 ? p.total_q : p.total_k, p.H, i == 1 ? p.d_rope : p.d)) return FA_ERR_SHAPE;
+    }
+    const int64_t kr[3] = {0, p.k_rope_stride, 0};
+    if (!strides_ok(kr, 1, p.total_k, 1, p.d_rope)) return FA_ERR_SHAPE;
+    if (p.B == 0 || p.total_q == 0 || p.max_seqlen_q == 0) return FA_OK;
+    if (!p.q || !p.q_rope || !p.o || !p.cu_seqlens_q || !p.cu_seqlens_k) return FA_ERR_NULL;
+    if (p.total_k > 0 && (!p.k || !p.k_rope || !p.v)) return FA_ERR_NULL;
+    if (!aligned16(p.q) || !aligned16(p.q_rope) || !aligned16(p.k) || !aligned16(p.k_rope) || !aligned16(p.v) || !aligned16(p.o)) return FA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(p.cu_seqlens_q) | reinterpret_cast<uintptr_t>(p.cu_seqlens_k) | reinterpret_cast<uintptr_t>(p.lse)) & 3u)
+        return FA_ERR_ALIGN;
+    int rc = check_device();
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool bf16 = p.dtype == FA_DTYPE_BF16;
+    const fa::FwdParams fp = packed_fwd_params(p.o, p.lse, p.cu_seqlens_q, p.cu_seqlens_k, p.B, p.H, p.H, p.total_q, p.max_seqlen_q, p.max_seqlen_k, p.d,
+                                               p.causal, p.scale, nullptr, 1, 0);
+    if (p.total_k == 0 || p.max_seqlen_k == 0) return fill_packed(fp, bf16, st);
+    CUtensorMap tq, tk, tv, to, tqr, tkr;
+    rc = encode_map_tile(&tq, p.q, 1, p.total_q, p.H, 0, p.q_stride[0], p.q_stride[1], 128, bf16, p.d);
+    if (!rc) rc = encode_map(&tqr, p.q_rope, 1, p.total_q, p.H, 0, p.q_rope_stride[0], p.q_rope_stride[1], 128, bf16, p.d_rope);
+    if (!rc) rc = encode_map(&tk, p.k, 1, p.total_k, p.H, 0, p.k_stride[0], p.k_stride[1], 128, bf16, p.d);
+    if (!rc) rc = encode_map(&tkr, p.k_rope, 1, p.total_k, 1, 0, p.k_rope_stride, p.d_rope, 128, bf16, p.d_rope);
+    if (!rc) rc = encode_map_tile(&tv, p.v, 1, p.total_k, p.H, 0, p.v_stride[0], p.v_stride[1], 128, bf16, p.d);
+    if (!rc) rc = encode_map_tile(&to, p.o, 1, p.total_q, p.H, 0, (int64_t)p.H * p.d, p.d, 32, bf16, p.d);
+    if (rc) return rc;
+    return bf16 ? fa::launch_latent<__nv_bfloat16>(tq, tk, tv, to, tqr, tkr, fp, st, &t_last_cuda_error)
+                : fa::launch_latent<__half>(tq, tk, tv, to, tqr, tkr, fp, st, &t_last_cuda_error);
 }
 
 size_t fa_decode_workspace_bytes(int B, int Hq, int Hkv, int Skv_max, int d) {

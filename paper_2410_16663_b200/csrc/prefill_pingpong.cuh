@@ -56,15 +56,23 @@ static_assert((kPpQBufs + kPpNK + kPpNV) * kTileBytes + 3072 <= 232448, "shared 
 // Head dimension 64 (D; 16-bit operands only) has the same byte layout: a row of a Q, K or V tile
 // is 64 elements = 128 bytes, one box; Q K^T then contracts over four MMAs of 16 elements, P V is
 // eight MMAs of 16 keys with N = 64, and O takes 64 columns of tensor memory.
-template <bool kF8, int D = 128>
+//
+// Keys with a part that all heads share (DR = 64; latent attention's expanded form, D = 128 and 16-bit operands, packed batches): S gets
+// four more MMAs from a third box of Q and of K, whose map has one head.  224 KiB then hold one Q buffer, two V slots and seven K boxes, each
+// of which goes back when its own four MMAs are done.  (Two whole slots of three boxes left a K tile too little time to arrive.)
+template <bool kF8, int D = 128, int DR = 0>
 struct PpOperands {
     static_assert(D == 128 || (D == 64 && !kF8), "head dimension 128, or 64 with 16-bit operands");
+    static_assert(DR == 0 || (DR == 64 && D == 128 && !kF8), "a shared part of 64 behind 128 16-bit elements");
+    static constexpr int kQBufs = DR ? 1 : kPpQBufs;
+    static constexpr int kKSlots = DR ? 7 : kPpNK;                      // DR: boxes
     static constexpr bool kOneBox = kF8 || D == 64;                     // a tile row is 128 bytes
-    static constexpr int kKvSlotBytes = kOneBox ? 16384 : kTileBytes;   // one K ring slot, and the bytes of a K or V tile
+    static constexpr int kKvSlotBytes = kOneBox ? 16384 : kTileBytes;   // one K ring slot (DR: two boxes of it), and the bytes of a K or V tile
+    static constexpr int kKBytes = DR ? 16384 : kKvSlotBytes;           // one K ring slot
     static constexpr int kVSlotBytes = D == 64 ? 16384 : kTileBytes;    // one V ring slot: a V tile, later an output tile
-    static constexpr int kQBytes = kOneBox ? 16384 : kTileBytes;        // bytes a Q load delivers
-    static constexpr int kQBufBytes = kF8 ? 16384 : kTileBytes;         // one Q buffer (d = 64 with 16 KiB: 512 x 12 x 128 66.4 -> 66.8 us)
-    static constexpr int kSmem = kPpQBufs * kQBufBytes + kPpNK * kKvSlotBytes + kPpNV * kVSlotBytes;   // 224 KiB; 8-bit and d = 64 144
+    static constexpr int kQBytes = DR ? kTileBytes + 16384 : kOneBox ? 16384 : kTileBytes;   // bytes a Q load delivers
+    static constexpr int kQBufBytes = DR ? kQBytes : kF8 ? 16384 : kTileBytes;   // one Q buffer (d = 64 with 16 KiB: 512 x 12 x 128 66.4 -> 66.8 us)
+    static constexpr int kSmem = kQBufs * kQBufBytes + kKSlots * kKBytes + kPpNV * kVSlotBytes;   // 224 KiB; 8-bit and d = 64 144
     static constexpr int kSteps = kOneBox ? 4 : 8;                      // MMAs of Q K^T (32 bytes of every row each)
     static constexpr int kPvSteps = kF8 ? 4 : 8;                        // MMAs of P V (32 or 16 keys each)
     static constexpr int kPCols = kF8 ? 8 : 16;                         // tensor-memory columns of 32 probabilities
@@ -93,6 +101,10 @@ constexpr int m_ready = p_full + 2;             // [2]  softmax of step g -> sof
 constexpr int l_pub = m_ready + 2;              // [2]  softmax of an item's last-but-one step -> of its last step
 constexpr int o_free = l_pub + 2;               // [1]  epilogue -> PV thread
 constexpr int count = o_free + 1;
+// K in boxes (PpOperands, DR): full and empty, in place of k_full and k_empty
+constexpr int kb_full = count;                  // [7]
+constexpr int kb_empty = kb_full + 7;           // [7]
+constexpr int count_boxes = kb_empty + 7;
 }  // namespace ppb
 
 struct __align__(16) PpItem {
@@ -106,7 +118,7 @@ struct __align__(16) PpItem {
 };
 
 struct PpStatic {
-    uint64_t bars[ppb::count];
+    uint64_t bars[ppb::count_boxes];
     uint32_t tmem_holder;
     uint32_t abort_flag;
     float m_xch[2][128];   // [warpgroup][row]: reference max after that warpgroup's latest step
@@ -444,22 +456,38 @@ struct PpRing {
 };
 
 // The thread that issues S = Q K^T of every step.
-template <typename T, bool kVarlen, bool kF8, int D>
+template <typename T, bool kVarlen, bool kF8, int D, int DR = 0>
 __device__ __forceinline__ void pp_run_s(uint32_t bar0, uint32_t sQ, uint32_t sK, uint32_t tmem, const PpItem* slots,
                                          volatile uint32_t* abort_flag) {
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     constexpr uint32_t idesc = kF8 ? instr_desc_e4m3(128, 128, false, false) : instr_desc_f16(kBf16, 128, 128, false, false);
-    using Op = PpOperands<kF8, D>;
+    using Op = PpOperands<kF8, D, DR>;
     uint32_t g = 0;
-    PpRing<kPpNK> ring;
+    PpRing<Op::kKSlots> ring;
     PpTaker<kVarlen> items{slots, bar0, abort_flag};
     PpItem it;
     while (items.next(it, 133)) {
         const int ord = items.ord;
-        const uint32_t qb = ord & 1;
-        if (!mbar_wait(pp_bar(bar0, ppb::q_full + qb), (ord >> 1) & 1, abort_flag, 130)) return;
+        const uint32_t qb = DR ? 0 : ord & 1;
+        if (!mbar_wait(pp_bar(bar0, ppb::q_full + qb), (DR ? ord : ord >> 1) & 1, abort_flag, 130)) return;
         const uint32_t a_lo = desc_lo(sQ + qb * Op::kQBufBytes, 16);
-        for (int j = 0; j < it.n; ++j, ++g, ring.next()) {
+        if constexpr (DR > 0) {
+            for (int j = 0; j < it.n; ++j, ++g) {
+                const uint32_t buf = g & 1;
+#pragma unroll
+                for (int box = 0; box < 3; ++box, ring.next()) {
+                    if (!mbar_wait(pp_bar(bar0, ppb::kb_full + ring.slot), ring.par, abort_flag, 131)) return;
+                    if (box == 0 && g >= 2 && !mbar_wait(pp_bar(bar0, ppb::m_ready + buf), ((g >> 1) - 1) & 1, abort_flag, 132)) return;
+                    tc_fence_after();
+                    const uint32_t a_box = a_lo + box * (16384 >> 4), b_lo = desc_lo(sK + ring.slot * Op::kKBytes, 16);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks) mma_ss_lo(tmem + 128 + 128 * buf, a_box + ks * 2, b_lo + ks * 2, idesc, box > 0 || ks > 0 ? 1u : 0u);
+                    if (box == 2) mma_commit(pp_bar(bar0, ppb::s_full + buf));
+                    mma_commit(pp_bar(bar0, ppb::kb_empty + ring.slot));
+                }
+                if (j == it.n - 1) mma_commit(pp_bar(bar0, ppb::q_empty + qb));
+            }
+        } else for (int j = 0; j < it.n; ++j, ++g, ring.next()) {
             const uint32_t buf = g & 1;
             if (!mbar_wait(pp_bar(bar0, ppb::k_full + ring.slot), ring.par, abort_flag, 131)) return;
             // the softmax of step g-2 has read its scores out of this buffer (it says so together
@@ -559,14 +587,21 @@ __device__ __forceinline__ void pp_load_tile(uint32_t dst, const CUtensorMap* tm
     else tma_load_5d_hint(dst, tm, bar, 0, s0, 0, h, b, policy);
 }
 
-template <bool kVarlen, bool kF8, int D>
+// Keys with a shared part: tm_k's boxes are one block wide, tm_qr and tm_kr are over the third box.  The one Q buffer is free when the
+// item before has issued its last S, about two steps ahead of its end: the first K boxes are asked for before that is waited for.
+template <bool kVarlen, bool kF8, int D, int DR = 0>
 __device__ __forceinline__ void pp_run_load_qk(uint32_t bar0, uint32_t sQ, uint32_t sK, const CUtensorMap* tm_q,
                                                const CUtensorMap* tm_k, const FwdParams& p, int total_items, PpStatic& ss,
-                                               volatile uint32_t* abort_flag) {
+                                               volatile uint32_t* abort_flag, const CUtensorMap* tm_qr = nullptr,
+                                               const CUtensorMap* tm_kr = nullptr) {
     tma_prefetch_desc(tm_q);
     tma_prefetch_desc(tm_k);
+    if constexpr (DR > 0) {
+        tma_prefetch_desc(tm_qr);
+        tma_prefetch_desc(tm_kr);
+    }
     const uint64_t pol_q = l2_policy_evict_first(), pol_kv = l2_policy_evict_last();
-    PpRing<kPpNK> ring;
+    PpRing<PpOperands<kF8, D, DR>::kKSlots> ring;
     PpSource<kVarlen> source{p, total_items, pp_bar(bar0, ppb::claim), smem_u32(&ss.claim_answer), abort_flag,
                              {p.deal_ctas, p.deal_rounds}};
     source.walk.take(blockIdx.x);
@@ -591,22 +626,43 @@ __device__ __forceinline__ void pp_run_load_qk(uint32_t bar0, uint32_t sQ, uint3
             if (*abort_flag) return;   // (a role did not get the item in time: nothing is loaded)
         }
         if (it.n == 0) return;
-        const uint32_t qb = ord & 1;
-        // passes at once the first time each buffer is used
-        if (!mbar_wait(pp_bar(bar0, ppb::q_empty + qb), ((ord >> 1) & 1) ^ 1, abort_flag, 150)) return;
-        mbar_expect_tx(pp_bar(bar0, ppb::q_full + qb), PpOperands<kF8, D>::kQBytes);
-        pp_load_tile<PpOperands<kF8, D>::kOneBox>(sQ + qb * PpOperands<kF8, D>::kQBufBytes, tm_q, pp_bar(bar0, ppb::q_full + qb), it.h,
-                       kVarlen ? it.q_base + it.q0 : it.q0, kVarlen ? 0 : it.b, pol_q);
-        int page = (kVarlen && p.block_table != nullptr) ? it.page0 : 0;
-        for (int j = 0; j < it.n; ++j, ring.next()) {
-            const int page_next = pp_page_of<kVarlen>(p, it.b, j + 1, it.n, it.Skv);
-            if (j == it.n - 1) source.request_next();
-            if (!mbar_wait(pp_bar(bar0, ppb::k_empty + ring.slot), ring.par ^ 1, abort_flag, 151)) return;
-            mbar_expect_tx(pp_bar(bar0, ppb::k_full + ring.slot), PpOperands<kF8, D>::kKvSlotBytes);
-            int row = kVarlen ? it.k_base + j * kTile : (it.j0 + j) * kTile, slab = kVarlen ? 0 : it.b;
-            pp_paged_tile<kVarlen>(p, page, j, row, slab);
-            page = page_next;
-            pp_load_tile<PpOperands<kF8, D>::kOneBox>(sK + ring.slot * PpOperands<kF8, D>::kKvSlotBytes, tm_k, pp_bar(bar0, ppb::k_full + ring.slot), it.hk, row, slab, pol_kv);
+        if constexpr (DR > 0) {
+            int box = 0;
+            auto load_k = [&](int upto) {   // boxes of the item's K tiles, up to this one
+                for (; box < upto; ++box, ring.next()) {
+                    const int j = box / 3, part = box - 3 * j;
+                    if (box == 3 * (it.n - 1)) source.request_next();
+                    if (!mbar_wait(pp_bar(bar0, ppb::kb_empty + ring.slot), ring.par ^ 1, abort_flag, 151)) return false;
+                    mbar_expect_tx(pp_bar(bar0, ppb::kb_full + ring.slot), 16384);
+                    tma_load_4d_hint(sK + ring.slot * 16384, part < 2 ? tm_k : tm_kr, pp_bar(bar0, ppb::kb_full + ring.slot), part < 2 ? 64 * part : 0,
+                                     part < 2 ? it.hk : 0, it.k_base + j * kTile, 0, pol_kv);
+                }
+                return true;
+            };
+            if (!load_k(3)) return;
+            if (!mbar_wait(pp_bar(bar0, ppb::q_empty), (ord & 1) ^ 1, abort_flag, 150)) return;
+            mbar_expect_tx(pp_bar(bar0, ppb::q_full), PpOperands<kF8, D, DR>::kQBytes);
+            pp_load_tile<false>(sQ, tm_q, pp_bar(bar0, ppb::q_full), it.h, it.q_base + it.q0, 0, pol_q);
+            tma_load_4d_hint(sQ + kTileBytes, tm_qr, pp_bar(bar0, ppb::q_full), 0, it.h, it.q_base + it.q0, 0, pol_q);
+            if (!load_k(3 * it.n)) return;
+        } else {
+            const uint32_t qb = ord & 1;
+            // passes at once the first time each buffer is used
+            if (!mbar_wait(pp_bar(bar0, ppb::q_empty + qb), ((ord >> 1) & 1) ^ 1, abort_flag, 150)) return;
+            mbar_expect_tx(pp_bar(bar0, ppb::q_full + qb), PpOperands<kF8, D>::kQBytes);
+            pp_load_tile<PpOperands<kF8, D>::kOneBox>(sQ + qb * PpOperands<kF8, D>::kQBufBytes, tm_q, pp_bar(bar0, ppb::q_full + qb), it.h,
+                           kVarlen ? it.q_base + it.q0 : it.q0, kVarlen ? 0 : it.b, pol_q);
+            int page = (kVarlen && p.block_table != nullptr) ? it.page0 : 0;
+            for (int j = 0; j < it.n; ++j, ring.next()) {
+                const int page_next = pp_page_of<kVarlen>(p, it.b, j + 1, it.n, it.Skv);
+                if (j == it.n - 1) source.request_next();
+                if (!mbar_wait(pp_bar(bar0, ppb::k_empty + ring.slot), ring.par ^ 1, abort_flag, 151)) return;
+                mbar_expect_tx(pp_bar(bar0, ppb::k_full + ring.slot), PpOperands<kF8, D>::kKvSlotBytes);
+                int row = kVarlen ? it.k_base + j * kTile : (it.j0 + j) * kTile, slab = kVarlen ? 0 : it.b;
+                pp_paged_tile<kVarlen>(p, page, j, row, slab);
+                page = page_next;
+                pp_load_tile<PpOperands<kF8, D>::kOneBox>(sK + ring.slot * PpOperands<kF8, D>::kKvSlotBytes, tm_k, pp_bar(bar0, ppb::k_full + ring.slot), it.hk, row, slab, pol_kv);
+            }
         }
     }
 }
@@ -962,15 +1018,19 @@ __device__ __forceinline__ void pp_split_merge(const FwdParams& p, uint32_t part
 // them in done[batch * n_qtiles + query tile], 32 rows as one; four of them and Hq heads make a row
 // block of O complete.
 // The whole kernel but for the release of tensor memory; returns false if nothing was set up.
-template <typename T, bool kTmaOut, bool kVarlen, bool kF8, bool kProj, int D = 128, bool kSplit = false>
+// DR: see PpOperands (kVarlen alone; tm_qr, tm_kr: the maps of the third box).
+template <typename T, bool kTmaOut, bool kVarlen, bool kF8, bool kProj, int D = 128, bool kSplit = false, int DR = 0>
 __device__ __forceinline__ bool pp_attention(const CUtensorMap& tm_q, const CUtensorMap& tm_k, const CUtensorMap& tm_v,
                                              const CUtensorMap& tm_o, const FwdParams& p, const int total_items,
-                                             PpStatic& ss, const uint32_t smem_base, unsigned int* done) {
+                                             PpStatic& ss, const uint32_t smem_base, unsigned int* done,
+                                             const CUtensorMap* tm_qr = nullptr, const CUtensorMap* tm_kr = nullptr) {
+    static_assert(DR == 0 || kVarlen, "packed batches have a shared part");
     static_assert(!kSplit || (!kTmaOut && !kVarlen && !kF8 && !kProj && D == 128), "one form shares query tiles");
     static_assert(!kProj || (kTmaOut && !kVarlen && D == 128), "the projection phase reads a contiguous 16-bit O of d = 128");
     const uint32_t sQ = smem_base;
-    const uint32_t sK = sQ + kPpQBufs * PpOperands<kF8, D>::kQBufBytes;
-    const uint32_t sV = sK + kPpNK * PpOperands<kF8, D>::kKvSlotBytes;
+    using Op = PpOperands<kF8, D, DR>;
+    const uint32_t sK = sQ + Op::kQBufs * Op::kQBufBytes;
+    const uint32_t sV = sK + Op::kKSlots * Op::kKBytes;
     const uint32_t bar0 = smem_u32(&ss.bars[0]);
     volatile uint32_t* abort_flag = &ss.abort_flag;
 
@@ -982,10 +1042,10 @@ __device__ __forceinline__ bool pp_attention(const CUtensorMap& tm_q, const CUte
         return false;
     }
     if (tid == 0) {
-        for (int i = 0; i < ppb::count; ++i) {
+        for (int i = 0; i < (DR ? ppb::count_boxes : ppb::count); ++i) {
             const bool staged = i == ppb::o_staged || i == ppb::o_staged + 1;
             const bool slot_back = i >= ppb::item_empty && i < ppb::item_empty + kPpSlots;
-            mbar_init(pp_bar(bar0, i), i >= ppb::p_full ? 128 : (slot_back ? 11 : (staged ? 4 : 1)));
+            mbar_init(pp_bar(bar0, i), i >= ppb::p_full && (DR == 0 || i < ppb::count) ? 128 : (slot_back ? 11 : (staged ? 4 : 1)));
         }
         ss.abort_flag = 0;
         fence_mbar_init();
@@ -1184,9 +1244,9 @@ __device__ __forceinline__ bool pp_attention(const CUtensorMap& tm_q, const CUte
     } else {
         setmaxnreg_dec<kPipeOtherRegs>();
         if (elect_one()) {
-            if (warp == 8) pp_run_s<T, kVarlen, kF8, D>(bar0, sQ, sK, tmem_base, ss.items, abort_flag);
+            if (warp == 8) pp_run_s<T, kVarlen, kF8, D, DR>(bar0, sQ, sK, tmem_base, ss.items, abort_flag);
             else if (warp == 10) pp_run_pv<T, kVarlen, kF8, D>(bar0, sV, tmem_base, ss.items, abort_flag);
-            else if (warp == 9) pp_run_load_qk<kVarlen, kF8, D>(bar0, sQ, sK, &tm_q, &tm_k, p, total_items, ss, abort_flag);
+            else if (warp == 9) pp_run_load_qk<kVarlen, kF8, D, DR>(bar0, sQ, sK, &tm_q, &tm_k, p, total_items, ss, abort_flag, tm_qr, tm_kr);
             else pp_run_v<kTmaOut, kVarlen, kF8, kProj, D>(bar0, sV, &tm_v, &tm_o, p, ss.items, abort_flag, done);
         }
         __syncwarp();
@@ -1233,6 +1293,26 @@ fa_fwd_pingpong_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_co
     PpStatic& ss = *reinterpret_cast<PpStatic*>(static_raw);
     if (!pp_attention<T, kTmaOut, kVarlen, kF8, false, D>(tm_q, tm_k, tm_v, tm_o, p, total_items, ss, smem_u32(smem_raw),
                                                           nullptr))
+        return;
+    tc_fence_before();
+    __syncthreads();
+    if ((threadIdx.x >> 5) == 8) {
+        settle_if(ss.abort_flag);
+        __syncwarp();
+        tmem_dealloc(ss.tmem_holder, 512);
+    }
+}
+
+// Latent attention's expanded form: a packed batch whose keys end in a part that the heads share.
+template <typename T>
+__global__ void __launch_bounds__(kPipeThreads, 1)
+fa_fwd_latent_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                     const __grid_constant__ CUtensorMap tm_o, const __grid_constant__ CUtensorMap tm_qr, const __grid_constant__ CUtensorMap tm_kr,
+                     const FwdParams p, const int total_items) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(1024) uint8_t static_raw[kPpStaticBytes];
+    PpStatic& ss = *reinterpret_cast<PpStatic*>(static_raw);
+    if (!pp_attention<T, true, true, false, false, 128, false, 64>(tm_q, tm_k, tm_v, tm_o, p, total_items, ss, smem_u32(smem_raw), nullptr, &tm_qr, &tm_kr))
         return;
     tc_fence_before();
     __syncthreads();
@@ -1367,6 +1447,31 @@ int launch_pingpong(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensor
         grid = fpc.deal_ctas + (int)rest;
     }
     e = launch_dependent(kern, dim3(grid), kPipeThreads, smem, st, tq, tk, tv, to, fpc, (int)total);
+    if (e != cudaSuccess) { *cuda_err = (int)e; return -7; }
+    return 0;
+}
+
+// The same deal as for other packed batches: all claimed.
+template <typename T>
+int launch_latent(const CUtensorMap& tq, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& to, const CUtensorMap& tqr,
+                  const CUtensorMap& tkr, const FwdParams& fp, cudaStream_t st, int* cuda_err) {
+    auto kern = fa_fwd_latent_kernel<T>;
+    constexpr int smem = PpOperands<false, 128, 64>::kSmem;
+    int sm_count = 0;
+    if (int ce = prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) { *cuda_err = ce; return -7; }
+    const long long all_tiles = (long long)fp.n_qtiles * fp.B, packed_tiles = (long long)(fp.total_q >> 7) + fp.B;
+    const bool fixed_places = all_tiles <= packed_tiles;
+    const long long total = (fixed_places ? all_tiles : packed_tiles) * fp.Hq;
+    if (total > 0x7fffffffll) return -3;
+    const int grid = (int)(total < sm_count ? total : sm_count);
+    FwdParams fpc = pp_plan_items(fp, grid, 512.0);
+    fpc.split = 1;
+    fpc.fixed_places = fixed_places;
+    fpc.early_next = grid < sm_count;
+    fpc.deal_rounds = 0;
+    fpc.deal_ctas = 0;
+    fpc.claim_items = 1;
+    const cudaError_t e = launch_dependent(kern, dim3((unsigned)total), kPipeThreads, smem, st, tq, tk, tv, to, tqr, tkr, fpc, (int)total);
     if (e != cudaSuccess) { *cuda_err = (int)e; return -7; }
     return 0;
 }
