@@ -477,6 +477,39 @@ typedef struct fa_latent_params {
 int fa_forward_latent(const fa_latent_params* p, void* stream);
 
 /*
+ * fa_decode_latent, the absorbed form: the T new tokens of each sequence attend over the latent cache as it is, whose rows (l_j, r_j) are the
+ * keys, and in their first part the values, of all heads,
+ *     o[b,t,h,:] = sum_j softmax_j( scale * (<q[b,t,h,:], l_j> + <q_rope[b,t,h,:], r_j>) ) * l_j
+ * with queries that have taken up their head's key expansion (q = W_h^T q_nope; its value expansion is applied to o).  The T tokens are
+ * the last rows of their sequence's cache, token t sees the rows 0 .. seqlens_k[b] - T + t (T <= 64).
+ *   q [B,T,H,512], q_rope [B,T,H,64]: strides in elements from one sequence, token and head to the next, multiples of 8, the last dimension
+ *   contiguous; cache [B,Skv_max,576], or with block_table [B,table_stride] the pool [num_pages,page_size,576] (page sizes as for fa_decode_paged),
+ *   contiguous: fa_cache_append writes its rows.  o [B,T,H,512] contiguous, lse [B,H,T] float or NULL; seqlens_k int32 [B] on the DEVICE, the T tokens
+ *   included, clamped to [0, Skv_max].  All of dtype.  Rows past a sequence's end may hold anything; inside it rows must be finite for
+ *   the tokens that do not see them, too.  A token that sees no key gives o = 0 and lse = -inf.  d must be 512 and d_rope 64.
+ *   workspace: fa_decode_latent_workspace_bytes(B, T, H, Skv_max or max_pages * page_size, d) bytes, 16-byte aligned.
+ * Errors: as fa_decode_ex.
+ */
+typedef struct fa_latent_decode_params {
+    const void* q;
+    const void* q_rope;
+    const void* cache;
+    void* o;
+    float* lse;             /* may be NULL */
+    const int* seqlens_k;   /* [B], device */
+    const int* block_table; /* NULL, or [B,table_stride] on the device */
+    int64_t q_stride[3], q_rope_stride[3]; /* sequence, token, head */
+    int B, T, H, Skv_max, d, d_rope;
+    int dtype;
+    int num_pages, page_size, max_pages, table_stride;
+    float scale;
+    void* workspace;
+    size_t workspace_bytes;
+} fa_latent_decode_params;
+int fa_decode_latent(const fa_latent_decode_params* p, void* stream);
+size_t fa_decode_latent_workspace_bytes(int B, int T, int H, int Skv_max, int d);
+
+/*
  * Decode over an 8-bit cache (Appendix D.2 evaluates the operator with 8-bit operands; in the
  * decode stage the cache dominates the traffic, so here it is the cached K and V that are 8-bit):
  * the computation of fa_decode with K = k_scale * k_cache and V = v_scale * v_cache, where

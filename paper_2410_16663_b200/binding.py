@@ -101,6 +101,19 @@ lib.fa_forward_latent.restype = _i
 lib.fa_forward_latent.argtypes = [_p, _p]   # (an fa_latent_params by reference, or its bytes)
 _LATENT = struct.Struct("@9P9q10if0q")      # fa_latent_params
 assert _LATENT.size == ctypes.sizeof(fa_latent_params)
+class fa_latent_decode_params(ctypes.Structure):
+    _fields_ = [(name, _p) for name in ("q", "q_rope", "cache", "o", "lse", "seqlens_k", "block_table")]
+    _fields_ += [("q_stride", ctypes.c_int64 * 3), ("q_rope_stride", ctypes.c_int64 * 3)]
+    _fields_ += [(name, _i) for name in ("B", "T", "H", "Skv_max", "d", "d_rope", "dtype", "num_pages", "page_size", "max_pages", "table_stride")]
+    _fields_ += [("scale", _f), ("workspace", _p), ("workspace_bytes", _sz)]
+
+
+lib.fa_decode_latent.restype = _i
+lib.fa_decode_latent.argtypes = [_p, _p]    # (an fa_latent_decode_params by reference, or its bytes)
+_LATENT_DECODE = struct.Struct("@7P6q11ifPN")
+assert _LATENT_DECODE.size == ctypes.sizeof(fa_latent_decode_params)
+lib.fa_decode_latent_workspace_bytes.restype = _sz
+lib.fa_decode_latent_workspace_bytes.argtypes = [_i, _i, _i, _i, _i]
 _FA16 = {torch.float16: FA_DTYPE_FP16, torch.bfloat16: FA_DTYPE_BF16}
 _FA_PROBS = {**_FA16, torch.float32: FA_DTYPE_FP32}
 lib.fa_decode_tree_workspace_bytes.restype = _sz
@@ -155,6 +168,7 @@ FA_DECODE_NOALLOC_BYTES = 4 << 20
 EXPORTS = ["fa_forward", "fa_forward_bf16", "fa_forward_ex", "fa_forward_fp8", "fa_forward_proj", "fa_forward_proj_workspace_bytes", "fa_decode", "fa_decode_workspace_bytes",
            "fa_decode_noalloc", "fa_decode_paged", "fa_forward_varlen", "fa_decode_fp8", "fa_decode_fp8_paged", "fa_decode_fp8_bf16", "fa_decode_fp8_paged_bf16", "fa_decode_append", "fa_decode_append_workspace_bytes", "fa_decode_ex", "fa_forward_varlen_paged",
            "fa_decode_tree", "fa_decode_tree_workspace_bytes", "fa_spec_verify", "fa_cache_compact", "fa_pages_resize", "fa_pages_fork", "fa_rope", "fa_cache_append", "fa_forward_latent",
+           "fa_decode_latent", "fa_decode_latent_workspace_bytes",
            "fa_forward_host", "fa_forward_host_staging_bytes", "fa_device_status", "fa_selftest_wait", "fa_selftest_decode_cut", "fa_strerror",
            "fa_version", "fa_last_cuda_error"]
 
@@ -682,6 +696,46 @@ def fa_forward_latent(q, q_rope, k, k_rope, v, o, lse, cu_seqlens_q, cu_seqlens_
                      cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), qt, qh, rt, rh, kt, kh, vt, vh, k_rope.stride(0) if m > 1 else 0,
                      cu_seqlens_q.numel() - 1, H, n, m, max_seqlen_q, max_seqlen_k, d, rope, 1 if causal else 0, _FA16[dt], scale)
     rc = lib.fa_forward_latent(p, _stream())
+    return _check(rc, what, raise_on_error) if rc else rc
+
+
+def fa_decode_latent_workspace_bytes(B: int, T: int, H: int, Skv_max: int, d: int = 512) -> int:
+    return int(lib.fa_decode_latent_workspace_bytes(B, T, H, Skv_max, d))
+
+
+def fa_decode_latent(q, q_rope, cache, o, lse, seqlens_k, scale: float, workspace, block_table=None, max_pages: int = None,
+                     raise_on_error: bool = True) -> int:
+    """``fa_decode_latent``: q [B,T,H,512] and q_rope [B,T,H,64] of any strides (two parts of one tensor, for instance), cache [B,Smax,576] or with a
+    block table the pool [num_pages,page_size,576]; o [B,T,H,512] contiguous, lse [B,H,T] or None; seqlens_k int32 [B], the T tokens included."""
+    what, dt = "fa_decode_latent", q.dtype
+    if not (q_rope.dtype is dt and cache.dtype is dt and o.dtype is dt and (dt is _HALF or dt is _BF16)):
+        raise ValueError(f"{what}: q, q_rope, cache and o share one 16-bit type")
+    if not (cache.is_contiguous() and o.is_contiguous() and seqlens_k.dtype is _INT and seqlens_k.is_contiguous()
+            and (lse is None or (lse.is_contiguous() and lse.dtype is _FLOAT))):
+        _contiguous(what, cache, o, lse, seqlens_k)
+        _int32(what, seqlens_k)
+        raise ValueError(f"{what}: lse is float32")
+    B, T, H, d = shape = q.shape
+    rope = q_rope.shape[3]
+    slabs, rows, width = cache.shape
+    qb, qt, qh, q1 = q.stride()
+    rb, rt, rh, r1 = q_rope.stride()
+    if q1 != 1 or r1 != 1:
+        raise ValueError(f"{what}: the columns of a head are contiguous")
+    if block_table is None:
+        tables, Smax, sizes = slabs, rows, (0, 0, 0, 0)
+    else:
+        tables, pages = block_table.shape
+        Smax, sizes = 0, (slabs, rows, pages if max_pages is None else max_pages, _table(what, block_table))
+    if not (q_rope.shape[:3] == shape[:3] and o.shape == shape and width == d + rope and tables >= B and seqlens_k.numel() >= B
+            and (lse is None or lse.numel() >= B * H * T)):
+        _shapes(what, q=q, q_rope=q_rope, cache=cache, o=o, lse=lse, seqlens_k=seqlens_k, block_table=block_table)
+    # (the stride of an extent of 1 may be any number)
+    p = _LATENT_DECODE.pack(q.data_ptr(), q_rope.data_ptr(), cache.data_ptr(), o.data_ptr(), 0 if lse is None else lse.data_ptr(), seqlens_k.data_ptr(),
+                            0 if block_table is None else block_table.data_ptr(), qb if B > 1 else 0, qt if T > 1 else 0, qh if H > 1 else 0,
+                            rb if B > 1 else 0, rt if T > 1 else 0, rh if H > 1 else 0, B, T, H, Smax, d, rope, _FA16[dt], *sizes, scale,
+                            0 if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes)
+    rc = lib.fa_decode_latent(p, _stream())
     return _check(rc, what, raise_on_error) if rc else rc
 
 

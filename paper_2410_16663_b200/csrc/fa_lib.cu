@@ -12,6 +12,7 @@
 #include <mutex>
 
 #include "decode.cuh"
+#include "decode_latent.cuh"
 #include "decode_tree.cuh"
 #include "prefill_pingpong.cuh"
 #include "proj_gemm.cuh"
@@ -1528,6 +1529,115 @@ int fa_cache_append(const fa_append_params* pp, void* stream) {
     rp.k_scale = p.k_scale;
     rp.v_scale = p.v_scale;
     return rope_launch(rp, p.dtype == FA_DTYPE_BF16, f8, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+// How a sequence's rows are cut: blocks of equal size.
+struct LatentBlocks {
+    int blocks, rows;
+    LatentBlocks(int T, int H) {
+        const long long all = (long long)T * H;
+        blocks = (int)((all + 31) / 32);
+        rows = (int)((all + blocks - 1) / blocks);
+    }
+    size_t slots() const { return 2 * (size_t)fa::kTreeMaxSms; }   // partial results that a call may have: two for each worker
+};
+
+template <typename T, int N>
+int latent_launch(const CUtensorMap& tm, const CUtensorMap& tmr, fa::LatentParams& lp, int sms, cudaStream_t st) {
+    auto kern = fa::fa_decode_latent_kernel<T, N>;
+    int sm_count = 0;
+    if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), fa::LatShape<N>::kSmem, &sm_count))
+        return cuda_fail(static_cast<cudaError_t>(ce));
+    const int grid = sms < fa::kTreeMaxSms ? sms : fa::kTreeMaxSms;
+    lp.workers = grid;
+    lp.by_item = (long long)lp.B * lp.blocks < grid ? 1 : 0;
+    cudaError_t e = fa::launch_dependent(kern, dim3(grid), fa::LatShape<N>::kThreads, fa::LatShape<N>::kSmem, st, tm, tmr, lp);
+    if (e == cudaSuccess && grid > 1) {
+        const int y = lp.by_item ? lp.B * lp.blocks : grid - 1;
+        e = fa::launch_dependent(fa::fa_decode_latent_combine_kernel<T>, dim3(lp.rows, y), fa::kLatCombineThreads, 0, st, lp);
+    }
+    return e == cudaSuccess ? FA_OK : cuda_fail(e);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t fa_decode_latent_workspace_bytes(int B, int T, int H, int Skv_max, int d) {
+    if (B <= 0 || T <= 0 || T > 64 || H <= 0 || H > 65535 || Skv_max <= 0 || d != fa::kLatDim) return 0;
+    const LatentBlocks lb(T, H);
+    return lb.slots() * lb.rows * ((size_t)fa::kLatDim + 1) * sizeof(float) + fa::kTreeMaxSms * sizeof(int4);
+}
+
+int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
+    if (!pp) return FA_ERR_NULL;
+    const fa_latent_decode_params& p = *pp;
+    int Skv_max = p.Skv_max;
+    if (p.block_table) {
+        if (int rc = check_table(p.num_pages, p.page_size, p.max_pages, p.table_stride, p.block_table)) return rc;
+        Skv_max = p.max_pages * p.page_size;
+    }
+    if (p.B < 0 || p.H <= 0 || Skv_max < 0 || p.d <= 0 || p.d_rope <= 0 || p.T < 1) return FA_ERR_SHAPE;
+    if (p.T > 64 || p.T > Skv_max) return FA_ERR_UNSUPPORTED;   // the tokens are the LAST rows of the cache
+    if (p.d != fa::kLatDim || p.d_rope != fa::kLatRope) return FA_ERR_UNSUPPORTED;
+    if (p.dtype != FA_DTYPE_FP16 && p.dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
+    if (!(p.scale >= 0.f) || isinf(p.scale)) return FA_ERR_UNSUPPORTED;
+    if (p.B > 65535 || p.H > 65535) return FA_ERR_UNSUPPORTED;
+    if (!strides_ok(p.q_stride, p.B, p.T, p.H, p.d) || !strides_ok(p.q_rope_stride, p.B, p.T, p.H, p.d_rope)) return FA_ERR_SHAPE;
+    if (p.B == 0) return FA_OK;
+    if (!p.q || !p.q_rope || !p.cache || !p.o || !p.seqlens_k) return FA_ERR_NULL;
+    if (!aligned16(p.q) || !aligned16(p.q_rope) || !aligned16(p.cache) || !aligned16(p.o) || !aligned16(p.workspace)) return FA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(p.seqlens_k) | reinterpret_cast<uintptr_t>(p.lse)) & 3u) return FA_ERR_ALIGN;
+    if (!p.workspace || p.workspace_bytes < fa_decode_latent_workspace_bytes(p.B, p.T, p.H, Skv_max, p.d)) return FA_ERR_WORKSPACE;
+    const LatentBlocks lb(p.T, p.H);
+    const long long units = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile + fa::kTreeItemCost;
+    if (units * p.B * lb.blocks > 0x7fffffffll) return FA_ERR_UNSUPPORTED;   // (they are counted in 32 bits)
+    int sms = 0;
+    int rc = check_device(&sms);
+    if (rc) return rc;
+    fa::LatentParams lp;
+    lp.q = p.q;
+    lp.q_rope = p.q_rope;
+    lp.o = p.o;
+    lp.lse = p.lse;
+    lp.seqlens = p.seqlens_k;
+    lp.block_table = p.block_table;
+    lp.o_part = static_cast<float*>(p.workspace);
+    lp.lse_part = lp.o_part + lb.slots() * lb.rows * fa::kLatDim;
+    lp.merges = reinterpret_cast<int4*>(lp.lse_part + lb.slots() * lb.rows);   // (slots is a multiple of four)
+    lp.q_sb = p.q_stride[0]; lp.q_st = p.q_stride[1]; lp.q_sh = p.q_stride[2];
+    lp.r_sb = p.q_rope_stride[0]; lp.r_st = p.q_rope_stride[1]; lp.r_sh = p.q_rope_stride[2];
+    lp.B = p.B; lp.T = p.T; lp.H = p.H; lp.Smax = Skv_max;
+    lp.rows = lb.rows; lp.blocks = lb.blocks;
+    lp.page_size = p.block_table ? p.page_size : 1;
+    lp.table_stride = p.table_stride;
+    lp.num_pages = p.num_pages;
+    lp.by_H.set(p.H);
+    lp.scale_log2 = fmaxf(p.scale * 1.4426950408889634f, 1e-30f);   // (positive, as in dense_fwd_params)
+    const bool bf16 = p.dtype == FA_DTYPE_BF16;
+    // The dimensions are (64 elements, rows, 64-element blocks, slabs, 1), so that a box of a whole tile lands block by block and rows past a slab's end read
+    // as zeros; of pages smaller than a tile (64 elements, 8 rows, blocks, groups of 8 rows, pages): a box is a page, and lands group by group.
+    const cuuint64_t row = fa::kLatRow * 2, blocks = fa::kLatRow / 64;
+    const cuuint64_t slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : Skv_max;
+    CUtensorMap tm, tmr;
+    for (int i = 0; i < 2 && !rc; ++i) {
+        CUtensorMap* m = i ? &tmr : &tm;
+        const cuuint32_t wide = i ? 1 : 2;
+        if (p.block_table && p.page_size < fa::kDecTile)
+            rc = encode_tiled<5>(m, type16(bf16), p.cache, {64, 8, blocks, slab_rows / 8, slabs}, {row, 128, 8 * row, slab_rows * row},
+                                 {64, 8, wide, (cuuint32_t)slab_rows / 8, 1});
+        else
+            rc = encode_tiled<5>(m, type16(bf16), p.cache, {64, slab_rows, blocks, slabs, 1}, {row, 128, slab_rows * row, slabs * slab_rows * row},
+                                 {64, (cuuint32_t)fa::kDecTile, wide, 1, 1});
+    }
+    if (rc) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (lp.rows <= 16) return bf16 ? latent_launch<__nv_bfloat16, 16>(tm, tmr, lp, sms, st) : latent_launch<__half, 16>(tm, tmr, lp, sms, st);
+    return bf16 ? latent_launch<__nv_bfloat16, 32>(tm, tmr, lp, sms, st) : latent_launch<__half, 32>(tm, tmr, lp, sms, st);
 }
 
 // CTAs of the one cluster that looks a pool's reference counts over.

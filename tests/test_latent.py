@@ -50,3 +50,51 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                    dict(lse=torch.zeros(7)), dict(cu_seqlens_q=cu.long()), dict(q_rope=z(3, 2, 64)), dict(k_rope=z(64, 6).T), dict(q=z(4, 2, 256)[..., ::2])):
         with pytest.raises(ValueError):
             fa.fa_forward_latent(**{**ok, **change})
+
+
+def decode_params(**kw):
+    base = dict(q=A, q_rope=A, cache=A, o=A, lse=0, seqlens_k=A, block_table=0, q_stride=(4096, 2048, 512), q_rope_stride=(512, 256, 64), B=2, T=2, H=4,
+                Skv_max=100, d=512, d_rope=64, dtype=0, num_pages=0, page_size=0, max_pages=0, table_stride=0, scale=0.1, workspace=A, workspace_bytes=1 << 40)
+    p = fa.fa_latent_decode_params()
+    for name, x in {**base, **kw}.items():
+        if isinstance(x, tuple):
+            for i in range(3):
+                getattr(p, name)[i] = x[i]
+        else:
+            setattr(p, name, x)
+    return p
+
+
+PAGED = dict(block_table=A, num_pages=8, page_size=16, max_pages=4, table_stride=4)
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(B=-1), fa.FA_ERR_SHAPE), (dict(T=0), fa.FA_ERR_SHAPE), (dict(H=0), fa.FA_ERR_SHAPE), (dict(Skv_max=-1), fa.FA_ERR_SHAPE), (dict(d=0), fa.FA_ERR_SHAPE),
+    (dict(q_stride=(4096, 2048, 508)), fa.FA_ERR_SHAPE), (dict(q_rope_stride=(512, 256, 32)), fa.FA_ERR_SHAPE), (dict(q_stride=(4096, 0, 512)), fa.FA_ERR_SHAPE),
+    (dict(PAGED, page_size=24), fa.FA_ERR_SHAPE), (dict(PAGED, table_stride=3), fa.FA_ERR_SHAPE), (dict(PAGED, num_pages=0), fa.FA_ERR_SHAPE),
+    (dict(PAGED, max_pages=1 << 28, table_stride=1 << 28), fa.FA_ERR_SHAPE), (dict(T=65), fa.FA_ERR_UNSUPPORTED), (dict(T=64, Skv_max=63), fa.FA_ERR_UNSUPPORTED),
+    (dict(d=256), fa.FA_ERR_UNSUPPORTED), (dict(d_rope=128), fa.FA_ERR_UNSUPPORTED), (dict(dtype=2), fa.FA_ERR_UNSUPPORTED), (dict(scale=-0.1), fa.FA_ERR_UNSUPPORTED),
+    (dict(scale=math.nan), fa.FA_ERR_UNSUPPORTED), (dict(B=65536), fa.FA_ERR_UNSUPPORTED), (dict(H=65536), fa.FA_ERR_UNSUPPORTED),
+    (dict(B=65535, T=64, H=8192, Skv_max=1 << 28), fa.FA_ERR_UNSUPPORTED), (dict(q=0), fa.FA_ERR_NULL), (dict(q_rope=0), fa.FA_ERR_NULL),
+    (dict(cache=0), fa.FA_ERR_NULL), (dict(o=0), fa.FA_ERR_NULL), (dict(seqlens_k=0), fa.FA_ERR_NULL), (dict(cache=A + 8), fa.FA_ERR_ALIGN), (dict(o=A + 2), fa.FA_ERR_ALIGN),
+    (dict(workspace=A + 4), fa.FA_ERR_ALIGN), (dict(seqlens_k=A + 2), fa.FA_ERR_ALIGN), (dict(lse=A + 1), fa.FA_ERR_ALIGN), (dict(PAGED, block_table=A + 2), fa.FA_ERR_ALIGN),
+    (dict(workspace=0), fa.FA_ERR_WORKSPACE), (dict(workspace_bytes=1000), fa.FA_ERR_WORKSPACE), (dict(B=0, q=0), fa.FA_OK)], ids=str)
+def test_decode_refusals(change, code):
+    assert fa.lib.fa_decode_latent(ctypes.byref(decode_params(**change)), None) == code
+
+
+def test_decode_workspace():
+    size = fa.fa_decode_latent_workspace_bytes
+    assert size(2, 2, 4, 100) > 0 and size(2, 65, 4, 100) == size(0, 1, 4, 100) == size(1, 0, 4, 100) == size(1, 1, 0, 100) == size(1, 1, 4, 0) == size(1, 1, 4, 100, 256) == 0
+    assert fa.lib.fa_decode_latent(ctypes.byref(decode_params(workspace_bytes=size(2, 2, 4, 100) - 1)), None) == fa.FA_ERR_WORKSPACE
+
+
+def test_the_decode_binding_refuses_what_the_library_cannot_see():
+    z, i = lambda *s: torch.zeros(*s, dtype=torch.half), torch.int32
+    ok = dict(q=z(2, 1, 4, 512), q_rope=z(2, 1, 4, 64), cache=z(2, 20, 576), o=z(2, 1, 4, 512), lse=None, seqlens_k=torch.zeros(2, dtype=i), scale=0.1, workspace=None)
+    for change in (dict(cache=z(2, 20, 576).float()), dict(cache=z(2, 20, 512)), dict(cache=z(1, 20, 576)), dict(o=z(2, 1, 4, 576)[..., :512]), dict(o=z(2, 1, 3, 512)),
+                   dict(q_rope=z(2, 1, 3, 64)), dict(lse=z(2, 4, 1)), dict(lse=torch.zeros(7)), dict(seqlens_k=torch.zeros(1, dtype=i)),
+                   dict(seqlens_k=torch.zeros(2)), dict(q=z(2, 1, 4, 1024)[..., ::2]), dict(block_table=torch.zeros(1, 4, dtype=i)),
+                   dict(block_table=torch.zeros(2, 4))):
+        with pytest.raises(ValueError):
+            fa.fa_decode_latent(**{**ok, **change})

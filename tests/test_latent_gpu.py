@@ -109,3 +109,166 @@ def test_expanded_without_keys():
     fa.fa_forward_latent(q[..., :128], q[..., 128:], none[..., :128], torch.empty(0, 64, dtype=torch.float16, device="cuda"), none[..., 128:], o, lse, ints([0, 5]),
                          ints([0, 0]), 5, 0, False, SCALE)
     assert bool((o == 0).all()) and bool(torch.isneginf(lse).all())
+
+
+# ------------------------------------------------------------------ the absorbed form
+def pool_of(rows, page, rng):
+    """rows: per sequence [n,576].  A pool whose pages are NaN wherever no row is, and the table; pages in a random order."""
+    need = [max(1, -(-len(r) // page)) for r in rows]
+    order = list(range(sum(need) + 2))
+    rng.shuffle(order)
+    pool = torch.full((len(order), page, 576), float("nan"), dtype=rows[0].dtype, device="cuda")
+    table, at = [], 0
+    for r, n in zip(rows, need):
+        ids = order[at:at + n]
+        at += n
+        for i, page_at in enumerate(ids):
+            part = r[i * page:(i + 1) * page]
+            pool[page_at, :len(part)] = part
+        table.append(ids + [-1] * (max(need) - n))
+    return pool, ints(table)
+
+
+def absorbed(lens, T, H, dt, page=0, seed=1, by=0.5, parts=True, room=0, samples=None):
+    rng, B = random.Random(seed), len(lens)
+    rows = [normal((n, 576), dt, seed + b) for b, n in enumerate(lens)]
+    table = None
+    if page:
+        cache, table = pool_of(rows, page, rng)
+        most = table.shape[1] * page
+    else:
+        most = max(max(lens), T) + room
+        cache = torch.full((B, most, 576), float("nan"), dtype=DT[dt], device="cuda")
+        for b, r in enumerate(rows):
+            cache[b, :len(r)] = r
+    if parts:     # two parts of one tensor
+        both = normal((B, T, H, 576), dt, seed + 100)
+        q, q_rope = both[..., :512], both[..., 512:]
+        q.mul_(by)
+    else:
+        q, q_rope = normal((B, T, H, 512), dt, seed + 100, by), normal((B, T, H, 64), dt, seed + 101)
+    o, lse = torch.full((B, T, H, 512), float("nan"), dtype=DT[dt], device="cuda"), torch.full((B, H, T), float("nan"), device="cuda")
+    ws = torch.full((fa.fa_decode_latent_workspace_bytes(B, T, H, most),), 0xff, dtype=torch.uint8, device="cuda")
+    if page and -(-T // page) > table.shape[1]:
+        pytest.skip("the tokens do not fit into the table")
+    fa.fa_decode_latent(q, q_rope, cache, o, lse, ints(lens), SCALE, ws, block_table=table)
+    # products of a score: 512 of 0.8 by and 64 of 0.8 squared on average
+    size = SCALE * (512 * 0.64 * by + 64 * 0.64)
+    for b in samples or range(B):
+        n = lens[b]
+        live = min(T, n)        # tokens that see a key
+        x = torch.cat([q[b], q_rope[b]], -1)[T - live:].cpu()
+        for h in sorted(set([0, 1 % H, H // 2, H - 1])):
+            want = oracle.attention(x[:, h], rows[b].cpu(), rows[b][:, :512].cpu(), SCALE, True)
+            check(o[b, T - live:, h], lse[b, h, T - live:], want, dt, size=size)
+        assert bool((o[b, :T - live] == 0).all()) and bool(torch.isneginf(lse[b, :, :T - live]).all())
+    assert bool(torch.isfinite(o.float()).all()) and fa.fa_device_status()[0] == 0
+    return q, q_rope, cache, table, ws, o, lse, most
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("page", [0, 16, 32, 64, 128, 256])
+@pytest.mark.parametrize("T, H", [(1, 16), (1, 20), (3, 5), (2, 16)])
+def test_absorbed(dt, page, T, H):
+    absorbed([700, 1, 128, 0, 129, 2, 383], T, H, dt, page=page)
+
+
+@pytest.mark.parametrize("T, H", [(1, 1), (1, 33), (1, 64), (1, 100), (1, 128), (2, 128), (7, 20), (64, 3), (5, 128)])
+def test_absorbed_row_blocks(T, H):
+    absorbed([300, 65, 1000], T, H, "bf16", page=64, parts=False)
+    absorbed([64, 300, 513], T, H, "fp16")
+
+
+@pytest.mark.parametrize("H", [16, 128])
+def test_absorbed_one_long_sequence(H):
+    absorbed([30011], 1, H, "fp16", page=64)
+
+
+def test_absorbed_many_short_sequences():
+    """More sequences than CTAs, several of them without keys; runs of many items."""
+    rng = random.Random(3)
+    lens = [rng.choice([0, 1, 2, 127, 128, 129, 200]) for _ in range(400)]
+    absorbed(lens, 1, 16, "bf16", page=16, samples=range(0, 400, 9))
+    absorbed(lens[:170], 2, 40, "fp16", samples=range(0, 170, 9))
+
+
+def test_absorbed_large_scores():
+    absorbed([900, 130], 2, 16, "fp16", by=20.0)
+    absorbed([900, 130], 2, 64, "fp16", by=20.0)
+
+
+def test_absorbed_without_keys_at_all():
+    o, lse = absorbed([0, 0, 0], 1, 16, "fp16", room=40)[5:7]
+    assert bool((o == 0).all()) and bool(torch.isneginf(lse).all())
+
+
+@pytest.mark.parametrize("H", [16, 32, 128])
+def test_absorbed_lengths_are_clamped(H):
+    """Lengths past the cache or below zero are those of the cache and none."""
+    q, r, cache, _, ws, o, lse, most = absorbed([300, 300], 1, H, "bf16")
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    fa.fa_decode_latent(q, r, cache, o2, lse2, ints([10 ** 9, -5]), SCALE, ws)
+    assert torch.equal(o2[0], o[0]) and torch.equal(lse2[0], lse[0]) and bool((o2[1] == 0).all()) and bool(torch.isneginf(lse2[1]).all())
+
+
+@pytest.mark.parametrize("H", [16, 128])
+def test_absorbed_pages_that_are_not_there_read_as_zeros(H):
+    """A page number outside the pool: rows of zeros, no fault."""
+    cache, q, r = normal((4, 64, 576), "fp16", 1), normal((1, 1, H, 512), "fp16", 2, 0.5), normal((1, 1, H, 64), "fp16", 3)
+    o, ws = torch.empty_like(q), torch.empty(fa.fa_decode_latent_workspace_bytes(1, 1, H, 256), dtype=torch.uint8, device="cuda")
+    for bad in (-1, 4, 2 ** 31 - 1):
+        fa.fa_decode_latent(q, r, cache, o, None, ints([256]), SCALE, ws, block_table=ints([[2, bad, 0, 1]]))
+        rows = torch.cat([cache[2], torch.zeros_like(cache[0]), cache[0], cache[1]])
+        want = oracle.attention(torch.cat([q, r], -1)[0, 0, :1].cpu(), rows.cpu(), rows[:, :512].cpu(), SCALE, False)
+        got = o[0, 0, :1].double().cpu()
+        assert bool(((got - want[0]).abs() <= 2.0 ** -11 * want[0].abs() + (2.0 ** -11 + 2.0 ** -13) * want[2] + 2.0 ** -25 * want[3] + 2.0 ** -24).all())
+
+
+def test_absorbed_nan_in_a_row_that_is_seen_stays_in_its_sequence():
+    q, r, cache, _, ws, o, lse, _ = absorbed([300, 400], 1, 16, "fp16")
+    cache[0, 17] = float("nan")
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    fa.fa_decode_latent(q, r, cache, o2, lse2, ints([300, 400]), SCALE, ws)
+    assert bool(torch.isnan(o2[0]).all()) and bool(torch.isnan(lse2[0]).all()) and torch.equal(o2[1], o[1]) and torch.equal(lse2[1], lse[1])
+
+
+@pytest.mark.parametrize("H", [16, 32, 128])
+def test_absorbed_in_a_graph(H):
+    """Lengths and rows of the replay count, and a workspace that two graphs share in turn."""
+    lens = [200, 900, 40]
+    q, r, cache, _, ws, o, lse, _ = absorbed(lens, 1, H, "bf16", room=600)
+    now, cache2 = ints(lens), normal(cache.shape, "bf16", 77)
+    out = [torch.empty_like(o), torch.empty_like(o)]
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    for g, to, c in zip(graphs, out, (cache, cache2)):
+        with torch.cuda.graph(g):
+            fa.fa_decode_latent(q, r, c, to, None, now, SCALE, ws)
+    for g in graphs:
+        g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out[0], o)
+    want = torch.empty_like(o)
+    now.copy_(ints([1500, 0, 777]))
+    cache.nan_to_num_(0.25)
+    for g in graphs:
+        g.replay()
+    for to, c in zip(out, (cache, cache2)):
+        fa.fa_decode_latent(q, r, c, want, None, now, SCALE, ws)
+        assert torch.equal(to, want)
+
+
+def test_absorbed_offsets_past_32_bits():
+    """A cache of more than 4 GiB: the last sequence's rows."""
+    B, n = 3, 1300000
+    cache = torch.zeros(B, n, 576, dtype=torch.float16, device="cuda")
+    cache[2, n - 300:] = normal((300, 576), "fp16", 1)
+    q, r = normal((B, 1, 16, 512), "fp16", 2, 0.5), normal((B, 1, 16, 64), "fp16", 3)
+    o, ws = torch.empty_like(q), torch.empty(fa.fa_decode_latent_workspace_bytes(B, 1, 16, n), dtype=torch.uint8, device="cuda")
+    fa.fa_decode_latent(q, r, cache, o, None, ints([0, 0, n]), SCALE, ws)
+    x = torch.cat([q, r], -1)[2, 0, :2].cpu()
+    want = oracle.attention(x, cache[2, n - 300:].cpu(), cache[2, n - 300:, :512].cpu(), SCALE, False)
+    # with the zeros before them: their scores are 0, their values nothing
+    rest = torch.log1p((n - 300) * torch.exp(-want[1]))[:, None]
+    got = o[2, 0, :2].double().cpu()
+    ref = want[0] * torch.exp(-rest)
+    assert bool(((got - ref).abs() <= 2.0 ** -10 * want[2] * torch.exp(-rest) + 2.0 ** -11 * ref.abs() + 2.0 ** -24).all())
