@@ -28,7 +28,7 @@ struct LatentParams {
     float* lse_part;          // [2 workers][rows]
     int4* merges;             // as TreeParams::merges
     int by_item;              // as TreeParams::by_item
-    int workers;              // CTAs of the grid
+    int workers;              // CTAs of the grid, or pairs of them
     long long q_sb, q_st, q_sh, r_sb, r_st, r_sh;   // elements
     int B, T, H, Smax;
     int rows, blocks;         // rows per block, blocks per sequence
@@ -163,7 +163,9 @@ struct LatBars {
     using Shape = LatShape<N>;
     static constexpr int full = 0, empty = full + Shape::kUnits, rope_full = empty + Shape::kUnits, rope_empty = rope_full + Shape::kRopes,
                          s_full = rope_empty + Shape::kRopes, s_read = s_full + 2, p_full = s_read + 2, pv = p_full + 1, q_full = pv + 1,
-                         q_empty = q_full + 1, seg_full = q_empty + 1, seg_empty = seg_full + kLatSegs, count = seg_empty + kLatSegs;
+                         q_empty = q_full + 1, seg_full = q_empty + 1, seg_empty = seg_full + kLatSegs,
+                         meet = seg_empty + kLatSegs,   // [2][2] by step and warpgroup: its maxima are there
+                         sums = meet + 4, count = sums + 2;   // [2] by warpgroup: an item's sums are there; they have been read
 };
 
 // The largest of a value over a warp.  (A NaN loses.)
@@ -202,7 +204,13 @@ __device__ __forceinline__ void lat_sts(uint32_t at, const float (&v)[C]) {
     for (int i = 0; i < C; i += 4)
         asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at + 4 * i), "f"(v[i]), "f"(v[i + 1]), "f"(v[i + 2]), "f"(v[i + 3]) : "memory");
 }
-__device__ __forceinline__ void lat_bar_sync(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
+// The four warps that have one another's rows meet: what each has written is there for the others.  (A bounded wait, as every other: a warp
+// that gives up elsewhere does not come.)
+__device__ __forceinline__ bool lat_meet(uint32_t bar, uint32_t parity, int lane, volatile uint32_t* abort_flag, unsigned int where) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+    return pp_warp_wait(bar, parity, abort_flag, where);
+}
 
 // grid: as many as run at once.  Warps 0 to 7: softmax and output (a key per thread, half the columns each); 8: segments and the cache; 9: Q;
 // 10: S^T; 11: O^T.
@@ -228,7 +236,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     if (tid == 0) {
         for (int i = 0; i < At::count; ++i) {
             const bool softmax = (i >= At::s_read && i < At::pv);
-            mbar_init(bar(i), softmax ? 8 : i >= At::seg_empty ? 11 : 1);
+            mbar_init(bar(i), softmax ? 8 : i >= At::meet ? 4 : i >= At::seg_empty ? 11 : 1);
         }
         abort_flag = 0;
         fence_mbar_init();
@@ -447,8 +455,9 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 float mx[C];
 #pragma unroll
                 for (int c = 0; c < C; ++c) mx[c] = warp_max(__uint_as_float(sc[c]));
+                if (j == 0 && ord > 0 && !(ok = pp_warp_wait(bar(At::sums + wg), 1, &abort_flag, 356))) break;   // (the last item's sums lie in one of them)
                 if (lane == 0) lat_sts<C>(smem_u32(&s_max[buf][quarter][col0]), mx);
-                lat_bar_sync(1 + wg, 128);
+                if (!(ok = lat_meet(bar(At::meet + 2 * buf + wg), (s >> 1) & 1, lane, &abort_flag, 357))) break;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     float other[C];
@@ -510,7 +519,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 #pragma unroll
                 for (int sh = 16; sh > 0; sh >>= 1) l_run[c] += __shfl_xor_sync(0xffffffffu, l_run[c], sh);
             if (lane == 0) lat_sts<C>(smem_u32(&s_max[other_buf][quarter][col0]), l_run);
-            lat_bar_sync(1 + wg, 128);
+            if (!(ok = lat_meet(bar(At::sums + wg), 0, lane, &abort_flag, 358))) break;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 float other[C];
@@ -518,7 +527,8 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 #pragma unroll
                 for (int c = 0; c < C; ++c) l_run[c] = w == 0 ? other[c] : l_run[c] + other[c];
             }
-            lat_bar_sync(1 + wg, 128);   // (the next item's first step writes there)
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(At::sums + wg));   // (the next item's first step may write there)
             const bool whole = seg.n == seg.of;
             const long long slot = 2ll * blockIdx.x + (seg.t0 > 0 ? 0 : 1);
             float inv[C];
@@ -565,6 +575,468 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     __syncthreads();
     tc_fence_after();
     if (warp == 10) tmem_dealloc(tmem, Shape::kTmemCols);
+}
+
+// ---------------------------------------------------------------------------------------
+// More than 32 rows: a pair of CTAs (a cluster) has blocks of 128, 64 rows in each, and issues matrix instructions of both (cta_group::2, M = 128).  Each
+// CTA's tensor memory then holds its 64 rows in the lanes 0 to 63 for the first half of the columns and in 64 to 127 for the second: 512
+// columns of output in 256 of its 512 columns, scores of 128 keys in 64 -- one CTA's tensor memory would be full with the output
+// of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 64 keys of a
+// tile), latent elements for the output (each loads 256 elements of all 128 keys): 1.9 times the tile over L2, once from HBM.
+struct LatPairShape {
+    static constexpr int kKUnitB = 64 * 192 * 2, kKUnits = 3;       // 64 keys x 192 elements: a third of a CTA's keys
+    static constexpr int kVUnitB = 128 * 128 * 2, kVUnits = 2;      // 128 keys x 128 elements: half of a CTA's latent elements
+    static constexpr int kQB = 64 * kLatRow * 2, kPB = 64 * 128 * 2;
+    static constexpr int kSmem = kQB + kPB + kKUnits * kKUnitB + kVUnits * kVUnitB;   // 224 KiB, behind kPairStaticBytes
+    static constexpr int kThreads = 416;
+    static constexpr int kTmemCols = 512;                           // scores [0,64) and [64,128), output [128,384)
+};
+namespace latp {   // barriers
+constexpr int k_full = 0;                                   // [3]  TMA -> S thread, and the other CTA's relay
+constexpr int k_peer = k_full + LatPairShape::kKUnits;      // [3]  first CTA: the other CTA's unit is there
+constexpr int k_empty = k_peer + LatPairShape::kKUnits;     // [3]  S thread (commit, to both)
+constexpr int v_full = k_empty + LatPairShape::kKUnits;     // [2]  TMA -> the CTA's softmax warps, whose probabilities say that it is there
+constexpr int v_empty = v_full + LatPairShape::kVUnits;     // [2]  PV thread (commit, to both)
+constexpr int s_full = v_empty + LatPairShape::kVUnits;     // [2]  S thread (commit, to both)
+constexpr int p_full = s_full + 2;                          // [2]  first CTA: sixteen softmax warps
+constexpr int pv = p_full + 2;                              // [1]  PV thread (commit, to both)
+constexpr int q_full = pv + 1;                              // [1]  first CTA: both Q warps
+constexpr int q_empty = q_full + 1;                         // [1]  S thread (commit, to both)
+constexpr int seg_full = q_empty + 1;                       // [4]
+constexpr int seg_empty = seg_full + kLatSegs;              // [4]  eight softmax warps, V, Q, and what else reads segments: two threads, in the second CTA one
+constexpr int meet = seg_empty + kLatSegs;                  // [2][2] by meeting and rows: the maxima of the four warps that have them are there
+constexpr int sums = meet + 4;                              // [2] by rows: an item's sums are there; they have been read
+constexpr int count = sums + 2;
+}  // namespace latp
+struct LatPairStatic {
+    uint64_t bars[latp::count];
+    LatentSegment segs[kLatSegs];
+    uint32_t tmem_holder;
+    uint32_t abort_flag;
+    float x[2][4][64];   // by meeting, (half of the keys, warpgroup), row: maxima; at an item's end the sums
+};
+constexpr int kPairStaticBytes = 3072;
+static_assert(sizeof(LatPairStatic) <= kPairStaticBytes && LatPairShape::kSmem + kPairStaticBytes <= 232448, "shared memory");
+
+__device__ __forceinline__ void pair_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\t"
+        "mov.b64 da, {%1, %5};\n\t"
+        "mov.b64 db, {%2, %6};\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], da, db, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(a_hi), "r"(b_hi)
+        : "memory");
+}
+// Arrives on the same barrier of both CTAs once what this thread has issued is done.
+__device__ __forceinline__ void pair_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// Arrives on a barrier of the cluster (an address of cluster_map).
+__device__ __forceinline__ void cluster_mbar_arrive(uint32_t addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+// A wait for such arrivals: what the other CTA's threads wrote is visible.
+__device__ __forceinline__ bool cluster_mbar_try_wait(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool cluster_mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned int where) {
+    if (!mbar_wait(bar, parity, abort_flag, where)) return false;
+    cluster_mbar_try_wait(bar, parity);   // (it has completed: for the order)
+    return true;
+}
+
+// grid: two CTAs per worker.  Warps 0 to 7: softmax and output -- lane and warp & 3 say the row and the half of the keys, warp >> 2 which
+// 32 of those; 8: segments and keys; 9: Q; 10: S (first CTA) or the relay of the keys' arrival; 11: O (first CTA); 12: values.
+// tm_k: boxes of 64 keys x 192 elements, tm_v: 128 keys x 128 elements (pages of less: as in fa_decode_latent_kernel).
+template <typename T>
+__global__ void __launch_bounds__(LatPairShape::kThreads, 1)
+fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const LatentParams p) {
+    using Shape = LatPairShape;
+    constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    __shared__ __align__(1024) uint8_t static_raw[kPairStaticBytes];
+    LatPairStatic& ss = *reinterpret_cast<LatPairStatic*>(static_raw);
+    const uint32_t sQ = smem_u32(smem_raw), sP = sQ + Shape::kQB, sK = sP + Shape::kPB, sV = sK + Shape::kKUnits * Shape::kKUnitB;
+    volatile uint32_t* abort_flag = &ss.abort_flag;
+    const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, worker = blockIdx.x >> 1, rank = blockIdx.x & 1;
+    auto bar = [&](int i) { return smem_u32(&ss.bars[i]); };
+    auto first_bar = [&](int i) { return cluster_map(smem_u32(&ss.bars[i]), 0); };
+    if (sQ & 1023u) {   // uniform for the grid: nothing has been set up yet
+        if (tid == 0) record_timeout(901);
+        return;
+    }
+    if (tid == 0) {
+        for (int i = 0; i < latp::count; ++i)
+            mbar_init(bar(i), i >= latp::p_full && i < latp::pv ? 16 : i == latp::q_full ? 2 : i >= latp::meet ? 4 : i >= latp::seg_empty ? 12 - rank : 1);
+        ss.abort_flag = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&tm_k);
+        tma_prefetch_desc(&tm_v);
+    }
+    if (warp == 10) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ss.tmem_holder)), "r"(Shape::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    LatentWalk walk(p, worker, lane);
+    if (warp == 8) {
+        grid_dep_wait();
+        walk.begin();
+    }
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync_all();   // (both CTAs' barriers are there)
+    tc_fence_after();
+    const uint32_t tmem = ss.tmem_holder, tmem_o = tmem + 128;
+    grid_dep_wait();
+
+    const int ps = p.page_size;
+    const bool small = p.block_table != nullptr && ps < kDecTile;
+    bool ok = true;
+    auto segment = [&](uint32_t ord, LatentSegment& s) {
+        if (!pp_warp_wait(bar(latp::seg_full + ord % kLatSegs), (ord / kLatSegs) & 1, abort_flag, 360)) return false;
+        s = ss.segs[ord % kLatSegs];
+        return true;
+    };
+    // Loads `units` boxes of `keys` keys per tile, the CTA's share of them, through a ring of as many slots.
+    auto load_tiles = [&](const LatentSegment& seg, uint32_t& u, bool values) {
+        const uint64_t policy = l2_policy_evict_last();   // (the pair reads everything twice, and other blocks of rows again)
+        const int keys = values ? kDecTile : 64, units = values ? Shape::kVUnits : Shape::kKUnits, blocks = values ? 2 : 3, skip = values ? 0 : rank * 64;
+        const uint32_t ring = values ? sV : sK, unit_b = values ? Shape::kVUnitB : Shape::kKUnitB;
+        const int full0 = values ? latp::v_full : latp::k_full, empty0 = values ? latp::v_empty : latp::k_empty;
+        const CUtensorMap* tm = values ? &tm_v : &tm_k;
+        const int* table = p.block_table ? p.block_table + (long long)seg.b * p.table_stride : nullptr;
+        auto lookup = [&](int key) {   // the page of this lane's part of the keys from `key` on, one tile ahead
+            if (!table || key >= seg.len) return -1;
+            return small ? (lane < keys / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
+        };
+        int page_next = lookup(seg.t0 * kDecTile + skip);
+        for (int j = 0; j < seg.n; ++j) {
+            const int key0 = (seg.t0 + j) * kDecTile + skip, page = (unsigned)page_next < (unsigned)p.num_pages ? page_next : -1;   // (none: zeros)
+            if (j + 1 < seg.n) page_next = lookup(key0 + kDecTile);
+            const int boxes = small ? (max(0, min(seg.len - key0, keys)) + ps - 1) / ps : 1, box_keys = small ? ps : keys;
+            const uint32_t bytes = box_keys * blocks * 128;
+            for (int i = 0; i < units; ++i, ++u) {
+                const uint32_t at = u % units, full = bar(full0 + at);
+                if (lane == 0) ok = mbar_wait(bar(empty0 + at), ((u / units) & 1) ^ 1, abort_flag, values ? 362 : 361);
+                if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; return; }
+                if (lane == 0) mbar_expect_tx(full, boxes * bytes);
+                __syncwarp();
+                if (lane < boxes) {
+                    const int c = values ? 4 * i + 2 * rank : 3 * i;
+                    const uint32_t dst = ring + at * unit_b + lane * bytes;
+                    if (small) tma_load_5d_hint(dst, tm, full, 0, 0, c, 0, page, policy);
+                    else tma_load_5d_hint(dst, tm, full, 0, table ? key0 % ps : key0, c, table ? page : seg.b, 0, policy);
+                }
+            }
+        }
+    };
+
+    if (warp == 8) {
+        // ---------------------------------------------------------------- segments and keys
+        uint32_t u = 0;
+        for (uint32_t ord = 0; ok; ++ord) {
+            const LatentSegment seg = walk.next(ord, rank == 0);
+            const int slot = ord % kLatSegs;
+            if (!(ok = pp_warp_wait(bar(latp::seg_empty + slot), ((ord / kLatSegs) & 1) ^ 1, abort_flag, 363))) break;
+            if (lane == 0) {
+                ss.segs[slot] = seg;
+                mbar_arrive(bar(latp::seg_full + slot));
+            }
+            if (seg.n <= 0) break;
+            load_tiles(seg, u, false);
+        }
+        __syncwarp();
+    } else if (warp == 12) {
+        // ---------------------------------------------------------------- values
+        uint32_t u = 0;
+        LatentSegment seg;
+        for (uint32_t ord = 0; ok; ++ord) {
+            if (!(ok = segment(ord, seg))) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(latp::seg_empty + ord % kLatSegs));
+            if (seg.n <= 0) break;
+            load_tiles(seg, u, true);
+        }
+        __syncwarp();
+    } else if (warp == 9) {
+        // ---------------------------------------------------------------- Q: this CTA's 64 rows
+        LatentSegment seg;
+        for (uint32_t ord = 0; ok; ++ord) {
+            if (!(ok = segment(ord, seg))) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(latp::seg_empty + ord % kLatSegs));
+            if (seg.n <= 0) break;
+            if (ord > 0 && !(ok = pp_warp_wait(bar(latp::q_empty), (ord - 1) & 1, abort_flag, 364))) break;
+            const int R0 = seg.block * p.rows + 64 * rank, rows = min(p.rows - 64 * rank, p.H * p.T - R0);
+            for (int x = 0; x < 64; ++x) {   // (rows that are none are zeros)
+                int token, head;
+                p.by_H.divmod(R0 + x, token, head);
+                const T* q = static_cast<const T*>(p.q) + seg.b * p.q_sb + token * p.q_st + head * p.q_sh;
+                const T* r = static_cast<const T*>(p.q_rope) + seg.b * p.r_sb + token * p.r_st + head * p.r_sh;
+#pragma unroll
+                for (int c = lane; c < kLatRow / 8; c += 32) {
+                    const uint32_t at = sQ + (c >> 3) * 8192u + x * 128u + (((c & 7) ^ (x & 7)) << 4);
+                    if (x < rows)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(c < kLatDim / 8 ? q + 8 * c : r + 8 * c - kLatDim) : "memory");
+                    else asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
+                }
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) cluster_mbar_arrive(first_bar(latp::q_full));
+        }
+        __syncwarp();
+    } else if (warp == 10) {
+        // ---------------------------------------------------------------- S = Q C^T
+        if (elect_one()) {
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, 128, false, false);
+            const uint32_t group = small ? 3072u : 1024u, block = small ? 1024u : 8192u;
+            const uint32_t b_hi = tree_desc_hi(group);
+            constexpr uint32_t q_hi = tree_desc_hi(1024);
+            const uint32_t k_lo = desc_lo(sK, 16), q_lo = desc_lo(sQ, 16);
+            uint32_t s = 0;
+            for (uint32_t ord = 0; ok; ++ord) {
+                const int slot = ord % kLatSegs;
+                if (!(ok = mbar_wait(bar(latp::seg_full + slot), (ord / kLatSegs) & 1, abort_flag, 365))) break;
+                const int n = ss.segs[slot].n;
+                mbar_arrive(bar(latp::seg_empty + slot));
+                if (n <= 0) break;
+                if (rank == 0 && !(ok = cluster_mbar_wait(bar(latp::q_full), ord & 1, abort_flag, 366))) break;
+                for (int j = 0; j < n && ok; ++j, ++s) {
+                    const uint32_t buf = s & 1;
+                    // the scores that lie there have become probabilities, in both CTAs
+                    if (rank == 0 && s >= 2 && !(ok = cluster_mbar_wait(bar(latp::p_full + buf), ((s >> 1) - 1) & 1, abort_flag, 367))) break;
+#pragma unroll
+                    for (int i = 0; i < Shape::kKUnits; ++i) {
+                        if (!(ok = mbar_wait(bar(latp::k_full + i), s & 1, abort_flag, 368))) break;
+                        if (rank == 1) {
+                            cluster_mbar_arrive(first_bar(latp::k_peer + i));
+                            continue;
+                        }
+                        if (!(ok = cluster_mbar_wait(bar(latp::k_peer + i), s & 1, abort_flag, 369))) break;
+                        tc_fence_after();
+                        const uint32_t b = k_lo + i * (Shape::kKUnitB >> 4), a = q_lo + ((3 * i * 8192) >> 4);
+#pragma unroll
+                        for (int ks = 0; ks < 12; ++ks)
+                            pair_mma_ss(tmem + buf * 64, a + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, q_hi, b + (ks >> 2) * (block >> 4) + (ks & 3) * 2, b_hi, idesc, i > 0 || ks > 0);
+                        pair_commit(bar(latp::k_empty + i));
+                    }
+                    if (!ok) break;
+                    if (rank == 0) pair_commit(bar(latp::s_full + buf));
+                }
+                if (rank == 0) pair_commit(bar(latp::q_empty));
+            }
+            // (what was committed last has arrived before the CTA ends)
+            if (ok && s > 0) ok = mbar_wait(bar(latp::s_full + ((s - 1) & 1)), ((s - 1) >> 1) & 1, abort_flag, 370);
+        }
+        __syncwarp();
+    } else if (warp == 11) {
+        // ---------------------------------------------------------------- O += P L
+        if (rank == 0 && elect_one()) {
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, 256, false, true);
+            const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 16384u;
+            const uint32_t b_hi = tree_desc_hi(group);
+            constexpr uint32_t p_hi = tree_desc_hi(1024);
+            const uint32_t v_lo = desc_lo(sV, block), p_lo = desc_lo(sP, 16);
+            uint32_t s = 0;
+            for (uint32_t ord = 0; ok; ++ord) {
+                const int slot = ord % kLatSegs;
+                if (!(ok = mbar_wait(bar(latp::seg_full + slot), (ord / kLatSegs) & 1, abort_flag, 371))) break;
+                const int n = ss.segs[slot].n;
+                mbar_arrive(bar(latp::seg_empty + slot));
+                if (n <= 0) break;
+                for (int j = 0; j < n; ++j, ++s) {
+                    if (!(ok = cluster_mbar_wait(bar(latp::p_full + (s & 1)), (s >> 1) & 1, abort_flag, 372))) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int i = 0; i < Shape::kVUnits; ++i) {
+                        const uint32_t b = v_lo + i * (Shape::kVUnitB >> 4);
+#pragma unroll
+                        for (int ks = 0; ks < 8; ++ks)
+                            pair_mma_ss(tmem_o + i * 128, p_lo + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, p_hi, b + ks * (2 * group >> 4), b_hi, idesc, j > 0 || ks > 0 ? 1u : 0u);
+                        pair_commit(bar(latp::v_empty + i));
+                    }
+                    pair_commit(bar(latp::pv));
+                }
+            }
+            if (ok && s > 0) ok = mbar_wait(bar(latp::pv), (s - 1) & 1, abort_flag, 373);
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- softmax: 32 keys of a row per thread
+        const int wg = warp >> 2, half = warp >> 1 & 1, r = (warp & 1) * 32 + lane, part = 2 * wg + half;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const int group = warp & 1;   // the four warps that have these rows
+        uint32_t s = 0, met = 0;   // steps; those of items that have rows here
+        latent_fill_empty<T>(p, worker, tid + 256 * rank, 512);
+        LatentSegment seg;
+        auto wait = [&](int i, uint32_t parity, unsigned int where) { return pp_warp_wait(bar(i), parity, abort_flag, where); };
+        for (uint32_t ord = 0;; ++ord) {
+            if (!(ok = segment(ord, seg)) || seg.n <= 0) break;
+            const int x = 64 * rank + r, R = seg.block * p.rows + x;   // row of the block, of the sequence
+            const bool mine = x < p.rows && R < p.H * p.T;
+            const bool some = __any_sync(0xffffffffu, mine);   // a warp without rows only keeps step
+            int token = 0, head = 0;
+            if (mine) p.by_H.divmod(R, token, head);
+            const int lim = seg.len - p.T + 1 + token;         // keys that the row sees
+            float m_run = -INFINITY, l_run = 0.f;
+            for (int j = 0; j < seg.n; ++j, ++s) {
+                const int key0 = (seg.t0 + j) * kDecTile;
+                const uint32_t buf = s & 1;
+                if (!(ok = wait(latp::s_full + buf, (s >> 1) & 1, 374))) break;
+                tc_fence_after();
+                float alpha = 1.f;
+                bool moved = false;
+                uint32_t pk[16];
+                if (some) {
+                    uint32_t sc[32];
+                    tmem_ld_x32(tmem + lanes + buf * 64 + wg * 32, sc);
+                    tmem_wait_ld();
+                    if (key0 + kDecTile > seg.len - p.T + 1) {
+                        // hidden scores become -inf, their exponentials exact zeros (the scale is positive)
+                        const uint32_t seen = low_bits(lim - key0 - half * 64 - wg * 32);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(seen & (1u << i))) sc[i] = 0xff800000u;
+                    }
+                    float mx = tree_row_max<32>(sc);
+                    if (j == 0 && ord > 0 && !(ok = wait(latp::sums + group, 1, 379))) break;   // (the last item's sums lie in one of them)
+                    ss.x[met & 1][part][r] = mx;
+                    if (!(ok = lat_meet(bar(latp::meet + 2 * (met & 1) + group), (met >> 1) & 1, lane, abort_flag, 380))) break;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, ss.x[met & 1][i][r]);
+                    ++met;
+                    // (the reference follows the maximum as in the other kernel)
+                    moved = (mx - m_run) * p.scale_log2 > kRescaleThreshold;   // (never on -inf)
+                    if (moved) {
+                        alpha = fast_exp2((m_run - mx) * p.scale_log2);
+                        m_run = mx;
+                    }
+                    const float neg = m_run == -INFINITY ? 0.f : -m_run * p.scale_log2;
+                    const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(neg, neg);
+                    uint64_t la = f2_pack(0.f, 0.f), lb = la;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        float e[4];
+#pragma unroll
+                        for (int k = 0; k < 4; k += 2) {
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[i + k]), __uint_as_float(sc[i + k + 1])), sc2, nm2), e[k], e[k + 1]);
+                            e[k] = fast_exp2(e[k]);
+                            e[k + 1] = fast_exp2(e[k + 1]);
+                        }
+                        la = f2_add(la, f2_pack(e[0], e[1]));
+                        lb = f2_add(lb, f2_pack(e[2], e[3]));
+                        pk[i / 2] = pack2<T>(e[0], e[1]);
+                        pk[i / 2 + 1] = pack2<T>(e[2], e[3]);
+                    }
+                    float a0, a1, b0, b1;
+                    f2_unpack(la, a0, a1);
+                    f2_unpack(lb, b0, b1);
+                    l_run = l_run * alpha + ((a0 + a1) + (b0 + b1));
+                }
+                // the probabilities of the step before have been read, and O holds the sums up to there
+                if (s > 0 && !(ok = wait(latp::pv, (s - 1) & 1, 375))) break;
+                if (some) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + half * 8192u + r * 128u + (uint32_t)(((4 * wg + c) ^ (r & 7)) << 4)), "r"(pk[4 * c]),
+                                     "r"(pk[4 * c + 1]), "r"(pk[4 * c + 2]), "r"(pk[4 * c + 3])
+                                     : "memory");
+                    if (j > 0 && __any_sync(0xffffffffu, moved)) {
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t o[16];
+                            tmem_ld_x16(tmem_o + lanes + wg * 128 + 16 * c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st_x16(tmem_o + lanes + wg * 128 + 16 * c, o);
+                        }
+                        tmem_wait_st();
+                    }
+                }
+                // this CTA's values are there; those of keys that are none may be anything, NaN too: they become zeros
+                if (!(ok = wait(latp::v_full, s & 1, 376)) || !(ok = wait(latp::v_full + 1, s & 1, 377))) break;
+                const int valid = seg.len - key0;
+                if (valid < kDecTile) {
+                    const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 16384u;
+                    for (int i = tid; i < (kDecTile - valid) * 32; i += 256) {
+                        const int key = valid + (i >> 5), piece = i & 31;
+                        const uint32_t at = sV + (piece >> 4) * Shape::kVUnitB + (uint32_t)(key >> 3) * group + (piece >> 3 & 1) * block + (uint32_t)(key & 7) * 128u + ((piece & 7) << 4);
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
+                    }
+                }
+                fence_proxy_async_smem();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) cluster_mbar_arrive(first_bar(latp::p_full + buf));
+            }
+            if (!ok) break;
+            if (some) {   // the row sums, in the buffer that the last step has not used
+                const uint32_t other = met & 1;
+                ss.x[other][part][r] = l_run;
+                if (!(ok = lat_meet(bar(latp::sums + group), 0, lane, abort_flag, 381))) break;
+                l_run = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l_run += ss.x[other][i][r];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(latp::sums + group));   // (the next item's first step may write there)
+            }
+            if (!(ok = wait(latp::pv, (s - 1) & 1, 378))) break;
+            tc_fence_after();
+            if (some) {
+                const bool whole = seg.n == seg.of, none = l_run == 0.f;
+                const long long slot = 2ll * worker + (seg.t0 > 0 ? 0 : 1);
+                const float inv = none ? 0.f : 1.f / l_run;
+                if (mine && part == 0) {
+                    const float lse = none ? -INFINITY : (m_run * p.scale_log2 + log2f(l_run)) * 0.6931471805599453f;
+                    if (!whole) p.lse_part[slot * p.rows + x] = lse;
+                    else if (p.lse) p.lse[((long long)seg.b * p.H + head) * p.T + token] = lse;
+                }
+                const int dim = wg * 256 + half * 128;
+                T* o_row = static_cast<T*>(p.o) + ((long long)seg.b * p.T * p.H + R) * kLatDim + dim;
+                float* o_part = p.o_part + (slot * p.rows + x) * kLatDim + dim;
+#pragma unroll 1
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t o[32];
+                    tmem_ld_x32(tmem_o + lanes + wg * 128 + 32 * c, o);
+                    tmem_wait_ld();
+                    auto f = [&](int i) { return none ? 0.f : __uint_as_float(o[i]) * inv; };
+                    if (!mine) continue;
+                    if (whole) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            *reinterpret_cast<uint4*>(o_row + 32 * c + i) = make_uint4(pack2<T>(f(i), f(i + 1)), pack2<T>(f(i + 2), f(i + 3)),
+                                                                                      pack2<T>(f(i + 4), f(i + 5)), pack2<T>(f(i + 6), f(i + 7)));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(o_part + 32 * c + i) = make_float4(f(i), f(i + 1), f(i + 2), f(i + 3));
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(latp::seg_empty + ord % kLatSegs));
+        }
+        __syncwarp();
+    }
+    settle_if(!ok);
+    tc_fence_before();
+    __syncwarp();
+    cluster_sync_all();   // (nothing of this CTA's memory is in use by the other any more)
+    tc_fence_after();
+    if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Shape::kTmemCols) : "memory");
 }
 
 // Merge of the rows that several workers have worked on (the recurrence of decode.cuh's merge): a thread has four columns of a row.

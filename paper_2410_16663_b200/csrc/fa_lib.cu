@@ -1535,29 +1535,33 @@ int fa_cache_append(const fa_append_params* pp, void* stream) {
 
 namespace {
 
-// How a sequence's rows are cut: blocks of equal size.
+// How a sequence's rows are cut: up to 32 are one CTA's, more are blocks of at most 128, of equal size, for pairs of CTAs.
 struct LatentBlocks {
     int blocks, rows;
     LatentBlocks(int T, int H) {
         const long long all = (long long)T * H;
-        blocks = (int)((all + 31) / 32);
+        blocks = (int)((all + 127) / 128);
         rows = (int)((all + blocks - 1) / blocks);
     }
+    bool pairs() const { return rows > 32 || blocks > 1; }
     size_t slots() const { return 2 * (size_t)fa::kTreeMaxSms; }   // partial results that a call may have: two for each worker
 };
 
+// N: the kernel of one CTA with so many columns; 0: that of pairs.
 template <typename T, int N>
-int latent_launch(const CUtensorMap& tm, const CUtensorMap& tmr, fa::LatentParams& lp, int sms, cudaStream_t st) {
-    auto kern = fa::fa_decode_latent_kernel<T, N>;
+int latent_launch(const CUtensorMap& tm, const CUtensorMap& tm2, fa::LatentParams& lp, int sms, cudaStream_t st) {
+    void (*kern)(CUtensorMap, CUtensorMap, fa::LatentParams);
+    int smem, threads;
+    if constexpr (N > 0) kern = fa::fa_decode_latent_kernel<T, N>, smem = fa::LatShape<N>::kSmem, threads = fa::LatShape<N>::kThreads;
+    else kern = fa::fa_decode_latent_pair_kernel<T>, smem = fa::LatPairShape::kSmem, threads = fa::LatPairShape::kThreads;
     int sm_count = 0;
-    if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), fa::LatShape<N>::kSmem, &sm_count))
-        return cuda_fail(static_cast<cudaError_t>(ce));
-    const int grid = sms < fa::kTreeMaxSms ? sms : fa::kTreeMaxSms;
-    lp.workers = grid;
-    lp.by_item = (long long)lp.B * lp.blocks < grid ? 1 : 0;
-    cudaError_t e = fa::launch_dependent(kern, dim3(grid), fa::LatShape<N>::kThreads, fa::LatShape<N>::kSmem, st, tm, tmr, lp);
-    if (e == cudaSuccess && grid > 1) {
-        const int y = lp.by_item ? lp.B * lp.blocks : grid - 1;
+    if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
+    const int ctas = N > 0 ? 1 : 2, most = sms / ctas;
+    lp.workers = most < fa::kTreeMaxSms ? most : fa::kTreeMaxSms;
+    lp.by_item = (long long)lp.B * lp.blocks < lp.workers ? 1 : 0;
+    cudaError_t e = fa::launch_dependent_clusters(kern, dim3(lp.workers * ctas), ctas, 1, threads, smem, st, tm, tm2, lp);
+    if (e == cudaSuccess && lp.workers > 1) {
+        const int y = lp.by_item ? lp.B * lp.blocks : lp.workers - 1;
         e = fa::launch_dependent(fa::fa_decode_latent_combine_kernel<T>, dim3(lp.rows, y), fa::kLatCombineThreads, 0, st, lp);
     }
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
@@ -1623,21 +1627,23 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
     // as zeros; of pages smaller than a tile (64 elements, 8 rows, blocks, groups of 8 rows, pages): a box is a page, and lands group by group.
     const cuuint64_t row = fa::kLatRow * 2, blocks = fa::kLatRow / 64;
     const cuuint64_t slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : Skv_max;
-    CUtensorMap tm, tmr;
+    CUtensorMap tm[2];
+    const bool pairs = lb.pairs(), paged_small = p.block_table && p.page_size < fa::kDecTile;
     for (int i = 0; i < 2 && !rc; ++i) {
-        CUtensorMap* m = i ? &tmr : &tm;
-        const cuuint32_t wide = i ? 1 : 2;
-        if (p.block_table && p.page_size < fa::kDecTile)
-            rc = encode_tiled<5>(m, type16(bf16), p.cache, {64, 8, blocks, slab_rows / 8, slabs}, {row, 128, 8 * row, slab_rows * row},
+        // one CTA: 128 elements, and the rotated 64, of a tile's keys; a pair: 192 of half a tile's, 128 of a tile's
+        const cuuint32_t wide = pairs ? (i ? 2 : 3) : (i ? 1 : 2), keys = pairs && i == 0 ? 64 : fa::kDecTile;
+        if (paged_small)
+            rc = encode_tiled<5>(&tm[i], type16(bf16), p.cache, {64, 8, blocks, slab_rows / 8, slabs}, {row, 128, 8 * row, slab_rows * row},
                                  {64, 8, wide, (cuuint32_t)slab_rows / 8, 1});
         else
-            rc = encode_tiled<5>(m, type16(bf16), p.cache, {64, slab_rows, blocks, slabs, 1}, {row, 128, slab_rows * row, slabs * slab_rows * row},
-                                 {64, (cuuint32_t)fa::kDecTile, wide, 1, 1});
+            rc = encode_tiled<5>(&tm[i], type16(bf16), p.cache, {64, slab_rows, blocks, slabs, 1}, {row, 128, slab_rows * row, slabs * slab_rows * row},
+                                 {64, keys, wide, 1, 1});
     }
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (lp.rows <= 16) return bf16 ? latent_launch<__nv_bfloat16, 16>(tm, tmr, lp, sms, st) : latent_launch<__half, 16>(tm, tmr, lp, sms, st);
-    return bf16 ? latent_launch<__nv_bfloat16, 32>(tm, tmr, lp, sms, st) : latent_launch<__half, 32>(tm, tmr, lp, sms, st);
+    if (pairs) return bf16 ? latent_launch<__nv_bfloat16, 0>(tm[0], tm[1], lp, sms, st) : latent_launch<__half, 0>(tm[0], tm[1], lp, sms, st);
+    if (lp.rows <= 16) return bf16 ? latent_launch<__nv_bfloat16, 16>(tm[0], tm[1], lp, sms, st) : latent_launch<__half, 16>(tm[0], tm[1], lp, sms, st);
+    return bf16 ? latent_launch<__nv_bfloat16, 32>(tm[0], tm[1], lp, sms, st) : latent_launch<__half, 32>(tm[0], tm[1], lp, sms, st);
 }
 
 // CTAs of the one cluster that looks a pool's reference counts over.
