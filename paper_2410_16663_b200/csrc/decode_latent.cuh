@@ -15,7 +15,11 @@
 namespace fa {
 
 constexpr int kLatDim = 512, kLatRope = 64, kLatRow = kLatDim + kLatRope;
+constexpr int kLatTile = 64;    // keys: shared memory holds two such tiles and more, so that one arrives while the other is worked on
 constexpr int kLatSegs = 4;
+// Work is dealt out in units as in decode_tree.cuh: a tile is one, an item's beginning and end two.
+constexpr int kLatItemCost = 2;
+__device__ __forceinline__ int latent_item_units(int len) { return len > 0 ? (len + kLatTile - 1) / kLatTile + kLatItemCost : 0; }
 
 struct LatentParams {
     const void* q;            // [B,T,H,512] by strides
@@ -33,6 +37,7 @@ struct LatentParams {
     int B, T, H, Smax;
     int rows, blocks;         // rows per block, blocks per sequence
     int page_size, table_stride, num_pages;
+    int q_boxes;              // tokens and heads are rows of one stride: Q comes by the tensor maps
     FastDiv by_H;
     float scale_log2;
 };
@@ -63,7 +68,7 @@ struct LatentWalk {
     __device__ __forceinline__ void begin() {
         int total = 0, mine = 0, upto = 0;
         auto scan = [&](int b0, int before) {
-            mine = tree_item_units(lens_at(b0)) * p.blocks;
+            mine = latent_item_units(lens_at(b0)) * p.blocks;
             upto = mine;
 #pragma unroll 1
             for (int sh = 1; sh < 32; sh <<= 1) {
@@ -92,7 +97,7 @@ struct LatentWalk {
         }
         next_b = b;
         next_len = pos < end ? len_of(b) : 0;
-        units = tree_item_units(next_len);
+        units = latent_item_units(next_len);
         item = pos < end ? in_seq / units : 0;
         unit = in_seq - item * units;
     }
@@ -100,13 +105,13 @@ struct LatentWalk {
     __device__ __forceinline__ LatentSegment next(int ord, bool entries) {
         int t0 = 0, n = 0, block = 0, len = 0, first = 0, last_tile = 0;
         while (pos < end && n == 0) {   // (a run may have an item's first units alone, and no tile)
-            first = pos - unit + kTreeItemCost;
+            first = pos - unit + kLatItemCost;
             last_tile = pos - unit + units - 1;
             const int last = min(units, unit + end - pos);
             b = next_b;
             len = next_len;
-            t0 = max(0, unit - kTreeItemCost);
-            n = max(0, last - kTreeItemCost) - t0;
+            t0 = max(0, unit - kLatItemCost);
+            n = max(0, last - kLatItemCost) - t0;
             block = item;
             pos += last - unit;
             unit = 0;
@@ -114,7 +119,7 @@ struct LatentWalk {
                 item = 0;
                 do next_len = len_of(++next_b);
                 while (next_len == 0);
-                units = tree_item_units(next_len);
+                units = latent_item_units(next_len);
             }
         }
         if (entries && lane == 0) {
@@ -125,7 +130,7 @@ struct LatentWalk {
                 p.merges[worker - 1] = make_int4(b, block, worker - 1, mine ? plan.owner(last_tile) : 0);
             }
         }
-        return {b, block, t0, n, (len + kDecTile - 1) / kDecTile, len};
+        return {b, block, t0, n, (len + kLatTile - 1) / kLatTile, len};
     }
 };
 
@@ -145,16 +150,16 @@ __device__ __forceinline__ void latent_fill_empty(const LatentParams& p, int wor
 // One CTA, N = 16 or 32 rows.
 template <int N>
 struct LatShape {
-    static constexpr int kUnitB = 128 * 128 * 2;                    // 128 keys x 128 latent elements: one of the second product's operands
-    static constexpr int kUnits = 5;                                // (a tile is four)
-    static constexpr int kRopeB = 128 * kLatRope * 2, kRopes = N == 16 ? 2 : 1;
-    static constexpr int kQB = N * kLatRow * 2, kPB = 128 * N * 2;
-    static constexpr int kSmem = 1024 + kUnits * kUnitB + kRopes * kRopeB + kQB + kPB;
+    static constexpr int kUnitB = kLatTile * 128 * 2;               // 64 keys x 128 latent elements: one of the second product's operands
+    static constexpr int kUnits = N == 16 ? 11 : 10;                // (a tile is four)
+    static constexpr int kRopeB = kLatTile * kLatRope * 2, kRopes = N == 16 ? 3 : 2;
+    static constexpr int kQB = N * kLatRow * 2, kPB = kLatTile * N * 2;
+    static constexpr int kSmem = 1024 + kUnits * kUnitB + kRopes * kRopeB + kQB + 2 * kPB;
     static constexpr int kThreads = 384;
     static constexpr int kTmemCols = N == 16 ? 128 : 256;           // two score buffers, four parts of the output
     static constexpr int kCols = N / 2;                             // columns of a softmax thread
-    static_assert((2 + 4) * N <= kTmemCols && kSmem <= 230 * 1024, "tensor and shared memory");
-    // P^T [128 keys][N rows]: a key's row of 2 N bytes, swizzled in 32 or 64 bytes
+    static_assert((2 + 4) * N <= kTmemCols && kSmem <= 229 * 1024, "tensor and shared memory");
+    // P^T [64 keys][N rows]: a key's row of 2 N bytes, swizzled in 32 or 64 bytes
     static constexpr uint32_t kPHi = ((8u * 2 * N) >> 4) | (1u << 14) | ((N == 16 ? 6u : 4u) << 29);
 };
 
@@ -162,7 +167,7 @@ template <int N>
 struct LatBars {
     using Shape = LatShape<N>;
     static constexpr int full = 0, empty = full + Shape::kUnits, rope_full = empty + Shape::kUnits, rope_empty = rope_full + Shape::kRopes,
-                         s_full = rope_empty + Shape::kRopes, s_read = s_full + 2, p_full = s_read + 2, pv = p_full + 1, q_full = pv + 1,
+                         s_full = rope_empty + Shape::kRopes, s_read = s_full + 2, p_full = s_read + 2, pv = p_full + 2, q_full = pv + 2,
                          q_empty = q_full + 1, seg_full = q_empty + 1, seg_empty = seg_full + kLatSegs,
                          meet = seg_empty + kLatSegs,   // [2][2] by step and warpgroup: its maxima are there
                          sums = meet + 4, count = sums + 2;   // [2] by warpgroup: an item's sums are there; they have been read
@@ -212,12 +217,15 @@ __device__ __forceinline__ bool lat_meet(uint32_t bar, uint32_t parity, int lane
     return pp_warp_wait(bar, parity, abort_flag, where);
 }
 
+// Scores of 64 keys are 16 lanes of each quarter of tensor memory, so that half of a softmax warp's lanes have one; with tiles of 128 keys all of
+// them had, but only one and a quarter tiles fit, and the chain of loading, both products and the softmax lay open.
 // grid: as many as run at once.  Warps 0 to 7: softmax and output (a key per thread, half the columns each); 8: segments and the cache; 9: Q;
 // 10: S^T; 11: O^T.
 // tm: boxes of 128 latent elements (whole tiles: block by block of 64; pages of less than a tile: eight keys after eight keys), tm_r: of the rotated part.
 template <typename T, int N>
 __global__ void __launch_bounds__(LatShape<N>::kThreads, 1)
-fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_r, const LatentParams p) {
+fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_r, const __grid_constant__ CUtensorMap tm_q,
+                        const __grid_constant__ CUtensorMap tm_qr, const LatentParams p) {
     using Shape = LatShape<N>;
     using At = LatBars<N>;
     constexpr int C = Shape::kCols;
@@ -259,8 +267,8 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     grid_dep_wait();
 
     const int ps = p.page_size;
-    const bool small = p.block_table != nullptr && ps < kDecTile;   // a tile is several pages
-    const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 16384u;   // bytes from eight keys of a unit to the next, from 64 elements to the next
+    const bool small = p.block_table != nullptr && ps < kLatTile;   // a tile is several pages
+    const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 8192u;   // bytes from eight keys of a unit to the next, from 64 elements to the next
     bool ok = true;
     auto segment = [&](uint32_t ord, LatentSegment& s) {
         if (!pp_warp_wait(bar(At::seg_full + ord % kLatSegs), (ord / kLatSegs) & 1, &abort_flag, 340)) return false;
@@ -271,7 +279,8 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     if (warp == 8) {
         // ---------------------------------------------------------------- segments and the cache
         const uint64_t policy = p.blocks > 1 ? l2_policy_evict_last() : l2_policy_evict_first();
-        uint32_t u = 0, r = 0;   // units and rotated parts asked for
+        PpRing<Shape::kUnits> units;
+        PpRing<Shape::kRopes> ropes;
         for (uint32_t ord = 0; ok; ++ord) {
             const LatentSegment seg = walk.next(ord, true);
             const int slot = ord % kLatSegs;
@@ -284,30 +293,49 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             const int* table = p.block_table ? p.block_table + (long long)seg.b * p.table_stride : nullptr;
             auto lookup = [&](int key) {   // the page of this lane's part of the tile at `key`, one tile ahead
                 if (!table || key >= seg.len) return -1;
-                return small ? (lane < kDecTile / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
+                const int page = small ? (lane < kLatTile / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
+                return (unsigned)page < (unsigned)p.num_pages ? page : -1;   // (none: zeros)
             };
-            int page_next = lookup(seg.t0 * kDecTile);
-            for (int j = 0; j < seg.n && ok; ++j) {
-                const int key0 = (seg.t0 + j) * kDecTile, page = (unsigned)page_next < (unsigned)p.num_pages ? page_next : -1;   // (none: zeros)
-                if (j + 1 < seg.n) page_next = lookup(key0 + kDecTile);
-                const int boxes = small ? (min(seg.len - key0, kDecTile) + ps - 1) / ps : 1, keys = small ? ps : kDecTile;   // of a unit, of a box
+            const int end = (seg.t0 + seg.n) * kLatTile, keys = small ? ps : kLatTile;   // of a box
+            int page = lookup(seg.t0 * kLatTile);
+            for (int key0 = seg.t0 * kLatTile; key0 < end && ok; key0 += kLatTile) {
+                const int next = key0 + kLatTile, page_next = next < end ? lookup(next) : -1;
+                const int boxes = small ? (min(seg.len - key0, kLatTile) + ps - 1) / ps : 1;   // of a unit
                 const int row = table ? key0 % ps : key0, slab = table ? page : seg.b;
-                for (int m = -1; m < 4 && ok; ++m) {   // the rotated part, and the units
-                    const bool rope = m < 0;
-                    const uint32_t n = rope ? r++ : u++, slots = rope ? Shape::kRopes : Shape::kUnits, at = n % slots;
-                    const uint32_t full = bar((rope ? At::rope_full : At::full) + at), empty = bar((rope ? At::rope_empty : At::empty) + at);
-                    if (lane == 0) ok = mbar_wait(empty, ((n / slots) & 1) ^ 1, &abort_flag, 342);
-                    if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; break; }
-                    const uint32_t bytes = keys * (rope ? 128u : 256u);   // of a box
-                    const uint32_t dst = (rope ? sRope + at * Shape::kRopeB : sUnits + at * Shape::kUnitB) + lane * bytes;
-                    if (lane == 0) mbar_expect_tx(full, boxes * bytes);
-                    __syncwarp();
-                    if (lane < boxes) {
-                        const int c = rope ? 8 : 2 * m;
-                        if (small) tma_load_5d_hint(dst, rope ? &tm_r : &tm, full, 0, 0, c, 0, page, policy);
-                        else tma_load_5d_hint(dst, rope ? &tm_r : &tm, full, 0, row, c, slab, 0, policy);
+                // (written out for each of the five: 660 clocks of a loop with divisions each were all that 64 keys have time for)
+                auto wait_for = [&](auto& ring, int full, int empty, uint32_t bytes) {
+                    if (!mbar_wait(bar(empty + ring.slot), ring.par ^ 1, &abort_flag, 342)) return false;
+                    mbar_expect_tx(bar(full + ring.slot), bytes);
+                    return true;
+                };
+                if (!small) {
+                    if (lane == 0) {
+                        ok = wait_for(ropes, At::rope_full, At::rope_empty, Shape::kRopeB);
+                        if (ok) tma_load_5d_hint(sRope + ropes.slot * Shape::kRopeB, &tm_r, bar(At::rope_full + ropes.slot), 0, row, 8, slab, 0, policy);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            ok = ok && wait_for(units, At::full, At::empty, Shape::kUnitB);
+                            if (ok) tma_load_5d_hint(sUnits + units.slot * Shape::kUnitB, &tm, bar(At::full + units.slot), 0, row, 2 * m, slab, 0, policy);
+                            units.next();
+                        }
+                        ropes.next();
+                    }
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                } else {
+                    if (lane == 0) ok = wait_for(ropes, At::rope_full, At::rope_empty, boxes * keys * 128);
+                    ok = __shfl_sync(0xffffffffu, ok, 0);
+                    if (ok && lane < boxes) tma_load_5d_hint(sRope + ropes.slot * Shape::kRopeB + lane * keys * 128, &tm_r, bar(At::rope_full + ropes.slot), 0, 0, 8, 0, page, policy);
+                    ropes.next();
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        if (ok && lane == 0) ok = wait_for(units, At::full, At::empty, boxes * keys * 256);
+                        ok = __shfl_sync(0xffffffffu, ok, 0);
+                        if (ok && lane < boxes)
+                            tma_load_5d_hint(sUnits + units.slot * Shape::kUnitB + lane * keys * 256, &tm, bar(At::full + units.slot), 0, 0, 2 * m, 0, page, policy);
+                        units.next();
                     }
                 }
+                page = page_next;
             }
         }
         __syncwarp();
@@ -321,6 +349,14 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             if (seg.n <= 0) break;
             if (ord > 0 && !(ok = pp_warp_wait(bar(At::q_empty), (ord - 1) & 1, &abort_flag, 343))) break;
             const int R0 = seg.block * p.rows, rows = min(p.rows, p.H * p.T - R0);
+            if (p.q_boxes) {   // (rows past the last are zeros, those of the next block are computed and left)
+                if (lane == 0) {
+                    mbar_expect_tx(bar(At::q_full), Shape::kQB);
+                    tma_load_4d(sQ, &tm_q, bar(At::q_full), 0, R0, 0, seg.b);
+                    tma_load_4d(sQ + 8 * N * 128, &tm_qr, bar(At::q_full), 0, R0, 0, seg.b);
+                }
+                continue;
+            }
             for (int i = lane; i < N * (kLatRow / 8); i += 32) {   // 16-byte pieces; rows that are none are zeros
                 const int x = i / (kLatRow / 8), c = i % (kLatRow / 8);
                 const uint32_t at = sQ + (c >> 3) * (N * 128u) + x * 128u + (((c & 7) ^ (x & 7)) << 4);
@@ -341,11 +377,13 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     } else if (warp == 10) {
         // ---------------------------------------------------------------- S^T = C Q^T
         if (elect_one()) {
-            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, N, false, false);
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 64, N, false, false);
             const uint32_t a_hi = tree_desc_hi(group);
             constexpr uint32_t rows_hi = tree_desc_hi(1024);
             const uint32_t u_lo = desc_lo(sUnits, 16), r_lo = desc_lo(sRope, 16), q_lo = desc_lo(sQ, 16);
             uint32_t s = 0;
+            PpRing<Shape::kUnits> units;
+            PpRing<Shape::kRopes> ropes;
             for (uint32_t ord = 0; ok; ++ord) {
                 const int slot = ord % kLatSegs;
                 if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kLatSegs) & 1, &abort_flag, 344))) break;
@@ -354,20 +392,20 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 if (n <= 0) break;
                 if (!(ok = mbar_wait(bar(At::q_full), ord & 1, &abort_flag, 345))) break;
                 for (int j = 0; j < n && ok; ++j, ++s) {
-                    const uint32_t buf = s & 1, d = tmem + buf * N, rs = s % Shape::kRopes;
+                    const uint32_t buf = s & 1, d = tmem + buf * N;
                     if (s >= 2 && !(ok = mbar_wait(bar(At::s_read + buf), ((s >> 1) - 1) & 1, &abort_flag, 346))) break;
-                    if (!(ok = mbar_wait(bar(At::rope_full + rs), (s / Shape::kRopes) & 1, &abort_flag, 347))) break;
+                    if (!(ok = mbar_wait(bar(At::rope_full + ropes.slot), ropes.par, &abort_flag, 347))) break;
                     tc_fence_after();
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        tree_mma_ss(d, r_lo + rs * (Shape::kRopeB >> 4) + ks * 2, rows_hi, q_lo + ((8 * N * 128) >> 4) + ks * 2, rows_hi, idesc, ks > 0);
-                    mma_commit(bar(At::rope_empty + rs));
+                        tree_mma_ss(d, r_lo + ropes.slot * (Shape::kRopeB >> 4) + ks * 2, rows_hi, q_lo + ((8 * N * 128) >> 4) + ks * 2, rows_hi, idesc, ks > 0);
+                    mma_commit(bar(At::rope_empty + ropes.slot));
+                    ropes.next();
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const uint32_t n_u = 4 * s + m, at = n_u % Shape::kUnits;
-                        if (!(ok = mbar_wait(bar(At::full + at), (n_u / Shape::kUnits) & 1, &abort_flag, 348))) break;
+                    for (int m = 0; m < 4; ++m, units.next()) {
+                        if (!(ok = mbar_wait(bar(At::full + units.slot), units.par, &abort_flag, 348))) break;
                         tc_fence_after();
-                        const uint32_t a = u_lo + at * (Shape::kUnitB >> 4);
+                        const uint32_t a = u_lo + units.slot * (Shape::kUnitB >> 4);
 #pragma unroll
                         for (int ks = 0; ks < 8; ++ks)
                             tree_mma_ss(d, a + (ks >> 2) * (block >> 4) + (ks & 3) * 2, a_hi, q_lo + (((2 * m + (ks >> 2)) * N * 128) >> 4) + (ks & 3) * 2, rows_hi, idesc, 1u);
@@ -388,6 +426,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             const uint32_t a_hi = tree_desc_hi(group);
             const uint32_t u_lo = desc_lo(sUnits, block), p_lo = desc_lo(sP, 16);
             uint32_t s = 0;
+            PpRing<Shape::kUnits> units;
             for (uint32_t ord = 0; ok; ++ord) {
                 const int slot = ord % kLatSegs;
                 if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kLatSegs) & 1, &abort_flag, 350))) break;
@@ -396,25 +435,26 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 if (n <= 0) break;
                 for (int j = 0; j < n; ++j, ++s) {
                     // (the probabilities come when the scores have, whose units are there; an item's first when the output before it has been read)
-                    if (!(ok = mbar_wait(bar(At::p_full), s & 1, &abort_flag, 351))) break;
+                    if (!(ok = mbar_wait(bar(At::p_full + (s & 1)), (s >> 1) & 1, &abort_flag, 351))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const uint32_t at = (4 * s + m) % Shape::kUnits, a = u_lo + at * (Shape::kUnitB >> 4);
+                    for (int m = 0; m < 4; ++m, units.next()) {
+                        const uint32_t a = u_lo + units.slot * (Shape::kUnitB >> 4);
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks)
-                            tree_mma_ss(tmem_o + m * N, a + ks * (2 * group >> 4), a_hi, p_lo + ((ks * 16 * 2 * N) >> 4), Shape::kPHi, idesc, j > 0 || ks > 0 ? 1u : 0u);
-                        mma_commit(bar(At::empty + at));
+                        for (int ks = 0; ks < kLatTile / 16; ++ks)
+                            tree_mma_ss(tmem_o + m * N, a + ks * (2 * group >> 4), a_hi, p_lo + (((s & 1) * Shape::kPB + ks * 16 * 2 * N) >> 4), Shape::kPHi, idesc, j > 0 || ks > 0 ? 1u : 0u);
+                        mma_commit(bar(At::empty + units.slot));
                     }
-                    mma_commit(bar(At::pv));
+                    mma_commit(bar(At::pv + (s & 1)));
                 }
             }
-            if (ok && s > 0) ok = mbar_wait(bar(At::pv), (s - 1) & 1, &abort_flag, 352);
+            if (ok && s > 0) ok = mbar_wait(bar(At::pv + ((s - 1) & 1)), ((s - 1) >> 1) & 1, &abort_flag, 352);
         }
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax: a key per thread, C columns
-        const int wg = warp >> 2, quarter = warp & 3, k = tid & 127, col0 = wg * C;
+        const int wg = warp >> 2, quarter = warp & 3, dim = tid & 127, col0 = wg * C;
+        const int k = quarter * 16 + (lane & 15);   // key of the tile; lanes 16 to 31 have none
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         uint32_t s = 0;
         latent_fill_empty<T>(p, blockIdx.x, tid, 256);
@@ -426,7 +466,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 #pragma unroll
             for (int c = 0; c < C; ++c) m_run[c] = -INFINITY, l_run[c] = 0.f;
             for (int j = 0; j < seg.n; ++j, ++s) {
-                const int key0 = (seg.t0 + j) * kDecTile, key = key0 + k;
+                const int key0 = (seg.t0 + j) * kLatTile, key = key0 + k;
                 const uint32_t buf = s & 1;
                 if (!(ok = pp_warp_wait(bar(At::s_full + buf), (s >> 1) & 1, &abort_flag, 353))) break;
                 tc_fence_after();
@@ -436,7 +476,11 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(At::s_read + buf));
-                if (key0 + kDecTile > seg.len - p.T + 1) {
+                if (lane >= 16) {
+#pragma unroll
+                    for (int c = 0; c < C; ++c) sc[c] = 0xff800000u;
+                }
+                if (key0 + kLatTile > seg.len - p.T + 1) {
                     // the tile holds keys that some row does not see, or that are none: -inf, an exact zero (the scale is positive)
 #pragma unroll
                     for (int c = 0; c < C; ++c) {
@@ -445,7 +489,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     }
                     // Keys that are none may be anything as values, NaN too: they become zeros.  (The scores have been formed: nothing else reads them.)
                     const int valid = seg.len - key0;
-                    for (int i = tid; i < (kDecTile - valid) * (kLatDim / 8); i += 256) {
+                    for (int i = tid; i < (kLatTile - valid) * (kLatDim / 8); i += 256) {
                         const int x = valid + i / (kLatDim / 8), piece = i % (kLatDim / 8);
                         const uint32_t unit = sUnits + (4 * s + (piece >> 4)) % Shape::kUnits * Shape::kUnitB;
                         const uint32_t at = unit + (uint32_t)(x >> 3) * group + (piece >> 3 & 1) * block + (uint32_t)(x & 7) * 128u + ((piece & 7) << 4);   // (swizzled or not)
@@ -457,7 +501,20 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 for (int c = 0; c < C; ++c) mx[c] = warp_max(__uint_as_float(sc[c]));
                 if (j == 0 && ord > 0 && !(ok = pp_warp_wait(bar(At::sums + wg), 1, &abort_flag, 356))) break;   // (the last item's sums lie in one of them)
                 if (lane == 0) lat_sts<C>(smem_u32(&s_max[buf][quarter][col0]), mx);
-                if (!(ok = lat_meet(bar(At::meet + 2 * buf + wg), (s >> 1) & 1, lane, &abort_flag, 357))) break;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(At::meet + 2 * buf + wg));
+                // The reference of the exponentials follows the row's maximum only where that has outgrown it by 2^8: P is at most 256 then,
+                // and O is seldom scaled.  So they are formed with the reference as it is while the warpgroup's warps meet.
+                float e[C], alpha[C];
+                auto exponentials = [&]() {
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        const float neg = m_run[c] == -INFINITY ? 0.f : -m_run[c] * p.scale_log2;
+                        e[c] = fast_exp2(fmaf(__uint_as_float(sc[c]), p.scale_log2, neg));
+                    }
+                };
+                if (j > 0) exponentials();
+                if (!(ok = pp_warp_wait(bar(At::meet + 2 * buf + wg), (s >> 1) & 1, &abort_flag, 357))) break;
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     float other[C];
@@ -465,36 +522,35 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 #pragma unroll
                     for (int c = 0; c < C; ++c) mx[c] = w == 0 ? other[c] : fmaxf(mx[c], other[c]);
                 }
-                // The reference of the exponentials follows the row's maximum only where that has outgrown it by 2^8: P is at most 256 then,
-                // and O is seldom scaled.
-                bool moved = false;
-                float alpha[C];
+                bool moved = false;   // (the same for the whole warpgroup)
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const bool grow = (mx[c] - m_run[c]) * p.scale_log2 > kRescaleThreshold;   // (never on -inf)
-                    alpha[c] = grow ? fast_exp2((m_run[c] - mx[c]) * p.scale_log2) : 1.f;
-                    if (grow) m_run[c] = mx[c];
-                    moved |= grow;
-                    l_run[c] *= alpha[c];
-                }
-                float e[C];
+                for (int c = 0; c < C; ++c) moved |= (mx[c] - m_run[c]) * p.scale_log2 > kRescaleThreshold;   // (never on -inf)
+                if (moved) {
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const float neg = m_run[c] == -INFINITY ? 0.f : -m_run[c] * p.scale_log2;
-                    e[c] = fast_exp2(fmaf(__uint_as_float(sc[c]), p.scale_log2, neg));
-                    l_run[c] += e[c];
+                    for (int c = 0; c < C; ++c) {
+                        const bool grow = (mx[c] - m_run[c]) * p.scale_log2 > kRescaleThreshold;
+                        alpha[c] = grow ? fast_exp2((m_run[c] - mx[c]) * p.scale_log2) : 1.f;
+                        if (grow) m_run[c] = mx[c];
+                        l_run[c] *= alpha[c];
+                    }
                 }
-                // P^T of the step before has been read, and O holds the sums up to there
-                if (s > 0 && !(ok = pp_warp_wait(bar(At::pv), (s - 1) & 1, &abort_flag, 354))) break;
+                if (moved || j == 0) exponentials();
+#pragma unroll
+                for (int c = 0; c < C; ++c) l_run[c] += e[c];
+                // P^T of two steps before has been read
+                if (s >= 2 && !(ok = pp_warp_wait(bar(At::pv + buf), ((s >> 1) - 1) & 1, &abort_flag, 354))) break;
+                if (lane < 16) {
 #pragma unroll
                 for (int c = 0; c < C; c += 8) {
                     const uint32_t chunk = (uint32_t)(col0 + c) >> 3, xored = N == 16 ? chunk ^ (k >> 2 & 1) : chunk ^ (k >> 1 & 3);
-                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + (uint32_t)k * (2 * N) + (xored << 4)), "r"(pack2<T>(e[c], e[c + 1])),
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + buf * Shape::kPB + (uint32_t)k * (2 * N) + (xored << 4)), "r"(pack2<T>(e[c], e[c + 1])),
                                  "r"(pack2<T>(e[c + 2], e[c + 3])), "r"(pack2<T>(e[c + 4], e[c + 5])), "r"(pack2<T>(e[c + 6], e[c + 7]))
                                  : "memory");
                 }
+                }
                 fence_proxy_async_smem();
-                if (j > 0 && moved) {   // (the same for the whole warpgroup)
+                if (j > 0 && moved) {
+                    if (!(ok = pp_warp_wait(bar(At::pv + (buf ^ 1)), ((s - 1) >> 1) & 1, &abort_flag, 359))) break;   // O holds the sums up to the step before
                     tc_fence_after();
 #pragma unroll 1
                     for (int m = 0; m < 4; ++m) {
@@ -509,7 +565,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(At::p_full));
+                if (lane == 0) mbar_arrive(bar(At::p_full + buf));
             }
             if (!ok) break;
             // the row sums over the keys, in the buffer that the last step has not used
@@ -545,7 +601,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     else if (p.lse) p.lse[((long long)seg.b * p.H + head) * p.T + token] = lse;
                 }
             }
-            if (!(ok = pp_warp_wait(bar(At::pv), (s - 1) & 1, &abort_flag, 355))) break;
+            if (!(ok = pp_warp_wait(bar(At::pv + ((s - 1) & 1)), ((s - 1) >> 1) & 1, &abort_flag, 355))) break;
             tc_fence_after();
             T* o_rows = static_cast<T*>(p.o) + ((long long)seg.b * p.T * p.H + R0) * kLatDim;
             float* o_part = p.o_part + slot * p.rows * kLatDim;
@@ -559,8 +615,8 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     const int x = col0 + c;
                     const float v = l_run[c] == 0.f ? 0.f : __uint_as_float(o[c]) * inv[c];
                     if (x < rows) {
-                        if (whole) o_rows[(long long)x * kLatDim + m * 128 + k] = static_cast<T>(v);
-                        else o_part[(long long)x * kLatDim + m * 128 + k] = v;
+                        if (whole) o_rows[(long long)x * kLatDim + m * 128 + dim] = static_cast<T>(v);
+                        else o_part[(long long)x * kLatDim + m * 128 + dim] = v;
                     }
                 }
             }
@@ -580,32 +636,32 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 // ---------------------------------------------------------------------------------------
 // More than 32 rows: a pair of CTAs (a cluster) has blocks of 128, 64 rows in each, and issues matrix instructions of both (cta_group::2, M = 128).  Each
 // CTA's tensor memory then holds its 64 rows in the lanes 0 to 63 for the first half of the columns and in 64 to 127 for the second: 512
-// columns of output in 256 of its 512 columns, scores of 128 keys in 64 -- one CTA's tensor memory would be full with the output
-// of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 64 keys of a
-// tile), latent elements for the output (each loads 256 elements of all 128 keys): 1.9 times the tile over L2, once from HBM.
+// columns of output in 256 of its 512 columns, scores of 64 keys in 32 -- one CTA's tensor memory would be full with the output
+// of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 32 keys of a
+// tile), latent elements for the output (each loads 256 elements of all 64 keys): 1.9 times the tile over L2, once from HBM.
 struct LatPairShape {
-    static constexpr int kKUnitB = 64 * 192 * 2, kKUnits = 3;       // 64 keys x 192 elements: a third of a CTA's keys
-    static constexpr int kVUnitB = 128 * 128 * 2, kVUnits = 2;      // 128 keys x 128 elements: half of a CTA's latent elements
-    static constexpr int kQB = 64 * kLatRow * 2, kPB = 64 * 128 * 2;
-    static constexpr int kSmem = kQB + kPB + kKUnits * kKUnitB + kVUnits * kVUnitB;   // 224 KiB, behind kPairStaticBytes
+    static constexpr int kKB = 32 * kLatRow * 2;                    // a CTA's keys of a tile: 32, all elements
+    static constexpr int kVB = kLatTile * 256 * 2;                  // its values: 64 keys, two times 128 elements
+    static constexpr int kQB = 64 * kLatRow * 2, kPB = 64 * kLatTile * 2;
+    static constexpr int kSmem = kQB + 2 * (kPB + kKB + kVB);       // 224 KiB, behind kPairStaticBytes
     static constexpr int kThreads = 416;
-    static constexpr int kTmemCols = 512;                           // scores [0,64) and [64,128), output [128,384)
+    static constexpr int kTmemCols = 512;                           // scores [0,32) and [32,64), output [128,384)
 };
 namespace latp {   // barriers
-constexpr int k_full = 0;                                   // [3]  TMA -> S thread, and the other CTA's relay
-constexpr int k_peer = k_full + LatPairShape::kKUnits;      // [3]  first CTA: the other CTA's unit is there
-constexpr int k_empty = k_peer + LatPairShape::kKUnits;     // [3]  S thread (commit, to both)
-constexpr int v_full = k_empty + LatPairShape::kKUnits;     // [2]  TMA -> the CTA's softmax warps, whose probabilities say that it is there
-constexpr int v_empty = v_full + LatPairShape::kVUnits;     // [2]  PV thread (commit, to both)
-constexpr int s_full = v_empty + LatPairShape::kVUnits;     // [2]  S thread (commit, to both)
-constexpr int p_full = s_full + 2;                          // [2]  first CTA: sixteen softmax warps
-constexpr int pv = p_full + 2;                              // [1]  PV thread (commit, to both)
-constexpr int q_full = pv + 1;                              // [1]  first CTA: both Q warps
-constexpr int q_empty = q_full + 1;                         // [1]  S thread (commit, to both)
-constexpr int seg_full = q_empty + 1;                       // [4]
-constexpr int seg_empty = seg_full + kLatSegs;              // [4]  eight softmax warps, V, Q, and what else reads segments: two threads, in the second CTA one
-constexpr int meet = seg_empty + kLatSegs;                  // [2][2] by meeting and rows: the maxima of the four warps that have them are there
-constexpr int sums = meet + 4;                              // [2] by rows: an item's sums are there; they have been read
+constexpr int k_full = 0;               // [2]  first CTA: TMA of both -> S thread
+constexpr int k_empty = k_full + 2;     // [2]  S thread (commit, to both)
+constexpr int v_full = k_empty + 2;     // [2]  TMA -> PV thread, or the relay
+constexpr int v_peer = v_full + 2;      // [2]  first CTA: the other's is there
+constexpr int s_full = v_peer + 2;      // [2]  S thread (commit, to both)
+constexpr int p_full = s_full + 2;      // [2]  first CTA: sixteen softmax warps
+constexpr int pv = p_full + 2;          // [2]  PV thread (commit, to both); the values have been read, too
+constexpr int q_full = pv + 2;          // [1]  as for the values
+constexpr int q_peer = q_full + 1;      // [1]
+constexpr int q_empty = q_peer + 1;     // [1]  S thread (commit, to both)
+constexpr int seg_full = q_empty + 1;   // [4]
+constexpr int seg_empty = seg_full + kLatSegs;   // [4]  eight softmax warps, and those of V, Q, S and PV (or their relays)
+constexpr int meet = seg_empty + kLatSegs;       // [2][2] by meeting and rows: the maxima of the four warps that have them are there
+constexpr int sums = meet + 4;                   // [2] by rows: an item's sums are there; they have been read
 constexpr int count = sums + 2;
 }  // namespace latp
 struct LatPairStatic {
@@ -632,40 +688,28 @@ __device__ __forceinline__ void pair_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint
 __device__ __forceinline__ void pair_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-// Arrives on a barrier of the cluster (an address of cluster_map).
+// Arrives on a barrier of the cluster (an address of cluster_map).  What the barrier is for are shared and tensor memory of the arriving CTA, which the
+// matrix instructions read there: whoever arrives has ordered its accesses before (fence_proxy_async_smem, tc_fence_before, a barrier that
+// TMA completes), and nobody reads the other CTA's memory by loads.  A release at the scope of the cluster would wait for everything that the
+// thread has under way, 2000 clocks and more.
 __device__ __forceinline__ void cluster_mbar_arrive(uint32_t addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
-}
-// A wait for such arrivals: what the other CTA's threads wrote is visible.
-__device__ __forceinline__ bool cluster_mbar_try_wait(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
-    return ok != 0;
-}
-__device__ __forceinline__ bool cluster_mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* abort_flag, unsigned int where) {
-    if (!mbar_wait(bar, parity, abort_flag, where)) return false;
-    cluster_mbar_try_wait(bar, parity);   // (it has completed: for the order)
-    return true;
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
 
 // grid: two CTAs per worker.  Warps 0 to 7: softmax and output -- lane and warp & 3 say the row and the half of the keys, warp >> 2 which
-// 32 of those; 8: segments and keys; 9: Q; 10: S (first CTA) or the relay of the keys' arrival; 11: O (first CTA); 12: values.
-// tm_k: boxes of 64 keys x 192 elements, tm_v: 128 keys x 128 elements (pages of less: as in fa_decode_latent_kernel).
+// 16 of those; 8: segments and keys; 9: Q; 10: S (first CTA), or a relay that tells the first CTA
+// that Q has arrived; 11: O, or the relay of the values; 12: values.
+// tm_k: boxes of 32 keys, all elements; tm_v: 64 keys x 128 elements (pages of less: as in fa_decode_latent_kernel).
 template <typename T>
 __global__ void __launch_bounds__(LatPairShape::kThreads, 1)
-fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const LatentParams p) {
+fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_q,
+                             const __grid_constant__ CUtensorMap tm_qr, const LatentParams p) {
     using Shape = LatPairShape;
     constexpr bool kBf16 = std::is_same<T, __nv_bfloat16>::value;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(1024) uint8_t static_raw[kPairStaticBytes];
     LatPairStatic& ss = *reinterpret_cast<LatPairStatic*>(static_raw);
-    const uint32_t sQ = smem_u32(smem_raw), sP = sQ + Shape::kQB, sK = sP + Shape::kPB, sV = sK + Shape::kKUnits * Shape::kKUnitB;
+    const uint32_t sQ = smem_u32(smem_raw), sP = sQ + Shape::kQB, sK = sP + 2 * Shape::kPB, sV = sK + 2 * Shape::kKB;
     volatile uint32_t* abort_flag = &ss.abort_flag;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, worker = blockIdx.x >> 1, rank = blockIdx.x & 1;
     auto bar = [&](int i) { return smem_u32(&ss.bars[i]); };
@@ -676,7 +720,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     }
     if (tid == 0) {
         for (int i = 0; i < latp::count; ++i)
-            mbar_init(bar(i), i >= latp::p_full && i < latp::pv ? 16 : i == latp::q_full ? 2 : i >= latp::meet ? 4 : i >= latp::seg_empty ? 12 - rank : 1);
+            mbar_init(bar(i), i >= latp::p_full && i < latp::pv ? 16 : i >= latp::meet ? 4 : i >= latp::seg_empty ? 12 : 1);
         ss.abort_flag = 0;
         fence_mbar_init();
         tma_prefetch_desc(&tm_k);
@@ -699,50 +743,27 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     grid_dep_wait();
 
     const int ps = p.page_size;
-    const bool small = p.block_table != nullptr && ps < kDecTile;
+    const bool small = p.block_table != nullptr && ps < kLatTile;
     bool ok = true;
     auto segment = [&](uint32_t ord, LatentSegment& s) {
         if (!pp_warp_wait(bar(latp::seg_full + ord % kLatSegs), (ord / kLatSegs) & 1, abort_flag, 360)) return false;
         s = ss.segs[ord % kLatSegs];
         return true;
     };
-    // Loads `units` boxes of `keys` keys per tile, the CTA's share of them, through a ring of as many slots.
-    auto load_tiles = [&](const LatentSegment& seg, uint32_t& u, bool values) {
-        const uint64_t policy = l2_policy_evict_last();   // (the pair reads everything twice, and other blocks of rows again)
-        const int keys = values ? kDecTile : 64, units = values ? Shape::kVUnits : Shape::kKUnits, blocks = values ? 2 : 3, skip = values ? 0 : rank * 64;
-        const uint32_t ring = values ? sV : sK, unit_b = values ? Shape::kVUnitB : Shape::kKUnitB;
-        const int full0 = values ? latp::v_full : latp::k_full, empty0 = values ? latp::v_empty : latp::k_empty;
-        const CUtensorMap* tm = values ? &tm_v : &tm_k;
-        const int* table = p.block_table ? p.block_table + (long long)seg.b * p.table_stride : nullptr;
-        auto lookup = [&](int key) {   // the page of this lane's part of the keys from `key` on, one tile ahead
-            if (!table || key >= seg.len) return -1;
-            return small ? (lane < keys / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
-        };
-        int page_next = lookup(seg.t0 * kDecTile + skip);
-        for (int j = 0; j < seg.n; ++j) {
-            const int key0 = (seg.t0 + j) * kDecTile + skip, page = (unsigned)page_next < (unsigned)p.num_pages ? page_next : -1;   // (none: zeros)
-            if (j + 1 < seg.n) page_next = lookup(key0 + kDecTile);
-            const int boxes = small ? (max(0, min(seg.len - key0, keys)) + ps - 1) / ps : 1, box_keys = small ? ps : keys;
-            const uint32_t bytes = box_keys * blocks * 128;
-            for (int i = 0; i < units; ++i, ++u) {
-                const uint32_t at = u % units, full = bar(full0 + at);
-                if (lane == 0) ok = mbar_wait(bar(empty0 + at), ((u / units) & 1) ^ 1, abort_flag, values ? 362 : 361);
-                if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; return; }
-                if (lane == 0) mbar_expect_tx(full, boxes * bytes);
-                __syncwarp();
-                if (lane < boxes) {
-                    const int c = values ? 4 * i + 2 * rank : 3 * i;
-                    const uint32_t dst = ring + at * unit_b + lane * bytes;
-                    if (small) tma_load_5d_hint(dst, tm, full, 0, 0, c, 0, page, policy);
-                    else tma_load_5d_hint(dst, tm, full, 0, table ? key0 % ps : key0, c, table ? page : seg.b, 0, policy);
-                }
-            }
-        }
+    // The page of this lane's part of `keys` keys from `key` on, or of all of them.
+    auto lookup = [&](const LatentSegment& seg, int key, int keys) {
+        if (!p.block_table || key >= seg.len) return -1;
+        const int* table = p.block_table + (long long)seg.b * p.table_stride;
+        const int page = small ? (lane < keys / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
+        return (unsigned)page < (unsigned)p.num_pages ? page : -1;   // (none: zeros)
     };
+    auto boxes_of = [&](const LatentSegment& seg, int key, int keys) { return small ? (max(0, min(seg.len - key, keys)) + ps - 1) / ps : 1; };
+    const uint64_t policy = l2_policy_evict_last();   // (the pair reads everything twice, and other blocks of rows again)
 
     if (warp == 8) {
         // ---------------------------------------------------------------- segments and keys
         uint32_t u = 0;
+        const uint32_t k_full0 = first_bar(latp::k_full);
         for (uint32_t ord = 0; ok; ++ord) {
             const LatentSegment seg = walk.next(ord, rank == 0);
             const int slot = ord % kLatSegs;
@@ -752,7 +773,25 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 mbar_arrive(bar(latp::seg_full + slot));
             }
             if (seg.n <= 0) break;
-            load_tiles(seg, u, false);
+            const int first = seg.t0 * kLatTile + 32 * rank, end = (seg.t0 + seg.n) * kLatTile;
+            const uint32_t bytes = (small ? ps : 32) * (kLatRow * 2);   // of a box
+            int page = lookup(seg, first, 32);
+            for (int key0 = first; key0 < end; key0 += kLatTile, ++u) {
+                const int next = key0 + kLatTile, page_next = next < end ? lookup(seg, next, 32) : -1;
+                const int boxes = boxes_of(seg, key0, 32), at = u & 1;
+                if (lane == 0) {
+                    ok = mbar_wait(bar(latp::k_empty + at), ((u >> 1) & 1) ^ 1, abort_flag, 361);
+                    // (the first CTA expects both's)
+                    if (ok && rank == 0) mbar_expect_tx(bar(latp::k_full + at), (boxes + boxes_of(seg, key0 + 32, 32)) * bytes);
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; break; }
+                if (lane < boxes) {
+                    const uint32_t dst = sK + at * Shape::kKB + lane * bytes, full = k_full0 + 8 * at;
+                    if (small) tma_load_5d_pair_hint(dst, &tm_k, full, 0, 0, 0, 0, page, policy);
+                    else tma_load_5d_pair_hint(dst, &tm_k, full, 0, p.block_table ? key0 % ps : key0, 0, p.block_table ? page : seg.b, 0, policy);
+                }
+                page = page_next;
+            }
         }
         __syncwarp();
     } else if (warp == 12) {
@@ -764,7 +803,27 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(latp::seg_empty + ord % kLatSegs));
             if (seg.n <= 0) break;
-            load_tiles(seg, u, true);
+            const int end = (seg.t0 + seg.n) * kLatTile;
+            const uint32_t bytes = (small ? ps : kLatTile) * 256;   // of a box
+            int page = lookup(seg, seg.t0 * kLatTile, kLatTile);
+            for (int key0 = seg.t0 * kLatTile; key0 < end; key0 += kLatTile, ++u) {
+                const int next = key0 + kLatTile, page_next = next < end ? lookup(seg, next, kLatTile) : -1;
+                const int boxes = boxes_of(seg, key0, kLatTile), at = u & 1;
+                if (lane == 0) {
+                    ok = u < 2 || mbar_wait(bar(latp::pv + at), ((u >> 1) - 1) & 1, abort_flag, 362);
+                    if (ok) mbar_expect_tx(bar(latp::v_full + at), 2 * boxes * bytes);
+                }
+                if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; break; }
+                if (lane < boxes) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t dst = sV + at * Shape::kVB + i * (Shape::kVB / 2) + lane * bytes;
+                        if (small) tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, 0, 4 * i + 2 * rank, 0, page, policy);
+                        else tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, p.block_table ? key0 % ps : key0, 4 * i + 2 * rank, p.block_table ? page : seg.b, 0, policy);
+                    }
+                }
+                page = page_next;
+            }
         }
         __syncwarp();
     } else if (warp == 9) {
@@ -777,6 +836,14 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             if (seg.n <= 0) break;
             if (ord > 0 && !(ok = pp_warp_wait(bar(latp::q_empty), (ord - 1) & 1, abort_flag, 364))) break;
             const int R0 = seg.block * p.rows + 64 * rank, rows = min(p.rows - 64 * rank, p.H * p.T - R0);
+            if (p.q_boxes) {
+                if (lane == 0) {
+                    mbar_expect_tx(bar(latp::q_full), Shape::kQB);
+                    tma_load_4d(sQ, &tm_q, bar(latp::q_full), 0, R0, 0, seg.b);
+                    tma_load_4d(sQ + 8 * 8192, &tm_qr, bar(latp::q_full), 0, R0, 0, seg.b);
+                }
+                continue;
+            }
             for (int x = 0; x < 64; ++x) {   // (rows that are none are zeros)
                 int token, head;
                 p.by_H.divmod(R0 + x, token, head);
@@ -793,15 +860,15 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             asm volatile("cp.async.wait_all;" ::: "memory");
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) cluster_mbar_arrive(first_bar(latp::q_full));
+            if (lane == 0) mbar_arrive(bar(latp::q_full));
         }
         __syncwarp();
     } else if (warp == 10) {
         // ---------------------------------------------------------------- S = Q C^T
         if (elect_one()) {
-            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, 128, false, false);
-            const uint32_t group = small ? 3072u : 1024u, block = small ? 1024u : 8192u;
-            const uint32_t b_hi = tree_desc_hi(group);
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kLatTile, false, false);
+            const uint32_t group = small ? 9216u : 1024u, block = small ? 1024u : 4096u;
+            const uint32_t k_hi = tree_desc_hi(group);
             constexpr uint32_t q_hi = tree_desc_hi(1024);
             const uint32_t k_lo = desc_lo(sK, 16), q_lo = desc_lo(sQ, 16);
             uint32_t s = 0;
@@ -811,30 +878,27 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 const int n = ss.segs[slot].n;
                 mbar_arrive(bar(latp::seg_empty + slot));
                 if (n <= 0) break;
-                if (rank == 0 && !(ok = cluster_mbar_wait(bar(latp::q_full), ord & 1, abort_flag, 366))) break;
+                if (!(ok = mbar_wait(bar(latp::q_full), ord & 1, abort_flag, 366))) break;
+                if (rank == 1) {
+                    cluster_mbar_arrive(first_bar(latp::q_peer));
+                    s += n;
+                    continue;
+                }
+                if (!(ok = mbar_wait(bar(latp::q_peer), ord & 1, abort_flag, 382))) break;
                 for (int j = 0; j < n && ok; ++j, ++s) {
                     const uint32_t buf = s & 1;
                     // the scores that lie there have become probabilities, in both CTAs
-                    if (rank == 0 && s >= 2 && !(ok = cluster_mbar_wait(bar(latp::p_full + buf), ((s >> 1) - 1) & 1, abort_flag, 367))) break;
+                    if (s >= 2 && !(ok = mbar_wait(bar(latp::p_full + buf), ((s >> 1) - 1) & 1, abort_flag, 367))) break;
+                    if (!(ok = mbar_wait(bar(latp::k_full + buf), (s >> 1) & 1, abort_flag, 368))) break;
+                    tc_fence_after();
+                    const uint32_t b = k_lo + buf * (Shape::kKB >> 4);
 #pragma unroll
-                    for (int i = 0; i < Shape::kKUnits; ++i) {
-                        if (!(ok = mbar_wait(bar(latp::k_full + i), s & 1, abort_flag, 368))) break;
-                        if (rank == 1) {
-                            cluster_mbar_arrive(first_bar(latp::k_peer + i));
-                            continue;
-                        }
-                        if (!(ok = cluster_mbar_wait(bar(latp::k_peer + i), s & 1, abort_flag, 369))) break;
-                        tc_fence_after();
-                        const uint32_t b = k_lo + i * (Shape::kKUnitB >> 4), a = q_lo + ((3 * i * 8192) >> 4);
-#pragma unroll
-                        for (int ks = 0; ks < 12; ++ks)
-                            pair_mma_ss(tmem + buf * 64, a + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, q_hi, b + (ks >> 2) * (block >> 4) + (ks & 3) * 2, b_hi, idesc, i > 0 || ks > 0);
-                        pair_commit(bar(latp::k_empty + i));
-                    }
-                    if (!ok) break;
-                    if (rank == 0) pair_commit(bar(latp::s_full + buf));
+                    for (int ks = 0; ks < kLatRow / 16; ++ks)
+                        pair_mma_ss(tmem + buf * 32, q_lo + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, q_hi, b + (ks >> 2) * (block >> 4) + (ks & 3) * 2, k_hi, idesc, ks > 0);
+                    pair_commit(bar(latp::k_empty + buf));
+                    pair_commit(bar(latp::s_full + buf));
                 }
-                if (rank == 0) pair_commit(bar(latp::q_empty));
+                pair_commit(bar(latp::q_empty));
             }
             // (what was committed last has arrived before the CTA ends)
             if (ok && s > 0) ok = mbar_wait(bar(latp::s_full + ((s - 1) & 1)), ((s - 1) >> 1) & 1, abort_flag, 370);
@@ -842,10 +906,10 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
         __syncwarp();
     } else if (warp == 11) {
         // ---------------------------------------------------------------- O += P L
-        if (rank == 0 && elect_one()) {
+        if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, 256, false, true);
-            const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 16384u;
-            const uint32_t b_hi = tree_desc_hi(group);
+            const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 8192u;
+            const uint32_t v_hi = tree_desc_hi(group);
             constexpr uint32_t p_hi = tree_desc_hi(1024);
             const uint32_t v_lo = desc_lo(sV, block), p_lo = desc_lo(sP, 16);
             uint32_t s = 0;
@@ -856,24 +920,30 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 mbar_arrive(bar(latp::seg_empty + slot));
                 if (n <= 0) break;
                 for (int j = 0; j < n; ++j, ++s) {
-                    if (!(ok = cluster_mbar_wait(bar(latp::p_full + (s & 1)), (s >> 1) & 1, abort_flag, 372))) break;
+                    const uint32_t buf = s & 1, parity = (s >> 1) & 1;
+                    if (!(ok = mbar_wait(bar(latp::v_full + buf), parity, abort_flag, 376))) break;
+                    if (rank == 1) {
+                        cluster_mbar_arrive(first_bar(latp::v_peer + buf));
+                        continue;
+                    }
+                    if (!(ok = mbar_wait(bar(latp::v_peer + buf), parity, abort_flag, 377))) break;
+                    if (!(ok = mbar_wait(bar(latp::p_full + buf), parity, abort_flag, 372))) break;
                     tc_fence_after();
 #pragma unroll
-                    for (int i = 0; i < Shape::kVUnits; ++i) {
-                        const uint32_t b = v_lo + i * (Shape::kVUnitB >> 4);
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int ks = 0; ks < 8; ++ks)
-                            pair_mma_ss(tmem_o + i * 128, p_lo + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, p_hi, b + ks * (2 * group >> 4), b_hi, idesc, j > 0 || ks > 0 ? 1u : 0u);
-                        pair_commit(bar(latp::v_empty + i));
-                    }
-                    pair_commit(bar(latp::pv));
+                        for (int ks = 0; ks < kLatTile / 16; ++ks)
+                            pair_mma_ss(tmem_o + i * 128, p_lo + (buf * Shape::kPB >> 4) + ks * 2, p_hi, v_lo + ((buf * Shape::kVB + i * (Shape::kVB / 2)) >> 4) + ks * (2 * group >> 4), v_hi, idesc,
+                                        j > 0 || ks > 0 ? 1u : 0u);
+                    pair_commit(bar(latp::pv + buf));
                 }
+                if (!ok) break;
             }
-            if (ok && s > 0) ok = mbar_wait(bar(latp::pv), (s - 1) & 1, abort_flag, 373);
+            if (ok && s > 0) ok = mbar_wait(bar(latp::pv + ((s - 1) & 1)), ((s - 1) >> 1) & 1, abort_flag, 373);
         }
         __syncwarp();
     } else {
-        // ---------------------------------------------------------------- softmax: 32 keys of a row per thread
+        // ---------------------------------------------------------------- softmax: 16 keys of a row per thread
         const int wg = warp >> 2, half = warp >> 1 & 1, r = (warp & 1) * 32 + lane, part = 2 * wg + half;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const int group = warp & 1;   // the four warps that have these rows
@@ -891,68 +961,76 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             const int lim = seg.len - p.T + 1 + token;         // keys that the row sees
             float m_run = -INFINITY, l_run = 0.f;
             for (int j = 0; j < seg.n; ++j, ++s) {
-                const int key0 = (seg.t0 + j) * kDecTile;
+                const int key0 = (seg.t0 + j) * kLatTile;
                 const uint32_t buf = s & 1;
                 if (!(ok = wait(latp::s_full + buf, (s >> 1) & 1, 374))) break;
                 tc_fence_after();
                 float alpha = 1.f;
                 bool moved = false;
-                uint32_t pk[16];
+                uint32_t pk[8];
                 if (some) {
-                    uint32_t sc[32];
-                    tmem_ld_x32(tmem + lanes + buf * 64 + wg * 32, sc);
+                    uint32_t sc[16];
+                    tmem_ld_x16(tmem + lanes + buf * 32 + wg * 16, sc);
                     tmem_wait_ld();
-                    if (key0 + kDecTile > seg.len - p.T + 1) {
+                    if (key0 + kLatTile > seg.len - p.T + 1) {
                         // hidden scores become -inf, their exponentials exact zeros (the scale is positive)
-                        const uint32_t seen = low_bits(lim - key0 - half * 64 - wg * 32);
+                        const uint32_t seen = low_bits(lim - key0 - half * 32 - wg * 16);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
+                        for (int i = 0; i < 16; ++i)
                             if (!(seen & (1u << i))) sc[i] = 0xff800000u;
                     }
-                    float mx = tree_row_max<32>(sc);
+                    float mx = tree_row_max<16>(sc);
                     if (j == 0 && ord > 0 && !(ok = wait(latp::sums + group, 1, 379))) break;   // (the last item's sums lie in one of them)
                     ss.x[met & 1][part][r] = mx;
-                    if (!(ok = lat_meet(bar(latp::meet + 2 * (met & 1) + group), (met >> 1) & 1, lane, abort_flag, 380))) break;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(latp::meet + 2 * (met & 1) + group));
+                    // (the exponentials with the reference as it is meanwhile, as in the other kernel)
+                    uint64_t la, lb;
+                    auto exponentials = [&]() {
+                        const float neg = m_run == -INFINITY ? 0.f : -m_run * p.scale_log2;
+                        const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(neg, neg);
+                        la = lb = f2_pack(0.f, 0.f);
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4) {
+                            float e[4];
+#pragma unroll
+                            for (int k = 0; k < 4; k += 2) {
+                                f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[i + k]), __uint_as_float(sc[i + k + 1])), sc2, nm2), e[k], e[k + 1]);
+                                e[k] = fast_exp2(e[k]);
+                                e[k + 1] = fast_exp2(e[k + 1]);
+                            }
+                            la = f2_add(la, f2_pack(e[0], e[1]));
+                            lb = f2_add(lb, f2_pack(e[2], e[3]));
+                            pk[i / 2] = pack2<T>(e[0], e[1]);
+                            pk[i / 2 + 1] = pack2<T>(e[2], e[3]);
+                        }
+                    };
+                    exponentials();
+                    if (!(ok = wait(latp::meet + 2 * (met & 1) + group, (met >> 1) & 1, 380))) break;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, ss.x[met & 1][i][r]);
                     ++met;
-                    // (the reference follows the maximum as in the other kernel)
                     moved = (mx - m_run) * p.scale_log2 > kRescaleThreshold;   // (never on -inf)
                     if (moved) {
                         alpha = fast_exp2((m_run - mx) * p.scale_log2);
                         m_run = mx;
-                    }
-                    const float neg = m_run == -INFINITY ? 0.f : -m_run * p.scale_log2;
-                    const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(neg, neg);
-                    uint64_t la = f2_pack(0.f, 0.f), lb = la;
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        float e[4];
-#pragma unroll
-                        for (int k = 0; k < 4; k += 2) {
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(sc[i + k]), __uint_as_float(sc[i + k + 1])), sc2, nm2), e[k], e[k + 1]);
-                            e[k] = fast_exp2(e[k]);
-                            e[k + 1] = fast_exp2(e[k + 1]);
-                        }
-                        la = f2_add(la, f2_pack(e[0], e[1]));
-                        lb = f2_add(lb, f2_pack(e[2], e[3]));
-                        pk[i / 2] = pack2<T>(e[0], e[1]);
-                        pk[i / 2 + 1] = pack2<T>(e[2], e[3]);
+                        exponentials();
                     }
                     float a0, a1, b0, b1;
                     f2_unpack(la, a0, a1);
                     f2_unpack(lb, b0, b1);
                     l_run = l_run * alpha + ((a0 + a1) + (b0 + b1));
                 }
-                // the probabilities of the step before have been read, and O holds the sums up to there
-                if (s > 0 && !(ok = wait(latp::pv, (s - 1) & 1, 375))) break;
+                // the probabilities of two steps before have been read
+                if (s >= 2 && !(ok = wait(latp::pv + buf, ((s >> 1) - 1) & 1, 375))) break;
                 if (some) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + half * 8192u + r * 128u + (uint32_t)(((4 * wg + c) ^ (r & 7)) << 4)), "r"(pk[4 * c]),
+                    for (int c = 0; c < 2; ++c)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + buf * Shape::kPB + r * 128u + (uint32_t)(((4 * half + 2 * wg + c) ^ (r & 7)) << 4)), "r"(pk[4 * c]),
                                      "r"(pk[4 * c + 1]), "r"(pk[4 * c + 2]), "r"(pk[4 * c + 3])
                                      : "memory");
                     if (j > 0 && __any_sync(0xffffffffu, moved)) {
+                        if (!(ok = wait(latp::pv + (buf ^ 1), ((s - 1) >> 1) & 1, 384))) break;   // O holds the sums up to the step before
                         tc_fence_after();
 #pragma unroll 1
                         for (int c = 0; c < 8; ++c) {
@@ -966,14 +1044,13 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                         tmem_wait_st();
                     }
                 }
-                // this CTA's values are there; those of keys that are none may be anything, NaN too: they become zeros
-                if (!(ok = wait(latp::v_full, s & 1, 376)) || !(ok = wait(latp::v_full + 1, s & 1, 377))) break;
                 const int valid = seg.len - key0;
-                if (valid < kDecTile) {
-                    const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 16384u;
-                    for (int i = tid; i < (kDecTile - valid) * 32; i += 256) {
+                if (valid < kLatTile) {   // values of keys that are none may be anything, NaN too: they become zeros
+                    if (!(ok = wait(latp::v_full + buf, (s >> 1) & 1, 385))) break;
+                    const uint32_t vgroup = small ? 2048u : 1024u, vblock = small ? 1024u : 8192u;
+                    for (int i = tid; i < (kLatTile - valid) * 32; i += 256) {
                         const int key = valid + (i >> 5), piece = i & 31;
-                        const uint32_t at = sV + (piece >> 4) * Shape::kVUnitB + (uint32_t)(key >> 3) * group + (piece >> 3 & 1) * block + (uint32_t)(key & 7) * 128u + ((piece & 7) << 4);
+                        const uint32_t at = sV + buf * Shape::kVB + (piece >> 4) * (Shape::kVB / 2) + (uint32_t)(key >> 3) * vgroup + (piece >> 3 & 1) * vblock + (uint32_t)(key & 7) * 128u + ((piece & 7) << 4);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
                     }
                 }
@@ -993,7 +1070,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(latp::sums + group));   // (the next item's first step may write there)
             }
-            if (!(ok = wait(latp::pv, (s - 1) & 1, 378))) break;
+            if (!(ok = wait(latp::pv + ((s - 1) & 1), ((s - 1) >> 1) & 1, 378))) break;
             tc_fence_after();
             if (some) {
                 const bool whole = seg.n == seg.of, none = l_run == 0.f;

@@ -1549,8 +1549,8 @@ struct LatentBlocks {
 
 // N: the kernel of one CTA with so many columns; 0: that of pairs.
 template <typename T, int N>
-int latent_launch(const CUtensorMap& tm, const CUtensorMap& tm2, fa::LatentParams& lp, int sms, cudaStream_t st) {
-    void (*kern)(CUtensorMap, CUtensorMap, fa::LatentParams);
+int latent_launch(const CUtensorMap (&tm)[4], fa::LatentParams& lp, int sms, cudaStream_t st) {
+    void (*kern)(CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap, fa::LatentParams);
     int smem, threads;
     if constexpr (N > 0) kern = fa::fa_decode_latent_kernel<T, N>, smem = fa::LatShape<N>::kSmem, threads = fa::LatShape<N>::kThreads;
     else kern = fa::fa_decode_latent_pair_kernel<T>, smem = fa::LatPairShape::kSmem, threads = fa::LatPairShape::kThreads;
@@ -1559,7 +1559,7 @@ int latent_launch(const CUtensorMap& tm, const CUtensorMap& tm2, fa::LatentParam
     const int ctas = N > 0 ? 1 : 2, most = sms / ctas;
     lp.workers = most < fa::kTreeMaxSms ? most : fa::kTreeMaxSms;
     lp.by_item = (long long)lp.B * lp.blocks < lp.workers ? 1 : 0;
-    cudaError_t e = fa::launch_dependent_clusters(kern, dim3(lp.workers * ctas), ctas, 1, threads, smem, st, tm, tm2, lp);
+    cudaError_t e = fa::launch_dependent_clusters(kern, dim3(lp.workers * ctas), ctas, 1, threads, smem, st, tm[0], tm[1], tm[2], tm[3], lp);
     if (e == cudaSuccess && lp.workers > 1) {
         const int y = lp.by_item ? lp.B * lp.blocks : lp.workers - 1;
         e = fa::launch_dependent(fa::fa_decode_latent_combine_kernel<T>, dim3(lp.rows, y), fa::kLatCombineThreads, 0, st, lp);
@@ -1598,7 +1598,7 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
     if ((reinterpret_cast<uintptr_t>(p.seqlens_k) | reinterpret_cast<uintptr_t>(p.lse)) & 3u) return FA_ERR_ALIGN;
     if (!p.workspace || p.workspace_bytes < fa_decode_latent_workspace_bytes(p.B, p.T, p.H, Skv_max, p.d)) return FA_ERR_WORKSPACE;
     const LatentBlocks lb(p.T, p.H);
-    const long long units = ((long long)Skv_max + fa::kDecTile - 1) / fa::kDecTile + fa::kTreeItemCost;
+    const long long units = ((long long)Skv_max + fa::kLatTile - 1) / fa::kLatTile + fa::kLatItemCost;
     if (units * p.B * lb.blocks > 0x7fffffffll) return FA_ERR_UNSUPPORTED;   // (they are counted in 32 bits)
     int sms = 0;
     int rc = check_device(&sms);
@@ -1627,11 +1627,11 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
     // as zeros; of pages smaller than a tile (64 elements, 8 rows, blocks, groups of 8 rows, pages): a box is a page, and lands group by group.
     const cuuint64_t row = fa::kLatRow * 2, blocks = fa::kLatRow / 64;
     const cuuint64_t slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : Skv_max;
-    CUtensorMap tm[2];
-    const bool pairs = lb.pairs(), paged_small = p.block_table && p.page_size < fa::kDecTile;
+    CUtensorMap tm[4];
+    const bool pairs = lb.pairs(), paged_small = p.block_table && p.page_size < fa::kLatTile;
     for (int i = 0; i < 2 && !rc; ++i) {
-        // one CTA: 128 elements, and the rotated 64, of a tile's keys; a pair: 192 of half a tile's, 128 of a tile's
-        const cuuint32_t wide = pairs ? (i ? 2 : 3) : (i ? 1 : 2), keys = pairs && i == 0 ? 64 : fa::kDecTile;
+        // one CTA: 128 elements, and the rotated 64, of a tile's keys; a pair: all of half a tile's, 128 of a tile's
+        const cuuint32_t wide = pairs ? (i ? 2 : (cuuint32_t)blocks) : (i ? 1 : 2), keys = pairs && i == 0 ? 32 : fa::kLatTile;
         if (paged_small)
             rc = encode_tiled<5>(&tm[i], type16(bf16), p.cache, {64, 8, blocks, slab_rows / 8, slabs}, {row, 128, 8 * row, slab_rows * row},
                                  {64, 8, wide, (cuuint32_t)slab_rows / 8, 1});
@@ -1639,11 +1639,24 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
             rc = encode_tiled<5>(&tm[i], type16(bf16), p.cache, {64, slab_rows, blocks, slabs, 1}, {row, 128, slab_rows * row, slabs * slab_rows * row},
                                  {64, keys, wide, 1, 1});
     }
+    // Q: the (token, head) rows of a sequence are of one stride (all that tensors and parts of them usually have), and a box is a CTA's rows; otherwise
+    // a warp copies them.
+    const cuuint32_t q_rows = pairs ? 64 : lp.rows <= 16 ? 16 : 32;
+    lp.q_boxes = 1;
+    for (int i = 0; i < 2 && !rc; ++i) {
+        const int64_t* st = i ? p.q_rope_stride : p.q_stride;
+        const Strides l = legal_strides(p.B, p.T, p.H, st[0], st[1], st[2], i ? p.d_rope : p.d);
+        const int64_t one = p.H > 1 ? l.h : l.s;
+        if (p.T > 1 && l.s != one * p.H) lp.q_boxes = 0;
+        const cuuint64_t wide = i ? 1 : fa::kLatDim / 64, all = (cuuint64_t)p.H * p.T;
+        const cuuint64_t batch = p.B > 1 ? (cuuint64_t)l.b * 2 : (cuuint64_t)one * 2 * all;
+        rc = encode_tiled<4>(&tm[2 + i], type16(bf16), i ? p.q_rope : p.q, {64, all, wide, (cuuint64_t)p.B}, {(cuuint64_t)one * 2, 128, batch}, {64, q_rows, (cuuint32_t)wide, 1});
+    }
     if (rc) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (pairs) return bf16 ? latent_launch<__nv_bfloat16, 0>(tm[0], tm[1], lp, sms, st) : latent_launch<__half, 0>(tm[0], tm[1], lp, sms, st);
-    if (lp.rows <= 16) return bf16 ? latent_launch<__nv_bfloat16, 16>(tm[0], tm[1], lp, sms, st) : latent_launch<__half, 16>(tm[0], tm[1], lp, sms, st);
-    return bf16 ? latent_launch<__nv_bfloat16, 32>(tm[0], tm[1], lp, sms, st) : latent_launch<__half, 32>(tm[0], tm[1], lp, sms, st);
+    if (pairs) return bf16 ? latent_launch<__nv_bfloat16, 0>(tm, lp, sms, st) : latent_launch<__half, 0>(tm, lp, sms, st);
+    if (lp.rows <= 16) return bf16 ? latent_launch<__nv_bfloat16, 16>(tm, lp, sms, st) : latent_launch<__half, 16>(tm, lp, sms, st);
+    return bf16 ? latent_launch<__nv_bfloat16, 32>(tm, lp, sms, st) : latent_launch<__half, 32>(tm, lp, sms, st);
 }
 
 // CTAs of the one cluster that looks a pool's reference counts over.

@@ -262,6 +262,16 @@ __device__ __forceinline__ void tma_load_5d_hint(uint32_t dst, const CUtensorMap
           "r"(c3), "r"(c4), "l"(policy)
         : "memory");
 }
+// The same for a pair of CTAs (cta_group::2): into this CTA's shared memory, completing on a barrier of either (an address of cluster_map).
+__device__ __forceinline__ void tma_load_5d_pair_hint(uint32_t dst, const CUtensorMap* tm, uint32_t cluster_bar, int c0, int c1, int c2, int c3, int c4, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2.L2::cache_hint"
+        " [%0], [%1, {%3, %4, %5, %6, %7}], [%2], %8;"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "l"(policy)
+        : "memory");
+}
+// A line of global memory on its way into L2.
+__device__ __forceinline__ void l2_prefetch(const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at) : "memory"); }
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* tm, uint32_t src, int c0, int c1,
                                              int c2, int c3) {
     asm volatile(

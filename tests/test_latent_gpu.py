@@ -272,3 +272,15 @@ def test_absorbed_offsets_past_32_bits():
     got = o[2, 0, :2].double().cpu()
     ref = want[0] * torch.exp(-rest)
     assert bool(((got - ref).abs() <= 2.0 ** -10 * want[2] * torch.exp(-rest) + 2.0 ** -11 * ref.abs() + 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("T, H", [(3, 5), (4, 20), (2, 128)])
+def test_absorbed_queries_of_any_strides(T, H):
+    """Heads before tokens, a tensor with room between the rows: the result is that of the same queries put together."""
+    q, r, cache, table, ws, o, lse, most = absorbed([300, 41, 0, 700], T, H, "bf16", page=32)
+    far = normal((4, H, T, 1024), "bf16", 5)
+    q2, r2 = far[..., :512].transpose(1, 2), far[..., 640:704].transpose(1, 2)
+    q2.copy_(q), r2.copy_(r)
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    fa.fa_decode_latent(q2, r2, cache, o2, lse2, ints([300, 41, 0, 700]), SCALE, ws, block_table=table)
+    assert torch.equal(o2, o) and torch.equal(lse2, lse)
