@@ -15,11 +15,13 @@
 namespace fa {
 
 constexpr int kLatDim = 512, kLatRope = 64, kLatRow = kLatDim + kLatRope;
-constexpr int kLatTile = 64;    // keys: shared memory holds two such tiles and more, so that one arrives while the other is worked on
+constexpr int kLatTile = 64;        // keys: one CTA's shared memory holds two such tiles and more, so that one arrives while the other is worked on
+constexpr int kLatPairTile = 128;   // a pair's
 constexpr int kLatSegs = 4;
 // Work is dealt out in units as in decode_tree.cuh: a tile is one, an item's beginning and end two.
 constexpr int kLatItemCost = 2;
-__device__ __forceinline__ int latent_item_units(int len) { return len > 0 ? (len + kLatTile - 1) / kLatTile + kLatItemCost : 0; }
+template <int kTile>
+__device__ __forceinline__ int latent_item_units(int len) { return len > 0 ? (len + kTile - 1) / kTile + kLatItemCost : 0; }
 
 struct LatentParams {
     const void* q;            // [B,T,H,512] by strides
@@ -48,6 +50,7 @@ struct LatentSegment {
 };
 
 // A worker's run, segment by segment: what decode_tree.cuh's loading warp does, over all its lanes.
+template <int kTile>
 struct LatentWalk {
     const LatentParams& p;
     int lane, worker;
@@ -68,7 +71,7 @@ struct LatentWalk {
     __device__ __forceinline__ void begin() {
         int total = 0, mine = 0, upto = 0;
         auto scan = [&](int b0, int before) {
-            mine = latent_item_units(lens_at(b0)) * p.blocks;
+            mine = latent_item_units<kTile>(lens_at(b0)) * p.blocks;
             upto = mine;
 #pragma unroll 1
             for (int sh = 1; sh < 32; sh <<= 1) {
@@ -97,7 +100,7 @@ struct LatentWalk {
         }
         next_b = b;
         next_len = pos < end ? len_of(b) : 0;
-        units = latent_item_units(next_len);
+        units = latent_item_units<kTile>(next_len);
         item = pos < end ? in_seq / units : 0;
         unit = in_seq - item * units;
     }
@@ -119,7 +122,7 @@ struct LatentWalk {
                 item = 0;
                 do next_len = len_of(++next_b);
                 while (next_len == 0);
-                units = latent_item_units(next_len);
+                units = latent_item_units<kTile>(next_len);
             }
         }
         if (entries && lane == 0) {
@@ -130,7 +133,7 @@ struct LatentWalk {
                 p.merges[worker - 1] = make_int4(b, block, worker - 1, mine ? plan.owner(last_tile) : 0);
             }
         }
-        return {b, block, t0, n, (len + kLatTile - 1) / kLatTile, len};
+        return {b, block, t0, n, (len + kTile - 1) / kTile, len};
     }
 };
 
@@ -255,7 +258,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
         tmem_alloc(smem_u32(&tmem_holder), Shape::kTmemCols);
         tmem_relinquish();
     }
-    LatentWalk walk(p, blockIdx.x, lane);
+    LatentWalk<kLatTile> walk(p, blockIdx.x, lane);
     if (warp == 8) {
         grid_dep_wait();
         walk.begin();
@@ -636,25 +639,26 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 // ---------------------------------------------------------------------------------------
 // More than 32 rows: a pair of CTAs (a cluster) has blocks of 128, 64 rows in each, and issues matrix instructions of both (cta_group::2, M = 128).  Each
 // CTA's tensor memory then holds its 64 rows in the lanes 0 to 63 for the first half of the columns and in 64 to 127 for the second: 512
-// columns of output in 256 of its 512 columns, scores of 64 keys in 32 -- one CTA's tensor memory would be full with the output
-// of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 32 keys of a
-// tile), latent elements for the output (each loads 256 elements of all 64 keys): 1.9 times the tile over L2, once from HBM.
+// columns of output in 256 of its 512 columns, scores of 128 keys in 64 -- one CTA's tensor memory would be full with the output
+// of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 64 keys of a
+// tile), latent elements for the output (each loads 256 elements of all 128 keys): 1.9 times the tile over L2, once from HBM.
 struct LatPairShape {
-    static constexpr int kKB = 32 * kLatRow * 2;                    // a CTA's keys of a tile: 32, all elements
-    static constexpr int kVB = kLatTile * 256 * 2;                  // its values: 64 keys, two times 128 elements
-    static constexpr int kQB = 64 * kLatRow * 2, kPB = 64 * kLatTile * 2;
-    static constexpr int kSmem = kQB + 2 * (kPB + kKB + kVB);       // 224 KiB, behind kPairStaticBytes
+    static constexpr int kKB = 64 * 192 * 2;                        // a third of a CTA's keys of a tile: 64, 192 elements; all three lie ready
+    static constexpr int kVB = 64 * 256 * 2;                        // half of its values: 64 keys, two times 128 elements; both lie ready
+    static constexpr int kQB = 64 * kLatRow * 2, kPB = 64 * 64 * 2; // (P: two halves by keys)
+    static constexpr int kSmem = kQB + 2 * kPB + 3 * kKB + 2 * kVB; // 224 KiB, behind kPairStaticBytes
     static constexpr int kThreads = 416;
-    static constexpr int kTmemCols = 512;                           // scores [0,32) and [32,64), output [128,384)
+    static constexpr int kTmemCols = 512;                           // scores [0,64) and [64,128), output [128,384)
 };
 namespace latp {   // barriers
-constexpr int k_full = 0;               // [2]  first CTA: TMA of both -> S thread
-constexpr int k_empty = k_full + 2;     // [2]  S thread (commit, to both)
-constexpr int v_full = k_empty + 2;     // [2]  TMA -> PV thread, or the relay
+constexpr int k_full = 0;               // [3]  first CTA: TMA of both -> S thread
+constexpr int k_empty = k_full + 3;     // [3]  S thread (commit, to both)
+constexpr int v_full = k_empty + 3;     // [2]  TMA -> PV thread, or the relay
 constexpr int v_peer = v_full + 2;      // [2]  first CTA: the other's is there
-constexpr int s_full = v_peer + 2;      // [2]  S thread (commit, to both)
-constexpr int p_full = s_full + 2;      // [2]  first CTA: sixteen softmax warps
-constexpr int pv = p_full + 2;          // [2]  PV thread (commit, to both); the values have been read, too
+constexpr int s_full = v_peer + 2;      // [2]  S thread (commit, to both), by step
+constexpr int s_read = s_full + 2;      // [2]  first CTA: sixteen softmax warps have the scores in registers
+constexpr int p_full = s_read + 2;      // [1]  first CTA: sixteen softmax warps
+constexpr int pv = p_full + 1;          // [2]  PV thread (commit, to both), by half: its values and probabilities have been read
 constexpr int q_full = pv + 2;          // [1]  as for the values
 constexpr int q_peer = q_full + 1;      // [1]
 constexpr int q_empty = q_peer + 1;     // [1]  S thread (commit, to both)
@@ -697,9 +701,9 @@ __device__ __forceinline__ void cluster_mbar_arrive(uint32_t addr) {
 }
 
 // grid: two CTAs per worker.  Warps 0 to 7: softmax and output -- lane and warp & 3 say the row and the half of the keys, warp >> 2 which
-// 16 of those; 8: segments and keys; 9: Q; 10: S (first CTA), or a relay that tells the first CTA
+// 32 of those; 8: segments and keys; 9: Q; 10: S (first CTA), or a relay that tells the first CTA
 // that Q has arrived; 11: O, or the relay of the values; 12: values.
-// tm_k: boxes of 32 keys, all elements; tm_v: 64 keys x 128 elements (pages of less: as in fa_decode_latent_kernel).
+// tm_k: boxes of 64 keys x 192 elements, tm_v: 64 keys x 128 elements (pages of less: as in fa_decode_latent_kernel).
 template <typename T>
 __global__ void __launch_bounds__(LatPairShape::kThreads, 1)
 fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_q,
@@ -709,7 +713,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     __shared__ __align__(1024) uint8_t static_raw[kPairStaticBytes];
     LatPairStatic& ss = *reinterpret_cast<LatPairStatic*>(static_raw);
-    const uint32_t sQ = smem_u32(smem_raw), sP = sQ + Shape::kQB, sK = sP + 2 * Shape::kPB, sV = sK + 2 * Shape::kKB;
+    const uint32_t sQ = smem_u32(smem_raw), sP = sQ + Shape::kQB, sK = sP + 2 * Shape::kPB, sV = sK + 3 * Shape::kKB;
     volatile uint32_t* abort_flag = &ss.abort_flag;
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31, worker = blockIdx.x >> 1, rank = blockIdx.x & 1;
     auto bar = [&](int i) { return smem_u32(&ss.bars[i]); };
@@ -720,7 +724,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     }
     if (tid == 0) {
         for (int i = 0; i < latp::count; ++i)
-            mbar_init(bar(i), i >= latp::p_full && i < latp::pv ? 16 : i >= latp::meet ? 4 : i >= latp::seg_empty ? 12 : 1);
+            mbar_init(bar(i), i >= latp::s_read && i < latp::pv ? 16 : i >= latp::meet ? 4 : i >= latp::seg_empty ? 12 : 1);
         ss.abort_flag = 0;
         fence_mbar_init();
         tma_prefetch_desc(&tm_k);
@@ -730,7 +734,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ss.tmem_holder)), "r"(Shape::kTmemCols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
-    LatentWalk walk(p, worker, lane);
+    LatentWalk<kLatPairTile> walk(p, worker, lane);
     if (warp == 8) {
         grid_dep_wait();
         walk.begin();
@@ -743,21 +747,21 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     grid_dep_wait();
 
     const int ps = p.page_size;
-    const bool small = p.block_table != nullptr && ps < kLatTile;
+    const bool small = p.block_table != nullptr && ps < 64;
     bool ok = true;
     auto segment = [&](uint32_t ord, LatentSegment& s) {
         if (!pp_warp_wait(bar(latp::seg_full + ord % kLatSegs), (ord / kLatSegs) & 1, abort_flag, 360)) return false;
         s = ss.segs[ord % kLatSegs];
         return true;
     };
-    // The page of this lane's part of `keys` keys from `key` on, or of all of them.
-    auto lookup = [&](const LatentSegment& seg, int key, int keys) {
+    // Half a tile, 64 keys from `key` on: the page of this lane's part of them, or of all; and how many pages, or boxes, they are.
+    auto lookup = [&](const LatentSegment& seg, int key) {
         if (!p.block_table || key >= seg.len) return -1;
         const int* table = p.block_table + (long long)seg.b * p.table_stride;
-        const int page = small ? (lane < keys / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
+        const int page = small ? (lane < 64 / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
         return (unsigned)page < (unsigned)p.num_pages ? page : -1;   // (none: zeros)
     };
-    auto boxes_of = [&](const LatentSegment& seg, int key, int keys) { return small ? (max(0, min(seg.len - key, keys)) + ps - 1) / ps : 1; };
+    auto boxes_of = [&](const LatentSegment& seg, int key) { return small ? (max(0, min(seg.len - key, 64)) + ps - 1) / ps : 1; };
     const uint64_t policy = l2_policy_evict_last();   // (the pair reads everything twice, and other blocks of rows again)
 
     if (warp == 8) {
@@ -773,23 +777,26 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 mbar_arrive(bar(latp::seg_full + slot));
             }
             if (seg.n <= 0) break;
-            const int first = seg.t0 * kLatTile + 32 * rank, end = (seg.t0 + seg.n) * kLatTile;
-            const uint32_t bytes = (small ? ps : 32) * (kLatRow * 2);   // of a box
-            int page = lookup(seg, first, 32);
-            for (int key0 = first; key0 < end; key0 += kLatTile, ++u) {
-                const int next = key0 + kLatTile, page_next = next < end ? lookup(seg, next, 32) : -1;
-                const int boxes = boxes_of(seg, key0, 32), at = u & 1;
-                if (lane == 0) {
-                    ok = mbar_wait(bar(latp::k_empty + at), ((u >> 1) & 1) ^ 1, abort_flag, 361);
-                    // (the first CTA expects both's)
-                    if (ok && rank == 0) mbar_expect_tx(bar(latp::k_full + at), (boxes + boxes_of(seg, key0 + 32, 32)) * bytes);
+            const int first = seg.t0 * kLatPairTile + 64 * rank, end = (seg.t0 + seg.n) * kLatPairTile;
+            const uint32_t bytes = (small ? ps : 64) * 384;   // of a box
+            int page = lookup(seg, first);
+            for (int key0 = first; key0 < end && ok; key0 += kLatPairTile, ++u) {
+                const int next = key0 + kLatPairTile, page_next = next < end ? lookup(seg, next) : -1;
+                const int boxes = boxes_of(seg, key0), row = p.block_table ? key0 % ps : key0, slab = p.block_table ? page : seg.b;
+                const uint32_t both = rank == 0 ? (boxes + boxes_of(seg, key0 + 64)) * bytes : 0;   // (the first CTA expects both's)
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    if (lane == 0 && ok) {
+                        ok = mbar_wait(bar(latp::k_empty + i), (u & 1) ^ 1, abort_flag, 361);
+                        if (ok && rank == 0) mbar_expect_tx(bar(latp::k_full + i), both);
+                        if (ok && !small) tma_load_5d_pair_hint(sK + i * Shape::kKB, &tm_k, k_full0 + 8 * i, 0, row, 3 * i, slab, 0, policy);
+                    }
+                    if (small) {
+                        ok = __shfl_sync(0xffffffffu, ok, 0);
+                        if (ok && lane < boxes) tma_load_5d_pair_hint(sK + i * Shape::kKB + lane * bytes, &tm_k, k_full0 + 8 * i, 0, 0, 3 * i, 0, page, policy);
+                    }
                 }
-                if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; break; }
-                if (lane < boxes) {
-                    const uint32_t dst = sK + at * Shape::kKB + lane * bytes, full = k_full0 + 8 * at;
-                    if (small) tma_load_5d_pair_hint(dst, &tm_k, full, 0, 0, 0, 0, page, policy);
-                    else tma_load_5d_pair_hint(dst, &tm_k, full, 0, p.block_table ? key0 % ps : key0, 0, p.block_table ? page : seg.b, 0, policy);
-                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
                 page = page_next;
             }
         }
@@ -803,23 +810,23 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(latp::seg_empty + ord % kLatSegs));
             if (seg.n <= 0) break;
-            const int end = (seg.t0 + seg.n) * kLatTile;
-            const uint32_t bytes = (small ? ps : kLatTile) * 256;   // of a box
-            int page = lookup(seg, seg.t0 * kLatTile, kLatTile);
-            for (int key0 = seg.t0 * kLatTile; key0 < end; key0 += kLatTile, ++u) {
-                const int next = key0 + kLatTile, page_next = next < end ? lookup(seg, next, kLatTile) : -1;
-                const int boxes = boxes_of(seg, key0, kLatTile), at = u & 1;
+            const int end = (seg.t0 + seg.n) * kLatPairTile;
+            const uint32_t bytes = (small ? ps : 64) * 256;   // of a box
+            int page = lookup(seg, seg.t0 * kLatPairTile);
+            for (int key0 = seg.t0 * kLatPairTile; key0 < end && ok; key0 += 64, ++u) {
+                const int next = key0 + 64, page_next = next < end ? lookup(seg, next) : -1;
+                const int boxes = boxes_of(seg, key0), at = u & 1, row = p.block_table ? key0 % ps : key0, slab = p.block_table ? page : seg.b;
                 if (lane == 0) {
                     ok = u < 2 || mbar_wait(bar(latp::pv + at), ((u >> 1) - 1) & 1, abort_flag, 362);
                     if (ok) mbar_expect_tx(bar(latp::v_full + at), 2 * boxes * bytes);
                 }
-                if (!__shfl_sync(0xffffffffu, ok, 0)) { ok = false; break; }
-                if (lane < boxes) {
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (ok && lane < boxes) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t dst = sV + at * Shape::kVB + i * (Shape::kVB / 2) + lane * bytes;
                         if (small) tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, 0, 4 * i + 2 * rank, 0, page, policy);
-                        else tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, p.block_table ? key0 % ps : key0, 4 * i + 2 * rank, p.block_table ? page : seg.b, 0, policy);
+                        else tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, row, 4 * i + 2 * rank, slab, 0, policy);
                     }
                 }
                 page = page_next;
@@ -866,8 +873,8 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     } else if (warp == 10) {
         // ---------------------------------------------------------------- S = Q C^T
         if (elect_one()) {
-            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kLatTile, false, false);
-            const uint32_t group = small ? 9216u : 1024u, block = small ? 1024u : 4096u;
+            constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kLatPairTile, false, false);
+            const uint32_t group = small ? 3072u : 1024u, block = small ? 1024u : 8192u;
             const uint32_t k_hi = tree_desc_hi(group);
             constexpr uint32_t q_hi = tree_desc_hi(1024);
             const uint32_t k_lo = desc_lo(sK, 16), q_lo = desc_lo(sQ, 16);
@@ -887,15 +894,18 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 if (!(ok = mbar_wait(bar(latp::q_peer), ord & 1, abort_flag, 382))) break;
                 for (int j = 0; j < n && ok; ++j, ++s) {
                     const uint32_t buf = s & 1;
-                    // the scores that lie there have become probabilities, in both CTAs
-                    if (s >= 2 && !(ok = mbar_wait(bar(latp::p_full + buf), ((s >> 1) - 1) & 1, abort_flag, 367))) break;
-                    if (!(ok = mbar_wait(bar(latp::k_full + buf), (s >> 1) & 1, abort_flag, 368))) break;
-                    tc_fence_after();
-                    const uint32_t b = k_lo + buf * (Shape::kKB >> 4);
+                    if (s >= 2 && !(ok = mbar_wait(bar(latp::s_read + buf), ((s >> 1) - 1) & 1, abort_flag, 367))) break;
 #pragma unroll
-                    for (int ks = 0; ks < kLatRow / 16; ++ks)
-                        pair_mma_ss(tmem + buf * 32, q_lo + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, q_hi, b + (ks >> 2) * (block >> 4) + (ks & 3) * 2, k_hi, idesc, ks > 0);
-                    pair_commit(bar(latp::k_empty + buf));
+                    for (int i = 0; i < 3; ++i) {
+                        if (!(ok = mbar_wait(bar(latp::k_full + i), s & 1, abort_flag, 368))) break;
+                        tc_fence_after();
+                        const uint32_t b = k_lo + i * (Shape::kKB >> 4), a = q_lo + ((3 * i * 8192) >> 4);
+#pragma unroll
+                        for (int ks = 0; ks < 12; ++ks)
+                            pair_mma_ss(tmem + buf * 64, a + (ks >> 2) * (8192 >> 4) + (ks & 3) * 2, q_hi, b + (ks >> 2) * (block >> 4) + (ks & 3) * 2, k_hi, idesc, i > 0 || ks > 0);
+                        pair_commit(bar(latp::k_empty + i));
+                    }
+                    if (!ok) break;
                     pair_commit(bar(latp::s_full + buf));
                 }
                 pair_commit(bar(latp::q_empty));
@@ -919,31 +929,33 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 const int n = ss.segs[slot].n;
                 mbar_arrive(bar(latp::seg_empty + slot));
                 if (n <= 0) break;
-                for (int j = 0; j < n; ++j, ++s) {
-                    const uint32_t buf = s & 1, parity = (s >> 1) & 1;
-                    if (!(ok = mbar_wait(bar(latp::v_full + buf), parity, abort_flag, 376))) break;
-                    if (rank == 1) {
-                        cluster_mbar_arrive(first_bar(latp::v_peer + buf));
-                        continue;
+                for (int j = 0; j < n && ok; ++j, ++s) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (!(ok = mbar_wait(bar(latp::v_full + h), s & 1, abort_flag, 376))) break;
+                        if (rank == 1) {
+                            cluster_mbar_arrive(first_bar(latp::v_peer + h));
+                            continue;
+                        }
+                        if (h == 0 && !(ok = mbar_wait(bar(latp::p_full), s & 1, abort_flag, 372))) break;
+                        if (!(ok = mbar_wait(bar(latp::v_peer + h), s & 1, abort_flag, 377))) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                pair_mma_ss(tmem_o + i * 128, p_lo + (h * Shape::kPB >> 4) + ks * 2, p_hi, v_lo + ((h * Shape::kVB + i * (Shape::kVB / 2)) >> 4) + ks * (2 * group >> 4), v_hi, idesc,
+                                            j > 0 || h > 0 || ks > 0 ? 1u : 0u);
+                        pair_commit(bar(latp::pv + h));
                     }
-                    if (!(ok = mbar_wait(bar(latp::v_peer + buf), parity, abort_flag, 377))) break;
-                    if (!(ok = mbar_wait(bar(latp::p_full + buf), parity, abort_flag, 372))) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int ks = 0; ks < kLatTile / 16; ++ks)
-                            pair_mma_ss(tmem_o + i * 128, p_lo + (buf * Shape::kPB >> 4) + ks * 2, p_hi, v_lo + ((buf * Shape::kVB + i * (Shape::kVB / 2)) >> 4) + ks * (2 * group >> 4), v_hi, idesc,
-                                        j > 0 || ks > 0 ? 1u : 0u);
-                    pair_commit(bar(latp::pv + buf));
                 }
                 if (!ok) break;
             }
-            if (ok && s > 0) ok = mbar_wait(bar(latp::pv + ((s - 1) & 1)), ((s - 1) >> 1) & 1, abort_flag, 373);
+            if (ok && s > 0) ok = mbar_wait(bar(latp::pv + 1), (s - 1) & 1, abort_flag, 373);
         }
         __syncwarp();
     } else {
-        // ---------------------------------------------------------------- softmax: 16 keys of a row per thread
+        // ---------------------------------------------------------------- softmax: 32 keys of a row per thread
         const int wg = warp >> 2, half = warp >> 1 & 1, r = (warp & 1) * 32 + lane, part = 2 * wg + half;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const int group = warp & 1;   // the four warps that have these rows
@@ -961,25 +973,29 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             const int lim = seg.len - p.T + 1 + token;         // keys that the row sees
             float m_run = -INFINITY, l_run = 0.f;
             for (int j = 0; j < seg.n; ++j, ++s) {
-                const int key0 = (seg.t0 + j) * kLatTile;
+                const int key0 = (seg.t0 + j) * kLatPairTile;
                 const uint32_t buf = s & 1;
                 if (!(ok = wait(latp::s_full + buf, (s >> 1) & 1, 374))) break;
                 tc_fence_after();
                 float alpha = 1.f;
                 bool moved = false;
-                uint32_t pk[8];
+                uint32_t pk[16], sc[32];
                 if (some) {
-                    uint32_t sc[16];
-                    tmem_ld_x16(tmem + lanes + buf * 32 + wg * 16, sc);
+                    tmem_ld_x32(tmem + lanes + buf * 64 + wg * 32, sc);
                     tmem_wait_ld();
-                    if (key0 + kLatTile > seg.len - p.T + 1) {
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) cluster_mbar_arrive(first_bar(latp::s_read + buf));
+                if (some) {
+                    if (key0 + kLatPairTile > seg.len - p.T + 1) {
                         // hidden scores become -inf, their exponentials exact zeros (the scale is positive)
-                        const uint32_t seen = low_bits(lim - key0 - half * 32 - wg * 16);
+                        const uint32_t seen = low_bits(lim - key0 - half * 64 - wg * 32);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
+                        for (int i = 0; i < 32; ++i)
                             if (!(seen & (1u << i))) sc[i] = 0xff800000u;
                     }
-                    float mx = tree_row_max<16>(sc);
+                    float mx = tree_row_max<32>(sc);
                     if (j == 0 && ord > 0 && !(ok = wait(latp::sums + group, 1, 379))) break;   // (the last item's sums lie in one of them)
                     ss.x[met & 1][part][r] = mx;
                     __syncwarp();
@@ -991,7 +1007,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                         const uint64_t sc2 = f2_pack(p.scale_log2, p.scale_log2), nm2 = f2_pack(neg, neg);
                         la = lb = f2_pack(0.f, 0.f);
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4) {
+                        for (int i = 0; i < 32; i += 4) {
                             float e[4];
 #pragma unroll
                             for (int k = 0; k < 4; k += 2) {
@@ -1021,16 +1037,16 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                     f2_unpack(lb, b0, b1);
                     l_run = l_run * alpha + ((a0 + a1) + (b0 + b1));
                 }
-                // the probabilities of two steps before have been read
-                if (s >= 2 && !(ok = wait(latp::pv + buf, ((s >> 1) - 1) & 1, 375))) break;
+                // the probabilities of this half of the step before have been read
+                if (s > 0 && !(ok = wait(latp::pv + half, (s - 1) & 1, 375))) break;
                 if (some) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + buf * Shape::kPB + r * 128u + (uint32_t)(((4 * half + 2 * wg + c) ^ (r & 7)) << 4)), "r"(pk[4 * c]),
+                    for (int c = 0; c < 4; ++c)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sP + half * Shape::kPB + r * 128u + (uint32_t)(((4 * wg + c) ^ (r & 7)) << 4)), "r"(pk[4 * c]),
                                      "r"(pk[4 * c + 1]), "r"(pk[4 * c + 2]), "r"(pk[4 * c + 3])
                                      : "memory");
                     if (j > 0 && __any_sync(0xffffffffu, moved)) {
-                        if (!(ok = wait(latp::pv + (buf ^ 1), ((s - 1) >> 1) & 1, 384))) break;   // O holds the sums up to the step before
+                        if (!(ok = wait(latp::pv + (half ^ 1), (s - 1) & 1, 384))) break;   // O holds the sums up to the step before
                         tc_fence_after();
 #pragma unroll 1
                         for (int c = 0; c < 8; ++c) {
@@ -1045,19 +1061,20 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                     }
                 }
                 const int valid = seg.len - key0;
-                if (valid < kLatTile) {   // values of keys that are none may be anything, NaN too: they become zeros
-                    if (!(ok = wait(latp::v_full + buf, (s >> 1) & 1, 385))) break;
+                if (valid < kLatPairTile) {   // values of keys that are none may be anything, NaN too: they become zeros
+                    if (!(ok = wait(latp::v_full, s & 1, 385)) || !(ok = wait(latp::v_full + 1, s & 1, 383))) break;
                     const uint32_t vgroup = small ? 2048u : 1024u, vblock = small ? 1024u : 8192u;
-                    for (int i = tid; i < (kLatTile - valid) * 32; i += 256) {
+                    for (int i = tid; i < (kLatPairTile - valid) * 32; i += 256) {
                         const int key = valid + (i >> 5), piece = i & 31;
-                        const uint32_t at = sV + buf * Shape::kVB + (piece >> 4) * (Shape::kVB / 2) + (uint32_t)(key >> 3) * vgroup + (piece >> 3 & 1) * vblock + (uint32_t)(key & 7) * 128u + ((piece & 7) << 4);
+                        const uint32_t at = sV + (key >> 6) * Shape::kVB + (piece >> 4) * (Shape::kVB / 2) + (uint32_t)(key >> 3 & 7) * vgroup + (piece >> 3 & 1) * vblock +
+                                            (uint32_t)(key & 7) * 128u + ((piece & 7) << 4);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
                     }
                 }
                 fence_proxy_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) cluster_mbar_arrive(first_bar(latp::p_full + buf));
+                if (lane == 0) cluster_mbar_arrive(first_bar(latp::p_full));
             }
             if (!ok) break;
             if (some) {   // the row sums, in the buffer that the last step has not used
@@ -1070,7 +1087,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(latp::sums + group));   // (the next item's first step may write there)
             }
-            if (!(ok = wait(latp::pv + ((s - 1) & 1), ((s - 1) >> 1) & 1, 378))) break;
+            if (!(ok = wait(latp::pv, (s - 1) & 1, 378)) || !(ok = wait(latp::pv + 1, (s - 1) & 1, 386))) break;
             tc_fence_after();
             if (some) {
                 const bool whole = seg.n == seg.of, none = l_run == 0.f;
