@@ -30,7 +30,7 @@ struct LatentParams {
     float* lse;               // [B,H,T] or nullptr
     const int* seqlens;       // [B]
     const int* block_table;   // nullptr: contiguous
-    float* o_part;            // [2 workers][rows][512]
+    float* o_part;            // [2 workers][rows][512], 32-byte aligned
     float* lse_part;          // [2 workers][rows]
     int4* merges;             // as TreeParams::merges
     int by_item;              // as TreeParams::by_item
@@ -104,9 +104,9 @@ struct LatentWalk {
         item = pos < end ? in_seq / units : 0;
         unit = in_seq - item * units;
     }
-    // The next segment, and its entry for the merge (`entries`: this worker writes it).
-    __device__ __forceinline__ LatentSegment next(int ord, bool entries) {
-        int t0 = 0, n = 0, block = 0, len = 0, first = 0, last_tile = 0;
+    int first = 0, last_tile = 0;   // units of the last segment's first tile, and of its item's last
+    __device__ __forceinline__ LatentSegment next() {
+        int t0 = 0, n = 0, block = 0, len = 0;
         while (pos < end && n == 0) {   // (a run may have an item's first units alone, and no tile)
             first = pos - unit + kLatItemCost;
             last_tile = pos - unit + units - 1;
@@ -125,15 +125,16 @@ struct LatentWalk {
                 units = latent_item_units<kTile>(next_len);
             }
         }
-        if (entries && lane == 0) {
-            if (p.by_item) {
-                if (n > 0 && t0 == 0) p.merges[b * p.blocks + block] = make_int4(b, block, worker, plan.owner(last_tile));
-            } else if (ord == 0 && worker > 0) {
-                const bool mine = n > 0 && t0 > 0 && plan.owner(first) + 1 == worker;
-                p.merges[worker - 1] = make_int4(b, block, worker - 1, mine ? plan.owner(last_tile) : 0);
-            }
-        }
         return {b, block, t0, n, (len + kTile - 1) / kTile, len};
+    }
+    // The last segment's entry for the merge (by one thread, when what the segment needs is on its way).
+    __device__ __forceinline__ void enter(int ord, const LatentSegment& seg) const {
+        if (p.by_item) {
+            if (seg.n > 0 && seg.t0 == 0) p.merges[seg.b * p.blocks + seg.block] = make_int4(seg.b, seg.block, worker, plan.owner(last_tile));
+        } else if (ord == 0 && worker > 0) {
+            const bool mine = seg.n > 0 && seg.t0 > 0 && plan.owner(first) + 1 == worker;
+            p.merges[worker - 1] = make_int4(seg.b, seg.block, worker - 1, mine ? plan.owner(last_tile) : 0);
+        }
     }
 };
 
@@ -285,14 +286,17 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
         PpRing<Shape::kUnits> units;
         PpRing<Shape::kRopes> ropes;
         for (uint32_t ord = 0; ok; ++ord) {
-            const LatentSegment seg = walk.next(ord, true);
+            const LatentSegment seg = walk.next();
             const int slot = ord % kLatSegs;
             if (!(ok = pp_warp_wait(bar(At::seg_empty + slot), ((ord / kLatSegs) & 1) ^ 1, &abort_flag, 341))) break;
             if (lane == 0) {
                 segs[slot] = seg;
                 mbar_arrive(bar(At::seg_full + slot));
             }
-            if (seg.n <= 0) break;
+            if (seg.n <= 0) {
+                if (lane == 0) walk.enter(ord, seg);
+                break;
+            }
             const int* table = p.block_table ? p.block_table + (long long)seg.b * p.table_stride : nullptr;
             auto lookup = [&](int key) {   // the page of this lane's part of the tile at `key`, one tile ahead
                 if (!table || key >= seg.len) return -1;
@@ -339,6 +343,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     }
                 }
                 page = page_next;
+                if (lane == 0 && key0 == seg.t0 * kLatTile) walk.enter(ord, seg);
             }
         }
         __syncwarp();
@@ -573,11 +578,27 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             if (!ok) break;
             // the row sums over the keys, in the buffer that the last step has not used
             const uint32_t other_buf = s & 1;
+            // (of the 16 lanes that have keys: half of the columns go to the lane on the other side, then half of what is left)
+            {
+                float part[C];
 #pragma unroll
-            for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c) part[c] = l_run[c];
+                int col = 0;
 #pragma unroll
-                for (int sh = 16; sh > 0; sh >>= 1) l_run[c] += __shfl_xor_sync(0xffffffffu, l_run[c], sh);
-            if (lane == 0) lat_sts<C>(smem_u32(&s_max[other_buf][quarter][col0]), l_run);
+                for (int i = 0; i < 4; ++i) {
+                    const int sh = 8 >> i, n = (C / 2) >> i;
+                    const bool up = lane & sh;
+                    if (n > 0) {
+#pragma unroll
+                        for (int c = 0; c < n; ++c) {
+                            const float keep = up ? part[n + c] : part[c], give = up ? part[c] : part[n + c];
+                            part[c] = keep + __shfl_xor_sync(0xffffffffu, give, sh);
+                        }
+                        col += up ? n : 0;
+                    } else part[0] += __shfl_xor_sync(0xffffffffu, part[0], sh);
+                }
+                if (lane < 16) s_max[other_buf][quarter][col0 + col] = part[0];
+            }
             if (!(ok = lat_meet(bar(At::sums + wg), 0, lane, &abort_flag, 358))) break;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -606,20 +627,23 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             }
             if (!(ok = pp_warp_wait(bar(At::pv + ((s - 1) & 1)), ((s - 1) >> 1) & 1, &abort_flag, 355))) break;
             tc_fence_after();
-            T* o_rows = static_cast<T*>(p.o) + ((long long)seg.b * p.T * p.H + R0) * kLatDim;
-            float* o_part = p.o_part + slot * p.rows * kLatDim;
-#pragma unroll 1
-            for (int m = 0; m < 4; ++m) {
-                uint32_t o[C];
-                lat_ld<C>(tmem_o + lanes + m * N + col0, o);
+            T* o_rows = static_cast<T*>(p.o) + ((long long)seg.b * p.T * p.H + R0 + col0) * kLatDim + dim;
+            float* o_part = p.o_part + (slot * p.rows + col0) * kLatDim + dim;
+            const int mine = rows - col0;   // of the thread's columns, those that are rows
+#pragma unroll
+            for (int m = 0; m < 4; m += 2) {
+                uint32_t o[2][C];
+                lat_ld<C>(tmem_o + lanes + m * N + col0, o[0]);
+                lat_ld<C>(tmem_o + lanes + (m + 1) * N + col0, o[1]);
                 tmem_wait_ld();
 #pragma unroll
                 for (int c = 0; c < C; ++c) {
-                    const int x = col0 + c;
-                    const float v = l_run[c] == 0.f ? 0.f : __uint_as_float(o[c]) * inv[c];
-                    if (x < rows) {
-                        if (whole) o_rows[(long long)x * kLatDim + m * 128 + dim] = static_cast<T>(v);
-                        else o_part[(long long)x * kLatDim + m * 128 + dim] = v;
+                    if (c < mine)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float v = l_run[c] == 0.f ? 0.f : __uint_as_float(o[k][c]) * inv[c];
+                        if (whole) o_rows[c * kLatDim + (m + k) * 128] = static_cast<T>(v);
+                        else o_part[c * kLatDim + (m + k) * 128] = v;
                     }
                 }
             }
@@ -769,14 +793,17 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
         uint32_t u = 0;
         const uint32_t k_full0 = first_bar(latp::k_full);
         for (uint32_t ord = 0; ok; ++ord) {
-            const LatentSegment seg = walk.next(ord, rank == 0);
+            const LatentSegment seg = walk.next();
             const int slot = ord % kLatSegs;
             if (!(ok = pp_warp_wait(bar(latp::seg_empty + slot), ((ord / kLatSegs) & 1) ^ 1, abort_flag, 363))) break;
             if (lane == 0) {
                 ss.segs[slot] = seg;
                 mbar_arrive(bar(latp::seg_full + slot));
             }
-            if (seg.n <= 0) break;
+            if (seg.n <= 0) {
+                if (lane == 0 && rank == 0) walk.enter(ord, seg);
+                break;
+            }
             const int first = seg.t0 * kLatPairTile + 64 * rank, end = (seg.t0 + seg.n) * kLatPairTile;
             const uint32_t bytes = (small ? ps : 64) * 384;   // of a box
             int page = lookup(seg, first);
@@ -798,6 +825,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 }
                 ok = __shfl_sync(0xffffffffu, ok, 0);
                 page = page_next;
+                if (lane == 0 && rank == 0 && key0 == first) walk.enter(ord, seg);
             }
         }
         __syncwarp();
@@ -1113,9 +1141,11 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                         for (int i = 0; i < 32; i += 8)
                             *reinterpret_cast<uint4*>(o_row + 32 * c + i) = make_uint4(pack2<T>(f(i), f(i + 1)), pack2<T>(f(i + 2), f(i + 3)),
                                                                                       pack2<T>(f(i + 4), f(i + 5)), pack2<T>(f(i + 6), f(i + 7)));
-                    } else {
+                    } else {   // (whole sectors: a lane has a row of its own)
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(o_part + 32 * c + i) = make_float4(f(i), f(i + 1), f(i + 2), f(i + 3));
+                        for (int i = 0; i < 32; i += 8)
+                            st_global_v8(o_part + 32 * c + i, __float_as_uint(f(i)), __float_as_uint(f(i + 1)), __float_as_uint(f(i + 2)), __float_as_uint(f(i + 3)),
+                                         __float_as_uint(f(i + 4)), __float_as_uint(f(i + 5)), __float_as_uint(f(i + 6)), __float_as_uint(f(i + 7)));
                     }
                 }
             }
@@ -1133,42 +1163,68 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Shape::kTmemCols) : "memory");
 }
 
-// Merge of the rows that several workers have worked on (the recurrence of decode.cuh's merge): a thread has four columns of a row.
-// grid: (blocks that share an item's rows, entries of LatentParams::merges).
-constexpr int kLatCombineThreads = 128;
+// Merge of the rows that several workers have worked on (the recurrence of decode.cuh's merge): a thread has four columns of a row.  (A part that a row
+// sees nothing of weighs nothing, whatever it holds; a NaN gets through.)
+struct LatentMerge {
+    int b, block, c0, parts, R0, rows;
+    __device__ __forceinline__ bool find(const LatentParams& p, int entry) {
+        const int4 m = p.merges[entry];
+        if (!tree_merge_there(m, p.B, p.blocks, p.workers)) return false;   // (an item's only part is where it belongs)
+        b = m.x, block = m.y, c0 = m.z, parts = m.w - m.z + 1;
+        R0 = block * p.rows, rows = min(p.rows, p.H * p.T - R0);
+        return true;
+    }
+    __device__ __forceinline__ long long at(const LatentParams& p, int part, int row) const {   // (the first part begins the item)
+        return (2ll * (c0 + part) + (part == 0 ? 1 : 0)) * p.rows + row;
+    }
+    template <typename T>
+    __device__ __forceinline__ void store(const LatentParams& p, int row, int piece, const float (&acc)[4], float M, float sum) const {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + ((long long)b * p.T * p.H + R0 + row) * kLatDim + 4 * piece) =
+            make_uint2(pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv));
+        if (p.lse && piece == 0) {
+            int token, head;
+            p.by_H.divmod(R0 + row, token, head);
+            p.lse[((long long)b * p.H + head) * p.T + token] = sum == 0.f ? -INFINITY : M + logf(sum);
+        }
+    }
+};
+
+// Items of a few parts.  grid: (blocks of eight rows, entries of LatentParams::merges); two rows at a time of 256 threads.
+constexpr int kLatCombineThreads = 256, kLatCombineRows = 8;
 template <typename T>
 __global__ void __launch_bounds__(kLatCombineThreads) fa_decode_latent_combine_kernel(const LatentParams p) {
     grid_dep_wait();
-    const int4 merge = p.merges[blockIdx.y];
-    const int b = merge.x, block = merge.y, c0 = merge.z, c1 = merge.w;
-    if (!tree_merge_there(merge, p.B, p.blocks, p.workers)) return;   // (an item's only part is where it belongs)
-    const int R0 = block * p.rows, rows = min(p.rows, p.H * p.T - R0);
-    for (int row = blockIdx.x; row < rows; row += gridDim.x) {
+    LatentMerge m;
+    if (!m.find(p, blockIdx.y)) return;
+    const int piece = threadIdx.x & 127;
+    const int end = min(m.rows, (int)(blockIdx.x + 1) * kLatCombineRows);
+    for (int row = blockIdx.x * kLatCombineRows + (threadIdx.x >> 7); row < end; row += 2) {
         float M = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int kN = 8;
-        for (int at = c0; at <= c1; at += kN) {
-            float l[kN], m = M;
+        constexpr int kN = 4;
+        for (int at = 0; at < m.parts; at += kN) {
+            float l[kN], top = M;
             float4 v[kN];
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
                 l[i] = -INFINITY;
                 v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (at + i <= c1) {
-                    const long long slot = 2ll * (at + i) + (at + i == c0 ? 1 : 0);   // (the first part begins the item)
-                    l[i] = p.lse_part[slot * p.rows + row];
-                    v[i] = reinterpret_cast<const float4*>(p.o_part)[(slot * p.rows + row) * (kLatDim / 4) + threadIdx.x];
+                if (at + i < m.parts) {
+                    const long long slot = m.at(p, at + i, row);
+                    l[i] = p.lse_part[slot];
+                    v[i] = reinterpret_cast<const float4*>(p.o_part)[slot * (kLatDim / 4) + piece];
                 }
             }
 #pragma unroll
-            for (int i = 0; i < kN; ++i) m = fmaxf(m, l[i]);
-            const float ref = m == -INFINITY ? 0.f : m, keep = __expf(M - ref);
+            for (int i = 0; i < kN; ++i) top = fmaxf(top, l[i]);
+            const float ref = top == -INFINITY ? 0.f : top, keep = __expf(M - ref);
             sum *= keep;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) acc[q] *= keep;
-            M = m;
+            for (int k = 0; k < 4; ++k) acc[k] *= keep;
+            M = top;
 #pragma unroll
             for (int i = 0; i < kN; ++i) {
-                if (l[i] == -INFINITY) continue;   // (a part that the row sees nothing of; a NaN gets through)
+                if (l[i] == -INFINITY) continue;
                 const float w = __expf(l[i] - ref);
                 sum += w;
                 acc[0] = fmaf(w, v[i].x, acc[0]);
@@ -1177,13 +1233,67 @@ __global__ void __launch_bounds__(kLatCombineThreads) fa_decode_latent_combine_k
                 acc[3] = fmaf(w, v[i].w, acc[3]);
             }
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        int token, head;
-        p.by_H.divmod(R0 + row, token, head);
-        *reinterpret_cast<uint2*>(static_cast<T*>(p.o) + ((long long)b * p.T * p.H + R0 + row) * kLatDim + 4 * threadIdx.x) =
-            make_uint2(pack2<T>(acc[0] * inv, acc[1] * inv), pack2<T>(acc[2] * inv, acc[3] * inv));
-        if (p.lse && threadIdx.x == 0) p.lse[((long long)b * p.H + head) * p.T + token] = sum == 0.f ? -INFINITY : M + logf(sum);
+        m.store<T>(p, row, piece, acc, M, sum);
     }
+}
+
+// Items of many parts: a block has a row, whose parts' weights it works out first; four groups of threads then share the parts.
+// grid: (rows, entries of LatentParams::merges).
+constexpr int kLatCombineManyThreads = 512;
+template <typename T>
+__global__ void __launch_bounds__(kLatCombineManyThreads) fa_decode_latent_combine_many_kernel(const LatentParams p) {
+    constexpr int kGroups = kLatCombineManyThreads / 128, kWarps = kLatCombineManyThreads / 32;
+    static_assert(kTreeMaxSms <= kLatCombineManyThreads, "a thread to a part");
+    __shared__ float weights[kTreeMaxSms], totals[2][kWarps];
+    __shared__ float4 sums[kGroups][128];
+    grid_dep_wait();
+    LatentMerge m;
+    if (!m.find(p, blockIdx.y) || (int)blockIdx.x >= m.rows) return;
+    const int tid = threadIdx.x, lane = tid & 31, piece = tid & 127, group = tid >> 7, row = blockIdx.x;
+    const float l = tid < m.parts ? p.lse_part[m.at(p, tid, row)] : -INFINITY;
+    float M = l;
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, sh));
+    if (lane == 0) totals[0][tid >> 5] = M;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) M = fmaxf(M, totals[0][i]);
+    const float w = l == -INFINITY ? -1.f : __expf(l - (M == -INFINITY ? 0.f : M));
+    if (tid < m.parts) weights[tid] = w;
+    float sum = w == -1.f ? 0.f : w;
+#pragma unroll
+    for (int sh = 16; sh > 0; sh >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, sh);
+    if (lane == 0) totals[1][tid >> 5] = sum;
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) sum += totals[1][i];
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kN = 8;
+    for (int at = group * kN; at < m.parts; at += kGroups * kN) {
+        float4 v[kN];
+#pragma unroll
+        for (int i = 0; i < kN; ++i)
+            if (at + i < m.parts) v[i] = reinterpret_cast<const float4*>(p.o_part)[m.at(p, at + i, row) * (kLatDim / 4) + piece];
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+            const float f = at + i < m.parts ? weights[at + i] : -1.f;
+            if (f == -1.f) continue;
+            acc[0] = fmaf(f, v[i].x, acc[0]);
+            acc[1] = fmaf(f, v[i].y, acc[1]);
+            acc[2] = fmaf(f, v[i].z, acc[2]);
+            acc[3] = fmaf(f, v[i].w, acc[3]);
+        }
+    }
+    sums[group][piece] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) {
+        const float4 v = sums[g][piece];
+        acc[0] += v.x, acc[1] += v.y, acc[2] += v.z, acc[3] += v.w;
+    }
+    m.store<T>(p, row, piece, acc, M, sum);
 }
 
 }  // namespace fa
