@@ -85,7 +85,7 @@ class fa_append_params(ctypes.Structure):
 
 
 lib.fa_rope.restype = _i
-lib.fa_rope.argtypes = [_p] * 4 + [_i] * 6 + [_f] + [ctypes.c_int64] * 4 + [_i, _p]
+lib.fa_rope.argtypes = [_p] * 4 + [_p] * 6 + [_f] + [_p] * 6   # (sizes as words, see fa_spec_verify)
 lib.fa_cache_append.restype = _i
 lib.fa_cache_append.argtypes = [_p, _p]     # (an fa_append_params by reference, or its bytes)
 _APPEND = struct.Struct("@12P12q17i3f")     # fa_append_params
@@ -575,47 +575,63 @@ def fa_rope(x, out, positions, turns, offset: int = 0, interleaved: bool = False
     """``fa_rope``: x, out [n,H,d] (out may be x), fp16 or bf16, any strides of tokens and heads; positions int32 [n]; turns from
     ``rope_turns``, for the 2 * len(turns) columns of each head from ``offset`` on."""
     dt = x.dtype
-    if not (out.dtype is dt and (dt is _HALF or dt is _BF16)):
-        raise ValueError("fa_rope: x and out share one 16-bit type")
-    n, H, d = x.shape
-    rot = _turns("fa_rope", turns)
+    n, H, d = shape = x.shape
     xt, xh, xd = x.stride()
     ot, oh, od = out.stride()
-    if out.shape != x.shape or xd != 1 or od != 1 or positions.numel() < n or positions.dtype is not _INT or not positions.is_contiguous():
+    if not (out.dtype is dt and (dt is _HALF or dt is _BF16) and out.shape == shape and xd == 1 and od == 1 and positions.dtype is _INT
+            and positions.numel() >= n and positions.is_contiguous()):
+        if out.dtype is not dt or dt not in _FA16:
+            raise ValueError("fa_rope: x and out share one 16-bit type")
         _contiguous("fa_rope", positions)
         _int32("fa_rope", positions)
         if xd != 1 or od != 1:
             raise ValueError("fa_rope: the columns of a head are contiguous")
         _shapes("fa_rope", x=x, out=out, positions=positions)
-    # (the stride of an extent of 1 may be any number)
+    rot = _turns("fa_rope", turns)
+    if n <= 1:   # (the stride of an extent of 1 may be any number)
+        xt = ot = 0
+    if H <= 1:
+        xh = oh = 0
     rc = lib.fa_rope(x.data_ptr(), out.data_ptr(), positions.data_ptr(), turns.data_ptr(), n, H, d, rot, offset, 1 if interleaved else 0, factor,
-                     xt if n > 1 else 0, xh if H > 1 else 0, ot if n > 1 else 0, oh if H > 1 else 0, _FA16[dt], _stream())
+                     xt, xh, ot, oh, _FA16[dt], _stream())
     return _check(rc, "fa_rope", raise_on_error) if rc else rc
 
 
 def _tokens(what: str, t):
     """(tokens, heads, width, stride of a token, stride of a head) of [n,H,d] or [B,T,H,d]."""
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
+    if len(shape) == 3 and t.is_contiguous():
+        n, H, d = shape
+        return n, H, d, H * d, d
+    stride = t.stride()
     if stride[-1] != 1 and shape[-1] != 1:
         raise ValueError(f"{what}: the columns of a head are contiguous")
-    H, d = shape[-2:]
-    head = stride[-2] if H > 1 else 0
     if len(shape) == 3:
-        return shape[0], H, d, stride[0] if shape[0] > 1 else 0, head
-    B, T = shape[:2]
+        n, H, d = shape
+        return n, H, d, stride[0] if n > 1 else 0, stride[1] if H > 1 else 0
+    B, T, H, d = shape
     if B > 1 and T > 1 and stride[0] != T * stride[1]:
         raise ValueError(f"{what}: the tokens of [B,T,H,d] are as far apart from one sequence to the next as inside it")
-    return B * T, H, d, (stride[1] if T > 1 else stride[0]) if B * T > 1 else 0, head
+    return B * T, H, d, (stride[1] if T > 1 else stride[0]) if B * T > 1 else 0, stride[2] if H > 1 else 0
 
 
 def _rows(what: str, cache, Hkv: int, d: int):
     """(slabs, rows of a slab, stride of a slab, stride of a row) of a cache [slabs,rows,Hkv,d], or [slabs,rows,d] for one head."""
-    shape, stride = cache.shape, cache.stride()
-    if shape[2:] != (Hkv, d) and not (Hkv == 1 and shape[2:] == (d,)):
+    shape = cache.shape
+    if len(shape) == 4 and shape[2] == Hkv and shape[3] == d and cache.is_contiguous():
+        return shape[0], shape[1], shape[1] * Hkv * d, Hkv * d
+    stride = cache.stride()
+    if len(shape) == 4:
+        slabs, rows, heads, width = shape
+        good = stride[3] == 1 and (Hkv == 1 or stride[2] == d)
+    else:
+        slabs, rows, width = shape
+        heads, good = 1, stride[2] == 1
+    if heads != Hkv or width != d:
         raise ValueError(f"{what}: a cache of shape {tuple(shape)} for {Hkv} heads of {d}")
-    if stride[-1] != 1 or (Hkv > 1 and stride[2] != d):
+    if not good:
         raise ValueError(f"{what}: a row of a cache is contiguous, not of strides {stride[2:]}")
-    return shape[0], shape[1], stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0
+    return slabs, rows, stride[0] if slabs > 1 else 0, stride[1] if rows > 1 else 0
 
 
 def fa_cache_append(q, q_out, k, v, k_cache, v_cache, first_rows, turns=None, positions=None, counts=None, cu_seqlens=None,
@@ -632,10 +648,11 @@ def fa_cache_append(q, q_out, k, v, k_cache, v_cache, first_rows, turns=None, po
     f8 = ct is torch.float8_e4m3fn or ct is torch.uint8
     if not (f8 or ct is dt) or (v is not None and v_cache.dtype is not ct):
         raise ValueError(f"{what}: caches are of the inputs' type or e4m3, both of one type")
-    for t in (first_rows, positions, counts, cu_seqlens):
-        if t is not None and not (t.dtype is _INT and t.is_contiguous()):
-            _int32(what, t)
-            _contiguous(what, t)
+    if not (first_rows.dtype is _INT and first_rows.is_contiguous() and (positions is None or (positions.dtype is _INT and positions.is_contiguous()))
+            and (counts is None or (counts.dtype is _INT and counts.is_contiguous()))
+            and (cu_seqlens is None or (cu_seqlens.dtype is _INT and cu_seqlens.is_contiguous()))):
+        _int32(what, first_rows, positions, counts, cu_seqlens)
+        _contiguous(what, first_rows, positions, counts, cu_seqlens)
     n, Hkv, d, kt, kh = _tokens(what, k)
     slabs, rows, ks, kr = _rows(what, k_cache, Hkv, d)
     fits = True
@@ -677,24 +694,26 @@ def fa_forward_latent(q, q_rope, k, k_rope, v, o, lse, cu_seqlens_q, cu_seqlens_
     """``fa_forward_latent``: a packed batch, q [total_q,H,128] and q_rope [total_q,H,64], k, v [total_k,H,128], k_rope [total_k,64] shared
     by the heads, all with any strides of tokens and heads; o [total_q,H,128] contiguous, lse [H,total_q] or None; cu_seqlens_* int32 [B+1]."""
     what, dt = "fa_forward_latent", q.dtype
-    if not ((dt is _HALF or dt is _BF16) and all(t.dtype is dt for t in (q_rope, k, k_rope, v, o))):
+    if not ((dt is _HALF or dt is _BF16) and q_rope.dtype is dt and k.dtype is dt and k_rope.dtype is dt and v.dtype is dt and o.dtype is dt):
         raise ValueError(f"{what}: q, q_rope, k, k_rope, v and o share one 16-bit type")
-    if lse is not None and lse.dtype is not _FLOAT:
+    if not (o.is_contiguous() and cu_seqlens_q.dtype is _INT and cu_seqlens_k.dtype is _INT and cu_seqlens_q.is_contiguous() and cu_seqlens_k.is_contiguous()
+            and (lse is None or (lse.dtype is _FLOAT and lse.is_contiguous()))):
+        _int32(what, cu_seqlens_q, cu_seqlens_k)
+        _contiguous(what, o, lse, cu_seqlens_q, cu_seqlens_k)
         raise ValueError(f"{what}: lse is float32")
-    _int32(what, cu_seqlens_q, cu_seqlens_k)
-    _contiguous(what, o, lse, cu_seqlens_q, cu_seqlens_k)
     n, H, d, qt, qh = _tokens(what, q)
     nr, hr, rope, rt, rh = _tokens(what, q_rope)
     m, hk, dk, kt, kh = _tokens(what, k)
     mv, hv, dv, vt, vh = _tokens(what, v)
+    B = cu_seqlens_q.shape[0] - 1
     if not (nr == n and hr == hk == hv == H and dk == dv == d and mv == m and k_rope.shape == (m, rope) and o.shape == (n, H, d)
-            and (lse is None or lse.numel() == H * n) and cu_seqlens_k.numel() == cu_seqlens_q.numel() >= 1):
+            and (lse is None or lse.numel() == H * n) and cu_seqlens_k.shape[0] == B + 1 >= 1):
         _shapes(what, q=q, q_rope=q_rope, k=k, k_rope=k_rope, v=v, o=o, lse=lse, cu_seqlens_q=cu_seqlens_q, cu_seqlens_k=cu_seqlens_k)
     if k_rope.stride(1) != 1:
         raise ValueError(f"{what}: the columns of k_rope are contiguous")
     p = _LATENT.pack(q.data_ptr(), q_rope.data_ptr(), k.data_ptr(), k_rope.data_ptr(), v.data_ptr(), o.data_ptr(), 0 if lse is None else lse.data_ptr(),
                      cu_seqlens_q.data_ptr(), cu_seqlens_k.data_ptr(), qt, qh, rt, rh, kt, kh, vt, vh, k_rope.stride(0) if m > 1 else 0,
-                     cu_seqlens_q.numel() - 1, H, n, m, max_seqlen_q, max_seqlen_k, d, rope, 1 if causal else 0, _FA16[dt], scale)
+                     B, H, n, m, max_seqlen_q, max_seqlen_k, d, rope, 1 if causal else 0, _FA16[dt], scale)
     rc = lib.fa_forward_latent(p, _stream())
     return _check(rc, what, raise_on_error) if rc else rc
 
