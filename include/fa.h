@@ -410,15 +410,16 @@ int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turn
  * of sequence b gets row first_rows[b] + t of its cache, and its position is positions[token], or that row where positions is NULL.
  *   q, q_out [n,Hq,d] (NULL: no queries), k [n,Hkv,d], v [n,Hkv,dv] (NULL: keys alone): of dtype, with strides in elements from one
  *   token and head to the next; q_out may be q with its strides.  turns == NULL: nothing is turned (queries are copied).
- *   Caches of cache_dtype: dtype, or FA_DTYPE_E4M3, where what is written is x / k_scale and x / v_scale, rounded to the nearest
- *   and at most 448.  A row holds Hkv * d (v: Hkv * dv) contiguous elements; k_cache_stride, v_cache_stride: elements from one slab to the next
+ *   Caches of cache_dtype: dtype, or FA_DTYPE_E4M3, where what is written is x / k_scale and x / v_scale (x times the factor's
+ *   reciprocal in 32 bits), rounded to the nearest and at most 448.  A row holds Hkv * d (v: Hkv * dv) contiguous elements; k_cache_stride, v_cache_stride: elements from one slab to the next
  *   and from one row to the next, where a slab is a sequence (block_table == NULL: slabs of Skv_max rows) or a page of page_size rows (any
  *   positive number) behind block_table [B,table_stride].  So both caches may be parts of one row: of latent attention's cache
  *   (fa_decode_latent) the vectors' rotated ends are "keys" of one head of 64, and the vectors are its "values", of 512.
  *   counts int32 [B] (NULL: all): only the first counts[b] tokens of sequence b are written.  Rows outside the cache, and pages outside
  *   [0, num_pages), are passed over.  Tokens behind the last sequence (cu_seqlens[B] < n) are nobody's: nothing of theirs is written.  No two tokens may have one row.
  *   d, dv multiples of 16 up to 1024; rotation as for fa_rope; caches and their strides in whole 16 bytes.  Outputs share no memory with the inputs otherwise.
- * Errors: as fa_rope; FA_ERR_SHAPE also for n != B * T, table_stride < max_pages; FA_ERR_UNSUPPORTED for a k_scale or v_scale that is not positive and finite.
+ * Errors: as fa_rope; FA_ERR_SHAPE also for n != B * T, table_stride < max_pages; FA_ERR_UNSUPPORTED for a k_scale or v_scale that is not positive and finite, or
+ * whose reciprocal is not finite.
  */
 typedef struct fa_append_params {
     const void* q;

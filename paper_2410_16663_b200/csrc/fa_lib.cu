@@ -1397,7 +1397,8 @@ int fa_cache_compact(void* k, void* v, const int* block_table, const int* seqlen
 
 namespace {
 
-bool finite_positive(float x) { return x > 0.f && !isinf(x); }
+// A factor that has a reciprocal.
+bool finite_positive(float x) { return x > 0.f && !isinf(x) && !isinf(1.f / x); }
 
 // Strides of [tokens, heads, width] in elements.
 bool token_strides_ok(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && !(s[0] & 7) && !(s[1] & 7) && s[0] < (1ll << 38) && s[1] < (1ll << 38); }
@@ -1424,8 +1425,11 @@ int rope_launch(fa::RopeParams& rp, bool bf16, bool f8, cudaStream_t st) {
         while (2 * rp.tokens <= 4 && 2 * rp.tokens * half <= fa::kRopeMostAngles && (long long)rp.n >= 8ll * sms * rp.tokens) rp.tokens *= 2;
     }
     rp.by_units.set(rp.units);
-    const auto kern = bf16 ? (f8 ? fa::fa_rope_append_kernel<__nv_bfloat16, true> : fa::fa_rope_append_kernel<__nv_bfloat16, false>)
-                           : (f8 ? fa::fa_rope_append_kernel<__half, true> : fa::fa_rope_append_kernel<__half, false>);
+    using Kernel = void (*)(fa::RopeParams);
+    static const Kernel kernels[2][3] = {{fa::fa_rope_append_kernel<__half, false, false>, fa::fa_rope_append_kernel<__half, true, false>, fa::fa_rope_append_kernel<__half, true, true>},
+                                         {fa::fa_rope_append_kernel<__nv_bfloat16, false, false>, fa::fa_rope_append_kernel<__nv_bfloat16, true, false>,
+                                          fa::fa_rope_append_kernel<__nv_bfloat16, true, true>}};
+    const Kernel kern = kernels[bf16][rp.k == nullptr ? 0 : f8 ? 2 : 1];
     const cudaError_t e = fa::launch_dependent(kern, dim3((rp.n + rp.tokens - 1) / rp.tokens, split), fa::kRopeThreads, 0, st, rp);
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
@@ -1526,8 +1530,7 @@ int fa_cache_append(const fa_append_params* pp, void* stream) {
     rp.by_dv.set(rp.dv / 16);
     rp.by_T.set(p.cu_seqlens || p.T < 1 ? 1 : p.T);
     rp.factor = p.factor;
-    rp.k_scale = p.k_scale;
-    rp.v_scale = p.v_scale;
+    if (f8) rp.k_inv = 1.f / p.k_scale, rp.v_inv = p.v ? 1.f / p.v_scale : 0.f;
     return rope_launch(rp, p.dtype == FA_DTYPE_BF16, f8, static_cast<cudaStream_t>(stream));
 }
 

@@ -40,7 +40,7 @@ struct RopeParams {
     int tokens;                 // of a CTA
     int max_rows, page_size, table_stride, num_pages;
     FastDiv by_units, by_d, by_dv, by_T;   // units; d / 16, dv / 16; T
-    float factor, k_scale, v_scale;
+    float factor, k_inv, v_inv;    // (the 8-bit caches' factors, as their reciprocals)
 };
 
 // The last j in [0, B) with cu[j] <= token, by a warp: 33 parts at a time, so that a few hundred sequences are two loads after another.
@@ -76,20 +76,65 @@ __device__ __forceinline__ uint4 rope_pack(const float (&x)[8]) {
     return make_uint4(pack2<T>(x[0], x[1]), pack2<T>(x[2], x[3]), pack2<T>(x[4], x[5]), pack2<T>(x[6], x[7]));
 }
 
-// kF8: the caches hold e4m3 (q and q_out are 16 bit all the same).
-template <typename T, bool kF8>
-__global__ void __launch_bounds__(kRopeThreads) fa_rope_append_kernel(const RopeParams p) {
+// A pair of a head's vectors: columns x0 .. x0 + 7 and x1 .. x1 + 7 of head h of q, k or v (part 0, 1, 2) of the CTA's g-th token; pair: turned against
+// each other.
+struct RopeUnit {
+    int g, part, h, x0, x1;
+    bool pair;
+};
+
+// kAppend: there are keys for a cache (otherwise q alone).  kF8: the caches hold e4m3 (q and q_out are 16 bit all the same).
+template <typename T, bool kAppend, bool kF8>
+__global__ void __launch_bounds__(kRopeThreads, kAppend ? 5 : 6) fa_rope_append_kernel(const RopeParams p) {
     __shared__ __align__(16) float s_cos[kRopeMostAngles], s_sin[kRopeMostAngles];
-    __shared__ long long s_at[kRopeMostTokens][2];   // of a token: where its rows of the two caches begin (bytes); < 0: it has none
+    __shared__ long long s_at[kAppend ? kRopeMostTokens : 1][2];   // of a token: where its rows of the two caches begin (bytes); < 0: it has none
     __shared__ long long s_pos[kRopeMostTokens];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int token0 = blockIdx.x * p.tokens, tokens = min(p.tokens, p.n - token0);
+    const int half = p.turns ? p.rot / 2 : 0, total = tokens * p.units;
+    RopeUnit unit;
+    uint4 n0, n1;
+    auto load = [&](int i) {
+        int u;
+        p.by_units.divmod(i, unit.g, u);
+        const long long token = token0 + unit.g;
+        const T* src;
+        if (!kAppend || u < p.q_units) {
+            unit.part = 0;
+            p.by_d.divmod(u, unit.h, u);
+            src = static_cast<const T*>(p.q) + token * p.q_st + unit.h * p.q_sh;
+        } else if (u < p.k_units) {
+            unit.part = 1;
+            p.by_d.divmod(u - p.q_units, unit.h, u);
+            src = static_cast<const T*>(p.k) + token * p.k_st + unit.h * p.k_sh;
+        } else {
+            unit.part = 2;
+            p.by_dv.divmod(u - p.k_units, unit.h, u);
+            src = static_cast<const T*>(p.v) + token * p.v_st + unit.h * p.v_sh;
+        }
+        unit.x0 = 16 * u, unit.x1 = 16 * u + 8;
+        const bool halves = (!kAppend || unit.part < 2) && p.turns && !p.interleaved;
+        unit.pair = halves && u < p.rot / 16;
+        if (unit.pair) {
+            unit.x0 = p.offset + 8 * u;
+            unit.x1 = unit.x0 + half;
+        } else if (halves) {   // of the columns that stay as they are
+            unit.x0 -= p.rot;
+            unit.x0 += unit.x0 < p.offset ? 0 : p.rot;
+            unit.x1 -= p.rot;
+            unit.x1 += unit.x1 < p.offset ? 0 : p.rot;
+        }
+        n0 = *reinterpret_cast<const uint4*>(src + unit.x0);
+        n1 = *reinterpret_cast<const uint4*>(src + unit.x1);
+    };
     grid_dep_wait();
+    int i = blockIdx.y * kRopeThreads + tid;
+    if (kAppend && i < total) load(i);   // (on its way while the token is looked up)
     if (warp < tokens) {
         const int token = token0 + warp;
         long long pos = p.positions ? p.positions[token] : 0;
         long long at_k = -1, at_v = -1;
-        if (p.k) {
+        if (kAppend) {
             int b, t;
             if (p.cu) {
                 b = rope_sequence(p.cu, p.B, token, lane);
@@ -114,62 +159,32 @@ __global__ void __launch_bounds__(kRopeThreads) fa_rope_append_kernel(const Rope
         }
         if (lane == 0) {
             s_pos[warp] = pos;
-            s_at[warp][0] = at_k;
-            s_at[warp][1] = at_v;
+            if (kAppend) s_at[warp][0] = at_k, s_at[warp][1] = at_v;
         }
     }
     __syncthreads();
-    const int half = p.turns ? p.rot / 2 : 0;
-    for (int i = tid; i < tokens * half; i += kRopeThreads) {
-        const int g = i / half;
-        const unsigned long long turn = (unsigned long long)s_pos[g] * p.turns[i - g * half];
+    for (int k = tid; k < tokens * half; k += kRopeThreads) {
+        const int g = k / half;
+        const unsigned long long turn = (unsigned long long)s_pos[g] * p.turns[k - g * half];
         float s, c;
         sincospif((float)(int)(turn >> 32) * 4.656612873077393e-10f, &s, &c);   // (2^-31: half turns)
-        s_cos[i] = c * p.factor;
-        s_sin[i] = s * p.factor;
+        s_cos[k] = c * p.factor;
+        s_sin[k] = s * p.factor;
     }
     __syncthreads();
-    for (int i = blockIdx.y * kRopeThreads + tid; i < tokens * p.units; i += kRopeThreads * gridDim.y) {
-        int g, u, h;
-        p.by_units.divmod(i, g, u);
-        const T* src;
-        char* dst;
-        bool f8 = kF8, turned = p.turns != nullptr;
-        float scale = 1.f;
+    const int stride = kRopeThreads * gridDim.y;
+    for (bool first = true; i < total; i += stride, first = false) {
+        if (!kAppend || !first) load(i);
+        const RopeUnit& now = unit;
+        const uint4 w0 = n0, w1 = n1;
+        const int g = now.g;
+        if (kAppend && (s_at[g][0] == kRopeNobodys || (now.part > 0 && s_at[g][0] < 0))) continue;
         const long long token = token0 + g;
-        if (u < p.q_units) {
-            if (s_at[g][0] == kRopeNobodys) continue;
-            p.by_d.divmod(u, h, u);
-            src = static_cast<const T*>(p.q) + token * p.q_st + h * p.q_sh;
-            dst = reinterpret_cast<char*>(static_cast<T*>(p.q_out) + token * p.o_st + h * p.o_sh);
-            f8 = false;
-        } else if (u < p.k_units) {
-            if (s_at[g][0] < 0) continue;
-            p.by_d.divmod(u - p.q_units, h, u);
-            src = static_cast<const T*>(p.k) + token * p.k_st + h * p.k_sh;
-            dst = p.k_cache + s_at[g][0] + (long long)h * p.d * (kF8 ? 1 : 2);
-            scale = p.k_scale;
-        } else {
-            if (s_at[g][0] < 0) continue;
-            p.by_dv.divmod(u - p.k_units, h, u);
-            src = static_cast<const T*>(p.v) + token * p.v_st + h * p.v_sh;
-            dst = p.v_cache + s_at[g][1] + (long long)h * p.dv * (kF8 ? 1 : 2);
-            scale = p.v_scale;
-            turned = false;
-        }
-        // The unit's two vectors: columns x0 .. x0 + 7 and x1 .. x1 + 7.
-        int x0 = 16 * u, x1 = 16 * u + 8;
-        const bool halves = turned && !p.interleaved, pair = halves && u < p.rot / 16;
-        if (pair) {
-            x0 = p.offset + 8 * u;
-            x1 = x0 + half;
-        } else if (halves) {   // of the columns that stay as they are
-            x0 -= p.rot;
-            x0 += x0 < p.offset ? 0 : p.rot;
-            x1 -= p.rot;
-            x1 += x1 < p.offset ? 0 : p.rot;
-        }
-        uint4 w0 = *reinterpret_cast<const uint4*>(src + x0), w1 = *reinterpret_cast<const uint4*>(src + x1);
+        char* dst = !kAppend || now.part == 0 ? reinterpret_cast<char*>(static_cast<T*>(p.q_out) + token * p.o_st + now.h * p.o_sh)
+                  : now.part == 1 ? p.k_cache + s_at[g][0] + (long long)now.h * p.d * (kF8 ? 1 : 2)
+                                  : p.v_cache + s_at[g][1] + (long long)now.h * p.dv * (kF8 ? 1 : 2);
+        const bool f8 = kF8 && now.part > 0, turned = (!kAppend || now.part < 2) && p.turns != nullptr, pair = now.pair;
+        const int x0 = now.x0, x1 = now.x1;
         const bool in0 = turned && p.interleaved && x0 >= p.offset && x0 < p.offset + p.rot, in1 = turned && p.interleaved && x1 >= p.offset && x1 < p.offset + p.rot;
         if (!f8 && !pair && !in0 && !in1) {
             *reinterpret_cast<uint4*>(dst + 2 * x0) = w0;
@@ -180,8 +195,8 @@ __global__ void __launch_bounds__(kRopeThreads) fa_rope_append_kernel(const Rope
         rope_unpack<T>(w0, a);
         rope_unpack<T>(w1, b);
         if (pair) {
-            const float* c = s_cos + g * half + 8 * u;
-            const float* s = s_sin + g * half + 8 * u;
+            const float* c = s_cos + g * half + x0 - p.offset;
+            const float* s = s_sin + g * half + x0 - p.offset;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float x = a[j] * c[j] - b[j] * s[j];
@@ -203,11 +218,12 @@ __global__ void __launch_bounds__(kRopeThreads) fa_rope_append_kernel(const Rope
                 }
             }
         }
-        if (f8) {   // (a true division: the cache holds the nearest share, whatever the factor)
+        if (f8) {
+            const float inv = now.part == 1 ? p.k_inv : p.v_inv;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                a[j] = __fdiv_rn(a[j], scale);
-                b[j] = __fdiv_rn(b[j], scale);
+                a[j] *= inv;
+                b[j] *= inv;
             }
             *reinterpret_cast<uint2*>(dst + x0) = make_uint2(pack4_e4m3(a[0], a[1], a[2], a[3]), pack4_e4m3(a[4], a[5], a[6], a[7]));
             *reinterpret_cast<uint2*>(dst + x1) = make_uint2(pack4_e4m3(b[0], b[1], b[2], b[3]), pack4_e4m3(b[4], b[5], b[6], b[7]));

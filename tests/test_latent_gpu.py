@@ -284,3 +284,84 @@ def test_absorbed_queries_of_any_strides(T, H):
     o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
     fa.fa_decode_latent(q2, r2, cache, o2, lse2, ints([300, 41, 0, 700]), SCALE, ws, block_table=table)
     assert torch.equal(o2, o) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("H", [16, 40, 128])
+def test_calls_at_once(H):
+    """Two calls on two streams, with workspaces of their own, while a third takes its turns on one: each gives what it gives alone."""
+    cases = [absorbed([400, 3000, 77], 1, H, dt, page=page) for dt, page in (("fp16", 64), ("bf16", 0), ("fp16", 16))]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    lens = ints([400, 3000, 77])
+    torch.cuda.synchronize()
+    outs = []
+    for turn in range(6):
+        for i, (q, r, cache, table, ws, o, lse, _) in enumerate(cases):
+            with torch.cuda.stream(streams[i % 2]):
+                o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+                fa.fa_decode_latent(q, r, cache, o2, lse2, lens, SCALE, ws, block_table=table)
+                outs.append((o2, o, lse2, lse))
+    torch.cuda.synchronize()
+    for o2, o, lse2, lse in outs:
+        assert torch.equal(o2, o) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("H, T", [(16, 1), (40, 2), (128, 1)])
+def test_a_prompt_and_the_tokens_after_it(H, T):
+    """A layer's calls as they follow one another: the prompt's latent vectors and rotated keys go to a paged cache, its queries are rotated on the
+    way and attend in the expanded form; then new tokens are appended and attend in the absorbed form, to what the appends have written."""
+    dt, page, lens = "fp16", 16, [70, 131, 1]
+    B, n = len(lens), sum(lens)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    w_k = torch.empty(H, 128, 512, device="cuda").normal_(generator=g).mul_(512 ** -0.5)       # key and value expansion of each head
+    w_v = torch.empty(H, 128, 512, device="cuda").normal_(generator=g).mul_(512 ** -0.5)
+    turns = fa.rope_turns(fa.rope_frequencies(64))
+    need = [-(-(x + T) // page) for x in lens]
+    pages, at, table = list(range(sum(need))), 0, []
+    random.Random(1).shuffle(pages)
+    for x in need:
+        table.append(pages[at:at + x] + [-1] * (max(need) - x))
+        at += x
+    table = ints(table)
+    cache = torch.full((sum(need), page, 576), float("nan"), dtype=torch.float16, device="cuda")
+    cu = ints([0, 70, 201, 202])
+    # the prompt
+    q, c, kr = normal((n, H, 192), dt, 11), normal((n, 1, 512), dt, 12), normal((n, 1, 64), dt, 13)
+    raw = q.clone()
+    fa.fa_cache_append(q[..., 128:], q[..., 128:], kr, c, cache[..., 512:], cache[..., :512], ints([0] * B), turns=turns, cu_seqlens=cu, block_table=table)
+    slots = torch.cat([table[b, torch.arange(x, device="cuda") // page].long() * page + torch.arange(x, device="cuda") % page for b, x in enumerate(lens)])
+    rows = cache.view(-1, 576)[slots]
+    assert torch.equal(rows[:, :512], c[:, 0]) and torch.equal(q[..., :128], raw[..., :128])
+    k = torch.einsum("nc,hdc->nhd", rows[:, :512].float(), w_k).half()
+    v = torch.einsum("nc,hdc->nhd", rows[:, :512].float(), w_v).half()
+    o, lse = torch.empty(n, H, 128, dtype=torch.float16, device="cuda"), torch.empty(H, n, device="cuda")
+    fa.fa_forward_latent(q[..., :128], q[..., 128:], k, rows[:, 512:], v, o, lse, cu, cu, max(lens), max(lens), True, SCALE)
+    at = 0
+    for x in lens:
+        for h in (0, H - 1):
+            want = oracle.attention(q[at:at + x, h].cpu(), torch.cat([k[at:at + x, h], rows[at:at + x, 512:]], -1).cpu(), v[at:at + x, h].cpu(), SCALE, True)
+            check(o[at:at + x, h], lse[h, at:at + x], want, dt)
+        at += x
+    # T tokens more; the second sequence's do not get room
+    q2, c2, kr2 = normal((B, T, H, 192), dt, 21), normal((B, T, 1, 512), dt, 22), normal((B, T, 1, 64), dt, 23)
+    before = cache.clone()
+    fa.fa_cache_append(q2[..., 128:], q2[..., 128:], kr2, c2, cache[..., 512:], cache[..., :512], ints(lens), turns=turns, counts=ints([T, 0, T]), block_table=table)
+    changed = (cache.view(torch.int16) != before.view(torch.int16)).any(-1).sum()
+    assert int(changed) == 2 * T
+    now = [lens[0] + T, lens[1], lens[2] + T]
+    absorbed_q = torch.einsum("bthd,hdc->bthc", q2[..., :128].float(), w_k).half()
+    ol, lse2 = torch.empty(B, T, H, 512, dtype=torch.float16, device="cuda"), torch.empty(B, H, T, device="cuda")
+    ws = torch.empty(fa.fa_decode_latent_workspace_bytes(B, T, H, table.shape[1] * page), dtype=torch.uint8, device="cuda")
+    fa.fa_decode_latent(absorbed_q, q2[..., 128:], cache, ol, lse2, ints(now), SCALE, ws, block_table=table)
+    for b, x in enumerate(now):
+        slots = table[b, torch.arange(x, device="cuda") // page].long() * page + torch.arange(x, device="cuda") % page
+        rows = cache.view(-1, 576)[slots]
+        live = min(T, x)
+        for h in (0, H - 1):
+            want = oracle.attention(torch.cat([absorbed_q[b, T - live:, h], q2[b, T - live:, h, 128:]], -1).cpu(), rows.cpu(), rows[:, :512].cpu(), SCALE, True)
+            check(ol[b, T - live:, h], lse2[b, h, T - live:], want, dt, size=40.0)
+            # And the two forms agree: of the absorbed output expanded, and of expanded keys and values.  Queries, keys, values and outputs are rounded to half a
+            # step (2^-11) each on the way: scores move by 2^-11 of some tens of products' root sum square, below 0.01, and the output by less than 0.02 of its size.
+            kk, vv = rows[:, :512].double() @ w_k[h].double().T, rows[:, :512].double() @ w_v[h].double().T
+            full = oracle.attention(q2[b, T - live:, h].cpu(), torch.cat([kk, rows[:, 512:].double()], -1).cpu(), vv.cpu(), SCALE, True)[0]
+            got = (ol[b, T - live:, h].double() @ w_v[h].double().T).cpu()
+            assert float((got - full).norm() / full.norm()) < 0.02
