@@ -1563,7 +1563,8 @@ int latent_launch(const CUtensorMap (&tm)[4], fa::LatentParams& lp, int sms, cud
     lp.workers = most < fa::kTreeMaxSms ? most : fa::kTreeMaxSms;
     lp.by_item = (long long)lp.B * lp.blocks < lp.workers ? 1 : 0;
     cudaError_t e = fa::launch_dependent_clusters(kern, dim3(lp.workers * ctas), ctas, 1, threads, smem, st, tm[0], tm[1], tm[2], tm[3], lp);
-    if (e == cudaSuccess && lp.workers > 1) {
+    // (an item of one tile is nobody's but one worker's)
+    if (e == cudaSuccess && lp.workers > 1 && lp.Smax > (N > 0 ? fa::kLatTile : fa::kLatPairTile)) {
         const int y = lp.by_item ? lp.B * lp.blocks : lp.workers - 1;
         // parts of an item, on average (one sequence of 8000 keys, 16 heads: 23.5 -> 14.8 us; 32 of 8192 with 128 heads, three parts each: 90 -> 110)
         const bool many = lp.workers >= 8ll * lp.B * lp.blocks;

@@ -365,3 +365,22 @@ def test_a_prompt_and_the_tokens_after_it(H, T):
             full = oracle.attention(q2[b, T - live:, h].cpu(), torch.cat([kk, rows[:, 512:].double()], -1).cpu(), vv.cpu(), SCALE, True)[0]
             got = (ol[b, T - live:, h].double() @ w_v[h].double().T).cpu()
             assert float((got - full).norm() / full.norm()) < 0.02
+
+
+@pytest.mark.parametrize("H", [5, 32, 128])
+@pytest.mark.parametrize("most", [1, 10, 64, 65, 128, 129])
+def test_absorbed_small_caches(H, most):
+    """Caches that are less than a tile, one tile (of which nothing is to merge) and a little more."""
+    absorbed([most, 0, max(1, most // 2)], 1, H, "fp16")
+
+
+@pytest.mark.parametrize("H", [16, 128])
+def test_absorbed_scale_of_zero(H):
+    """All keys weigh the same."""
+    cache, q, r = normal((2, 200, 576), "fp16", 1), normal((2, 1, H, 512), "fp16", 2), normal((2, 1, H, 64), "fp16", 3)
+    o, lse, ws = torch.empty_like(q), torch.empty(2, H, 1, device="cuda"), torch.empty(fa.fa_decode_latent_workspace_bytes(2, 1, H, 200), dtype=torch.uint8, device="cuda")
+    fa.fa_decode_latent(q, r, cache, o, lse, ints([200, 7]), 0.0, ws)
+    for b, n in enumerate((200, 7)):
+        want = cache[b, :n, :512].double().mean(0)
+        allow = 2.0 ** -11 * want.abs() + 2.0 ** -13 * cache[b, :n, :512].double().abs().mean(0)
+        assert bool(((o[b, 0].double() - want).abs() <= allow).all()) and bool((lse[b].double() - torch.log(torch.tensor(float(n)))).abs().max() < 1e-4)
