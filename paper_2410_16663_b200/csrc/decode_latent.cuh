@@ -1190,16 +1190,15 @@ struct LatentMerge {
     }
 };
 
-// Items of a few parts.  grid: (blocks of eight rows, entries of LatentParams::merges); two rows at a time of 256 threads.
-constexpr int kLatCombineThreads = 256, kLatCombineRows = 8;
+// Items of a few parts, two rows at a time to a block.  grid: (blocks that share an item's rows, as many as run at once; entries of LatentParams::merges).
+constexpr int kLatCombineThreads = 256, kLatCombinePerSm = 6;
 template <typename T>
-__global__ void __launch_bounds__(kLatCombineThreads) fa_decode_latent_combine_kernel(const LatentParams p) {
+__global__ void __launch_bounds__(kLatCombineThreads, kLatCombinePerSm) fa_decode_latent_combine_kernel(const LatentParams p) {
     grid_dep_wait();
     LatentMerge m;
     if (!m.find(p, blockIdx.y)) return;
     const int piece = threadIdx.x & 127;
-    const int end = min(m.rows, (int)(blockIdx.x + 1) * kLatCombineRows);
-    for (int row = blockIdx.x * kLatCombineRows + (threadIdx.x >> 7); row < end; row += 2) {
+    for (int row = 2 * blockIdx.x + (threadIdx.x >> 7); row < m.rows; row += 2 * gridDim.x) {
         float M = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
         constexpr int kN = 4;
         for (int at = 0; at < m.parts; at += kN) {

@@ -1568,8 +1568,9 @@ int latent_launch(const CUtensorMap (&tm)[4], fa::LatentParams& lp, int sms, cud
         const int y = lp.by_item ? lp.B * lp.blocks : lp.workers - 1;
         // parts of an item, on average (one sequence of 8000 keys, 16 heads: 23.5 -> 14.8 us; 32 of 8192 with 128 heads, three parts each: 90 -> 110)
         const bool many = lp.workers >= 8ll * lp.B * lp.blocks;
+        const int pairs_of_rows = (lp.rows + 1) / 2, room = fa::kLatCombinePerSm * sms / y;
         e = many ? fa::launch_dependent(fa::fa_decode_latent_combine_many_kernel<T>, dim3(lp.rows, y), fa::kLatCombineManyThreads, 0, st, lp)
-                 : fa::launch_dependent(fa::fa_decode_latent_combine_kernel<T>, dim3((lp.rows + fa::kLatCombineRows - 1) / fa::kLatCombineRows, y), fa::kLatCombineThreads, 0, st, lp);
+                 : fa::launch_dependent(fa::fa_decode_latent_combine_kernel<T>, dim3(pairs_of_rows < room ? pairs_of_rows : room > 0 ? room : 1, y), fa::kLatCombineThreads, 0, st, lp);
     }
     return e == cudaSuccess ? FA_OK : cuda_fail(e);
 }
