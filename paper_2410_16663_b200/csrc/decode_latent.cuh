@@ -1,13 +1,19 @@
 // Latent attention's absorbed form: a few new tokens per sequence over a cache whose rows (576 elements: a latent vector of 512 and a rotated
-// part of 64) are the keys, and in their first 512 elements the values, of all heads.
+// part of 64) are the keys, and in their first 512 elements the values, of all heads.  A key is 1152 bytes and 2176 operations for each of
+// the H heads times T tokens, the rows that read it: up to some hundred rows HBM is the floor, beyond them the tensor cores.
 //
-// The H heads times T tokens of a sequence are rows that read the same keys.  Up to 32 of them: the keys are the rows of the matrix
-// instructions and the (token, head) rows their columns, so that nothing is padded to 128 -- S^T = C Q^T (128 keys x N), O^T += L^T P^T (512
-// latent elements, four products of 128, x N).  A tile of the cache is loaded once and is the first operand of both products: with its elements
-// contiguous for the scores, with its keys contiguous for the output.
+// Up to 32 rows: one CTA, and the keys are the rows of the matrix instructions, the (token, head) rows their columns, so that nothing is padded to
+// 128 -- S^T = C Q^T (64 keys x N), O^T += L^T P^T (512 latent elements, four products of 128, x N).  A tile of the cache is loaded once and is the
+// first operand of both products: with its elements contiguous for the scores, with its keys contiguous for the output.  HBM bounds it: 64
+// sequences of 8192 keys, 16 heads, 100 us, 6.0 TB/s (0.93 of a copy); with 32 heads 112 us.  What it took (us, the first of these): tiles of 128 keys, of
+// which one and a quarter fit, so that loads, products and softmax waited for each other in a chain, 115; 64-key tiles 114, bound by
+// the loading warp, which spent 660 clocks on each of five boxes with divisions and shuffles; its loops written out 100.6.
+// More rows: pairs of CTAs (see there).
 //
 // The tiles of all items (a sequence's block of rows), one after the other, are dealt out in equal runs to as many CTAs as run at
 // once, as in decode_tree.cuh; what several CTAs share of an item goes to the workspace, and a second kernel merges it.
+// Short calls (one sequence of 1000 keys, 16 heads: 10.8 us) are their beginning -- 4500 clocks to the first load: the lengths, the run, the page, each
+// a cold read and cold code --, 1500 for scores and softmax, 2500 for the output, and the merge's launch.
 #pragma once
 
 #include "decode_tree.cuh"
@@ -221,8 +227,8 @@ __device__ __forceinline__ bool lat_meet(uint32_t bar, uint32_t parity, int lane
     return pp_warp_wait(bar, parity, abort_flag, where);
 }
 
-// Scores of 64 keys are 16 lanes of each quarter of tensor memory, so that half of a softmax warp's lanes have one; with tiles of 128 keys all of
-// them had, but only one and a quarter tiles fit, and the chain of loading, both products and the softmax lay open.
+// (Scores of 64 keys are 16 lanes of each quarter of tensor memory: half of a softmax warp's lanes have one.  For 64 rows, 32 columns a thread, that
+// chain is longer than a tile may take, 103 us on 32 sequences of 8192 keys, 64 heads, where a pair, half of its rows empty, takes 80.)
 // grid: as many as run at once.  Warps 0 to 7: softmax and output (a key per thread, half the columns each); 8: segments and the cache; 9: Q;
 // 10: S^T; 11: O^T.
 // tm: boxes of 128 latent elements (whole tiles: block by block of 64; pages of less than a tile: eight keys after eight keys), tm_r: of the rotated part.
@@ -666,6 +672,12 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 // columns of output in 256 of its 512 columns, scores of 128 keys in 64 -- one CTA's tensor memory would be full with the output
 // of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 64 keys of a
 // tile), latent elements for the output (each loads 256 elements of all 128 keys): 1.9 times the tile over L2, once from HBM.
+// A tile of 128 keys takes 3700 clocks: 2200 for the products (36 of 32 clocks, 16 of 65), 3060 for what the operands, the loads and P take of shared
+// memory's 128 bytes a clock, and the rings, which hold a tile of keys in thirds and one of values in halves beside Q's 72 KiB, refill while they are read.
+// 32 sequences of 8192 keys, 128 heads: 85 us (855 TFLOP/s, 3.6 TB/s; floor 48), 64 of them 155 (940).  On the way (us, the first of these): 132; without
+// releases at cluster scope and with Q by tensor maps 98, with tiles of 64 keys; thirds and halves of 128-key tiles 90, the merge's blocks 85.  Keys in
+// boxes of 8 KiB, one 64-element block each: 117 (a box costs the loading thread and TMA 160 ns).  Keys asked into L2 ahead: 86 to 95.  Keeping P in the
+// tensor cores' collector for both halves of its values: level.
 struct LatPairShape {
     static constexpr int kKB = 64 * 192 * 2;                        // a third of a CTA's keys of a tile: 64, 192 elements; all three lie ready
     static constexpr int kVB = 64 * 256 * 2;                        // half of its values: 64 keys, two times 128 elements; both lie ready

@@ -7,6 +7,12 @@
 // A CTA takes a few tokens.  A warp each finds a token's sequence and its cache row, a thread each forms a token's cosine and sine of
 // one frequency (every head needs them), and then a thread takes two 16-byte vectors of a head at a time: with the halves of a
 // head rotated against each other those are the vectors that belong together.
+//
+// HBM bounds many tokens: 16384 of 40 heads of 128 (bf16) 56 us, 6.0 TB/s of the 6.5 of a copy; into caches, where a row's pieces are written far apart, 8000
+// tokens of 32/8 heads 34.7 us (5.7), latent rows with 128 query heads 71 (5.5), 8-bit caches 35 (5.1).  Few tokens are latency: 2.2 us for one of 40 heads, 7.5 for
+// 768 tokens of 256 sequences into an 8-bit cache, whose look-ups (sequence, row, page, angle) are a chain; the first pieces are on their way meanwhile
+// (8.9 -> 7.8 us, and 57 -> 60 for plain rotations, which have no look-ups and too few registers for it: they load in the loop).  Everything loaded one round
+// ahead took 60 instead of 56 us: what is in flight is there by occupancy, six CTAs to an SM, five with look-ups.
 #pragma once
 
 #include "prefill_simple.cuh"
