@@ -270,8 +270,6 @@ __device__ __forceinline__ void tma_load_5d_pair_hint(uint32_t dst, const CUtens
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "l"(policy)
         : "memory");
 }
-// A line of global memory on its way into L2.
-__device__ __forceinline__ void l2_prefetch(const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at) : "memory"); }
 __device__ __forceinline__ void tma_store_4d(const CUtensorMap* tm, uint32_t src, int c0, int c1,
                                              int c2, int c3) {
     asm volatile(
