@@ -1403,6 +1403,9 @@ bool finite_positive(float x) { return x > 0.f && !isinf(x) && !isinf(1.f / x); 
 // Strides of [tokens, heads, width] in elements.
 bool token_strides_ok(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && !(s[0] & 7) && !(s[1] & 7) && s[0] < (1ll << 38) && s[1] < (1ll << 38); }
 
+// What is written may not lie over itself: strides of a and b steps each pass over width elements.
+bool apart(const int64_t s[2], int a, int b, long long width) { return (a <= 1 || s[0] >= width) && (b <= 1 || s[1] >= width); }
+
 // What a rotation asks of its sizes.
 int check_rotation(int d, int rot, int offset, float factor) {
     if (rot < 0 || offset < 0 || (long long)offset + rot > d) return FA_ERR_SHAPE;
@@ -1445,7 +1448,7 @@ int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turn
     if (int rc = check_rotation(d, rot_dim, rot_offset, factor)) return rc;
     if (dtype != FA_DTYPE_FP16 && dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
     const int64_t xs[2] = {x_token_stride, x_head_stride}, os[2] = {out_token_stride, out_head_stride};
-    if (!token_strides_ok(xs) || !token_strides_ok(os)) return FA_ERR_SHAPE;
+    if (!token_strides_ok(xs) || !token_strides_ok(os) || !apart(os, n, H, d)) return FA_ERR_SHAPE;
     if ((long long)H * d > (1 << 24)) return FA_ERR_UNSUPPORTED;
     if (n == 0) return FA_OK;
     if (!x || !out || !positions || (rot_dim > 0 && !turns)) return FA_ERR_NULL;
@@ -1484,6 +1487,10 @@ int fa_cache_append(const fa_append_params* pp, void* stream) {
     } else if (p.Skv_max < 0) return FA_ERR_SHAPE;
     if (!token_strides_ok(p.k_stride) || (p.v && !token_strides_ok(p.v_stride)) || (p.q && (!token_strides_ok(p.q_stride) || !token_strides_ok(p.q_out_stride))))
         return FA_ERR_SHAPE;
+    if (p.q && !apart(p.q_out_stride, p.n, p.Hq, p.d)) return FA_ERR_SHAPE;
+    const int slabs = p.block_table ? p.num_pages : p.B, slab_rows = p.block_table ? p.page_size : p.Skv_max;
+    if (!apart(p.k_cache_stride, slabs, slab_rows, (long long)p.Hkv * p.d)) return FA_ERR_SHAPE;
+    if (p.v && !apart(p.v_cache_stride, slabs, slab_rows, (long long)p.Hkv * p.dv)) return FA_ERR_SHAPE;
     const int64_t unit = f8 ? 15 : 7;   // 16 bytes
     for (int i = 0; i < 2; ++i) {
         if (p.k_cache_stride[i] < 0 || p.k_cache_stride[i] >= (1ll << 42) || (p.k_cache_stride[i] & unit)) return FA_ERR_SHAPE;

@@ -110,3 +110,17 @@ def test_scaled_frequencies():
     assert torch.equal(by_parts[over >= 32], w[over >= 32]) and torch.allclose(by_parts[over <= 1], w[over <= 1] / 8, rtol=1e-15)
     mid = (over > 1) & (over < 32)
     assert bool(mid.any()) and bool(((by_parts < w) & (by_parts > w / 8))[mid].all())
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(q_out_stride=(0, 128)), fa.FA_ERR_SHAPE), (dict(q_out_stride=(512, 0)), fa.FA_ERR_SHAPE), (dict(q_out_stride=(512, 120)), fa.FA_ERR_SHAPE),
+    (dict(k_cache_stride=(64 * 256, 0)), fa.FA_ERR_SHAPE), (dict(k_cache_stride=(0, 256)), fa.FA_ERR_SHAPE), (dict(v_cache_stride=(64 * 256, 128)), fa.FA_ERR_SHAPE),
+    (dict(Skv_max=1, k_cache_stride=(256, 0), n=0, T=0), fa.FA_OK), (dict(q_out_stride=(128, 1024), n=0, T=0), fa.FA_OK)])
+def test_outputs_that_lie_over_themselves_are_refused(change, code):
+    """Rows or heads one over the other (an expanded tensor) would hold whatever came last; dimensions of one, and heads before tokens, stay open."""
+    assert fa.lib.fa_cache_append(ctypes.byref(append_params(**change)), None) == code
+
+
+def test_rope_outputs_that_lie_over_themselves_are_refused():
+    for change in (dict(ot=0), dict(oh=0), dict(oh=8)):
+        assert fa.lib.fa_rope(*rope_args(**change), None) == fa.FA_ERR_SHAPE
