@@ -667,7 +667,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 }
 
 // ---------------------------------------------------------------------------------------
-// More than 32 rows: a pair of CTAs (a cluster) has blocks of 128, 64 rows in each, and issues matrix instructions of both (cta_group::2, M = 128).  Each
+// More than 32 rows: a pair of CTAs (a cluster) has blocks of up to 128, half of the rows in each, and issues matrix instructions of both (cta_group::2, M = 128).  Each
 // CTA's tensor memory then holds its 64 rows in the lanes 0 to 63 for the first half of the columns and in 64 to 127 for the second: 512
 // columns of output in 256 of its 512 columns, scores of 128 keys in 64 -- one CTA's tensor memory would be full with the output
 // of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 64 keys of a
@@ -784,6 +784,8 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
 
     const int ps = p.page_size;
     const bool small = p.block_table != nullptr && ps < 64;
+    // Rows of a CTA: half of them each, also where one could have all, so that both write the output (7 x 8000 keys, 60 rows: 32 -> 28 us).
+    const int per = (p.rows + 1) / 2;
     bool ok = true;
     auto segment = [&](uint32_t ord, LatentSegment& s) {
         if (!pp_warp_wait(bar(latp::seg_full + ord % kLatSegs), (ord / kLatSegs) & 1, abort_flag, 360)) return false;
@@ -882,7 +884,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             if (lane == 0) mbar_arrive(bar(latp::seg_empty + ord % kLatSegs));
             if (seg.n <= 0) break;
             if (ord > 0 && !(ok = pp_warp_wait(bar(latp::q_empty), (ord - 1) & 1, abort_flag, 364))) break;
-            const int R0 = seg.block * p.rows + 64 * rank, rows = min(p.rows - 64 * rank, p.H * p.T - R0);
+            const int R0 = seg.block * p.rows + per * rank, rows = min(min(per, p.rows - per * rank), p.H * p.T - R0);
             if (p.q_boxes) {
                 if (lane == 0) {
                     mbar_expect_tx(bar(latp::q_full), Shape::kQB);
@@ -1005,8 +1007,8 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
         auto wait = [&](int i, uint32_t parity, unsigned int where) { return pp_warp_wait(bar(i), parity, abort_flag, where); };
         for (uint32_t ord = 0;; ++ord) {
             if (!(ok = segment(ord, seg)) || seg.n <= 0) break;
-            const int x = 64 * rank + r, R = seg.block * p.rows + x;   // row of the block, of the sequence
-            const bool mine = x < p.rows && R < p.H * p.T;
+            const int x = per * rank + r, R = seg.block * p.rows + x;   // row of the block, of the sequence
+            const bool mine = r < per && x < p.rows && R < p.H * p.T;
             const bool some = __any_sync(0xffffffffu, mine);   // a warp without rows only keeps step
             int token = 0, head = 0;
             if (mine) p.by_H.divmod(R, token, head);
