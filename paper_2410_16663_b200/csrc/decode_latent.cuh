@@ -306,15 +306,15 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             const int* table = p.block_table ? p.block_table + (long long)seg.b * p.table_stride : nullptr;
             auto lookup = [&](int key) {   // the page of this lane's part of the tile at `key`, one tile ahead
                 if (!table || key >= seg.len) return -1;
-                const int page = small ? (lane < kLatTile / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
-                return (unsigned)page < (unsigned)p.num_pages ? page : -1;   // (none: zeros)
+                return small ? (lane < kLatTile / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
             };
+            auto there = [&](int page) { return (unsigned)page < (unsigned)p.num_pages ? page : -1; };   // (none: zeros; asked when it is needed, not waited for ahead)
             const int end = (seg.t0 + seg.n) * kLatTile, keys = small ? ps : kLatTile;   // of a box
             int page = lookup(seg.t0 * kLatTile);
             for (int key0 = seg.t0 * kLatTile; key0 < end && ok; key0 += kLatTile) {
                 const int next = key0 + kLatTile, page_next = next < end ? lookup(next) : -1;
                 const int boxes = small ? (min(seg.len - key0, kLatTile) + ps - 1) / ps : 1;   // of a unit
-                const int row = table ? key0 % ps : key0, slab = table ? page : seg.b;
+                const int row = table ? key0 % ps : key0, slab = table ? there(page) : seg.b;
                 // (written out for each of the five: 660 clocks of a loop with divisions each were all that 64 keys have time for)
                 auto wait_for = [&](auto& ring, int full, int empty, uint32_t bytes) {
                     if (!mbar_wait(bar(empty + ring.slot), ring.par ^ 1, &abort_flag, 342)) return false;
@@ -337,14 +337,14 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                 } else {
                     if (lane == 0) ok = wait_for(ropes, At::rope_full, At::rope_empty, boxes * keys * 128);
                     ok = __shfl_sync(0xffffffffu, ok, 0);
-                    if (ok && lane < boxes) tma_load_5d_hint(sRope + ropes.slot * Shape::kRopeB + lane * keys * 128, &tm_r, bar(At::rope_full + ropes.slot), 0, 0, 8, 0, page, policy);
+                    if (ok && lane < boxes) tma_load_5d_hint(sRope + ropes.slot * Shape::kRopeB + lane * keys * 128, &tm_r, bar(At::rope_full + ropes.slot), 0, 0, 8, 0, slab, policy);
                     ropes.next();
 #pragma unroll
                     for (int m = 0; m < 4; ++m) {
                         if (ok && lane == 0) ok = wait_for(units, At::full, At::empty, boxes * keys * 256);
                         ok = __shfl_sync(0xffffffffu, ok, 0);
                         if (ok && lane < boxes)
-                            tma_load_5d_hint(sUnits + units.slot * Shape::kUnitB + lane * keys * 256, &tm, bar(At::full + units.slot), 0, 0, 2 * m, 0, page, policy);
+                            tma_load_5d_hint(sUnits + units.slot * Shape::kUnitB + lane * keys * 256, &tm, bar(At::full + units.slot), 0, 0, 2 * m, 0, slab, policy);
                         units.next();
                     }
                 }
@@ -796,9 +796,9 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
     auto lookup = [&](const LatentSegment& seg, int key) {
         if (!p.block_table || key >= seg.len) return -1;
         const int* table = p.block_table + (long long)seg.b * p.table_stride;
-        const int page = small ? (lane < 64 / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
-        return (unsigned)page < (unsigned)p.num_pages ? page : -1;   // (none: zeros)
+        return small ? (lane < 64 / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
     };
+    auto there = [&](int page) { return (unsigned)page < (unsigned)p.num_pages ? page : -1; };   // (none: zeros; asked when it is needed, not waited for ahead)
     auto boxes_of = [&](const LatentSegment& seg, int key) { return small ? (max(0, min(seg.len - key, 64)) + ps - 1) / ps : 1; };
     const uint64_t policy = l2_policy_evict_last();   // (the pair reads everything twice, and other blocks of rows again)
 
@@ -823,7 +823,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             int page = lookup(seg, first);
             for (int key0 = first; key0 < end && ok; key0 += kLatPairTile, ++u) {
                 const int next = key0 + kLatPairTile, page_next = next < end ? lookup(seg, next) : -1;
-                const int boxes = boxes_of(seg, key0), row = p.block_table ? key0 % ps : key0, slab = p.block_table ? page : seg.b;
+                const int boxes = boxes_of(seg, key0), row = p.block_table ? key0 % ps : key0, slab = p.block_table ? there(page) : seg.b;
                 const uint32_t both = rank == 0 ? (boxes + boxes_of(seg, key0 + 64)) * bytes : 0;   // (the first CTA expects both's)
 #pragma unroll
                 for (int i = 0; i < 3; ++i) {
@@ -834,7 +834,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                     }
                     if (small) {
                         ok = __shfl_sync(0xffffffffu, ok, 0);
-                        if (ok && lane < boxes) tma_load_5d_pair_hint(sK + i * Shape::kKB + lane * bytes, &tm_k, k_full0 + 8 * i, 0, 0, 3 * i, 0, page, policy);
+                        if (ok && lane < boxes) tma_load_5d_pair_hint(sK + i * Shape::kKB + lane * bytes, &tm_k, k_full0 + 8 * i, 0, 0, 3 * i, 0, slab, policy);
                     }
                 }
                 ok = __shfl_sync(0xffffffffu, ok, 0);
@@ -857,7 +857,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
             int page = lookup(seg, seg.t0 * kLatPairTile);
             for (int key0 = seg.t0 * kLatPairTile; key0 < end && ok; key0 += 64, ++u) {
                 const int next = key0 + 64, page_next = next < end ? lookup(seg, next) : -1;
-                const int boxes = boxes_of(seg, key0), at = u & 1, row = p.block_table ? key0 % ps : key0, slab = p.block_table ? page : seg.b;
+                const int boxes = boxes_of(seg, key0), at = u & 1, row = p.block_table ? key0 % ps : key0, slab = p.block_table ? there(page) : seg.b;
                 if (lane == 0) {
                     ok = u < 2 || mbar_wait(bar(latp::pv + at), ((u >> 1) - 1) & 1, abort_flag, 362);
                     if (ok) mbar_expect_tx(bar(latp::v_full + at), 2 * boxes * bytes);
@@ -867,7 +867,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t dst = sV + at * Shape::kVB + i * (Shape::kVB / 2) + lane * bytes;
-                        if (small) tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, 0, 4 * i + 2 * rank, 0, page, policy);
+                        if (small) tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, 0, 4 * i + 2 * rank, 0, slab, policy);
                         else tma_load_5d_hint(dst, &tm_v, bar(latp::v_full + at), 0, row, 4 * i + 2 * rank, slab, 0, policy);
                     }
                 }
