@@ -183,6 +183,16 @@ struct LatBars {
                          sums = meet + 4, count = sums + 2;   // [2] by warpgroup: an item's sums are there; they have been read
 };
 
+struct LatentRing {
+    uint32_t slot, par, end;
+    __device__ __forceinline__ void next() {
+        if (++slot == end) {
+            slot = 0;
+            par ^= 1;
+        }
+    }
+};
+
 // The largest of a value over a warp.  (A NaN loses.)
 __device__ __forceinline__ float warp_max(float x) {
     float y;
@@ -231,7 +241,7 @@ __device__ __forceinline__ bool lat_meet(uint32_t bar, uint32_t parity, int lane
 // chain is longer than a tile may take, 103 us on 32 sequences of 8192 keys, 64 heads, where a pair, half of its rows empty, takes 80.)
 // grid: as many as run at once.  Warps 0 to 7: softmax and output (a key per thread, half the columns each); 8: segments and the cache; 9: Q;
 // 10: S^T; 11: O^T.
-// tm: boxes of 128 latent elements (whole tiles: block by block of 64; pages of less than a tile: eight keys after eight keys), tm_r: of the rotated part.
+// tm: boxes of 128 latent elements (whole tiles: block by block of 64), or 256 (pages of less than a tile: eight keys after eight keys), tm_r: of the rotated part.
 template <typename T, int N>
 __global__ void __launch_bounds__(LatShape<N>::kThreads, 1)
 fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ CUtensorMap tm_r, const __grid_constant__ CUtensorMap tm_q,
@@ -278,7 +288,11 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 
     const int ps = p.page_size;
     const bool small = p.block_table != nullptr && ps < kLatTile;   // a tile is several pages
-    const uint32_t group = small ? 2048u : 1024u, block = small ? 1024u : 8192u;   // bytes from eight keys of a unit to the next, from 64 elements to the next
+    // Bytes from eight keys of a unit to the next, and from 64 elements to the next.  Two units of small pages are one box and lie in each other:
+    // four blocks of 64 elements after eight keys (64 sequences of 8192 keys in pages of 16: 119 -> 106 us; a box costs 160 ns).
+    const uint32_t group = small ? 4096u : 1024u, block = small ? 1024u : 8192u;
+    const uint32_t ring = small ? Shape::kUnits & ~1u : Shape::kUnits;   // (a box must not go round the end)
+    auto unit_at = [&](uint32_t slot, int m) { return slot * Shape::kUnitB - (small && (m & 1) ? Shape::kUnitB - 2048u : 0u); };
     bool ok = true;
     auto segment = [&](uint32_t ord, LatentSegment& s) {
         if (!pp_warp_wait(bar(At::seg_full + ord % kLatSegs), (ord / kLatSegs) & 1, &abort_flag, 340)) return false;
@@ -289,7 +303,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     if (warp == 8) {
         // ---------------------------------------------------------------- segments and the cache
         const uint64_t policy = p.blocks > 1 ? l2_policy_evict_last() : l2_policy_evict_first();
-        PpRing<Shape::kUnits> units;
+        LatentRing units{0, 0, ring};
         PpRing<Shape::kRopes> ropes;
         for (uint32_t ord = 0; ok; ++ord) {
             const LatentSegment seg = walk.next();
@@ -340,11 +354,13 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     if (ok && lane < boxes) tma_load_5d_hint(sRope + ropes.slot * Shape::kRopeB + lane * keys * 128, &tm_r, bar(At::rope_full + ropes.slot), 0, 0, 8, 0, slab, policy);
                     ropes.next();
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        if (ok && lane == 0) ok = wait_for(units, At::full, At::empty, boxes * keys * 256);
+                    for (int m = 0; m < 4; m += 2) {   // (the first one's barrier is both units')
+                        if (ok && lane == 0)
+                            ok = mbar_wait(bar(At::empty + units.slot + 1), units.par ^ 1, &abort_flag, 342) && wait_for(units, At::full, At::empty, boxes * keys * 512);
                         ok = __shfl_sync(0xffffffffu, ok, 0);
                         if (ok && lane < boxes)
-                            tma_load_5d_hint(sUnits + units.slot * Shape::kUnitB + lane * keys * 256, &tm, bar(At::full + units.slot), 0, 0, 2 * m, 0, slab, policy);
+                            tma_load_5d_hint(sUnits + units.slot * Shape::kUnitB + lane * keys * 512, &tm, bar(At::full + units.slot), 0, 0, 2 * m, 0, slab, policy);
+                        units.next();
                         units.next();
                     }
                 }
@@ -396,7 +412,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             constexpr uint32_t rows_hi = tree_desc_hi(1024);
             const uint32_t u_lo = desc_lo(sUnits, 16), r_lo = desc_lo(sRope, 16), q_lo = desc_lo(sQ, 16);
             uint32_t s = 0;
-            PpRing<Shape::kUnits> units;
+            LatentRing units{0, 0, ring};
             PpRing<Shape::kRopes> ropes;
             for (uint32_t ord = 0; ok; ++ord) {
                 const int slot = ord % kLatSegs;
@@ -417,9 +433,9 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     ropes.next();
 #pragma unroll
                     for (int m = 0; m < 4; ++m, units.next()) {
-                        if (!(ok = mbar_wait(bar(At::full + units.slot), units.par, &abort_flag, 348))) break;
+                        if (!(small && (m & 1)) && !(ok = mbar_wait(bar(At::full + units.slot), units.par, &abort_flag, 348))) break;
                         tc_fence_after();
-                        const uint32_t a = u_lo + units.slot * (Shape::kUnitB >> 4);
+                        const uint32_t a = u_lo + (unit_at(units.slot, m) >> 4);
 #pragma unroll
                         for (int ks = 0; ks < 8; ++ks)
                             tree_mma_ss(d, a + (ks >> 2) * (block >> 4) + (ks & 3) * 2, a_hi, q_lo + (((2 * m + (ks >> 2)) * N * 128) >> 4) + (ks & 3) * 2, rows_hi, idesc, 1u);
@@ -440,7 +456,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
             const uint32_t a_hi = tree_desc_hi(group);
             const uint32_t u_lo = desc_lo(sUnits, block), p_lo = desc_lo(sP, 16);
             uint32_t s = 0;
-            PpRing<Shape::kUnits> units;
+            LatentRing units{0, 0, ring};
             for (uint32_t ord = 0; ok; ++ord) {
                 const int slot = ord % kLatSegs;
                 if (!(ok = mbar_wait(bar(At::seg_full + slot), (ord / kLatSegs) & 1, &abort_flag, 350))) break;
@@ -453,7 +469,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     tc_fence_after();
 #pragma unroll
                     for (int m = 0; m < 4; ++m, units.next()) {
-                        const uint32_t a = u_lo + units.slot * (Shape::kUnitB >> 4);
+                        const uint32_t a = u_lo + (unit_at(units.slot, m) >> 4);
 #pragma unroll
                         for (int ks = 0; ks < kLatTile / 16; ++ks)
                             tree_mma_ss(tmem_o + m * N, a + ks * (2 * group >> 4), a_hi, p_lo + (((s & 1) * Shape::kPB + ks * 16 * 2 * N) >> 4), Shape::kPHi, idesc, j > 0 || ks > 0 ? 1u : 0u);
@@ -505,7 +521,7 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
                     const int valid = seg.len - key0;
                     for (int i = tid; i < (kLatTile - valid) * (kLatDim / 8); i += 256) {
                         const int x = valid + i / (kLatDim / 8), piece = i % (kLatDim / 8);
-                        const uint32_t unit = sUnits + (4 * s + (piece >> 4)) % Shape::kUnits * Shape::kUnitB;
+                        const uint32_t unit = sUnits + unit_at((4 * s + (piece >> 4)) % ring, piece >> 4);
                         const uint32_t at = unit + (uint32_t)(x >> 3) * group + (piece >> 3 & 1) * block + (uint32_t)(x & 7) * 128u + ((piece & 7) << 4);   // (swizzled or not)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0u) : "memory");
                     }

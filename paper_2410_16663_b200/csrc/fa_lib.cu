@@ -1645,8 +1645,8 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
     CUtensorMap tm[4];
     const bool pairs = lb.pairs(), paged_small = p.block_table && p.page_size < fa::kLatTile;
     for (int i = 0; i < 2 && !rc; ++i) {
-        // of 64 keys -- one CTA: 128 elements, and the rotated 64; a pair: 192 elements as keys, 128 as values
-        const cuuint32_t wide = pairs ? (i ? 2 : 3) : (i ? 1 : 2), keys = 64;
+        // of 64 keys -- one CTA: 128 elements (256 of small pages), and the rotated 64; a pair: 192 elements as keys, 128 as values
+        const cuuint32_t wide = pairs ? (i ? 2 : 3) : i ? 1 : paged_small ? 4 : 2, keys = 64;
         if (paged_small)
             rc = encode_tiled<5>(&tm[i], type16(bf16), p.cache, {64, 8, blocks, slab_rows / 8, slabs}, {row, 128, 8 * row, slab_rows * row},
                                  {64, 8, wide, (cuuint32_t)slab_rows / 8, 1});
