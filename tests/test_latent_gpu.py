@@ -184,6 +184,13 @@ def test_absorbed_one_long_sequence(H):
     absorbed([30011], 1, H, "fp16", page=64)
 
 
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("T, H", [(1, 16), (1, 32), (2, 20), (3, 40)])
+def test_absorbed_long_runs_of_small_pages(T, H, page):
+    """Several tiles of a sequence for every worker, so that the buffers of small pages go round more than once."""
+    absorbed([30011, 20000, 17], T, H, "fp16", page=page)
+
+
 def test_absorbed_many_short_sequences():
     """More sequences than CTAs, several of them without keys; runs of many items."""
     rng = random.Random(3)
