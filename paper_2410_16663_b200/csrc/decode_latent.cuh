@@ -727,7 +727,7 @@ struct LatPairStatic {
     uint32_t abort_flag;
     float x[2][4][64];   // by meeting, (half of the keys, warpgroup), row: maxima; at an item's end the sums
 };
-constexpr int kPairStaticBytes = 3072;
+constexpr int kPairStaticBytes = 3 * 1024;
 static_assert(sizeof(LatPairStatic) <= kPairStaticBytes && LatPairShape::kSmem + kPairStaticBytes <= 232448, "shared memory");
 
 __device__ __forceinline__ void pair_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate) {
@@ -932,7 +932,7 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
         // ---------------------------------------------------------------- S = Q C^T
         if (elect_one()) {
             constexpr uint32_t idesc = instr_desc_f16(kBf16, 128, kLatPairTile, false, false);
-            const uint32_t group = small ? 3072u : 1024u, block = small ? 1024u : 8192u;
+            const uint32_t group = small ? 3u * 1024u : 1024u, block = small ? 1024u : 8192u;
             const uint32_t k_hi = tree_desc_hi(group);
             constexpr uint32_t q_hi = tree_desc_hi(1024);
             const uint32_t k_lo = desc_lo(sK, 16), q_lo = desc_lo(sQ, 16);
