@@ -396,8 +396,9 @@ int fa_pages_fork(void* k, void* v, int* block_table, int* held, int* seqlens_k,
  *   out may be x with its strides, and shares no memory with it otherwise.  positions int32 [n] on the DEVICE.  The arithmetic is in 32 bits, the
  *   results are rounded once.
  *   d a multiple of 16 up to 1024, rot_dim a multiple of 16 up to min(d, 512), rot_offset a multiple of 8 with rot_offset + rot_dim <= d.
- * Errors: FA_ERR_SHAPE (negative sizes, rotated columns outside the head, strides that are negative, not multiples of 8, or of out below d), FA_ERR_UNSUPPORTED (those
- * sizes, dtype, a factor that is not finite), FA_ERR_NULL, FA_ERR_ALIGN (x and out 16 bytes, turns 8).
+ * Errors: FA_ERR_SHAPE (negative sizes, rotated columns outside the head, strides that are negative or not multiples of 8, an out that lies over itself:
+ * the shorter of its strides below d, or the longer one ending before the last step of the shorter), FA_ERR_UNSUPPORTED (those sizes, dtype,
+ * a factor that is not finite), FA_ERR_NULL, FA_ERR_ALIGN (x and out 16 bytes, turns 8).
  */
 int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turns, int n, int H, int d, int rot_dim, int rot_offset,
             int interleaved, float factor, int64_t x_token_stride, int64_t x_head_stride, int64_t out_token_stride,
@@ -418,8 +419,8 @@ int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turn
  *   counts int32 [B] (NULL: all): only the first counts[b] tokens of sequence b are written.  Rows outside the cache, and pages outside
  *   [0, num_pages), are passed over.  Tokens behind the last sequence (cu_seqlens[B] < n) are nobody's: nothing of theirs is written.  No two tokens may have one row.
  *   d, dv multiples of 16 up to 1024; rotation as for fa_rope; caches and their strides in whole 16 bytes.  Outputs share no memory with the inputs otherwise.
- * Errors: as fa_rope; FA_ERR_SHAPE also for n != B * T, table_stride < max_pages, strides of a cache below a row's elements; FA_ERR_UNSUPPORTED for a k_scale or v_scale that is not positive and finite, or
- * whose reciprocal is not finite.
+ * Errors: as fa_rope; FA_ERR_SHAPE also for n != B * T, table_stride < max_pages, a cache that lies over itself (as an out of fa_rope: slabs and rows of them, a row's
+ * elements each); FA_ERR_UNSUPPORTED for a k_scale or v_scale that is not positive and finite, or whose reciprocal is not finite.
  */
 typedef struct fa_append_params {
     const void* q;

@@ -1403,8 +1403,14 @@ bool finite_positive(float x) { return x > 0.f && !isinf(x) && !isinf(1.f / x); 
 // Strides of [tokens, heads, width] in elements.
 bool token_strides_ok(const int64_t s[2]) { return s[0] >= 0 && s[1] >= 0 && !(s[0] & 7) && !(s[1] & 7) && s[0] < (1ll << 38) && s[1] < (1ll << 38); }
 
-// What is written may not lie over itself: strides of a and b steps each pass over width elements.
-bool apart(const int64_t s[2], int a, int b, long long width) { return (a <= 1 || s[0] >= width) && (b <= 1 || s[1] >= width); }
+// What is written may not lie over itself: a and b steps by the strides, each over width elements.  The longer stride passes over all that the steps of
+// the shorter one reach (by division: the product may pass 64 bits).
+bool apart(const int64_t s[2], int a, int b, long long width) {
+    if (a <= 1 || b <= 1) return (a <= 1 || s[0] >= width) && (b <= 1 || s[1] >= width);
+    const bool second = s[1] <= s[0];
+    const int64_t inner = second ? s[1] : s[0], outer = second ? s[0] : s[1];
+    return inner >= width && (outer - width) / inner >= (second ? b : a) - 1;
+}
 
 // What a rotation asks of its sizes.
 int check_rotation(int d, int rot, int offset, float factor) {
@@ -1448,8 +1454,9 @@ int fa_rope(const void* x, void* out, const int* positions, const uint64_t* turn
     if (int rc = check_rotation(d, rot_dim, rot_offset, factor)) return rc;
     if (dtype != FA_DTYPE_FP16 && dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
     const int64_t xs[2] = {x_token_stride, x_head_stride}, os[2] = {out_token_stride, out_head_stride};
-    if (!token_strides_ok(xs) || !token_strides_ok(os) || !apart(os, n, H, d)) return FA_ERR_SHAPE;
+    if (!token_strides_ok(xs) || !token_strides_ok(os)) return FA_ERR_SHAPE;
     if ((long long)H * d > (1 << 24)) return FA_ERR_UNSUPPORTED;
+    if (!apart(os, n, H, d)) return FA_ERR_SHAPE;
     if (n == 0) return FA_OK;
     if (!x || !out || !positions || (rot_dim > 0 && !turns)) return FA_ERR_NULL;
     if (!aligned16(x) || !aligned16(out) || (reinterpret_cast<uintptr_t>(turns) & 7u) || (reinterpret_cast<uintptr_t>(positions) & 3u))

@@ -124,3 +124,23 @@ def test_outputs_that_lie_over_themselves_are_refused(change, code):
 def test_rope_outputs_that_lie_over_themselves_are_refused():
     for change in (dict(ot=0), dict(oh=0), dict(oh=8)):
         assert fa.lib.fa_rope(*rope_args(**change), None) == fa.FA_ERR_SHAPE
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(q_out_stride=(128, 128)), fa.FA_ERR_SHAPE), (dict(q_out_stride=(504, 128)), fa.FA_ERR_SHAPE), (dict(q_out_stride=(128, 504)), fa.FA_ERR_SHAPE),
+    (dict(k_cache_stride=(256, 256)), fa.FA_ERR_SHAPE), (dict(v_cache_stride=(256, 256)), fa.FA_ERR_SHAPE), (dict(k_cache_stride=(64 * 256 - 8, 256)), fa.FA_ERR_SHAPE),
+    (dict(v_cache_stride=(256, 504)), fa.FA_ERR_SHAPE), (dict(k_cache_stride=(1 << 41, 1 << 41)), fa.FA_ERR_SHAPE),
+    (dict(block_table=A, num_pages=1 << 30, page_size=1 << 20, max_pages=4, table_stride=4, k_cache_stride=(1 << 41, 1 << 40)), fa.FA_ERR_SHAPE),
+    (dict(k=0, q_out_stride=(512, 128)), fa.FA_ERR_NULL), (dict(k=0, q_out_stride=(128, 512)), fa.FA_ERR_NULL), (dict(k=0, q_out_stride=(576, 144)), fa.FA_ERR_NULL),
+    (dict(k=0, k_cache_stride=(256, 512), v_cache_stride=(256, 1024)), fa.FA_ERR_NULL), (dict(k=0, v_cache_stride=(63 * 1152 + 256, 1152)), fa.FA_ERR_NULL),
+    (dict(k=0, n=1, B=1, T=1, q_out_stride=(0, 128), k_cache_stride=(0, 256)), fa.FA_ERR_NULL)])
+def test_outputs_that_lie_over_themselves_by_both_strides_are_refused(change, code):
+    """Each stride is wide enough, but steps of the one end where steps of the other do.  (What is open gets as far as the missing k.)"""
+    assert fa.lib.fa_cache_append(ctypes.byref(append_params(**change)), None) == code
+
+
+def test_rope_outputs_that_lie_over_themselves_by_both_strides_are_refused():
+    for change in (dict(ot=128, oh=128), dict(ot=248, oh=128), dict(ot=128, oh=504)):
+        assert fa.lib.fa_rope(*rope_args(**change), None) == fa.FA_ERR_SHAPE
+    for change in (dict(ot=128, oh=512), dict(ot=256, oh=128), dict(n=1, ot=0), dict(H=1, oh=0, ot=128), dict(xt=128, xh=128), dict(xt=0, xh=0)):
+        assert fa.lib.fa_rope(*rope_args(**{**change, "x": 0}), None) == fa.FA_ERR_NULL
