@@ -490,7 +490,7 @@ int fa_forward_latent(const fa_latent_params* p, void* stream);
  *   included, clamped to [0, Skv_max].  All of dtype.  Rows past a sequence's end may hold anything; inside it rows must be finite for
  *   the tokens that do not see them, too.  A token that sees no key gives o = 0 and lse = -inf.  d must be 512 and d_rope 64.
  *   workspace: fa_decode_latent_workspace_bytes(B, T, H, Skv_max or max_pages * page_size, d) bytes, 16-byte aligned.
- * Errors: as fa_decode_ex.
+ * Errors: as fa_decode_ex; FA_ERR_UNSUPPORTED also for a capacity (Skv_max, or max_pages * page_size) above 2^31 - 257 keys.
  */
 typedef struct fa_latent_decode_params {
     const void* q;

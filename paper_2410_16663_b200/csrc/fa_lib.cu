@@ -1609,6 +1609,7 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
     }
     if (p.B < 0 || p.H <= 0 || Skv_max < 0 || p.d <= 0 || p.d_rope <= 0 || p.T < 1) return FA_ERR_SHAPE;
     if (p.T > 64 || p.T > Skv_max) return FA_ERR_UNSUPPORTED;   // the tokens are the LAST rows of the cache
+    if (Skv_max > 0x7fffffff - 2 * fa::kLatPairTile) return FA_ERR_UNSUPPORTED;   // (keys are counted in 32 bits, up to the end of a tile and half of one more)
     if (p.d != fa::kLatDim || p.d_rope != fa::kLatRope) return FA_ERR_UNSUPPORTED;
     if (p.dtype != FA_DTYPE_FP16 && p.dtype != FA_DTYPE_BF16) return FA_ERR_UNSUPPORTED;
     if (!(p.scale >= 0.f) || isinf(p.scale)) return FA_ERR_UNSUPPORTED;

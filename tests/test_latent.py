@@ -98,3 +98,12 @@ def test_the_decode_binding_refuses_what_the_library_cannot_see():
                    dict(block_table=torch.zeros(2, 4))):
         with pytest.raises(ValueError):
             fa.fa_decode_latent(**{**ok, **change})
+
+
+@pytest.mark.parametrize("change, code", [
+    (dict(PAGED, max_pages=(1 << 27) - 1, table_stride=1 << 27), fa.FA_ERR_UNSUPPORTED), (dict(Skv_max=0x7fffffff), fa.FA_ERR_UNSUPPORTED),
+    (dict(H=128, Skv_max=0x7fffffff - 255), fa.FA_ERR_UNSUPPORTED), (dict(Skv_max=0x7fffffff - 256, q=0), fa.FA_ERR_NULL),
+    (dict(PAGED, max_pages=(1 << 27) - 17, table_stride=1 << 27, q=0), fa.FA_ERR_NULL)], ids=str)
+def test_a_capacity_whose_end_passes_32_bits_is_refused(change, code):
+    """The position behind the last tile's last key, and half a tile beyond it, are formed in 32 bits.  (What is open gets as far as the missing q.)"""
+    assert fa.lib.fa_decode_latent(ctypes.byref(decode_params(**change)), None) == code
