@@ -1561,7 +1561,8 @@ struct LatentBlocks {
         rows = (int)((all + blocks - 1) / blocks);
     }
     bool pairs() const { return rows > 32 || blocks > 1; }
-    size_t slots() const { return 2 * (size_t)fa::kTreeMaxSms; }   // partial results that a call may have: two for each worker
+    int workers() const { return fa::kTreeMaxSms / (pairs() ? 2 : 1); }   // at most: CTAs, or pairs of them
+    size_t slots() const { return 2 * (size_t)workers(); }                // partial results that a call may have
 };
 
 // N: the kernel of one CTA with so many columns; 0: that of pairs.
@@ -1574,7 +1575,7 @@ int latent_launch(const CUtensorMap (&tm)[4], fa::LatentParams& lp, int sms, cud
     int sm_count = 0;
     if (int ce = fa::prepare_big_smem_kernel(reinterpret_cast<const void*>(kern), smem, &sm_count)) return cuda_fail(static_cast<cudaError_t>(ce));
     const int ctas = N > 0 ? 1 : 2, most = sms / ctas;
-    lp.workers = most < fa::kTreeMaxSms ? most : fa::kTreeMaxSms;
+    lp.workers = most < fa::kTreeMaxSms / ctas ? most : fa::kTreeMaxSms / ctas;
     lp.by_item = (long long)lp.B * lp.blocks < lp.workers ? 1 : 0;
     cudaError_t e = fa::launch_dependent_clusters(kern, dim3(lp.workers * ctas), ctas, 1, threads, smem, st, tm[0], tm[1], tm[2], tm[3], lp);
     // (an item of one tile is nobody's but one worker's)
@@ -1595,8 +1596,12 @@ extern "C" {
 
 size_t fa_decode_latent_workspace_bytes(int B, int T, int H, int Skv_max, int d) {
     if (B <= 0 || T <= 0 || T > 64 || H <= 0 || H > 65535 || Skv_max <= 0 || d != fa::kLatDim) return 0;
-    const LatentBlocks lb(T, H);
-    return 32 + lb.slots() * lb.rows * ((size_t)fa::kLatDim + 1) * sizeof(float) + fa::kTreeMaxSms * sizeof(int4);
+    // Never less for more tokens, heads or keys, so that a workspace for the most of a program's steps does for all; an item of one tile has no partial results.
+    const LatentBlocks lb(T, H), one_cta(1, 32);
+    const size_t full = (size_t)T * H < 128 ? (size_t)T * H : 128, least = one_cta.slots() * one_cta.rows;
+    size_t rows = Skv_max > fa::kLatTile ? lb.slots() * full : 0;
+    if (rows > 0 && lb.pairs() && rows < least) rows = least;
+    return 32 + rows * ((size_t)fa::kLatDim + 1) * sizeof(float) + fa::kTreeMaxSms * sizeof(int4);
 }
 
 int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {

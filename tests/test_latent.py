@@ -107,3 +107,18 @@ def test_the_decode_binding_refuses_what_the_library_cannot_see():
 def test_a_capacity_whose_end_passes_32_bits_is_refused(change, code):
     """The position behind the last tile's last key, and half a tile beyond it, are formed in 32 bits.  (What is open gets as far as the missing q.)"""
     assert fa.lib.fa_decode_latent(ctypes.byref(decode_params(**change)), None) == code
+
+
+def test_decode_workspace_holds_what_a_call_can_use():
+    """Two partial results for each worker at most -- a CTA (up to 32 rows) or a pair of them (of up to 128 rows), of 160 SMs -- of 512 + 1 floats a row; a cache of
+    one tile has none.  And a workspace for the most tokens, heads and keys does for fewer."""
+    size = fa.fa_decode_latent_workspace_bytes
+    rest = 32 + 160 * 16
+    for B, T, H, slots, rows in ((1, 1, 128, 160, 128), (64, 1, 128, 160, 128), (2, 64, 128, 160, 128), (4, 1, 100, 160, 100), (4, 1, 16, 320, 16), (4, 2, 16, 320, 32)):
+        assert size(B, T, H, 10000) <= slots * rows * 513 * 4 + rest, (B, T, H)
+        assert size(B, T, H, 64) <= rest
+    for H in (1, 5, 16, 20, 33, 43, 64, 128):
+        for most in (64, 65, 100, 128, 129, 10000):
+            sizes = [size(3, T, H, most) for T in range(1, 65)]
+            assert sizes == sorted(sizes), (H, most)
+            assert size(3, 2, H, most) <= size(3, 2, H + 1, most) and size(3, 2, H, most) <= size(3, 2, H, most + 1)
