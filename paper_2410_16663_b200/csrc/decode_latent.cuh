@@ -168,7 +168,7 @@ struct LatShape {
     static constexpr int kThreads = 384;
     static constexpr int kTmemCols = N == 16 ? 128 : 256;           // two score buffers, four parts of the output
     static constexpr int kCols = N / 2;                             // columns of a softmax thread
-    static_assert((2 + 4) * N <= kTmemCols && kSmem <= 229 * 1024, "tensor and shared memory");
+    static_assert((2 + 4) * N <= kTmemCols, "tensor memory");
     // P^T [64 keys][N rows]: a key's row of 2 N bytes, swizzled in 32 or 64 bytes
     static constexpr uint32_t kPHi = ((8u * 2 * N) >> 4) | (1u << 14) | ((N == 16 ? 6u : 4u) << 29);
 };
@@ -258,6 +258,8 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
     __shared__ __align__(16) float s_max[2][4][N];   // by step, quarter of the keys, column; of the sums at an item's end, too
     __shared__ uint32_t tmem_holder;
     __shared__ volatile uint32_t abort_flag;
+    // (a CTA's 227 KiB hold these as well, with 16 bytes for what lies between them)
+    static_assert(Shape::kSmem + sizeof(bars) + sizeof(segs) + sizeof(s_max) + sizeof(tmem_holder) + sizeof(abort_flag) + 16 <= 232448, "shared memory");
 
     const int tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
