@@ -1431,7 +1431,7 @@ int rope_launch(fa::RopeParams& rp, bool bf16, bool f8, cudaStream_t st) {
         const int room = 4 * sms / rp.n > 0 ? 4 * sms / rp.n : 1;
         if (split > room) split = room;
     } else {
-        while (2 * rp.tokens <= 4 && 2 * rp.tokens * half <= fa::kRopeMostAngles && (long long)rp.n >= 8ll * sms * rp.tokens) rp.tokens *= 2;
+        while (2 * rp.tokens <= fa::kRopeMostTokens && 2 * rp.tokens * half <= fa::kRopeMostAngles && (long long)rp.n >= 8ll * sms * rp.tokens) rp.tokens *= 2;
     }
     rp.by_units.set(rp.units);
     using Kernel = void (*)(fa::RopeParams);

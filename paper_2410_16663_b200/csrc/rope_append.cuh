@@ -21,7 +21,7 @@
 namespace fa {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeMostTokens = 8;      // of a CTA: a warp each
+constexpr int kRopeMostTokens = 4;      // of a CTA: a warp each
 constexpr int kRopeMostAngles = 512;    // of a CTA: tokens times frequencies
 constexpr long long kRopeNobodys = -2;  // a token before the first sequence or behind the last: its q_out stays as it was, too
 
