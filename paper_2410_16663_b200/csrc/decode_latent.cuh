@@ -1122,6 +1122,10 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
                 }
                 const int valid = seg.len - key0;
                 if (valid < kLatPairTile) {   // values of keys that are none may be anything, NaN too: they become zeros
+                    // (First the products of the step before, of both halves: a warp has waited for one alone.  While the other half's values of that step are on
+                    // their way, their barrier's last phase is of the step before it, whose parity is this step's: the wait would pass at once, and
+                    // clear values that are still to be read, or have this step's arrive after the clearing.)
+                    if (s > 0 && !(ok = wait(latp::pv + (half ^ 1), (s - 1) & 1, 387))) break;
                     if (!(ok = wait(latp::v_full, s & 1, 385)) || !(ok = wait(latp::v_full + 1, s & 1, 383))) break;
                     const uint32_t vgroup = small ? 2048u : 1024u, vblock = small ? 1024u : 8192u;
                     for (int i = tid; i < (kLatPairTile - valid) * 32; i += 256) {

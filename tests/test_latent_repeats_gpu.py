@@ -1,0 +1,30 @@
+"""Attention over latent vectors, called again and again: values of keys that are none are cleared in shared memory while products and loads of other steps are
+under way, and none of those may take any harm."""
+import random
+
+import pytest
+import torch
+
+from paper_2410_16663_b200 import binding as fa
+from tests.test_latent_gpu import SCALE, absorbed, ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("B, lo, hi, T, H, page", [
+    (1, 1000, 1000, 1, 16, 64), (64, 2980, 3000, 1, 16, 0), (64, 100, 3000, 1, 32, 16), (3, 4000, 5000, 1, 32, 32),        # one CTA
+    (20, 2000, 2000, 1, 128, 0), (20, 1980, 2000, 1, 64, 64), (32, 500, 4000, 1, 128, 0), (90, 486, 500, 2, 100, 16),      # pairs
+    (74, 129, 400, 1, 40, 0), (150, 65, 260, 3, 30, 64), (7, 500, 9000, 3, 20, 64)])
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+def test_the_same_call_gives_the_same_bits(B, lo, hi, T, H, page, dt):
+    """All rows behind a sequence's end are NaN; every fourth sequence is held against the definition."""
+    rng = random.Random(B)
+    lens = [rng.randint(lo, hi) for _ in range(B)]
+    q, r, cache, table, ws, o, lse, _ = absorbed(lens, T, H, dt, page=page, samples=range(0, B, 4) if B < 40 else range(0, B, 16))
+    now = ints(lens)
+    for _ in range(12):
+        o2, lse2 = torch.full_like(o, float("nan")), torch.full_like(lse, float("nan"))
+        ws.fill_(255)
+        fa.fa_decode_latent(q, r, cache, o2, lse2, now, SCALE, ws, block_table=table)
+        assert torch.equal(o2, o) and torch.equal(lse2, lse)
+    assert fa.fa_device_status()[0] == 0
