@@ -817,7 +817,9 @@ fa_decode_latent_pair_kernel(const __grid_constant__ CUtensorMap tm_k, const __g
         return small ? (lane < 64 / ps && key + lane * ps < seg.len ? table[(key + lane * ps) / ps] : -1) : table[key / ps];
     };
     auto there = [&](int page) { return (unsigned)page < (unsigned)p.num_pages ? page : -1; };   // (none: zeros; asked when it is needed, not waited for ahead)
-    auto boxes_of = [&](const LatentSegment& seg, int key) { return small ? (max(0, min(seg.len - key, 64)) + ps - 1) / ps : 1; };
+    // One at least, of zeros where the half has no keys: the first CTA's barrier takes part of its bytes from the other, which so has to have seen a tile's
+    // boxes go back before the next tile is there.  (Without, two tiles could go back before it looked, and it waited for good.)
+    auto boxes_of = [&](const LatentSegment& seg, int key) { return small ? max(1, (min(seg.len - key, 64) + ps - 1) / ps) : 1; };
     const uint64_t policy = l2_policy_evict_last();   // (the pair reads everything twice, and other blocks of rows again)
 
     if (warp == 8) {
