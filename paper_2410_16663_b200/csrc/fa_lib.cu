@@ -1638,9 +1638,10 @@ int fa_decode_latent(const fa_latent_decode_params* pp, void* stream) {
     lp.lse = p.lse;
     lp.seqlens = p.seqlens_k;
     lp.block_table = p.block_table;
-    lp.o_part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(p.workspace) + 31) & ~(uintptr_t)31);
+    // The list of merges comes first: where there are no partial results, it is all that the workspace has room for.
+    lp.merges = reinterpret_cast<int4*>((reinterpret_cast<uintptr_t>(p.workspace) + 31) & ~(uintptr_t)31);
+    lp.o_part = reinterpret_cast<float*>(lp.merges + fa::kTreeMaxSms);
     lp.lse_part = lp.o_part + lb.slots() * lb.rows * fa::kLatDim;
-    lp.merges = reinterpret_cast<int4*>(lp.lse_part + lb.slots() * lb.rows);   // (slots is a multiple of four)
     lp.q_sb = p.q_stride[0]; lp.q_st = p.q_stride[1]; lp.q_sh = p.q_stride[2];
     lp.r_sb = p.q_rope_stride[0]; lp.r_st = p.q_rope_stride[1]; lp.r_sh = p.q_rope_stride[2];
     lp.B = p.B; lp.T = p.T; lp.H = p.H; lp.Smax = Skv_max;
