@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2410_16663_b200 import binding as fa
-from tests.test_latent_gpu import SCALE, absorbed, ints
+from tests.test_latent_gpu import SCALE, absorbed, expanded, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +43,14 @@ def test_halves_of_tiles_without_keys(T, H, page):
         fa.fa_decode_latent(q, r, cache, o2, lse2, now, SCALE, ws, block_table=table)
         assert torch.equal(o2, o) and torch.equal(lse2, lse)
     assert fa.fa_device_status()[0] == 0
+
+
+@pytest.mark.parametrize("dt", ["fp16", "bf16"])
+@pytest.mark.parametrize("nq, nk, H", [([2000, 1, 700, 129, 64, 1500], [2000, 300, 700, 900, 64, 1777], 16), ([60] * 40, [60 + 7 * i for i in range(40)], 5)])
+def test_the_same_prompts_give_the_same_bits(nq, nk, H, dt):
+    q, kv, both, o, lse = expanded(nq, nk, H, dt, True, heads=[0])
+    cq, ck = ([sum(x[:i]) for i in range(len(x) + 1)] for x in (nq, nk))
+    for _ in range(12):
+        o2, lse2 = torch.full_like(o, float("nan")), torch.full_like(lse, float("nan"))
+        fa.fa_forward_latent(q[..., :128], q[..., 128:], kv[..., :128], both[:, 512:], kv[..., 128:], o2, lse2, ints(cq), ints(ck), max(nq), max(nk), True, SCALE)
+        assert torch.equal(o2, o) and torch.equal(lse2, lse)
