@@ -1581,8 +1581,12 @@ int latent_launch(const CUtensorMap (&tm)[4], fa::LatentParams& lp, int sms, cud
     // (an item of one tile is nobody's but one worker's)
     if (e == cudaSuccess && lp.workers > 1 && lp.Smax > (N > 0 ? fa::kLatTile : fa::kLatPairTile)) {
         const int y = lp.by_item ? lp.B * lp.blocks : lp.workers - 1;
-        // parts of an item, on average (one sequence of 8000 keys, 16 heads: 23.5 -> 14.8 us; 32 of 8192 with 128 heads, three parts each: 90 -> 110)
-        const bool many = lp.workers >= 8ll * lp.B * lp.blocks;
+        // A block for each row pays where an item has many parts and the blocks are few.  Two rows at a time / a row to a block, us of a call:
+        //   16 rows, 2000 keys, by parts of an item: 74 13.9 / 11.4, 25 15.0 / 13.0, 16 13.9 / 13.6, 12 14.3 / 14.6, 8 16.3 / 16.7;
+        //   6000 keys, by rows and blocks: 32 rows 288 22.7 / 22.6, 384 27.7 / 29.7; 64 rows 256 18.8 / 18.0, 320 19.9 / 21.1; 100 rows 200 21.1 / 18.4, 300 19.3 / 20.1;
+        //   128 rows, 16000 keys: 256 24.5 / 22.7, 384 26.6 / 27.4, 1152 51.5 / 58.1.
+        const long long items = (long long)lp.B * lp.blocks;
+        const bool many = lp.workers >= 14 * items && lp.rows * items <= 2ll * sms;
         const int pairs_of_rows = (lp.rows + 1) / 2, room = fa::kLatCombinePerSm * sms / y;
         e = many ? fa::launch_dependent(fa::fa_decode_latent_combine_many_kernel<T>, dim3(lp.rows, y), fa::kLatCombineManyThreads, 0, st, lp)
                  : fa::launch_dependent(fa::fa_decode_latent_combine_kernel<T>, dim3(pairs_of_rows < room ? pairs_of_rows : room > 0 ? room : 1, y), fa::kLatCombineThreads, 0, st, lp);
