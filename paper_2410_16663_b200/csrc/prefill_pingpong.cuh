@@ -60,8 +60,8 @@ static_assert((kPpQBufs + kPpNK + kPpNV) * kTileBytes + 3072 <= 232448, "shared 
 // Keys with a part that all heads share (DR = 64; latent attention's expanded form, D = 128 and 16-bit operands, packed batches): S gets
 // four more MMAs from a third box of Q and of K, whose map has one head.  224 KiB then hold one Q buffer, two V slots and seven K boxes, each
 // of which goes back when its own four MMAs are done: a K tile needs as long to arrive as a step takes, and two whole slots of three boxes would leave it
-// less.  (8192 x 32 heads causal fp16: 546 to 606 us by the clock, 1.13 to 1.26 PFLOP/s, where d = 128 alone takes 505 of the same batch form, 1.09; nine prompts
-// of 60 to 1500 tokens, 16 heads, 67 to 79, 0.68 to 0.80 and 0.74.  Two Q buffers and four K boxes instead: level on short items, 10 % behind from a thousand tokens on.)
+// less.  (8192 x 32 heads causal fp16: 520 to 650 us by the clock that the power cap leaves, 1.06 to 1.32 PFLOP/s, where d = 128 alone takes 505 of the same batch form, 1.09; nine
+// prompts of 60 to 1500 tokens, 16 heads, 67 to 81, 0.66 to 0.80 and 0.74.  Two Q buffers and four K boxes instead: level on short items, 10 % behind from a thousand tokens on.)
 template <bool kF8, int D = 128, int DR = 0>
 struct PpOperands {
     static_assert(D == 128 || (D == 64 && !kF8), "head dimension 128, or 64 with 16-bit operands");

@@ -9,7 +9,7 @@
 // head rotated against each other those are the vectors that belong together.
 //
 // HBM bounds many tokens: 16384 of 40 heads of 128 (bf16) 56 us, 6.0 TB/s of the 6.5 of a copy; into caches, where a row's pieces are written far apart, 8000
-// tokens of 32/8 heads 34.7 us (5.7), latent rows with 128 query heads 71 (5.5), 8-bit caches 35 (5.1).  Few tokens are latency: 2.2 us for one of 40 heads, 7.5 for
+// tokens of 32/8 heads 34.7 us (5.7), into 8-bit caches 35 (5.1); 11114 tokens' latent rows with 128 query heads 71 (5.5).  Few tokens are latency: 2.2 us for one of 40 heads, 7.5 for
 // 768 tokens of 256 sequences into an 8-bit cache, whose look-ups (sequence, row, page, angle) are a chain; the first pieces are on their way meanwhile
 // (8.9 -> 7.8 us, and 57 -> 60 for plain rotations, which have no look-ups and too few registers for it: they load in the loop).  Everything loaded one round
 // ahead took 60 instead of 56 us: what is in flight is there by occupancy, six CTAs to an SM, five with look-ups.
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kRopeThreads, kAppend ? 5 : 6) fa_rope_append_
                 }
             }
         }
-        if (f8) {
+        if (f8) {   // (by the factor's reciprocal: a division rounded as IEEE's is 14 % slower, 8000 tokens 35.2 -> 39.9 us, and no nearer to 64 bits)
             const float inv = now.part == 1 ? p.k_inv : p.v_inv;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
