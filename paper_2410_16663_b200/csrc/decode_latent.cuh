@@ -690,13 +690,13 @@ fa_decode_latent_kernel(const __grid_constant__ CUtensorMap tm, const __grid_con
 // columns of output in 256 of its 512 columns, scores of 128 keys in 64 -- one CTA's tensor memory would be full with the output
 // of 128 rows.  The second operand's columns come half from each CTA: keys for the scores (each CTA loads all 576 elements of 64 keys of a
 // tile), latent elements for the output (each loads 256 elements of all 128 keys): 1.9 times the tile over L2, once from HBM.
-// A tile of 128 keys takes 3600 clocks, at 1.25 GHz as at 1.66 (the slowest pair of 74; the median 3520, the quickest 2800): 2200 for the products (36 of 32 clocks, 16 of 65), 3060 for what the operands, the loads and P take of shared
-// memory's 128 bytes a clock, and the rings, which hold a tile of keys in thirds and one of values in halves beside Q's 72 KiB, refill while they are read.
-// 32 sequences of 8192 keys, 128 heads: 86 us at 1.66 GHz, 102 at the 1.35 that the power cap leaves calls without a pause (850 to 715 TFLOP/s; floor 48), 64 of them 156
-// at 1.5, 192 at 1.25.  On the way (us, the first of these): 132; without
-// releases at cluster scope and with Q by tensor maps 98, with tiles of 64 keys; thirds and halves of 128-key tiles 90, the merge's blocks 85.  Keys in
-// boxes of 8 KiB, one 64-element block each: 117 (a box costs the loading thread and TMA 160 ns).  Keys asked into L2 ahead: 86 to 95.  Keeping P in the
-// tensor cores' collector for both halves of its values: level.
+// A tile of 128 keys takes 3600 clocks, at 1.25 GHz as at 1.66 (the slowest pair of 74; the median 3520, the quickest 2800): 2200 for the products (36 of 32
+// clocks, 16 of 65), 3060 for what the operands, the loads and P take of shared memory's 128 bytes a clock, and the rings, which hold a tile of keys in
+// thirds and one of values in halves beside Q's 72 KiB, refill while they are read.  32 sequences of 8192 keys, 128 heads: 86 us at 1.66 GHz, 102 at the 1.35
+// that the power cap leaves calls without a pause (850 to 715 TFLOP/s; floor 48), 64 of them 156 at 1.5, 192 at 1.25.
+// On the way (us, the first of these): 132; without releases at cluster scope and with Q by tensor maps 98, with tiles of 64 keys; thirds and halves of 128-key
+// tiles 90, the merge's blocks 85.  Keys in boxes of 8 KiB, one 64-element block each: 117 (a box costs the loading thread and TMA 160 ns).  Keys asked into
+// L2 ahead: 86 to 95.  Keeping P in the tensor cores' collector for both halves of its values: level.
 struct LatPairShape {
     static constexpr int kKB = 64 * 192 * 2;                        // a third of a CTA's keys of a tile: 64, 192 elements; all three lie ready
     static constexpr int kVB = 64 * 256 * 2;                        // half of its values: 64 keys, two times 128 elements; both lie ready

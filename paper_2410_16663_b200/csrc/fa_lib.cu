@@ -1423,9 +1423,9 @@ int rope_launch(fa::RopeParams& rp, bool bf16, bool f8, cudaStream_t st) {
     int sms = 0;
     if (int rc = check_device(&sms)) return rc;
     const int half = rp.turns ? rp.rot / 2 : 1;
-    // Few tokens: a token's heads are shared by CTAs, a vector pair to a thread (40 heads of 128, one CTA to a token / two: one token 2.54 / 2.16 us, 148 2.63 / 2.45, 250
-    // 2.96 / 2.86, 400 3.17 / 3.26).  Many: several tokens to a CTA, a warp each to look up (one / two / four of them: 592 3.58 / 3.81 / 4.30, 1184 6.11 / 5.03 / 5.53, 2368 9.11 / 8.41 /
-    // 7.66, 16384 65.4 / 56.8 / 54.1; 8 heads, 1184 3.58 / 2.58 / 2.63, 2368 5.13 / 4.07 / 3.26, 16384 23.4 / 15.5 / 13.2).
+    // Few tokens: a token's heads are shared by CTAs, a vector pair to a thread (40 heads of 128, one CTA to a token / two: one token 2.54 / 2.16 us, 148 2.63 /
+    // 2.45, 250 2.96 / 2.86, 400 3.17 / 3.26).  Many: several tokens to a CTA, a warp each to look up (one / two / four of them: 592 tokens 3.58 / 3.81 / 4.30,
+    // 1184 6.11 / 5.03 / 5.53, 2368 9.11 / 8.41 / 7.66, 16384 65.4 / 56.8 / 54.1; 8 heads, 1184 3.58 / 2.58 / 2.63, 2368 5.13 / 4.07 / 3.26, 16384 23.4 / 15.5 / 13.2).
     int split = 1;
     rp.tokens = 1;
     if (rp.n < 2 * sms) {
